@@ -372,6 +372,44 @@ int32_t swapmoe_route_static(const void* x_dev, const void* Wr_dev, const int32_
                              float* mgate_dev, int32_t* slot_dev, float* xnorm_dev, int32_t* count_dev,
                              int32_t* offset_dev, float* imp_dev, void* stream);
 
+/*
+ * Operators around the experts of a served MoE block: the norm in front of a layer.  They need no layer object.
+ */
+
+/* Root-mean-square norm of n_rows rows with the residual's addition, and an output in 8 bits with scales.  Per row
+ *   h = x + residual                      (h = x without a residual)
+ *   residual_out = h                      (rounded to residual_dtype)
+ *   y = h * weight / sqrt(mean(h^2) + eps)
+ *   out = y                               (rounded to dtype)
+ *   scales = max |y| / 448, out8 = y / scales, rounded to e4m3 (finite values saturate): one scale per row (group = 0) or
+ *            per `group` consecutive columns (32, 64, 128 or 256; the last group may be shorter)
+ * The sum enters the norm unrounded; everything is computed in fp32 and holds over the whole range of fp32 (rows whose squares
+ * leave it are normed by their largest magnitude).  A group of zeros has scale 0 and 8-bit zeros; other scales are at least
+ * 2^-120.  A NaN in a row makes its y and its scales NaN; an infinity makes the row's finite columns 0 and itself NaN, as the
+ * formula does.
+ * Strides count elements; any start and stride that keep elements aligned are taken, and rows that start at multiples of 16
+ * bytes (8 for out8) with d a multiple of 8 run fastest.  residual_out may be residual or x, and out may be x or residual, with
+ * the same stride (and type); other overlaps are not allowed.  Nothing behind column d or row n_rows is written.  Work is
+ * enqueued on `stream` of the CURRENT device; no allocation, no synchronisation, no state: calls may run side by side.
+ * Errors: INVALID_ARG (null or misaligned pointer, bad dtype, stride or group, residual_out without residual, out8
+ * without scales, no output at all), UNSUPPORTED (d > 16384), CUDA.  n_rows = 0 is a no-op. */
+typedef struct {
+  const void* x;            /* [n_rows, d] dtype                                                    */
+  const void* residual;     /* [n_rows, d] residual_dtype, or NULL                                  */
+  const void* weight;       /* [d] dtype                                                            */
+  void* residual_out;       /* [n_rows, d] residual_dtype, or NULL                                  */
+  void* out;                /* [n_rows, d] dtype, or NULL                                           */
+  void* out8;               /* [n_rows, d] e4m3 bytes, or NULL                                      */
+  float* scales;            /* [n_rows, ceil(d / group)] ([n_rows, 1] for group = 0), with out8     */
+  int64_t x_stride, residual_stride, residual_out_stride, out_stride, out8_stride, scales_stride;
+  int32_t n_rows, d;
+  int32_t dtype;            /* SWAPMOE_F32 or SWAPMOE_BF16                                          */
+  int32_t residual_dtype;   /* dtype, or SWAPMOE_F32                                                */
+  int32_t group;            /* columns per scale: 0 (the row), 32, 64, 128 or 256                   */
+  float eps;                /* >= 0                                                                 */
+} swapmoe_rms_norm_t;
+int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* args, void* stream);
+
 const char* swapmoe_status_string(int32_t status);
 
 #ifdef __cplusplus

@@ -39,6 +39,7 @@ EXPORTS = [
     "swapmoe_workspace_bytes", "swapmoe_set_gemm_path", "swapmoe_status_string",
     "swapmoe_route_static", "swapmoe_selftest_bounded_wait", "swapmoe_read_touched_slots",
     "swapmoe_read_scores_async", "swapmoe_read_decode_prefetch",
+    "swapmoe_rms_norm",
 ]
 
 
@@ -52,6 +53,13 @@ class Config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("E", "d_model", "d_ff", "top_k", "K", "dtype", "act", "renorm_topk",
                  "max_tokens", "spare_slots")]
+
+
+class RmsNormArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "weight", "residual_out", "out", "out8", "scales")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "out_stride", "out8_stride",
+                                              "scales_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_rows", "d", "dtype", "residual_dtype", "group")] + [("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -94,6 +102,7 @@ def lib() -> ctypes.CDLL:
         L.swapmoe_read_touched_slots.argtypes = [vp, vp, i32, vp]
         L.swapmoe_read_scores_async.argtypes = [vp, i32, vp, i32, vp]
         L.swapmoe_read_decode_prefetch.argtypes = [vp, vp, vp, i32, vp]
+        L.swapmoe_rms_norm.argtypes = [ctypes.POINTER(RmsNormArgs), vp]
         L.swapmoe_status_string.argtypes = [i32]
         L.swapmoe_status_string.restype = ctypes.c_char_p
         for n in EXPORTS:
@@ -151,6 +160,89 @@ def route_static(x, Wr, expert_to_slot, enorm, top_k: int, K: int, dtype: int, r
         int(K), int(dtype), int(renorm_topk), logits.data_ptr(), uidx.data_ptr(), ugate.data_ptr(),
         midx.data_ptr(), mgate.data_ptr(), slot.data_ptr(), xnorm.data_ptr(), count.data_ptr(),
         offset.data_ptr(), imp.data_ptr(), _stream_ptr(stream)), "swapmoe_route_static")
+
+
+# ------------------------------------------------------------------ operators around the experts
+def _invalid(where: str, what: str) -> SwapMoEError:
+    return SwapMoEError(-1, "%s: %s" % (where, what))
+
+
+def _dtype_of(t, where: str) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise _invalid(where, "float32 or bfloat16 rows expected, got %s" % t.dtype)
+
+
+def _row_stride(t, n_rows: int, width: int, dtype, device, where: str, name: str) -> int:
+    """Stride of the rows of a CUDA tensor [>= n_rows, width] of `dtype` on `device` whose rows are contiguous."""
+    if t.dtype != dtype or t.device != device or t.dim() != 2:
+        raise _invalid(where, "%s: a 2-d %s tensor on %s expected, got %d-d %s on %s" % (
+            name, dtype, device, t.dim(), t.dtype, t.device))
+    rows, w = t.shape
+    if rows < n_rows or w != width or (width > 1 and t.stride(1) != 1):
+        raise _invalid(where, "%s: [%d, %d] with contiguous rows expected, got %s, strides %s" % (
+            name, n_rows, width, tuple(t.shape), t.stride()))
+    return t.stride(0) if rows > 1 else max(width, t.stride(0))
+
+
+def _vector(t, n: int, dtype, device, where: str, name: str) -> int:
+    if t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
+        raise _invalid(where, "%s: %d contiguous values of %s on %s expected, got %s of %s on %s" % (
+            name, n, dtype, device, tuple(t.shape), t.dtype, t.device))
+    return t.data_ptr()
+
+
+def _enqueue(where: str, device, stream, fn, *args) -> None:
+    """Calls fn(*args, stream) with `device` current; without a stream on the device's current one."""
+    import torch
+    if device.type != "cuda":
+        raise _invalid(where, "CUDA tensors expected, got %s" % device)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream_ptr(stream)), where)
+    else:
+        _check(fn(*args, _stream_ptr(stream)), where)
+
+
+def rms_norm(x, weight, eps: float, out=None, residual=None, residual_out=None, out8=None, scales=None, group: int = 0,
+             stream=None) -> None:
+    """Root-mean-square norm of the rows of ``x`` [T, d], float32 or bfloat16, with the residual's addition.
+
+    h = x + residual; residual_out = h; y = h * weight / sqrt(mean(h^2) + eps); out = y; and in 8 bits
+    out8 (torch.float8_e4m3fn) = y / scales with scales = max |y| / 448 per row (group = 0, scales [T, 1] or [T]) or per
+    ``group`` columns (32, 64, 128 or 256; scales [T, ceil(d / group)]).  ``residual`` may be float32 beside bfloat16
+    rows.  Rows may be strided; residual_out may be residual or x, out may be x.
+    """
+    import torch
+    where = "swapmoe_rms_norm"
+    if x.dim() != 2:
+        raise _invalid(where, "x: [T, d] expected, got %s" % (tuple(x.shape),))
+    T, d = x.shape
+    dev, dtype = x.device, _dtype_of(x, where)
+    rdtype = dtype if residual is None else _dtype_of(residual, where)
+    rt = None if residual is None else residual.dtype
+    if residual_out is not None and residual is None:
+        raise _invalid(where, "residual_out without residual")
+    if (out8 is None) != (scales is None):
+        raise _invalid(where, "out8 and scales go together")
+    n_scales = -(-d // group) if group > 0 else 1
+    if scales is not None and scales.dim() == 1 and n_scales == 1:
+        scales = scales.unsqueeze(1)
+    a = RmsNormArgs(
+        x.data_ptr(), None if residual is None else residual.data_ptr(), _vector(weight, d, x.dtype, dev, where, "weight"),
+        None if residual_out is None else residual_out.data_ptr(), None if out is None else out.data_ptr(),
+        None if out8 is None else out8.data_ptr(), None if scales is None else scales.data_ptr(),
+        _row_stride(x, T, d, x.dtype, dev, where, "x"),
+        0 if residual is None else _row_stride(residual, T, d, rt, dev, where, "residual"),
+        0 if residual_out is None else _row_stride(residual_out, T, d, rt, dev, where, "residual_out"),
+        0 if out is None else _row_stride(out, T, d, x.dtype, dev, where, "out"),
+        0 if out8 is None else _row_stride(out8, T, d, torch.float8_e4m3fn, dev, where, "out8"),
+        0 if scales is None else _row_stride(scales, T, n_scales, torch.float32, dev, where, "scales"),
+        T, d, dtype, rdtype, int(group), eps)
+    _enqueue(where, dev, stream, lib().swapmoe_rms_norm, ctypes.byref(a))
 
 
 class Layer:

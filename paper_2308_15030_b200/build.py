@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libswapmoe.so")
 TRACE_LIB = os.path.join(_HERE, "libswapmoe_trace.so")
-SOURCES = ["api.cu", "route_static.cu"]
+SOURCES = ["api.cu", "route_static.cu", "block_ops.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
               # beyond a certain size nvcc compresses the kernels' image by itself, and unpacking it costs a process's first

@@ -1,0 +1,82 @@
+// C ABI of the operators around the experts of a served MoE block (see include/swapmoe.h): argument checks and launches.
+#include "../../include/swapmoe.h"
+
+#include <cuda_runtime.h>
+
+#include <cmath>
+
+#include "common.cuh"
+#include "rms_norm.cuh"
+
+using namespace swapmoe;
+
+namespace {
+
+// SMs of the current device, or 0 (the launch that follows then fails by itself).
+int current_sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  return n;
+}
+
+int32_t launched(cudaError_t e) {
+  if (e == cudaSuccess) e = cudaGetLastError();
+  else cudaGetLastError();
+  return e == cudaSuccess ? SWAPMOE_OK : SWAPMOE_ERR_CUDA;
+}
+
+// Whether rows of `elem`-byte values at p, `stride` values apart, all start on multiples of `bytes`.
+bool rows_aligned(const void* p, long long stride, size_t elem, size_t bytes) {
+  return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (size_t)stride * elem % bytes == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* p, void* stream) {
+  if (!p || p->n_rows < 0 || p->d < 1) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->dtype != SWAPMOE_F32 && p->dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->residual_dtype != p->dtype && p->residual_dtype != SWAPMOE_F32) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->group != 0 && p->group != 32 && p->group != 64 && p->group != 128 && p->group != 256) return SWAPMOE_ERR_INVALID_ARG;
+  if (!(p->eps >= 0.f) || std::isinf(p->eps)) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->d > kNormMaxWidth) return SWAPMOE_ERR_UNSUPPORTED;
+  if (p->n_rows == 0) return SWAPMOE_OK;
+  if (!p->x || !p->weight || (!p->out && !p->out8 && !p->residual_out) || (p->residual_out && !p->residual) ||
+      (p->out8 == nullptr) != (p->scales == nullptr))
+    return SWAPMOE_ERR_INVALID_ARG;
+  const size_t elem = p->dtype == SWAPMOE_BF16 ? 2 : 4, relem = p->residual_dtype == SWAPMOE_BF16 ? 2 : 4;
+  const long long d = p->d, n_scales = p->group ? (d + p->group - 1) / p->group : 1;
+  struct { const void* p; long long stride, width; size_t elem, vec; } rows[] = {
+      {p->x, p->x_stride, d, elem, 16},
+      {p->residual, p->residual_stride, d, relem, 16},
+      {p->residual_out, p->residual_out_stride, d, relem, 16},
+      {p->out, p->out_stride, d, elem, 16},
+      {p->out8, p->out8_stride, d, 1, 8},
+      {p->scales, p->scales_stride, n_scales, 4, 4},
+      {p->weight, d, d, elem, 16}};
+  bool vec = d % 8 == 0;
+  for (const auto& r : rows) {
+    if (!r.p) continue;
+    if (r.stride < r.width || reinterpret_cast<uintptr_t>(r.p) % r.elem) return SWAPMOE_ERR_INVALID_ARG;
+    vec = vec && rows_aligned(r.p, p->n_rows > 1 && r.p != p->weight ? r.stride : 0, r.elem, r.vec);
+  }
+  RmsNormArgs a;
+  a.x = p->x; a.residual = p->residual; a.weight = p->weight;
+  a.residual_out = p->residual_out; a.out = p->out;
+  a.out8 = static_cast<uint8_t*>(p->out8); a.scales = p->scales;
+  a.x_stride = p->x_stride; a.residual_stride = p->residual_stride; a.residual_out_stride = p->residual_out_stride;
+  a.out_stride = p->out_stride; a.out8_stride = p->out8_stride; a.scales_stride = p->scales_stride;
+  a.T = p->n_rows; a.d = p->d; a.group = p->group; a.eps = p->eps;
+  a.warps_per_row = a.rows_per_cta = 1;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int sms = current_sm_count();
+  if (p->dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<float, float>(a, vec, sms, st, true));
+  if (p->residual_dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<bf16, float>(a, vec, sms, st, true));
+  return launched(rms_norm_launch_typed<bf16, bf16>(a, vec, sms, st, true));
+}
+
+}  // extern "C"

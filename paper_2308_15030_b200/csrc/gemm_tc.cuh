@@ -17,6 +17,7 @@
 
 #include "../../include/swapmoe.h"
 #include "common.cuh"
+#include "launch.cuh"
 
 namespace swapmoe {
 
@@ -766,21 +767,6 @@ inline int32_t tc_bind_arena(TcState& s, const swapmoe_config_t& c, const void* 
   }
   s.arena_bound = true;
   return SWAPMOE_OK;
-}
-
-// Launch helper: programmatic dependent launch lets the kernel's prologue overlap the tail of
-// the kernel before it on the stream.
-template <typename... KArgs, typename... Args>
-inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                                 bool pdl, Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = pdl ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
 // Column-tile width (index into `options`) that minimises the bytes the busiest SM has to pull:
