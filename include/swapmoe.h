@@ -410,6 +410,36 @@ typedef struct {
 } swapmoe_rms_norm_t;
 int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* args, void* stream);
 
+/* A gate: how a token's logits become experts and weights.  Over the experts that a token may use
+ *   s = softmax(logits), or sigmoid(logits);  c = s + bias
+ *   value of a group (E / n_groups consecutive experts) = sum of its group_top largest c (of all it has, if fewer)
+ *   the topk_groups most valuable groups are kept, and further ones as long as they hold fewer than top_k experts
+ *   the top_k largest c of the kept groups are chosen, by descending c
+ *   weight = scale * s, or with renorm scale * s / (sum of the chosen s)
+ * Ties go to the lowest index.  Choices are ordered as 64-bit scores are, weights are fp32.  A NaN logit counts as -infinity.
+ * n_groups = 1 means no groups. */
+enum { SWAPMOE_SCORE_SOFTMAX = 0, SWAPMOE_SCORE_SIGMOID = 1 };
+typedef struct {
+  int32_t score;            /* SWAPMOE_SCORE_SOFTMAX or SWAPMOE_SCORE_SIGMOID                       */
+  int32_t n_groups;         /* 1 .. 32, divides E                                                   */
+  int32_t topk_groups;      /* 1 .. n_groups                                                        */
+  int32_t group_top;        /* 1 or 2                                                               */
+  int32_t renorm;           /* 0 or 1                                                               */
+  float scale;              /* finite                                                               */
+} swapmoe_gate_t;
+
+/* Routing of n_tokens rows of fp32 logits [n_tokens, E] (row stride in elements) by a gate.  bias_dev [E] fp32 or NULL.
+ * expert_to_slot_dev [E] int32 or NULL: with it only experts whose entry is >= 0 may be used (Masked Gating, Fig. 4), and
+ * slots_dev [n_tokens, top_k] (then required, else NULL) receives the entries of the chosen ones.  experts_dev [n_tokens,
+ * top_k] int32, weights_dev [n_tokens, top_k] fp32.  Where a token may use fewer than top_k experts the rest of its row
+ * is expert -1, weight 0, slot -1.  Work is enqueued on `stream` of the CURRENT device; no allocation, no synchronisation,
+ * no state: calls may run side by side.  Errors: INVALID_ARG (null or misaligned pointer, bad gate, n_groups that does
+ * not divide E, top_k > E, topk_groups groups with fewer than top_k experts, stride < E, slots without a table or the other way round), UNSUPPORTED (E > 512,
+ * top_k > 16), CUDA.  n_tokens = 0 is a no-op. */
+int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits_dev, int64_t logits_stride, const float* bias_dev,
+                      const int32_t* expert_to_slot_dev, int32_t n_tokens, int32_t E, int32_t top_k,
+                      int32_t* experts_dev, float* weights_dev, int32_t* slots_dev, void* stream);
+
 const char* swapmoe_status_string(int32_t status);
 
 #ifdef __cplusplus

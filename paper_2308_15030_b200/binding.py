@@ -39,7 +39,7 @@ EXPORTS = [
     "swapmoe_workspace_bytes", "swapmoe_set_gemm_path", "swapmoe_status_string",
     "swapmoe_route_static", "swapmoe_selftest_bounded_wait", "swapmoe_read_touched_slots",
     "swapmoe_read_scores_async", "swapmoe_read_decode_prefetch",
-    "swapmoe_rms_norm",
+    "swapmoe_rms_norm", "swapmoe_route",
 ]
 
 
@@ -60,6 +60,25 @@ class RmsNormArgs(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "out_stride", "out8_stride",
                                               "scales_stride")] + \
                [(n, ctypes.c_int32) for n in ("n_rows", "d", "dtype", "residual_dtype", "group")] + [("eps", ctypes.c_float)]
+
+
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+class Gate(ctypes.Structure):
+    """How logits become experts and weights: softmax or sigmoid scores, groups of experts, renormalised weights.
+
+    The ``topk_groups`` of ``n_groups`` groups with the largest sum of their ``group_top`` (1 or 2) best choices are
+    kept, the best choices in them win; weights are scores, with ``renorm`` divided by their sum, times ``scale``.
+    """
+    _fields_ = [(n, ctypes.c_int32) for n in ("score", "n_groups", "topk_groups", "group_top", "renorm")] + \
+               [("scale", ctypes.c_float)]
+
+    def __init__(self, score: str = "softmax", n_groups: int = 1, topk_groups: int = 1, group_top: int = 1, renorm: bool = False,
+                 scale: float = 1.0):
+        if score not in SCORES:
+            raise SwapMoEError(-1, "Gate: score %r, one of %s expected" % (score, sorted(SCORES)))
+        super().__init__(SCORES[score], n_groups, topk_groups, group_top, int(bool(renorm)), scale)
 
 
 _lib = None
@@ -102,6 +121,7 @@ def lib() -> ctypes.CDLL:
         L.swapmoe_read_touched_slots.argtypes = [vp, vp, i32, vp]
         L.swapmoe_read_scores_async.argtypes = [vp, i32, vp, i32, vp]
         L.swapmoe_read_decode_prefetch.argtypes = [vp, vp, vp, i32, vp]
+        L.swapmoe_route.argtypes = [ctypes.POINTER(Gate), vp, i64, vp, vp, i32, i32, i32, vp, vp, vp, vp]
         L.swapmoe_rms_norm.argtypes = [ctypes.POINTER(RmsNormArgs), vp]
         L.swapmoe_status_string.argtypes = [i32]
         L.swapmoe_status_string.restype = ctypes.c_char_p
@@ -243,6 +263,29 @@ def rms_norm(x, weight, eps: float, out=None, residual=None, residual_out=None, 
         0 if scales is None else _row_stride(scales, T, n_scales, torch.float32, dev, where, "scales"),
         T, d, dtype, rdtype, int(group), eps)
     _enqueue(where, dev, stream, lib().swapmoe_rms_norm, ctypes.byref(a))
+
+
+def route(gate: Gate, logits, experts, weights, bias=None, expert_to_slot=None, slots=None, stream=None) -> None:
+    """Routes the rows of ``logits`` [T, E] (float32, rows may be strided) by ``gate``.
+
+    ``experts`` [T, top_k] int32 and ``weights`` [T, top_k] float32 receive the choice, best first.  ``bias`` [E] float32 is
+    added to the scores for the choice only.  With ``expert_to_slot`` [E] int32 (-1 = not resident) only resident experts are
+    chosen and ``slots`` [T, top_k] int32 receives their entries.
+    """
+    import torch
+    where = "swapmoe_route"
+    if logits.dim() != 2 or experts.dim() != 2:
+        raise _invalid(where, "logits [T, E] and experts [T, top_k] expected")
+    (T, E), k, dev = logits.shape, experts.shape[1], logits.device
+    stride = _row_stride(logits, T, E, torch.float32, dev, where, "logits")
+    if (expert_to_slot is None) != (slots is None):
+        raise _invalid(where, "expert_to_slot and slots go together")
+    _enqueue(where, dev, stream, lib().swapmoe_route, ctypes.byref(gate), logits.data_ptr(), stride,
+             None if bias is None else _vector(bias, E, torch.float32, dev, where, "bias"),
+             None if expert_to_slot is None else _vector(expert_to_slot, E, torch.int32, dev, where, "expert_to_slot"),
+             T, E, k, _vector(experts, T * k, torch.int32, dev, where, "experts"),
+             _vector(weights, T * k, torch.float32, dev, where, "weights"),
+             None if slots is None else _vector(slots, T * k, torch.int32, dev, where, "slots"))
 
 
 class Layer:

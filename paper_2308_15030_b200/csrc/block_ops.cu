@@ -4,9 +4,11 @@
 #include <cuda_runtime.h>
 
 #include <cmath>
+#include <initializer_list>
 
 #include "common.cuh"
 #include "rms_norm.cuh"
+#include "route_groups.cuh"
 
 using namespace swapmoe;
 
@@ -32,6 +34,21 @@ int32_t launched(cudaError_t e) {
 bool rows_aligned(const void* p, long long stride, size_t elem, size_t bytes) {
   return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (size_t)stride * elem % bytes == 0;
 }
+
+// Checks a gate for layers of E experts and top_k of them per token.
+bool gate_from(const swapmoe_gate_t& g, int E, int top_k, RouteGate* out) {
+  if (g.score != SWAPMOE_SCORE_SOFTMAX && g.score != SWAPMOE_SCORE_SIGMOID) return false;
+  if (g.n_groups < 1 || g.n_groups > kRouteMaxGroups || g.n_groups > E || E % g.n_groups) return false;
+  if (g.topk_groups < 1 || g.topk_groups > g.n_groups || g.topk_groups * (E / g.n_groups) < top_k) return false;
+  if ((g.group_top != 1 && g.group_top != 2) || (g.renorm != 0 && g.renorm != 1) || !std::isfinite(g.scale)) return false;
+  out->score = g.score; out->n_groups = g.n_groups; out->topk_groups = g.topk_groups; out->group_top = g.group_top;
+  out->renorm = g.renorm; out->scale = g.scale;
+  out->group_size = E / g.n_groups;
+  out->group_magic = (uint32_t)((0x80000000ull + out->group_size - 1) / out->group_size);
+  return true;
+}
+
+bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
 
 }  // namespace
 
@@ -77,6 +94,23 @@ int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* p, void* stream) {
   if (p->dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<float, float>(a, vec, sms, st, true));
   if (p->residual_dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<bf16, float>(a, vec, sms, st, true));
   return launched(rms_norm_launch_typed<bf16, bf16>(a, vec, sms, st, true));
+}
+
+int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits, int64_t stride, const float* bias,
+                      const int32_t* expert_to_slot, int32_t T, int32_t E, int32_t top_k, int32_t* experts, float* weights,
+                      int32_t* slots, void* stream) {
+  RouteGroupsArgs a;
+  if (!gate || T < 0 || E < 1 || top_k < 1 || top_k > E || stride < E) return SWAPMOE_ERR_INVALID_ARG;
+  if (E > kRouteMaxE || top_k > kRouteMaxTopK) return SWAPMOE_ERR_UNSUPPORTED;
+  if (!gate_from(*gate, E, top_k, &a.gate)) return SWAPMOE_ERR_INVALID_ARG;
+  if (T == 0) return SWAPMOE_OK;
+  if (!logits || !experts || !weights || (expert_to_slot == nullptr) != (slots == nullptr)) return SWAPMOE_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)logits, (const void*)bias, (const void*)expert_to_slot, (const void*)experts, (const void*)weights, (const void*)slots})
+    if (misaligned(p, 4)) return SWAPMOE_ERR_INVALID_ARG;
+  a.logits = logits; a.bias = bias; a.expert_to_slot = expert_to_slot;
+  a.experts = experts; a.weights = weights; a.slots = slots;
+  a.stride = stride; a.T = T; a.E = E; a.k = top_k;
+  return launched(route_groups_launch(a, static_cast<cudaStream_t>(stream), true));
 }
 
 }  // extern "C"
