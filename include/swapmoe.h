@@ -440,6 +440,38 @@ int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits_dev, int64
                       const int32_t* expert_to_slot_dev, int32_t n_tokens, int32_t E, int32_t top_k,
                       int32_t* experts_dev, float* weights_dev, int32_t* slots_dev, void* stream);
 
+/* Low-rank adapters of many requests beside a projection that all of them share:
+ *   out[t] = y[t] + scale[a] * B[a] (A[a] x[t]),  a = ids[t]
+ * y is the shared projection's result (of this layer, or of any other product of the caller's).  A bank holds up to
+ * n_adapters adapters of one shape in device memory that the caller owns; an adapter of a smaller rank is padded with zeros.
+ * Like a layer, a bank may be driven from one stream at a time (its workspace is used by every call). */
+typedef struct swapmoe_adapters swapmoe_adapters_t; /* opaque, owned by the library */
+typedef struct {
+  int32_t n_adapters;       /* 1 .. 4096                                                            */
+  int32_t d_in, d_out;      /* multiples of 8                                                       */
+  int32_t rank;             /* multiple of 8, up to 128                                             */
+  int32_t dtype;            /* SWAPMOE_F32 or SWAPMOE_BF16: y, out, A, B (and x)                    */
+  int32_t max_tokens;       /* largest n_tokens of any forward; the workspace is sized for it       */
+} swapmoe_adapters_config_t;
+/* Allocates the bank's workspace on the CURRENT device.  *out is written only on success.  Errors: INVALID_ARG,
+ * UNSUPPORTED, CUDA, NO_MEMORY. */
+int32_t swapmoe_adapters_create(swapmoe_adapters_t** out, const swapmoe_adapters_config_t* cfg);
+/* The caller must have synchronised the streams that used the bank.  NULL is accepted. */
+int32_t swapmoe_adapters_destroy(swapmoe_adapters_t* bank);
+/* A_dev [n_adapters, rank, d_in], B_dev [n_adapters, d_out, rank] in dtype (16-byte aligned), scale_dev [n_adapters] fp32 or
+ * NULL (all 1): device memory, not copied.  Takes effect for forwards enqueued after this call. */
+int32_t swapmoe_adapters_set_weights(swapmoe_adapters_t* bank, const void* A_dev, const void* B_dev, const float* scale_dev);
+/* One pass.  x_dev [n_tokens, d_in] in dtype, or e4m3 bytes (bf16 banks only) with x_scales_dev [n_tokens] fp32, one scale per row;
+ * ids_dev [n_tokens] int32, in any order: a negative id, or one that is not in the bank, means no adapter (out = y, to
+ * the last bit).  y_dev [n_tokens, d_out] or NULL (zeros); out_dev may be y_dev with the same stride, otherwise nothing may
+ * overlap out.  Row strides count elements; rows start at multiples of 16 bytes.  Sums are fp32 (bf16 banks round
+ * A x * scale to bf16 once before B, results are rounded once).  The same call
+ * returns the same bits.  Work is enqueued on `stream`; no allocation, no synchronisation.  Errors: NOT_READY (no
+ * weights), TOO_MANY_TOKENS, INVALID_ARG, CUDA.  n_tokens = 0 is a no-op. */
+int32_t swapmoe_adapters_forward(swapmoe_adapters_t* bank, const void* x_dev, int64_t x_stride, const float* x_scales_dev,
+                                 const int32_t* ids_dev, const void* y_dev, int64_t y_stride, void* out_dev,
+                                 int64_t out_stride, int32_t n_tokens, void* stream);
+
 const char* swapmoe_status_string(int32_t status);
 
 #ifdef __cplusplus

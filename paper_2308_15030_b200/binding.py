@@ -40,6 +40,7 @@ EXPORTS = [
     "swapmoe_route_static", "swapmoe_selftest_bounded_wait", "swapmoe_read_touched_slots",
     "swapmoe_read_scores_async", "swapmoe_read_decode_prefetch",
     "swapmoe_rms_norm", "swapmoe_route",
+    "swapmoe_adapters_create", "swapmoe_adapters_destroy", "swapmoe_adapters_set_weights", "swapmoe_adapters_forward",
 ]
 
 
@@ -60,6 +61,10 @@ class RmsNormArgs(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "out_stride", "out8_stride",
                                               "scales_stride")] + \
                [(n, ctypes.c_int32) for n in ("n_rows", "d", "dtype", "residual_dtype", "group")] + [("eps", ctypes.c_float)]
+
+
+class AdaptersConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_adapters", "d_in", "d_out", "rank", "dtype", "max_tokens")]
 
 
 SCORES = {"softmax": 0, "sigmoid": 1}
@@ -122,6 +127,10 @@ def lib() -> ctypes.CDLL:
         L.swapmoe_read_scores_async.argtypes = [vp, i32, vp, i32, vp]
         L.swapmoe_read_decode_prefetch.argtypes = [vp, vp, vp, i32, vp]
         L.swapmoe_route.argtypes = [ctypes.POINTER(Gate), vp, i64, vp, vp, i32, i32, i32, vp, vp, vp, vp]
+        L.swapmoe_adapters_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(AdaptersConfig)]
+        L.swapmoe_adapters_destroy.argtypes = [vp]
+        L.swapmoe_adapters_set_weights.argtypes = [vp, vp, vp, vp]
+        L.swapmoe_adapters_forward.argtypes = [vp, vp, i64, vp, vp, vp, i64, vp, i64, i32, vp]
         L.swapmoe_rms_norm.argtypes = [ctypes.POINTER(RmsNormArgs), vp]
         L.swapmoe_status_string.argtypes = [i32]
         L.swapmoe_status_string.restype = ctypes.c_char_p
@@ -286,6 +295,58 @@ def route(gate: Gate, logits, experts, weights, bias=None, expert_to_slot=None, 
              T, E, k, _vector(experts, T * k, torch.int32, dev, where, "experts"),
              _vector(weights, T * k, torch.float32, dev, where, "weights"),
              None if slots is None else _vector(slots, T * k, torch.int32, dev, where, "slots"))
+
+
+class AdapterBank:
+    """Low-rank adapters of many requests beside a projection that all of them share (thin handle).
+
+    out[t] = y[t] + scale[a] * B[a] (A[a] x[t]) with a = ids[t]; a negative id means no adapter.
+    """
+
+    def __init__(self, n_adapters: int, d_in: int, d_out: int, rank: int, dtype: int, max_tokens: int = 1):
+        self.cfg = AdaptersConfig(n_adapters, d_in, d_out, rank, dtype, max_tokens)
+        self._h = ctypes.c_void_p()
+        _check(lib().swapmoe_adapters_create(ctypes.byref(self._h), ctypes.byref(self.cfg)), "swapmoe_adapters_create")
+        import torch
+        self._dtype = torch.bfloat16 if dtype == BF16 else torch.float32
+        self._device = torch.device("cuda", torch.cuda.current_device())
+        self._keep = None
+
+    def close(self) -> None:
+        if self._h:
+            lib().swapmoe_adapters_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def set_weights(self, A, B, scale=None) -> None:
+        """A [n_adapters, rank, d_in], B [n_adapters, d_out, rank] in the bank's dtype, scale [n_adapters] float32 (none:
+        all 1): CUDA tensors, not copied."""
+        import torch
+        c, where = self.cfg, "swapmoe_adapters_set_weights"
+        pa = _vector(A, c.n_adapters * c.rank * c.d_in, self._dtype, self._device, where, "A")
+        pb = _vector(B, c.n_adapters * c.d_out * c.rank, self._dtype, self._device, where, "B")
+        ps = None if scale is None else _vector(scale, c.n_adapters, torch.float32, self._device, where, "scale")
+        _check(lib().swapmoe_adapters_set_weights(self._h, pa, pb, ps), where)
+        self._keep = (A, B, scale)
+
+    def forward(self, x, ids, y, out, x_scales=None, stream=None) -> None:
+        """x [T, d_in] in the bank's dtype, or torch.float8_e4m3fn with x_scales [T] float32; ids [T] int32; y [T, d_out] or
+        None (zeros); out [T, d_out], may be y.  Rows may be strided."""
+        import torch
+        c, where, dev = self.cfg, "swapmoe_adapters_forward", self._device
+        T = x.shape[0]
+        _enqueue(where, dev, stream, lib().swapmoe_adapters_forward, self._h, x.data_ptr(),
+                 _row_stride(x, T, c.d_in, self._dtype if x_scales is None else torch.float8_e4m3fn, dev, where, "x"),
+                 None if x_scales is None else _vector(x_scales, T, torch.float32, dev, where, "x_scales"),
+                 _vector(ids, T, torch.int32, dev, where, "ids"),
+                 None if y is None else y.data_ptr(),
+                 0 if y is None else _row_stride(y, T, c.d_out, self._dtype, dev, where, "y"), out.data_ptr(),
+                 _row_stride(out, T, c.d_out, self._dtype, dev, where, "out"), T)
 
 
 class Layer:

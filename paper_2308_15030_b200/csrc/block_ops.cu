@@ -5,12 +5,22 @@
 
 #include <cmath>
 #include <initializer_list>
+#include <new>
 
+#include "adapters.cuh"
 #include "common.cuh"
 #include "rms_norm.cuh"
 #include "route_groups.cuh"
 
 using namespace swapmoe;
+
+struct swapmoe_adapters {
+  swapmoe_adapters_config_t cfg;
+  int sm_count;
+  float* u;                      // [max_tokens, rank]
+  const void *A, *B;
+  const float* scale;
+};
 
 namespace {
 
@@ -111,6 +121,66 @@ int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits, int64_t s
   a.experts = experts; a.weights = weights; a.slots = slots;
   a.stride = stride; a.T = T; a.E = E; a.k = top_k;
   return launched(route_groups_launch(a, static_cast<cudaStream_t>(stream), true));
+}
+
+int32_t swapmoe_adapters_create(swapmoe_adapters_t** out, const swapmoe_adapters_config_t* cfg) {
+  if (!out || !cfg) return SWAPMOE_ERR_INVALID_ARG;
+  const swapmoe_adapters_config_t c = *cfg;
+  if (c.n_adapters < 1 || c.d_in < 1 || c.d_out < 1 || c.rank < 1 || c.max_tokens < 1) return SWAPMOE_ERR_INVALID_ARG;
+  if (c.dtype != SWAPMOE_F32 && c.dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
+  if (c.n_adapters > kAdMaxCount || c.d_in % 8 || c.d_out % 8 || c.d_in > kAdMaxWidth || c.d_out > kAdMaxWidth || c.rank % 8 ||
+      c.rank > kAdMaxRank || c.max_tokens >= 1 << 24)
+    return SWAPMOE_ERR_UNSUPPORTED;
+  const int sms = current_sm_count();
+  if (sms == 0) return SWAPMOE_ERR_CUDA;
+  swapmoe_adapters* b = new (std::nothrow) swapmoe_adapters();
+  if (!b) return SWAPMOE_ERR_NO_MEMORY;
+  b->cfg = c;
+  b->sm_count = sms;
+  if (cudaMalloc(&b->u, sizeof(float) * c.max_tokens * c.rank) != cudaSuccess) {
+    cudaGetLastError();
+    delete b;
+    return SWAPMOE_ERR_NO_MEMORY;
+  }
+  *out = b;
+  return SWAPMOE_OK;
+}
+
+int32_t swapmoe_adapters_destroy(swapmoe_adapters_t* b) {
+  if (!b) return SWAPMOE_OK;
+  cudaFree(b->u);
+  delete b;
+  return SWAPMOE_OK;
+}
+
+int32_t swapmoe_adapters_set_weights(swapmoe_adapters_t* b, const void* A, const void* B, const float* scale) {
+  if (!b || !A || !B || misaligned(A, 16) || misaligned(B, 16) || misaligned(scale, 4)) return SWAPMOE_ERR_INVALID_ARG;
+  b->A = A; b->B = B; b->scale = scale;
+  return SWAPMOE_OK;
+}
+
+int32_t swapmoe_adapters_forward(swapmoe_adapters_t* b, const void* x, int64_t x_stride, const float* x_scales, const int32_t* ids,
+                                 const void* y, int64_t y_stride, void* out, int64_t out_stride, int32_t T, void* stream) {
+  if (!b || T < 0) return SWAPMOE_ERR_INVALID_ARG;
+  if (T == 0) return SWAPMOE_OK;
+  const swapmoe_adapters_config_t& c = b->cfg;
+  if (!x || !ids || !out || x_stride < c.d_in || out_stride < c.d_out || (y && y_stride < c.d_out)) return SWAPMOE_ERR_INVALID_ARG;
+  if (x_scales && c.dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
+  if (!b->A) return SWAPMOE_ERR_NOT_READY;
+  if (T > c.max_tokens) return SWAPMOE_ERR_TOO_MANY_TOKENS;
+  const size_t elem = c.dtype == SWAPMOE_BF16 ? 2 : 4;
+  const long long many = T > 1;
+  if (!rows_aligned(x, many * x_stride, x_scales ? 1 : elem, 16) || !rows_aligned(out, many * out_stride, elem, 16) ||
+      (y && !rows_aligned(y, many * y_stride, elem, 16)) || misaligned(ids, 4) || misaligned(x_scales, 4))
+    return SWAPMOE_ERR_INVALID_ARG;
+  AdapterArgs a;
+  a.x = x; a.x_scales = x_scales; a.ids = ids; a.y = y; a.out = out; a.A = b->A; a.B = b->B; a.scale = b->scale; a.u = b->u;
+  a.x_stride = x_stride; a.y_stride = y_stride; a.out_stride = out_stride;
+  a.T = T; a.d = c.d_in; a.n = c.d_out; a.r = c.rank; a.count = c.n_adapters;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (c.dtype == SWAPMOE_F32) return launched(adapters_launch<float, float>(a, st, true));
+  if (x_scales) return launched(adapters_launch<__nv_fp8_e4m3, bf16>(a, st, true));
+  return launched(adapters_launch<bf16, bf16>(a, st, true));
 }
 
 }  // extern "C"
