@@ -448,7 +448,7 @@ int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits_dev, int64
 typedef struct swapmoe_adapters swapmoe_adapters_t; /* opaque, owned by the library */
 typedef struct {
   int32_t n_adapters;       /* 1 .. 4096                                                            */
-  int32_t d_in, d_out;      /* multiples of 8                                                       */
+  int32_t d_in, d_out;      /* multiples of 8, up to 65536                                          */
   int32_t rank;             /* multiple of 8, up to 128                                             */
   int32_t dtype;            /* SWAPMOE_F32 or SWAPMOE_BF16: y, out, A, B (and x)                    */
   int32_t max_tokens;       /* largest n_tokens of any forward; the workspace is sized for it       */
@@ -467,10 +467,13 @@ int32_t swapmoe_adapters_set_weights(swapmoe_adapters_t* bank, const void* A_dev
  * overlap out.  Row strides count elements; rows start at multiples of 16 bytes.  Sums are fp32 (bf16 banks round
  * A x * scale to bf16 once before B, results are rounded once).  The same call
  * returns the same bits.  Work is enqueued on `stream`; no allocation, no synchronisation.  Errors: NOT_READY (no
- * weights), TOO_MANY_TOKENS, INVALID_ARG, CUDA.  n_tokens = 0 is a no-op. */
+ * weights), TOO_MANY_TOKENS, INVALID_ARG (also for e4m3 rows with d_in no multiple of 16), CUDA.  n_tokens = 0 is a
+ * no-op. */
 int32_t swapmoe_adapters_forward(swapmoe_adapters_t* bank, const void* x_dev, int64_t x_stride, const float* x_scales_dev,
                                  const int32_t* ids_dev, const void* y_dev, int64_t y_stride, void* out_dev,
                                  int64_t out_stride, int32_t n_tokens, void* stream);
+/* As swapmoe_device_status, for the bank's kernel. */
+int32_t swapmoe_adapters_device_status(swapmoe_adapters_t* bank, int32_t* detail, void* stream);
 
 const char* swapmoe_status_string(int32_t status);
 
