@@ -41,7 +41,6 @@ EXPORTS = [
     "swapmoe_read_scores_async", "swapmoe_read_decode_prefetch",
     "swapmoe_rms_norm", "swapmoe_route",
     "swapmoe_adapters_create", "swapmoe_adapters_destroy", "swapmoe_adapters_set_weights", "swapmoe_adapters_forward",
-    "swapmoe_adapters_device_status",
 ]
 
 
@@ -132,7 +131,6 @@ def lib() -> ctypes.CDLL:
         L.swapmoe_adapters_destroy.argtypes = [vp]
         L.swapmoe_adapters_set_weights.argtypes = [vp, vp, vp, vp]
         L.swapmoe_adapters_forward.argtypes = [vp, vp, i64, vp, vp, vp, i64, vp, i64, i32, vp]
-        L.swapmoe_adapters_device_status.argtypes = [vp, vp, vp]
         L.swapmoe_rms_norm.argtypes = [ctypes.POINTER(RmsNormArgs), vp]
         L.swapmoe_status_string.argtypes = [i32]
         L.swapmoe_status_string.restype = ctypes.c_char_p
@@ -349,11 +347,6 @@ class AdapterBank:
                  None if y is None else y.data_ptr(),
                  0 if y is None else _row_stride(y, T, c.d_out, self._dtype, dev, where, "y"), out.data_ptr(),
                  _row_stride(out, T, c.d_out, self._dtype, dev, where, "out"), T)
-
-    def device_status(self, stream=None):
-        detail = ctypes.c_int32(0)
-        st = lib().swapmoe_adapters_device_status(self._h, ctypes.byref(detail), _stream_ptr(stream))
-        return int(st), int(detail.value)
 
 
 class Layer:

@@ -3,32 +3,29 @@
 // A_a [rank, d_in], B_a [d_out, rank], y the shared projection's row.
 //
 // Bound by bytes: x, y and out once, the adapters that are asked for once per tile of tokens; the products are rank * 2 operations
-// per element of x and out.  One launch does both products.  Tokens of one adapter form tiles of up to TM; a cluster of eight
-// CTAs takes a tile: CTA c multiplies every eighth 256-byte chunk of the rows of x by A (warp-level mma, tokens as mma rows), the
-// CTAs exchange their parts of A x through distributed shared memory, and CTA c adds B (A x) to every eighth chunk of the rows of y.
-// Rows of x and y come in, and rows of out leave, by bulk copies of 256 bytes from and to wherever the token sits; the first chunks
-// of y are requested with those of x.  A and B go from L2 to registers: no two warps of a CTA need the same piece.
-//
-// Within a step of 64 bytes a thread's 16-byte piece holds its operands of two (bf16) mma: the contraction index is permuted
-// the same way for both operands.
+// per element of x and out.  One launch does both products.  Tokens of one adapter form tiles of up to 32; a cluster of 1 to 8 CTAs
+// takes a tile and splits the columns of x, then those of out.  All operands go from global memory straight to the registers of
+// the warp that multiplies them (warp-level mma, tokens as mma rows), 64 contiguous bytes of eight rows per load:
+//  - first product: the contraction is dealt out to the warps in steps of 64 bytes, so that a step's x and A belong to one warp
+//    (two or four warps share x from rank 40 on).  Within a step a lane's 16-byte piece holds its operands of two (bf16) mma: the
+//    contraction index is permuted the same way on both sides.  The warps' sums are added in shared memory, the CTAs' through
+//    distributed shared memory, in a fixed order.
+//  - second product: a warp owns 64 bytes of columns of all the tile's rows; the columns are dealt out to the mma's column tiles
+//    so that a lane's results are 16 contiguous bytes of a row, and y is read and out written from registers.
+// (With chunks of x and y staged in shared memory by bulk copies of 256 bytes, 8192 x 4096 at rank 64 took 229 us: issuing
+// 768 such copies per CTA takes longer than moving them.)
 #pragma once
 #include <cuda_fp8.h>
 
 #include "common.cuh"
 #include "launch.cuh"
-#include "ptx.cuh"
 
 namespace swapmoe {
 
 constexpr int kAdMaxRank = 128, kAdMaxCount = 4096, kAdMaxWidth = 1 << 16;
-constexpr int kAdCtas = 8;                 // CTAs per cluster
 constexpr int kAdThreads = 256, kAdWarps = kAdThreads / 32;
-constexpr int kAdChunk = 256;              // bytes of a row of weights, y and out that a CTA takes at a time
-constexpr int kAdSteps = kAdChunk / 64;    // steps of 64 bytes (four lanes' 16-byte pieces) per chunk
-constexpr int kAdStages = 2;               // chunks of x, and of y, in shared memory
-// Row pitches in shared memory: operand fragments (lanes g, q read piece q of row g) are free of bank conflicts at 64 bytes
-// modulo 128 (32 for 8-bit rows' 8-byte pieces), accumulator fragments (4 or 8 bytes at column 2 q) at 16.
-constexpr int kAdYPitch = kAdChunk + 16;
+constexpr int kAdMaxCtas = 8;              // most CTAs per cluster
+constexpr int kAdTile = 32, kAdMT = kAdTile / 16;   // tokens of a tile; mma row tiles
 constexpr int kAdDirect = 64;              // up to this many tokens every cluster finds its tile itself
 
 struct AdapterTile { int32_t adapter, first, rows, pad; };   // tokens perm[first] ... perm[first + rows - 1]; adapter -1: none
@@ -43,10 +40,10 @@ struct AdapterArgs {
   const float* scale;       // [count] or nullptr (ones)
   long long x_stride, y_stride, out_stride;
   int T, d, n, r, count;
+  int ctas;                 // CTAs per cluster
   int32_t* perm;            // [T]            } written by the plan kernel, for more than kAdDirect tokens
   AdapterTile* tiles;       // [max tiles]    }
   int32_t* n_tiles;         // [1]            }
-  int32_t* status;          // [2]
 };
 
 // ----------------------------------------------------------------------------- plan
@@ -157,77 +154,59 @@ __device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t v) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
   return pack_bf16x2(f.x, f.y);
 }
-// A lane's piece (16 bytes of weights' worth of columns) of a row of x in shared memory.
-__device__ __forceinline__ uint4 ad_lds_x(const unsigned char* p, int step, int q, float) {
-  return *reinterpret_cast<const uint4*>(p + step * 64 + q * 16);
-}
-__device__ __forceinline__ uint4 ad_lds_x(const unsigned char* p, int step, int q, bf16) {
-  return *reinterpret_cast<const uint4*>(p + step * 64 + q * 16);
-}
-__device__ __forceinline__ uint4 ad_lds_x(const unsigned char* p, int step, int q, __nv_fp8_e4m3) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p + step * 32 + q * 8);
+// A lane's piece of a row of x as it is loaded, and as an operand.
+template <typename X> struct AdPiece { typedef uint4 type; };
+template <> struct AdPiece<__nv_fp8_e4m3> { typedef uint2 type; };
+__device__ __forceinline__ uint4 ad_operand(const uint4& v) { return v; }
+__device__ __forceinline__ uint4 ad_operand(const uint2& v) {
   return make_uint4(e4m3x2_to_bf16x2(v.x), e4m3x2_to_bf16x2(v.x >> 16), e4m3x2_to_bf16x2(v.y), e4m3x2_to_bf16x2(v.y >> 16));
 }
+__device__ __forceinline__ void ad_zero(uint4& v) { v = make_uint4(0u, 0u, 0u, 0u); }
+__device__ __forceinline__ void ad_zero(uint2& v) { v = make_uint2(0u, 0u); }
 __device__ __forceinline__ void ad_store_u(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ void ad_store_u(bf16* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
 }
-// out = y + delta for two neighbouring columns in shared memory.
-__device__ __forceinline__ void ad_add2(unsigned char* p, bool have_y, float d0, float d1, float) {
-  float2* q = reinterpret_cast<float2*>(p);
-  const float2 y = have_y ? *q : make_float2(0.f, 0.f);
-  *q = make_float2(y.x + d0, y.y + d1);
+// Two neighbouring values of y, plus the sums, rounded once.
+__device__ __forceinline__ uint32_t ad_add2(uint32_t y, float d0, float d1) {
+  return pack_bf16x2(__uint_as_float(y << 16) + d0, __uint_as_float(y & 0xffff0000u) + d1);
 }
-__device__ __forceinline__ void ad_add2(unsigned char* p, bool have_y, float d0, float d1, bf16) {
-  uint32_t* q = reinterpret_cast<uint32_t*>(p);
-  const uint32_t y = have_y ? *q : 0u;
-  *q = pack_bf16x2(__uint_as_float(y << 16) + d0, __uint_as_float(y & 0xffff0000u) + d1);
+// A lane's 16 bytes of out from those of y and its accumulators of a row (columns 2 h, 2 h + 1 in tile h).
+__device__ __forceinline__ uint4 ad_finish(const uint4& y, const float (&c)[4][4], int e, bf16) {
+  return make_uint4(ad_add2(y.x, c[0][e], c[0][e + 1]), ad_add2(y.y, c[1][e], c[1][e + 1]), ad_add2(y.z, c[2][e], c[2][e + 1]),
+                    ad_add2(y.w, c[3][e], c[3][e + 1]));
+}
+__device__ __forceinline__ uint4 ad_finish(const uint4& y, const float (&c)[2][4], int e, float) {
+  return make_uint4(__float_as_uint(__uint_as_float(y.x) + c[0][e]), __float_as_uint(__uint_as_float(y.y) + c[0][e + 1]),
+                    __float_as_uint(__uint_as_float(y.z) + c[1][e]), __float_as_uint(__uint_as_float(y.w) + c[1][e + 1]));
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, int cta) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
-  return r;
-}
-__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+__device__ __forceinline__ float4 ld_cluster4(const float* mine, int cta) {        // the same place in that CTA's shared memory
+  uint32_t at;
   float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(cta));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ void bulk_store_1d(void* dst, const void* src_smem, uint32_t bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(ptx::smem_u32(src_smem)), "r"(bytes)
-               : "memory");
+
+// Rank tiles (of eight ranks) that a warp accumulates, warps side by side over the ranks, warps over the contraction.
+__host__ __device__ constexpr int ad_rank_warps(int r, int rtw) {
+  const int w = (r / 8 + rtw - 1) / rtw;
+  return w <= 1 ? 1 : w <= 2 ? 2 : 4;
 }
-
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
-// ----------------------------------------------------------------------------- shared memory
-struct AdapterSmem { int x, y, part, u, list, bars, total; };
-// x_pitch: bytes between rows of a chunk of x; slices: parts of a chunk's steps that run side by side; elem: bytes of a value of T.
-__host__ __device__ inline int ad_slices(int r) { return r <= 8 ? 8 : r <= 16 ? 4 : r <= 32 ? 2 : 1; }
-__host__ __device__ inline int ad_u_pitch(int r, int elem) {
+__host__ __device__ constexpr int ad_rtw(int r) { return r <= 8 ? 1 : r <= 16 ? 2 : 4; }
+// Pitch of u in shared memory: fragments (lanes g, q read piece q of row g) are free of bank conflicts at 64 bytes modulo 128.
+__host__ __device__ constexpr int ad_u_pitch(int r, int elem) {
   const int b = (r * elem + 63) & ~63;
   return b % 128 == 0 ? b + 64 : b;
 }
-__host__ __device__ inline AdapterSmem ad_layout(int tm, int r, int x_pitch, int elem) {
-  AdapterSmem m;
-  int o = 0;
-  m.x = o;    o += kAdStages * tm * x_pitch;
-  m.y = o;    o += kAdStages * tm * kAdYPitch;
-  m.part = o; o += ad_slices(r) * tm * r * 4;
-  m.u = o;    o += tm * ad_u_pitch(r, elem);
-  m.list = o; o += tm * 4;
-  m.bars = o; o += 2 * kAdStages * 8 + 16;
-  m.total = o;
-  return m;
-}
+__host__ __device__ constexpr int ad_part_bytes(int r) { return kAdWarps / ad_rank_warps(r, ad_rtw(r)) * kAdTile * r * 4; }
+__host__ __device__ constexpr int ad_smem_bytes(int r, int elem) { return ad_part_bytes(r) + kAdTile * ad_u_pitch(r, elem) + kAdTile * 4 + 16; }
 
-// The tile of cluster i without a plan: it has one if token i is the first, or the TM-th, ... of its adapter; then its tokens
-// are the next TM of that adapter from i on.  By one warp; T <= 64: lane l holds tokens l and l + 32.
-__device__ __forceinline__ int ad_direct_tile(const AdapterArgs& a, int i, int tm, int32_t* list, int* adapter) {
+// The tile of cluster i without a plan: it has one if token i is the first, or the 32nd, ... of its adapter; then its tokens
+// are the next 32 of that adapter from i on.  By one warp; T <= 64: lane l holds tokens l and l + 32.
+__device__ __forceinline__ int ad_direct_tile(const AdapterArgs& a, int i, int32_t* list, int* adapter) {
   const int lane = threadIdx.x & 31;
   int id[2];
 #pragma unroll
@@ -241,45 +220,32 @@ __device__ __forceinline__ int ad_direct_tile(const AdapterArgs& a, int i, int t
                                  __ballot_sync(0xffffffffu, id[0] == mine);
   const unsigned long long below = (1ull << i) - 1;
   *adapter = mine;
-  if (__popcll(all & below) % tm != 0) return 0;
+  if (__popcll(all & below) % kAdTile != 0) return 0;
   const unsigned long long rest = all & ~below;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int t = lane + 32 * h, at = __popcll(rest & ((1ull << t) - 1));
-    if ((rest >> t) & 1 && at < tm) list[at] = t;
+    if ((rest >> t) & 1 && at < kAdTile) list[at] = t;
   }
-  return min(tm, __popcll(rest));
+  return min(kAdTile, __popcll(rest));
 }
 
-// X: rows of x (T or e4m3), T: everything else, TM: most tokens of a tile.
-template <typename X, typename T, int TM>
-__global__ void __cluster_dims__(kAdCtas, 1, 1) __launch_bounds__(kAdThreads, TM == 64 ? 2 : 3) adapters_kernel(const AdapterArgs a) {
-  constexpr int kElem = (int)sizeof(T), kCols = kAdChunk / kElem;         // columns of a chunk
-  constexpr int kPiece = 16 / kElem;                                      // values of a lane's piece
-  constexpr int kXBytes = kCols * (int)sizeof(X);                         // bytes of a chunk of x
-  constexpr int kXPitch = kXBytes + (sizeof(X) == 1 ? 32 : 64);
-  constexpr int MT = TM / 16;                                             // mma row tiles
-  constexpr int NT = kCols / 8 / kAdWarps;                                // column tiles per warp in the second product
+// X: rows of x (T or e4m3), T: everything else, RTW: rank tiles per warp.
+template <typename X, typename T, int RTW>
+__global__ void __launch_bounds__(kAdThreads, 2) adapters_kernel(const AdapterArgs a) {
+  constexpr int kElem = (int)sizeof(T);
+  constexpr int P = 16 / kElem;                  // values of a lane's piece; a step or unit is 4 P values
+  constexpr int NT = P / 2;                      // column tiles of a unit of out
+  typedef typename AdPiece<X>::type XPiece;
   extern __shared__ __align__(128) unsigned char smem[];
-  const AdapterSmem lay = ad_layout(TM, a.r, kXPitch, kElem);
-  unsigned char* xs = smem + lay.x;
-  unsigned char* ys = smem + lay.y;
-  float* part = reinterpret_cast<float*>(smem + lay.part);
-  unsigned char* us = smem + lay.u;
-  int32_t* list = reinterpret_cast<int32_t*>(smem + lay.list);
-  uint64_t* bar_x = reinterpret_cast<uint64_t*>(smem + lay.bars);
-  uint64_t* bar_y = bar_x + kAdStages;
-  volatile int* ctl = reinterpret_cast<volatile int*>(bar_y + kAdStages);  // [0] a wait gave up, [1] rows, [2] adapter
+  const int r = a.r, rank_tiles = r / 8, u_pitch = ad_u_pitch(r, kElem);
+  const int rank_warps = ad_rank_warps(r, RTW), slices = kAdWarps / rank_warps;
+  float* part = reinterpret_cast<float*>(smem);                                 // [slices][tile][r]
+  unsigned char* us = smem + ad_part_bytes(r);                                  // [tile] rows of u in T
+  int32_t* list = reinterpret_cast<int32_t*>(us + kAdTile * u_pitch);           // [tile] tokens
+  volatile int* ctl = list + kAdTile;                                           // rows, adapter
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, q = lane & 3;
-  const int cta = blockIdx.x % kAdCtas, cluster = blockIdx.x / kAdCtas, n_clusters = gridDim.x / kAdCtas;
-  const int r = a.r, slices = ad_slices(r), rank_tiles = r / 8, u_pitch = ad_u_pitch(r, kElem);
-  const int x_chunks = (a.d + kCols - 1) / kCols, y_chunks = (a.n + kCols - 1) / kCols;
-  const int my_x = (x_chunks - cta + kAdCtas - 1) / kAdCtas, my_y = (y_chunks - cta + kAdCtas - 1) / kAdCtas;
-  if (tid == 0) {
-    for (int i = 0; i < kAdStages; ++i) { ptx::mbar_init(&bar_x[i], 1); ptx::mbar_init(&bar_y[i], 1); }
-    ctl[0] = 0;
-    ptx::fence_barrier_init();
-  }
+  const int C = a.ctas, cta = blockIdx.x % C, cluster = blockIdx.x / C, n_clusters = gridDim.x / C;
   pdl_wait();
   pdl_trigger();
   const bool direct = a.T <= kAdDirect;
@@ -287,260 +253,221 @@ __global__ void __cluster_dims__(kAdCtas, 1, 1) __launch_bounds__(kAdThreads, TM
   const X* x = static_cast<const X*>(a.x);
   const T* y = static_cast<const T*>(a.y);
   T* out = static_cast<T*>(a.out);
-  int x_seen = 0, y_seen = 0;              // chunks of the tiles in front: the stage and the barrier's parity follow from them
-  bool alive = true, owe_wait = false;     // owe_wait: this CTA has told the others that it has read their parts
+  bool owe_wait = false;                         // this CTA has told the others that it has read their parts
 #pragma unroll 1
   for (int tile = cluster; tile < n_tiles; tile += n_clusters) {
-    __syncthreads();                       // the tile in front is done with the list
+    __syncthreads();                             // the tile in front is done with the list
     if (direct) {
       if (warp == 0) {
         int adapter;
-        const int rows = ad_direct_tile(a, tile, TM, list, &adapter);
-        if (lane == 0) { ctl[1] = rows; ctl[2] = adapter; }
+        const int rows = ad_direct_tile(a, tile, list, &adapter);
+        if (lane == 0) { ctl[0] = rows; ctl[1] = adapter; }
       }
     } else {
       const AdapterTile td = a.tiles[tile];
       if (tid < td.rows) list[tid] = a.perm[td.first + tid];
-      if (tid == 0) { ctl[1] = td.rows; ctl[2] = td.adapter; }
+      if (tid == 0) { ctl[0] = td.rows; ctl[1] = td.adapter; }
     }
     __syncthreads();
-    const int rows = ctl[1], adapter = ctl[2];
-    if (rows == 0) continue;               // the same for the whole cluster
+    const int rows = ctl[0], adapter = ctl[1];
+    if (rows == 0) continue;                     // the same for the whole cluster
     const int mt = (rows + 15) >> 4;
     const bool work = adapter >= 0;
-    // chunk i of this CTA into its stage, by warp 0; a lane's rows lane, lane + 32
-    auto load_x = [&](int i) {
-      const int c0 = (cta + i * kAdCtas) * kCols, bytes = min(kCols, a.d - c0) * (int)sizeof(X), st = (x_seen + i) % kAdStages;
-      if (lane == 0) ptx::mbar_expect_tx(&bar_x[st], (uint32_t)(bytes * rows));
-      __syncwarp();
-      for (int t = lane; t < rows; t += 32)
-        ptx::bulk_load_1d(xs + (st * TM + t) * kXPitch, x + (long long)list[t] * a.x_stride + c0, (uint32_t)bytes, &bar_x[st]);
-    };
-    auto load_y = [&](int i) {
-      const int c0 = (cta + i * kAdCtas) * kCols, bytes = min(kCols, a.n - c0) * kElem, st = (y_seen + i) % kAdStages;
-      if (lane == 0) ptx::mbar_expect_tx(&bar_y[st], (uint32_t)(bytes * rows));
-      __syncwarp();
-      for (int t = lane; t < rows; t += 32)
-        ptx::bulk_load_1d(ys + (st * TM + t) * kAdYPitch, y + (long long)list[t] * a.y_stride + c0, (uint32_t)bytes, &bar_y[st]);
-    };
-    if (warp == 0 && alive) {
-      if (work)
-        for (int i = 0; i < min(my_x, kAdStages); ++i) load_x(i);
-      if (y != nullptr) {
-        bulk_wait_read();                  // the stores of the tile in front have left the stages of y
-        __syncwarp();
-        for (int i = 0; i < min(my_y, kAdStages); ++i) load_y(i);
-      }
-    }
+    // the lane's rows: g + 8 i; a row that the tile does not have repeats the first one and is not stored
+    int token[2 * kAdMT];
+#pragma unroll
+    for (int i = 0; i < 2 * kAdMT; ++i) token[i] = list[g + 8 * i < rows ? g + 8 * i : 0];
     if (work) {
-      // ---- first product: warp = (rank tile, slice of the steps); tokens are mma rows, ranks mma columns
+      // ---- first product
       const T* A = static_cast<const T*>(a.A) + (long long)adapter * r * a.d;
-      const int slice = slices > 1 ? warp % slices : 0, rt0 = slices > 1 ? warp / slices : warp;
-      float acc[2][MT][4];
+      const int slice = warp / rank_warps, rt0 = (warp % rank_warps) * RTW;
+      float acc[RTW][kAdMT][4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int h = 0; h < RTW; ++h)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < kAdMT; ++m)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][m][e] = 0.f;
+          for (int e = 0; e < 4; ++e) acc[h][m][e] = 0.f;
+      struct Step { XPiece x[2 * kAdMT]; uint4 w[RTW]; };
+      auto load = [&](Step& s, int c) {          // c: the lane's first column
+        const bool in = c < a.d;
+#pragma unroll
+        for (int i = 0; i < 2 * kAdMT; ++i) {
+          ad_zero(s.x[i]);
+          if (in && i < 2 * mt) s.x[i] = *reinterpret_cast<const XPiece*>(x + (long long)token[i] * a.x_stride + c);
+        }
+#pragma unroll
+        for (int h = 0; h < RTW; ++h) {
+          ad_zero(s.w[h]);
+          if (in && rt0 + h < rank_tiles) s.w[h] = __ldg(reinterpret_cast<const uint4*>(A + (long long)((rt0 + h) * 8 + g) * a.d + c));
+        }
+      };
+      auto multiply = [&](const Step& s) {
+#pragma unroll
+        for (int m = 0; m < kAdMT; ++m) {
+          if (m >= mt) break;
+          const uint4 p = ad_operand(s.x[2 * m]), p8 = ad_operand(s.x[2 * m + 1]);
+#pragma unroll
+          for (int h = 0; h < RTW; ++h) ad_step(acc[h][m], p, p8, s.w[h], T());
+        }
+      };
+      const int step = C * slices * 4 * P;
+      Step s0, s1;
+      int c = (cta * slices + slice) * 4 * P + q * P;
+      const int end = a.d + q * P;               // the same number of turns for all lanes
+      load(s0, c);
 #pragma unroll 1
-      for (int i = 0; i < my_x; ++i) {
-        const int c0 = (cta + i * kAdCtas) * kCols, st = (x_seen + i) % kAdStages;
-        uint4 w[2][kAdSteps];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int s = 0; s < kAdSteps; ++s) {
-            const int c = c0 + s * 4 * kPiece + q * kPiece, rt = rt0 + h * kAdWarps;
-            w[h][s] = make_uint4(0u, 0u, 0u, 0u);
-            if (rt < rank_tiles && ((i * kAdSteps + s) & (slices - 1)) == slice && c < a.d)
-              w[h][s] = __ldg(reinterpret_cast<const uint4*>(A + (long long)(rt * 8 + g) * a.d + c));
-          }
-        if (alive) alive = warp_wait(&bar_x[st], (x_seen + i) / kAdStages & 1, ctl, a.status, 41);
-        const unsigned char* xb = xs + st * TM * kXPitch;
-#pragma unroll
-        for (int s = 0; s < kAdSteps; ++s) {
-          if (((i * kAdSteps + s) & (slices - 1)) != slice) continue;
-          const bool in = c0 + s * 4 * kPiece + q * kPiece < a.d;
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            if (m >= mt) break;
-            const uint4 z = make_uint4(0u, 0u, 0u, 0u);
-            const uint4 p = in ? ad_lds_x(xb + (m * 16 + g) * kXPitch, s, q, X()) : z;
-            const uint4 p8 = in ? ad_lds_x(xb + (m * 16 + g + 8) * kXPitch, s, q, X()) : z;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (rt0 + h * kAdWarps < rank_tiles) ad_step(acc[h][m], p, p8, w[h][s], T());
-          }
-        }
-        if (i + kAdStages < my_x) {
-          __syncthreads();                 // all warps are done with the stage
-          if (warp == 0 && alive) load_x(i + kAdStages);
-        }
+      for (; c < end; c += 2 * step) {
+        load(s1, c + step);
+        multiply(s0);
+        if (c + step >= end) break;
+        load(s0, c + 2 * step);
+        multiply(s1);
       }
-      x_seen += my_x;
-      // parts of u to shared memory: [slice][token][rank]
-      if (owe_wait) cluster_wait();        // everybody has read the parts of the tile in front
+      if (owe_wait) cluster_wait();              // everybody has read the parts of the tile in front
       owe_wait = false;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int rt = rt0 + h * kAdWarps;
-        if (rt >= rank_tiles) continue;
+      for (int h = 0; h < RTW; ++h) {
+        if (rt0 + h >= rank_tiles) break;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
+        for (int m = 0; m < kAdMT; ++m) {
           if (m >= mt) break;
-          float* p = part + ((long long)slice * TM + m * 16 + g) * r + rt * 8 + 2 * q;
+          float* p = part + (slice * kAdTile + m * 16 + g) * r + (rt0 + h) * 8 + 2 * q;
           *reinterpret_cast<float2*>(p) = make_float2(acc[h][m][0], acc[h][m][1]);
           *reinterpret_cast<float2*>(p + 8 * r) = make_float2(acc[h][m][2], acc[h][m][3]);
         }
       }
-      if (slices > 1) {
-        __syncthreads();
-        for (int i = tid; i < rows * r; i += kAdThreads) {
-          float s = part[i];
-          for (int k = 1; k < slices; ++k) s += part[k * TM * r + i];
-          part[i] = s;
-        }
-      }
-      // ---- the CTAs' parts are added, each CTA for itself, in the order of the CTAs
-      cluster_arrive();
-      cluster_wait();
-      {
-        const float sc = a.scale != nullptr ? a.scale[adapter] : 1.f;
-        const uint32_t mine = ptx::smem_u32(part);
-        for (int i = tid * 4; i < rows * r; i += kAdThreads * 4) {
-          float4 v[kAdCtas];
-#pragma unroll
-          for (int c = 0; c < kAdCtas; ++c) v[c] = ld_cluster4(map_to_cta(mine + i * 4, c));
-          float4 s = v[0];
-#pragma unroll
-          for (int c = 1; c < kAdCtas; ++c) { s.x += v[c].x; s.y += v[c].y; s.z += v[c].z; s.w += v[c].w; }
-          const int t = i / r, j = i - t * r;
-          float f = sc;
-          if (a.x_scales != nullptr) f *= a.x_scales[list[t]];
-          ad_store_u(reinterpret_cast<T*>(us + t * u_pitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
-        }
-      }
-      cluster_arrive();
-      owe_wait = true;
-      __syncthreads();                     // u is complete
+      __syncthreads();
     }
-    // ---- second product: a warp owns NT tiles of eight columns of the chunk; u is the left operand, rows of B the right one
+    // ---- second product: the first unit's y is requested before the sums are exchanged
     const T* B = static_cast<const T*>(a.B) + (long long)(work ? adapter : 0) * a.n * r;
+    const int n_units = (a.n + 4 * P - 1) / (4 * P);
+    uint4 yv[2 * kAdMT];
+    auto load_y = [&](int unit) {
+      const int c = (unit * 4 + q) * P;
+#pragma unroll
+      for (int i = 0; i < 2 * kAdMT; ++i) {
+        ad_zero(yv[i]);
+        if (y != nullptr && c < a.n && i < 2 * mt) yv[i] = *reinterpret_cast<const uint4*>(y + (long long)token[i] * a.y_stride + c);
+      }
+    };
+    int unit = cta * kAdWarps + warp;
+    load_y(unit);
+    if (work) {
+      const float sc = a.scale != nullptr ? a.scale[adapter] : 1.f;
+      const int total = rows * r;
+      auto finish = [&](int i, float4 s) {
+        const int t = i / r, j = i - t * r;
+        float f = sc;
+        if (a.x_scales != nullptr) f *= a.x_scales[list[t]];
+        ad_store_u(reinterpret_cast<T*>(us + t * u_pitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
+      };
+      for (int i = tid * 4; i < total; i += kAdThreads * 4) {
+        float4 s = *reinterpret_cast<const float4*>(part + i);
+        for (int k = 1; k < slices; ++k) {
+          const float4 v = *reinterpret_cast<const float4*>(part + k * kAdTile * r + i);
+          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        if (C > 1) *reinterpret_cast<float4*>(part + i) = s;
+        else finish(i, s);
+      }
+      if (C > 1) {
+        cluster_arrive();
+        cluster_wait();
+        for (int i = tid * 4; i < total; i += kAdThreads * 4) {
+          float4 s = ld_cluster4(part + i, 0);
+#pragma unroll
+          for (int k = 1; k < kAdMaxCtas; ++k) {
+            if (k >= C) break;
+            const float4 v = ld_cluster4(part + i, k);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+          }
+          finish(i, s);
+        }
+        cluster_arrive();
+        owe_wait = true;
+      }
+      __syncthreads();                           // u is complete
+    }
 #pragma unroll 1
-    for (int i = 0; i < my_y; ++i) {
-      const int c0 = (cta + i * kAdCtas) * kCols, st = (y_seen + i) % kAdStages, cols = min(kCols, a.n - c0);
-      unsigned char* yb = ys + st * TM * kAdYPitch;
-      float acc[NT][MT][4];
+    for (; unit < n_units; unit += C * kAdWarps) {
+      const int c0 = unit * 4 * P;
+      float acc[kAdMT][NT][4];
 #pragma unroll
-      for (int h = 0; h < NT; ++h)
+      for (int m = 0; m < kAdMT; ++m)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int h = 0; h < NT; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[h][m][e] = 0.f;
+          for (int e = 0; e < 4; ++e) acc[m][h][e] = 0.f;
       if (work) {
 #pragma unroll 2
-        for (int k0 = 0; k0 < r; k0 += 4 * kPiece) {
-          const bool in = k0 + q * kPiece < r;
+        for (int k0 = 0; k0 < r; k0 += 4 * P) {
+          const int k = k0 + q * P;
           uint4 w[NT];
 #pragma unroll
           for (int h = 0; h < NT; ++h) {
-            const int c = (warp * NT + h) * 8 + g;
-            w[h] = make_uint4(0u, 0u, 0u, 0u);
-            if (in && c < cols) w[h] = __ldg(reinterpret_cast<const uint4*>(B + (long long)(c0 + c) * r + k0 + q * kPiece));
+            const int c = c0 + P * (g >> 1) + 2 * h + (g & 1);
+            ad_zero(w[h]);
+            if (k < r && c < a.n) w[h] = __ldg(reinterpret_cast<const uint4*>(B + (long long)c * r + k));
           }
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
+          for (int m = 0; m < kAdMT; ++m) {
             if (m >= mt) break;
-            const uint4 z = make_uint4(0u, 0u, 0u, 0u);
-            const unsigned char* up = us + (m * 16 + g) * u_pitch + (k0 * kElem + q * 16);
-            const uint4 p = in ? *reinterpret_cast<const uint4*>(up) : z, p8 = in ? *reinterpret_cast<const uint4*>(up + 8 * u_pitch) : z;
+            uint4 p, p8;
+            ad_zero(p);
+            ad_zero(p8);
+            if (k < r) {
+              p = *reinterpret_cast<const uint4*>(us + (m * 16 + g) * u_pitch + k * kElem);
+              p8 = *reinterpret_cast<const uint4*>(us + (m * 16 + g + 8) * u_pitch + k * kElem);
+            }
 #pragma unroll
-            for (int h = 0; h < NT; ++h) ad_step(acc[h][m], p, p8, w[h], T());
+            for (int h = 0; h < NT; ++h) ad_step(acc[m][h], p, p8, w[h], T());
           }
         }
       }
-      if (y != nullptr) {
-        if (alive) alive = warp_wait(&bar_y[st], (y_seen + i) / kAdStages & 1, ctl, a.status, 42);
-      } else {
-        if (warp == 0) bulk_wait_read();   // the stage's stores have left it
-        __syncthreads();
-      }
-      if (work || y == nullptr) {
+      uint4 res[2 * kAdMT];
 #pragma unroll
-        for (int h = 0; h < NT; ++h) {
-          const int c = (warp * NT + h) * 8;
-          if (c >= cols) continue;
+      for (int i = 0; i < 2 * kAdMT; ++i) res[i] = work ? ad_finish(yv[i], acc[i >> 1], (i & 1) * 2, T()) : yv[i];
+      load_y(unit + C * kAdWarps);
+      const int c = c0 + q * P;
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            if (m >= mt) break;
-            unsigned char* p = yb + (m * 16 + g) * kAdYPitch + (c + 2 * q) * kElem;
-            ad_add2(p, y != nullptr, acc[h][m][0], acc[h][m][1], T());
-            ad_add2(p + 8 * kAdYPitch, y != nullptr, acc[h][m][2], acc[h][m][3], T());
-          }
-        }
-      }
-      ptx::fence_proxy_async();            // what the threads wrote is to be seen by the bulk stores
-      __syncthreads();
-      if (warp == 0 && ctl[0] == 0) {
-        for (int t = lane; t < rows; t += 32)
-          bulk_store_1d(out + (long long)list[t] * a.out_stride + c0, yb + t * kAdYPitch, (uint32_t)(cols * kElem));
-        bulk_commit();
-        if (y != nullptr && i + kAdStages < my_y) {
-          bulk_wait_read();                // (by the lanes that issued the stores)
-          __syncwarp();
-          load_y(i + kAdStages);
-        }
-      }
+      for (int i = 0; i < 2 * kAdMT; ++i)
+        if (c < a.n && g + 8 * i < rows) *reinterpret_cast<uint4*>(out + (long long)token[i] * a.out_stride + c) = res[i];
     }
-    y_seen += my_y;
   }
-  if (warp == 0) bulk_wait_all();
-  if (owe_wait) cluster_wait();            // nobody leaves while others read its part
-  if (!alive && tid == 0) {
-    // a wait gave up: let copies that may still be in flight land before the shared memory is given back
-    const uint64_t t0 = ptx::globaltimer_ns();
-    while (ptx::globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
-  }
+  if (owe_wait) cluster_wait();                  // nobody leaves while others read its part
 }
 
 // Most tiles that T tokens on `count` adapters can make.
-inline int ad_max_tiles(int T, int count, int tm) { return T / tm + (T < count + 1 ? T : count + 1); }
-constexpr int kAdMaxClusters = 1024;
-constexpr int kAdMinTile = 32;
+inline int ad_max_tiles(int T, int count) { return T / kAdTile + (T < count + 1 ? T : count + 1); }
+constexpr int kAdMaxClusters = 2048;
 
-template <typename X, typename T, int TM>
-inline size_t adapters_smem_bytes(int r) {
-  return (size_t)ad_layout(TM, r, kAdChunk / (int)sizeof(T) * (int)sizeof(X) + (sizeof(X) == 1 ? 32 : 64), (int)sizeof(T)).total;
-}
-template <typename X, typename T, int TM>
-inline cudaError_t adapters_launch_tile(const AdapterArgs& a, cudaStream_t st, bool pdl) {
+template <typename X, typename T>
+inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st, bool pdl) {
   int tiles = a.T;
   if (a.T > kAdDirect) {
-    const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(kAdPlanThreads), 0, st, pdl, a, TM);
+    const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(kAdPlanThreads), 0, st, pdl, a, kAdTile);
     if (e != cudaSuccess) return e;
-    tiles = ad_max_tiles(a.T, a.count, TM);
+    tiles = ad_max_tiles(a.T, a.count);
   }
-  const size_t smem = adapters_smem_bytes<X, T, TM>(a.r);
-  return launch_kernel(adapters_kernel<X, T, TM>, dim3(kAdCtas * (tiles < kAdMaxClusters ? tiles : kAdMaxClusters)), dim3(kAdThreads),
-                       smem, st, pdl, a);
+  // CTAs per cluster: as many as it takes to fill the chip
+  a.ctas = 1;
+  while (a.ctas < kAdMaxCtas && tiles * a.ctas < 3 * sm_count) a.ctas *= 2;
+  const dim3 grid(a.ctas * (tiles < kAdMaxClusters ? tiles : kAdMaxClusters));
+  auto go = [&](auto kernel) {
+    return launch_cluster(kernel, a.ctas, grid, dim3(kAdThreads), ad_smem_bytes(a.r, (int)sizeof(T)), st, pdl, a);
+  };
+  return ad_rtw(a.r) == 1 ? go(adapters_kernel<X, T, 1>) : ad_rtw(a.r) == 2 ? go(adapters_kernel<X, T, 2>) : go(adapters_kernel<X, T, 4>);
 }
-template <typename X, typename T>
-inline cudaError_t adapters_launch(const AdapterArgs& a, cudaStream_t st, bool pdl) {
-  if (sizeof(T) == 2 && a.r >= 48 && a.T > kAdDirect) return adapters_launch_tile<X, T, sizeof(T) == 2 ? 64 : 32>(a, st, pdl);
-  return adapters_launch_tile<X, T, 32>(a, st, pdl);
-}
-// Raises the kernels' limit of dynamic shared memory (once per device and process would do).
+// Raises the kernels' limit of dynamic shared memory where the default does not do.
 inline cudaError_t adapters_set_limits() {
   cudaError_t e = cudaSuccess;
-  auto raise = [&](auto kernel, size_t bytes) {
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  auto raise = [&](auto kernel, int elem) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ad_smem_bytes(kAdMaxRank, elem));
   };
-  raise(adapters_kernel<float, float, 32>, adapters_smem_bytes<float, float, 32>(kAdMaxRank));
-  raise(adapters_kernel<bf16, bf16, 32>, adapters_smem_bytes<bf16, bf16, 32>(kAdMaxRank));
-  raise(adapters_kernel<bf16, bf16, 64>, adapters_smem_bytes<bf16, bf16, 64>(kAdMaxRank));
-  raise(adapters_kernel<__nv_fp8_e4m3, bf16, 32>, adapters_smem_bytes<__nv_fp8_e4m3, bf16, 32>(kAdMaxRank));
-  raise(adapters_kernel<__nv_fp8_e4m3, bf16, 64>, adapters_smem_bytes<__nv_fp8_e4m3, bf16, 64>(kAdMaxRank));
+  raise(adapters_kernel<float, float, 4>, 4);
+  raise(adapters_kernel<bf16, bf16, 4>, 2);
+  raise(adapters_kernel<__nv_fp8_e4m3, bf16, 4>, 2);
   return e;
 }
 

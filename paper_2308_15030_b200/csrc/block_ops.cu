@@ -17,8 +17,8 @@ using namespace swapmoe;
 struct swapmoe_adapters {
   swapmoe_adapters_config_t cfg;
   int sm_count;
-  char* ws;                      // workspace: plan of the tiles, status
-  int32_t *perm, *n_tiles, *status;
+  char* ws;                      // workspace: plan of the tiles
+  int32_t *perm, *n_tiles;
   AdapterTile* tiles;
   const void *A, *B;
   const float* scale;
@@ -139,7 +139,7 @@ int32_t swapmoe_adapters_create(swapmoe_adapters_t** out, const swapmoe_adapters
   if (!b) return SWAPMOE_ERR_NO_MEMORY;
   b->cfg = c;
   b->sm_count = sms;
-  const size_t tiles = (size_t)ad_max_tiles(c.max_tokens, c.n_adapters, kAdMinTile) * sizeof(AdapterTile);
+  const size_t tiles = (size_t)ad_max_tiles(c.max_tokens, c.n_adapters) * sizeof(AdapterTile);
   const size_t perm = sizeof(int32_t) * (size_t)c.max_tokens;
   if (cudaMalloc(&b->ws, tiles + 256 + perm) != cudaSuccess) {
     cudaGetLastError();
@@ -148,9 +148,8 @@ int32_t swapmoe_adapters_create(swapmoe_adapters_t** out, const swapmoe_adapters
   }
   b->tiles = reinterpret_cast<AdapterTile*>(b->ws);
   b->n_tiles = reinterpret_cast<int32_t*>(b->ws + tiles);
-  b->status = b->n_tiles + 4;
   b->perm = reinterpret_cast<int32_t*>(b->ws + tiles + 256);
-  if (cudaMemset(b->n_tiles, 0, 256) != cudaSuccess || adapters_set_limits() != cudaSuccess) {
+  if (adapters_set_limits() != cudaSuccess) {
     cudaGetLastError();
     swapmoe_adapters_destroy(b);
     return SWAPMOE_ERR_CUDA;
@@ -178,36 +177,23 @@ int32_t swapmoe_adapters_forward(swapmoe_adapters_t* b, const void* x, int64_t x
   if (T == 0) return SWAPMOE_OK;
   const swapmoe_adapters_config_t& c = b->cfg;
   if (!x || !ids || !out || x_stride < c.d_in || out_stride < c.d_out || (y && y_stride < c.d_out)) return SWAPMOE_ERR_INVALID_ARG;
-  if (x_scales && (c.dtype != SWAPMOE_BF16 || c.d_in % 16)) return SWAPMOE_ERR_INVALID_ARG;
+  if (x_scales && c.dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
   if (!b->A) return SWAPMOE_ERR_NOT_READY;
   if (T > c.max_tokens) return SWAPMOE_ERR_TOO_MANY_TOKENS;
   const size_t elem = c.dtype == SWAPMOE_BF16 ? 2 : 4;
   const long long many = T > 1;
-  if (!rows_aligned(x, many * x_stride, x_scales ? 1 : elem, 16) || !rows_aligned(out, many * out_stride, elem, 16) ||
+  if (!rows_aligned(x, many * x_stride, x_scales ? 1 : elem, x_scales ? 8 : 16) || !rows_aligned(out, many * out_stride, elem, 16) ||
       (y && !rows_aligned(y, many * y_stride, elem, 16)) || misaligned(ids, 4) || misaligned(x_scales, 4))
     return SWAPMOE_ERR_INVALID_ARG;
   AdapterArgs a;
   a.x = x; a.x_scales = x_scales; a.ids = ids; a.y = y; a.out = out; a.A = b->A; a.B = b->B; a.scale = b->scale;
-  a.perm = b->perm; a.tiles = b->tiles; a.n_tiles = b->n_tiles; a.status = b->status;
+  a.perm = b->perm; a.tiles = b->tiles; a.n_tiles = b->n_tiles; a.ctas = 1;
   a.x_stride = x_stride; a.y_stride = y_stride; a.out_stride = out_stride;
   a.T = T; a.d = c.d_in; a.n = c.d_out; a.r = c.rank; a.count = c.n_adapters;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (c.dtype == SWAPMOE_F32) return launched(adapters_launch<float, float>(a, st, true));
-  if (x_scales) return launched(adapters_launch<__nv_fp8_e4m3, bf16>(a, st, true));
-  return launched(adapters_launch<bf16, bf16>(a, st, true));
-}
-
-int32_t swapmoe_adapters_device_status(swapmoe_adapters_t* b, int32_t* detail, void* stream) {
-  if (!b) return SWAPMOE_ERR_INVALID_ARG;
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int32_t w[2] = {0, 0};
-  if (cudaMemcpyAsync(w, b->status, sizeof(w), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
-      cudaMemsetAsync(b->status, 0, sizeof(w), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
-    cudaGetLastError();
-    return SWAPMOE_ERR_CUDA;
-  }
-  if (detail) *detail = w[1];
-  return w[0] != 0 ? SWAPMOE_ERR_DEVICE_TIMEOUT : SWAPMOE_OK;
+  if (c.dtype == SWAPMOE_F32) return launched(adapters_launch<float, float>(a, b->sm_count, st, true));
+  if (x_scales) return launched(adapters_launch<__nv_fp8_e4m3, bf16>(a, b->sm_count, st, true));
+  return launched(adapters_launch<bf16, bf16>(a, b->sm_count, st, true));
 }
 
 }  // extern "C"

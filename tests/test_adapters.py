@@ -110,8 +110,6 @@ def _check(T, d, n, r, count, dtype="bf16", x8=False, ids=None, pad=0, with_y=Tr
                                            (200, 512, 768, 64, 9), (1000, 768, 960, 32, 4), (300, 72, 8, 24, 11), (130, 8, 200, 8, 300),
                                            (5, 48, 4104, 120, 2)])
 def test_shapes(T, d, n, r, count, dtype, x8):
-    if x8 and d % 16:
-        pytest.skip("rows of 8-bit values start at multiples of 16 bytes")
     _check(T, d, n, r, count, dtype, x8)
 
 
