@@ -3,17 +3,15 @@
 // A_a [rank, d_in], B_a [d_out, rank], y the shared projection's row.
 //
 // Bound by bytes: x, y and out once, the adapters that are asked for once per tile of tokens; the products are rank * 2 operations
-// per element of x and out.  One launch does both products.  Tokens of one adapter form tiles of up to 32; a cluster of 1 to 8 CTAs
-// takes a tile and splits the columns of x, then those of out.  All operands go from global memory straight to the registers of
-// the warp that multiplies them (warp-level mma, tokens as mma rows), 64 contiguous bytes of eight rows per load:
-//  - first product: the contraction is dealt out to the warps in steps of 64 bytes, so that a step's x and A belong to one warp
-//    (two or four warps share x from rank 40 on).  Within a step a lane's 16-byte piece holds its operands of two (bf16) mma: the
-//    contraction index is permuted the same way on both sides.  The warps' sums are added in shared memory, the CTAs' through
-//    distributed shared memory, in a fixed order.
-//  - second product: a warp owns 64 bytes of columns of all the tile's rows; the columns are dealt out to the mma's column tiles
-//    so that a lane's results are 16 contiguous bytes of a row, and y is read and out written from registers.
-// (With chunks of x and y staged in shared memory by bulk copies of 256 bytes, 8192 x 4096 at rank 64 took 229 us: issuing
-// 768 such copies per CTA takes longer than moving them.)
+// per element of x and out, warp-level mma with tokens as mma rows.  One launch does both products: tokens of one adapter form
+// tiles, a cluster of 1 to 8 CTAs takes a tile and splits the columns of x, then those of out; the CTAs' parts of A x are
+// added through distributed shared memory, in a fixed order.  Two forms:
+//  - up to 64 tokens (adapters_few_kernel, tiles of 32): all operands go from global memory straight to the registers of the warp
+//    that multiplies them, 64 contiguous bytes of eight rows per load; clusters find their tiles themselves.
+//  - more (adapters_tile_kernel, tiles of 64, a plan kernel in front that groups the tokens by adapter): x, A, y and B run through
+//    a ring in shared memory, so A and B are fetched once per 64 tokens and the loads run ahead of the products.
+// In the second product the columns are dealt out to the mma's column tiles so that a lane's results are 16 contiguous bytes of a
+// row: out is written from registers.
 #pragma once
 #include <cuda_fp8.h>
 
@@ -136,17 +134,21 @@ __device__ __forceinline__ void ad_step(float (&c)[4], const uint4& p, const uin
   mma_bf16_16x8x16(c, p.z, p8.z, p.w, p8.w, w.z, w.w);
 }
 __device__ __forceinline__ void ad_step(float (&c)[4], const uint4& p, const uint4& p8, const uint4& w, float) {
-  // fp32 products as three of TF32 pieces (lo * lo is below 2^-22)
+  // fp32 products as three of TF32 pieces (lo * lo is below 2^-22).  The tensor core's sums truncate, so a step's six are added
+  // to c by an ordinary addition: over d_in 4096 in one accumulator they drift by 3e-5 of the result.
+  float t[4] = {0.f, 0.f, 0.f, 0.f};
   auto two = [&](uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     uint32_t h[6], l[6];
     ad_split(a0, h[0], l[0]); ad_split(a1, h[1], l[1]); ad_split(a2, h[2], l[2]); ad_split(a3, h[3], l[3]);
     ad_split(b0, h[4], l[4]); ad_split(b1, h[5], l[5]);
-    ad_mma_tf32(c, l[0], l[1], l[2], l[3], h[4], h[5]);
-    ad_mma_tf32(c, h[0], h[1], h[2], h[3], l[4], l[5]);
-    ad_mma_tf32(c, h[0], h[1], h[2], h[3], h[4], h[5]);
+    ad_mma_tf32(t, l[0], l[1], l[2], l[3], h[4], h[5]);
+    ad_mma_tf32(t, h[0], h[1], h[2], h[3], l[4], l[5]);
+    ad_mma_tf32(t, h[0], h[1], h[2], h[3], h[4], h[5]);
   };
   two(p.x, p8.x, p.y, p8.y, w.x, w.y);
   two(p.z, p8.z, p.w, p8.w, w.z, w.w);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c[e] += t[e];
 }
 // Two e4m3 values as two bf16 (exact).
 __device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t v) {
@@ -230,9 +232,12 @@ __device__ __forceinline__ int ad_direct_tile(const AdapterArgs& a, int i, int32
   return min(kAdTile, __popcll(rest));
 }
 
+// First product: the contraction is dealt out to the warps in steps of 64 bytes (two or four warps share x from rank 40 on), and their
+// sums are added in shared memory.  Within a step a lane's 16-byte piece holds its operands of two (bf16) mma: the contraction
+// index is permuted the same way on both sides.  Second product: a warp owns 64 bytes of columns of all the tile's rows.
 // X: rows of x (T or e4m3), T: everything else, RTW: rank tiles per warp.
 template <typename X, typename T, int RTW>
-__global__ void __launch_bounds__(kAdThreads, 2) adapters_kernel(const AdapterArgs a) {
+__global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const AdapterArgs a) {
   constexpr int kElem = (int)sizeof(T);
   constexpr int P = 16 / kElem;                  // values of a lane's piece; a step or unit is 4 P values
   constexpr int NT = P / 2;                      // column tiles of a unit of out
@@ -245,229 +250,632 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_kernel(const AdapterAr
   int32_t* list = reinterpret_cast<int32_t*>(us + kAdTile * u_pitch);           // [tile] tokens
   volatile int* ctl = list + kAdTile;                                           // rows, adapter
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, q = lane & 3;
-  const int C = a.ctas, cta = blockIdx.x % C, cluster = blockIdx.x / C, n_clusters = gridDim.x / C;
+  const int C = a.ctas, cta = blockIdx.x % C;
   pdl_wait();
   pdl_trigger();
-  const bool direct = a.T <= kAdDirect;
-  const int n_tiles = direct ? a.T : *a.n_tiles;
   const X* x = static_cast<const X*>(a.x);
   const T* y = static_cast<const T*>(a.y);
   T* out = static_cast<T*>(a.out);
-  bool owe_wait = false;                         // this CTA has told the others that it has read their parts
-#pragma unroll 1
-  for (int tile = cluster; tile < n_tiles; tile += n_clusters) {
-    __syncthreads();                             // the tile in front is done with the list
-    if (direct) {
-      if (warp == 0) {
-        int adapter;
-        const int rows = ad_direct_tile(a, tile, list, &adapter);
-        if (lane == 0) { ctl[0] = rows; ctl[1] = adapter; }
-      }
-    } else {
-      const AdapterTile td = a.tiles[tile];
-      if (tid < td.rows) list[tid] = a.perm[td.first + tid];
-      if (tid == 0) { ctl[0] = td.rows; ctl[1] = td.adapter; }
-    }
-    __syncthreads();
-    const int rows = ctl[0], adapter = ctl[1];
-    if (rows == 0) continue;                     // the same for the whole cluster
-    const int mt = (rows + 15) >> 4;
-    const bool work = adapter >= 0;
-    // the lane's rows: g + 8 i; a row that the tile does not have repeats the first one and is not stored
-    int token[2 * kAdMT];
+  if (warp == 0) {
+    int adapter;
+    const int rows = ad_direct_tile(a, blockIdx.x / C, list, &adapter);
+    if (lane == 0) { ctl[0] = rows; ctl[1] = adapter; }
+  }
+  __syncthreads();
+  const int rows = ctl[0], adapter = ctl[1];
+  if (rows == 0) return;                         // the same for the whole cluster
+  const int mt = (rows + 15) >> 4;
+  const bool work = adapter >= 0;
+  // the lane's rows: g + 8 i; a row that the tile does not have repeats its first one and is not stored
+  int token[2 * kAdMT];
 #pragma unroll
-    for (int i = 0; i < 2 * kAdMT; ++i) token[i] = list[g + 8 * i < rows ? g + 8 * i : 0];
-    if (work) {
-      // ---- first product
-      const T* A = static_cast<const T*>(a.A) + (long long)adapter * r * a.d;
-      const int slice = warp / rank_warps, rt0 = (warp % rank_warps) * RTW;
-      float acc[RTW][kAdMT][4];
+  for (int i = 0; i < 2 * kAdMT; ++i) token[i] = list[g + 8 * i < rows ? g + 8 * i : 0];
+  if (work) {
+    // ---- first product.  Rank tiles that the warp does not have repeat the last one and are not stored: no load of a full
+    // step has a condition of its own.
+    const char* A = reinterpret_cast<const char*>(static_cast<const T*>(a.A) + (long long)adapter * r * a.d);
+    const int slice = warp / rank_warps, rt0 = (warp % rank_warps) * RTW;
+    const char* xp[2 * kAdMT];
 #pragma unroll
-      for (int h = 0; h < RTW; ++h)
+    for (int i = 0; i < 2 * kAdMT; ++i)
+      xp[i] = reinterpret_cast<const char*>(x + (long long)token[i] * a.x_stride);
+    uint32_t ap[RTW];
 #pragma unroll
-        for (int m = 0; m < kAdMT; ++m)
+    for (int h = 0; h < RTW; ++h) ap[h] = (uint32_t)((min(rt0 + h, rank_tiles - 1) * 8 + g) * a.d) * kElem;
+    float acc[RTW][kAdMT][4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[h][m][e] = 0.f;
-      struct Step { XPiece x[2 * kAdMT]; uint4 w[RTW]; };
-      auto load = [&](Step& s, int c) {          // c: the lane's first column
-        const bool in = c < a.d;
-#pragma unroll
-        for (int i = 0; i < 2 * kAdMT; ++i) {
-          ad_zero(s.x[i]);
-          if (in && i < 2 * mt) s.x[i] = *reinterpret_cast<const XPiece*>(x + (long long)token[i] * a.x_stride + c);
-        }
-#pragma unroll
-        for (int h = 0; h < RTW; ++h) {
-          ad_zero(s.w[h]);
-          if (in && rt0 + h < rank_tiles) s.w[h] = __ldg(reinterpret_cast<const uint4*>(A + (long long)((rt0 + h) * 8 + g) * a.d + c));
-        }
-      };
-      auto multiply = [&](const Step& s) {
-#pragma unroll
-        for (int m = 0; m < kAdMT; ++m) {
-          if (m >= mt) break;
-          const uint4 p = ad_operand(s.x[2 * m]), p8 = ad_operand(s.x[2 * m + 1]);
-#pragma unroll
-          for (int h = 0; h < RTW; ++h) ad_step(acc[h][m], p, p8, s.w[h], T());
-        }
-      };
-      const int step = C * slices * 4 * P;
-      Step s0, s1;
-      int c = (cta * slices + slice) * 4 * P + q * P;
-      const int end = a.d + q * P;               // the same number of turns for all lanes
-      load(s0, c);
-#pragma unroll 1
-      for (; c < end; c += 2 * step) {
-        load(s1, c + step);
-        multiply(s0);
-        if (c + step >= end) break;
-        load(s0, c + 2 * step);
-        multiply(s1);
-      }
-      if (owe_wait) cluster_wait();              // everybody has read the parts of the tile in front
-      owe_wait = false;
-#pragma unroll
-      for (int h = 0; h < RTW; ++h) {
-        if (rt0 + h >= rank_tiles) break;
-#pragma unroll
-        for (int m = 0; m < kAdMT; ++m) {
-          if (m >= mt) break;
-          float* p = part + (slice * kAdTile + m * 16 + g) * r + (rt0 + h) * 8 + 2 * q;
-          *reinterpret_cast<float2*>(p) = make_float2(acc[h][m][0], acc[h][m][1]);
-          *reinterpret_cast<float2*>(p + 8 * r) = make_float2(acc[h][m][2], acc[h][m][3]);
-        }
-      }
-      __syncthreads();
-    }
-    // ---- second product: the first unit's y is requested before the sums are exchanged
-    const T* B = static_cast<const T*>(a.B) + (long long)(work ? adapter : 0) * a.n * r;
-    const int n_units = (a.n + 4 * P - 1) / (4 * P);
-    uint4 yv[2 * kAdMT];
-    auto load_y = [&](int unit) {
-      const int c = (unit * 4 + q) * P;
-#pragma unroll
-      for (int i = 0; i < 2 * kAdMT; ++i) {
-        ad_zero(yv[i]);
-        if (y != nullptr && c < a.n && i < 2 * mt) yv[i] = *reinterpret_cast<const uint4*>(y + (long long)token[i] * a.y_stride + c);
-      }
-    };
-    int unit = cta * kAdWarps + warp;
-    load_y(unit);
-    if (work) {
-      const float sc = a.scale != nullptr ? a.scale[adapter] : 1.f;
-      const int total = rows * r;
-      auto finish = [&](int i, float4 s) {
-        const int t = i / r, j = i - t * r;
-        float f = sc;
-        if (a.x_scales != nullptr) f *= a.x_scales[list[t]];
-        ad_store_u(reinterpret_cast<T*>(us + t * u_pitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
-      };
-      for (int i = tid * 4; i < total; i += kAdThreads * 4) {
-        float4 s = *reinterpret_cast<const float4*>(part + i);
-        for (int k = 1; k < slices; ++k) {
-          const float4 v = *reinterpret_cast<const float4*>(part + k * kAdTile * r + i);
-          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        if (C > 1) *reinterpret_cast<float4*>(part + i) = s;
-        else finish(i, s);
-      }
-      if (C > 1) {
-        cluster_arrive();
-        cluster_wait();
-        for (int i = tid * 4; i < total; i += kAdThreads * 4) {
-          float4 s = ld_cluster4(part + i, 0);
-#pragma unroll
-          for (int k = 1; k < kAdMaxCtas; ++k) {
-            if (k >= C) break;
-            const float4 v = ld_cluster4(part + i, k);
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-          }
-          finish(i, s);
-        }
-        cluster_arrive();
-        owe_wait = true;
-      }
-      __syncthreads();                           // u is complete
-    }
-#pragma unroll 1
-    for (; unit < n_units; unit += C * kAdWarps) {
-      const int c0 = unit * 4 * P;
-      float acc[kAdMT][NT][4];
+    for (int h = 0; h < RTW; ++h)
 #pragma unroll
       for (int m = 0; m < kAdMT; ++m)
 #pragma unroll
-        for (int h = 0; h < NT; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[m][h][e] = 0.f;
-      if (work) {
-#pragma unroll 2
-        for (int k0 = 0; k0 < r; k0 += 4 * P) {
-          const int k = k0 + q * P;
-          uint4 w[NT];
-#pragma unroll
-          for (int h = 0; h < NT; ++h) {
-            const int c = c0 + P * (g >> 1) + 2 * h + (g & 1);
-            ad_zero(w[h]);
-            if (k < r && c < a.n) w[h] = __ldg(reinterpret_cast<const uint4*>(B + (long long)c * r + k));
-          }
-#pragma unroll
-          for (int m = 0; m < kAdMT; ++m) {
-            if (m >= mt) break;
-            uint4 p, p8;
-            ad_zero(p);
-            ad_zero(p8);
-            if (k < r) {
-              p = *reinterpret_cast<const uint4*>(us + (m * 16 + g) * u_pitch + k * kElem);
-              p8 = *reinterpret_cast<const uint4*>(us + (m * 16 + g + 8) * u_pitch + k * kElem);
-            }
-#pragma unroll
-            for (int h = 0; h < NT; ++h) ad_step(acc[m][h], p, p8, w[h], T());
-          }
-        }
-      }
-      uint4 res[2 * kAdMT];
-#pragma unroll
-      for (int i = 0; i < 2 * kAdMT; ++i) res[i] = work ? ad_finish(yv[i], acc[i >> 1], (i & 1) * 2, T()) : yv[i];
-      load_y(unit + C * kAdWarps);
-      const int c = c0 + q * P;
+        for (int e = 0; e < 4; ++e) acc[h][m][e] = 0.f;
+    struct Step { XPiece x[2 * kAdMT]; uint4 w[RTW]; };
+    auto load = [&](Step& s, uint32_t c) {     // c: the lane's first column
 #pragma unroll
       for (int i = 0; i < 2 * kAdMT; ++i)
-        if (c < a.n && g + 8 * i < rows) *reinterpret_cast<uint4*>(out + (long long)token[i] * a.out_stride + c) = res[i];
+        if (i < 2 || mt > 1) s.x[i] = *reinterpret_cast<const XPiece*>(xp[i] + c * (uint32_t)sizeof(X));
+#pragma unroll
+      for (int h = 0; h < RTW; ++h) s.w[h] = __ldg(reinterpret_cast<const uint4*>(A + (ap[h] + c * kElem)));
+    };
+    auto multiply = [&](const Step& s) {
+#pragma unroll
+      for (int m = 0; m < kAdMT; ++m) {
+        if (m > 0 && mt == 1) break;
+        const uint4 p = ad_operand(s.x[2 * m]), p8 = ad_operand(s.x[2 * m + 1]);
+#pragma unroll
+        for (int h = 0; h < RTW; ++h) ad_step(acc[h][m], p, p8, s.w[h], T());
+      }
+    };
+    const int step = C * slices * 4 * P;
+    int c0 = (cta * slices + slice) * 4 * P;   // the step's first column
+    Step s0, s1;
+    if (c0 + 4 * P <= a.d) {
+      load(s0, c0 + q * P);
+#pragma unroll 1
+      while (true) {
+        c0 += step;
+        const bool more = c0 + 4 * P <= a.d;
+        if (more) load(s1, c0 + q * P);
+        multiply(s0);
+        if (!more) break;
+        c0 += step;
+        const bool again = c0 + 4 * P <= a.d;
+        if (again) load(s0, c0 + q * P);
+        multiply(s1);
+        if (!again) break;
+      }
+    }
+    if (c0 < a.d) {                            // the last step of the rows, not all of whose pieces exist
+#pragma unroll
+      for (int i = 0; i < 2 * kAdMT; ++i) ad_zero(s0.x[i]);
+#pragma unroll
+      for (int h = 0; h < RTW; ++h) ad_zero(s0.w[h]);
+      if (c0 + q * P < a.d) load(s0, c0 + q * P);
+      multiply(s0);
+    }
+#pragma unroll
+    for (int h = 0; h < RTW; ++h) {
+      if (rt0 + h >= rank_tiles) break;
+#pragma unroll
+      for (int m = 0; m < kAdMT; ++m) {
+        if (m >= mt) break;
+        float* p = part + (slice * kAdTile + m * 16 + g) * r + (rt0 + h) * 8 + 2 * q;
+        *reinterpret_cast<float2*>(p) = make_float2(acc[h][m][0], acc[h][m][1]);
+        *reinterpret_cast<float2*>(p + 8 * r) = make_float2(acc[h][m][2], acc[h][m][3]);
+      }
+    }
+    __syncthreads();
+  }
+  // ---- second product: the first unit's y is requested before the sums are exchanged
+  const char* B = reinterpret_cast<const char*>(static_cast<const T*>(a.B) + (long long)(work ? adapter : 0) * a.n * r);
+  const int n_units = (a.n + 4 * P - 1) / (4 * P);
+  const char* yp[2 * kAdMT];
+  char* op[2 * kAdMT];
+#pragma unroll
+  for (int i = 0; i < 2 * kAdMT; ++i) {
+    yp[i] = reinterpret_cast<const char*>(y + (long long)token[i] * a.y_stride) + q * 16;
+    op[i] = reinterpret_cast<char*>(out + (long long)token[i] * a.out_stride) + q * 16;
+  }
+  uint4 yv[2 * kAdMT];
+#pragma unroll
+  for (int i = 0; i < 2 * kAdMT; ++i) ad_zero(yv[i]);
+  auto load_y = [&](int unit) {
+    if (y != nullptr && (unit * 4 + q) * P < a.n) {
+#pragma unroll
+      for (int i = 0; i < 2 * kAdMT; ++i)
+        if (i < 2 || mt > 1) yv[i] = *reinterpret_cast<const uint4*>(yp[i] + (uint32_t)unit * 64u);
+    }
+  };
+  // lane's row of B in column tile h of a unit: P (g / 2) + 2 h + g % 2
+  const int b_col = P * (g >> 1) + (g & 1);
+  const uint32_t b_row = (uint32_t)(r * kElem);
+  int unit = cta * kAdWarps + warp;
+  load_y(unit);
+  if (work) {
+    const float sc = a.scale != nullptr ? a.scale[adapter] : 1.f;
+    const int total = rows * r;
+    auto finish = [&](int i, float4 s) {
+      const int t = i / r, j = i - t * r;
+      float f = sc;
+      if (a.x_scales != nullptr) f *= a.x_scales[list[t]];
+      ad_store_u(reinterpret_cast<T*>(us + t * u_pitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
+    };
+    for (int i = tid * 4; i < total; i += kAdThreads * 4) {
+      float4 s = *reinterpret_cast<const float4*>(part + i);
+      for (int k = 1; k < slices; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(part + k * kAdTile * r + i);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+      if (C > 1) *reinterpret_cast<float4*>(part + i) = s;
+      else finish(i, s);
+    }
+    if (C > 1) {
+      cluster_arrive();
+      cluster_wait();
+      for (int i = tid * 4; i < total; i += kAdThreads * 4) {
+        float4 s = ld_cluster4(part + i, 0);
+#pragma unroll
+        for (int k = 1; k < kAdMaxCtas; ++k) {
+          if (k >= C) break;
+          const float4 v = ld_cluster4(part + i, k);
+          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        finish(i, s);
+      }
+      cluster_arrive();
+    }
+    __syncthreads();                           // u is complete
+  }
+#pragma unroll 1
+  for (; unit < n_units; unit += C * kAdWarps) {
+    const int c0 = unit * 4 * P;
+    float acc[kAdMT][NT][4];
+#pragma unroll
+    for (int m = 0; m < kAdMT; ++m)
+#pragma unroll
+      for (int h = 0; h < NT; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[m][h][e] = 0.f;
+    if (work) {
+      const uint32_t first = (uint32_t)(c0 + b_col) * b_row + q * 16;
+      const bool all = c0 + 4 * P <= a.n;
+      auto products = [&](int k0, bool in) {
+        uint4 w[NT], p[2 * kAdMT];
+#pragma unroll
+        for (int h = 0; h < NT; ++h) {
+          ad_zero(w[h]);
+          if (in && (all || c0 + b_col + 2 * h < a.n))
+            w[h] = __ldg(reinterpret_cast<const uint4*>(B + (first + 2 * h * b_row + k0 * kElem)));
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * kAdMT; ++i) {
+          ad_zero(p[i]);
+          if (in && (i < 2 || mt > 1)) p[i] = *reinterpret_cast<const uint4*>(us + (8 * i + g) * u_pitch + k0 * kElem + q * 16);
+        }
+#pragma unroll
+        for (int m = 0; m < kAdMT; ++m) {
+          if (m > 0 && mt == 1) break;
+#pragma unroll
+          for (int h = 0; h < NT; ++h) ad_step(acc[m][h], p[2 * m], p[2 * m + 1], w[h], T());
+        }
+      };
+      int k0 = 0;
+#pragma unroll 2
+      for (; k0 + 4 * P <= r; k0 += 4 * P) products(k0, true);
+      if (k0 < r) products(k0, k0 + q * P < r);
+    }
+    uint4 res[2 * kAdMT];
+#pragma unroll
+    for (int i = 0; i < 2 * kAdMT; ++i) res[i] = work ? ad_finish(yv[i], acc[i >> 1], (i & 1) * 2, T()) : yv[i];
+    load_y(unit + C * kAdWarps);
+    if (c0 + q * P < a.n) {
+#pragma unroll
+      for (int i = 0; i < 2 * kAdMT; ++i)
+        if (g + 8 * i < rows) *reinterpret_cast<uint4*>(op[i] + (uint32_t)unit * 64u) = res[i];
     }
   }
-  if (owe_wait) cluster_wait();                  // nobody leaves while others read its part
+  if (C > 1 && work) cluster_wait();              // nobody leaves while others read its part
+}
+
+// ----------------------------------------------------------------------------- many tokens
+constexpr int kAdTM = 64;                  // tokens of a tile
+constexpr int kAdChunk = 256;              // bytes of a row of x (bf16, fp32), A, y and out that a CTA takes at a time
+constexpr int kAdMaxStages = 6;
+// A stage holds the tile's rows of a chunk of x and the same columns of A, or the rows of a chunk of y and the rows of B behind its
+// columns: the same number of bytes.  The 16-byte pieces of a row trade places by an exclusive or with ad_swap of the row, so that
+// the lanes that are served together meet different banks: eight rows' pieces of one index (ldmatrix), and two rows of four pieces
+// (operands that are converted on the way).
+__host__ __device__ constexpr int ad_swap(int row) { return (row & 1) << 2 | (row >> 1 & 3); }
+// The same for rows of B, of `pieces` pieces: eight rows of one column tile lie at 8 a + b, a < 4, b < 2 (see from_b).
+__host__ __device__ constexpr int ad_swap_b(int row, int pieces) {
+  return pieces >= 8 ? (row & 1) << 2 | (row >> 3 & 3) : row >> 3 & (pieces - 1);
+}
+__host__ __device__ constexpr int ad_rank_up(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
+__host__ __device__ constexpr int ad_stage_bytes(int r) { return kAdTM * kAdChunk + kAdChunk * r; }
+__host__ __device__ constexpr int ad_tile_u_pitch(int r, int elem) { return elem == 2 ? r * 2 + 16 : ad_u_pitch(r, elem); }
+__host__ __device__ constexpr int ad_tile_rest(int r, int elem) { return kAdTM * ad_tile_u_pitch(r, elem) + kAdTM * 4 + 512; }
+// Stages: as many as fit with two CTAs per SM, or, where that leaves fewer than three, with one.
+inline int ad_stages(int r, int elem) {
+  const int two = (112 * 1024 - ad_tile_rest(r, elem)) / ad_stage_bytes(r);
+  const int n = two >= 3 ? two : (224 * 1024 - ad_tile_rest(r, elem)) / ad_stage_bytes(r);
+  return n < kAdMaxStages ? n : kAdMaxStages;
+}
+template <int kBytes>
+__device__ __forceinline__ void ad_copy(uint32_t d, const void* src) {               // to shared memory
+  if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(d), "l"(src) : "memory");
+}
+template <int kBytes>
+__device__ __forceinline__ void ad_clear(uint32_t d) {
+  if constexpr (kBytes == 16) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(d), "r"(0) : "memory");
+  else asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(d), "r"(0) : "memory");
+}
+__device__ __forceinline__ void ad_copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void ad_copy_wait(int pending) {            // at most `pending` groups are still on their way
+  switch (pending) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+  }
+}
+__device__ __forceinline__ void ad_store_u2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+__device__ __forceinline__ void ad_store_u2(bf16* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(a, b); }
+
+__device__ __forceinline__ uint4 ad_lds(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ uint4 ad_lds8(uint32_t at) {             // eight e4m3 values as bf16
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+  return ad_operand(v);
+}
+
+__device__ __forceinline__ void ad_ldmatrix(uint32_t (&v)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at));
+}
+__device__ __forceinline__ void ad_ldmatrix(uint32_t (&v)[2], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(at));
+}
+
+// Tiles of up to 64 tokens from the plan; a cluster takes a tile and deals its chunks of x, then of y, out to its CTAs.  The
+// chunks of both products run through one ring of stages, so the first of y and B are on their way while x is still multiplied; one
+// barrier per chunk.  Warp w multiplies 16 tokens (w % 4) by half the ranks, then by half the chunk's columns of out.
+// RP: the rank rounded up (16, 32, 64, 128), so that all places in shared memory are constants (places that hang on the rank
+// itself: 8192 x 4096 at rank 64 80 us, constants 67).  bf16 operands come by ldmatrix, whose four registers are an operand as it is;
+// from two rows' 16-byte pieces it has to be put together, which took more instructions than the products.
+template <typename X, typename T, int RP>
+__global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const AdapterArgs a, int stages) {
+  constexpr int kElem = (int)sizeof(T), P = 16 / kElem, NT = P / 2;
+  constexpr int kCols = kAdChunk / kElem;                    // columns of a chunk
+  constexpr int kXPiece = sizeof(X) == 1 ? 8 : 16;           // bytes of a lane's piece of x: P values
+  constexpr int kXRow = 16 * kXPiece;                        // bytes of a row of a chunk of x
+  constexpr int NTH = RP / 16;                               // rank tiles per warp
+  constexpr int kBRow = RP * kElem, kBPieces = kBRow / 16;   // a row of B in a stage
+  constexpr int kUPitch = ad_tile_u_pitch(RP, kElem);
+  constexpr uint32_t kStage = (uint32_t)ad_stage_bytes(RP), kW = kAdTM * kAdChunk;
+  constexpr bool kMatrixX = sizeof(X) == 2, kMatrixB = kElem == 2;     // operands of the two products by ldmatrix
+  extern __shared__ __align__(128) unsigned char smem_raw[];
+  // (a step's piece is found by an exclusive or with its index: stages start at multiples of the longest row)
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 511) & ~static_cast<uintptr_t>(511));
+  const int r = a.r;
+  unsigned char* us = smem + stages * kStage;
+  int32_t* list = reinterpret_cast<int32_t*>(us + kAdTM * kUPitch);
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, q = lane & 3;
+  const int mw = warp & 3, nh = warp >> 2;
+  const int C = a.ctas, cta = blockIdx.x % C, cluster = blockIdx.x / C, n_clusters = gridDim.x / C;
+  const int x_chunks = (a.d + kCols - 1) / kCols, y_chunks = (a.n + kCols - 1) / kCols;
+  const int x_iters = (x_chunks + C - 1) / C, y_iters = (y_chunks + C - 1) / C;     // the same for all CTAs of a cluster
+  const int per_row = r / P;                                 // pieces of a row of B
+  const uint32_t stage0 = (uint32_t)__cvta_generic_to_shared(smem), us0 = stage0 + stages * kStage;
+  // What a thread copies: piece tid % 16 of rows tid / 16 + 16 k of x, y and A; of B pieces tid + 256 k.
+  const int crow = tid >> 4, cpiece = tid & 15;
+  const uint32_t to_row = crow * 256 + ((cpiece ^ ad_swap(crow)) << 4);
+  const uint32_t to_x = kXPiece == 16 ? to_row : crow * 128 + ((cpiece ^ ((crow & 3) << 2)) << 3);
+  const uint32_t to_b = (uint32_t)(tid ^ ad_swap_b(tid / kBPieces, kBPieces)) * 16;
+  // Operands: the lane's places in a stage at contraction index 0 (further ones by an exclusive or with the piece's index)
+  const int row0 = mw * 16 + g, col = nh * (kCols / 2);      // the lane's first token, the warp's first column in a chunk of out
+  const int l8 = lane & 7, l1 = lane >> 3 & 1, l2 = lane >> 4;
+  const uint32_t from_x = kMatrixX ? (mw * 16 + l8 + 8 * l1) * 256 + ((l2 ^ ad_swap(l8)) << 4)
+                                   : kXPiece == 16 ? row0 * 256 + ((q ^ ad_swap(g)) << 4) : row0 * 128 + ((q ^ ((g & 3) << 2)) << 3);
+  const uint32_t from_a = kW + (kMatrixX ? (nh * NTH * 8 + l2 * 8 + l8) * 256 + ((l1 ^ ad_swap(l8)) << 4)
+                                         : (nh * NTH * 8 + g) * 256 + ((q ^ ad_swap(g)) << 4));
+  const int b_row = kMatrixB ? 8 * (l8 >> 1) + 2 * l2 + (l8 & 1) : P * (g >> 1) + (g & 1);      // (in column tile 0 of unit 0)
+  const uint32_t from_b = kW + (col + b_row) * kBRow + (((kMatrixB ? l1 : q) ^ ad_swap_b(b_row, kBPieces)) << 4);
+  const uint32_t from_u = us0 + (kMatrixB ? (mw * 16 + l8 + 8 * l1) * kUPitch + l2 * 16 : row0 * kUPitch + q * 16);
+  const uint32_t from_y = row0 * 256 + (((col / P + q) ^ ad_swap(g)) << 4);
+  pdl_wait();
+  pdl_trigger();
+  const int n_tiles = *a.n_tiles;
+  const X* x = static_cast<const X*>(a.x);
+  const T* y = static_cast<const T*>(a.y);
+  T* out = static_cast<T*>(a.out);
+#pragma unroll 1
+  for (int tile = cluster; tile < n_tiles; tile += n_clusters) {
+    const AdapterTile td = a.tiles[tile];
+    const int rows = td.rows, adapter = td.adapter;
+    __syncthreads();                                         // the tile in front is done with the list and the stages
+    if (tid < rows) list[tid] = a.perm[td.first + tid];
+    __syncthreads();
+    if (adapter < 0) {                                       // no adapter: rows of y as they are
+      const int pieces = rows * 16;
+      for (int i = cta; i < y_chunks; i += C) {
+        for (int p = tid; p < pieces; p += kAdThreads) {
+          const int t = p >> 4, c = i * kCols + (p & 15) * P;
+          if (c >= a.n) continue;
+          uint4 v;
+          ad_zero(v);
+          if (y != nullptr) v = *reinterpret_cast<const uint4*>(y + (long long)list[t] * a.y_stride + c);
+          *reinterpret_cast<uint4*>(out + (long long)list[t] * a.out_stride + c) = v;
+        }
+      }
+      continue;
+    }
+    // sources of the next chunk: they move on by C chunks with every request
+    const char *xp[kAdTM / 16], *yp[kAdTM / 16];
+#pragma unroll
+    for (int k = 0; k < kAdTM / 16; ++k) {
+      const long long t = list[min(crow + 16 * k, rows - 1)];
+      xp[k] = reinterpret_cast<const char*>(x + t * a.x_stride) + cpiece * kXPiece + cta * kXRow;
+      yp[k] = reinterpret_cast<const char*>(y + t * a.y_stride) + cpiece * 16 + cta * kAdChunk;
+    }
+    const char* ap = reinterpret_cast<const char*>(static_cast<const T*>(a.A) + ((long long)adapter * r + crow) * a.d) + cpiece * 16 +
+                     cta * kAdChunk;
+    const char* bp = reinterpret_cast<const char*>(static_cast<const T*>(a.B) + ((long long)adapter * a.n + cta * kCols) * r);
+    const int a_step = 16 * a.d * kElem;
+    const int n_rows = (rows - crow + 15) >> 4, n_ranks = (r - crow + 15) >> 4;      // rows crow + 16 k below rows, r
+    int cx = cta * kCols, cy = cta * kCols;                  // first column of the next chunk of x, of y
+    auto request_x = [&](uint32_t stage) {
+      if (cx + cpiece * P < a.d) {
+#pragma unroll
+        for (int k = 0; k < kAdTM / 16; ++k) {
+          if (k < n_rows) ad_copy<kXPiece>(stage + to_x + k * (16 * kXRow), xp[k]);
+          xp[k] += C * kXRow;
+        }
+#pragma unroll
+        for (int k = 0; k < NTH; ++k)
+          if (k < n_ranks) ad_copy<16>(stage + kW + to_row + k * 4096, ap + k * a_step);
+        ap += C * kAdChunk;
+      } else if (cx < a.d) {                                 // beyond the rows: zeros
+#pragma unroll
+        for (int k = 0; k < kAdTM / 16; ++k) ad_clear<kXPiece>(stage + to_x + k * (16 * kXRow));
+#pragma unroll
+        for (int k = 0; k < NTH; ++k)
+          if (k < n_ranks) ad_clear<16>(stage + kW + to_row + k * 4096);
+      }
+      cx += C * kCols;
+    };
+    auto request_y = [&](uint32_t stage) {
+      if (y != nullptr && cy + cpiece * P < a.n) {
+#pragma unroll
+        for (int k = 0; k < kAdTM / 16; ++k) {
+          if (k < n_rows) ad_copy<16>(stage + to_row + k * 4096, yp[k]);
+          yp[k] += C * kAdChunk;
+        }
+      }
+      const int pieces = min(kCols, a.n - cy) * kBPieces;
+      if (r == RP) {
+#pragma unroll
+        for (int k = 0; k < NTH; ++k)                        // 16 r pieces in all
+          if (tid + kAdThreads * k < pieces)
+            ad_copy<16>(stage + kW + (to_b ^ (ad_swap_b(kAdThreads * k / kBPieces, kBPieces) << 4)) + k * 4096, bp + (tid + kAdThreads * k) * 16);
+      } else {                                               // ranks that B does not have: zeros
+        for (int p = tid; p < pieces; p += kAdThreads) {
+          const int c = p / kBPieces, j = p % kBPieces;
+          const uint32_t at = stage + kW + c * kBRow + ((j ^ ad_swap_b(c, kBPieces)) << 4);
+          if (j < per_row) ad_copy<16>(at, bp + (c * per_row + j) * 16);
+          else ad_clear<16>(at);
+        }
+      }
+      bp += (long long)C * kCols * r * kElem;
+      cy += C * kCols;
+    };
+    const int items = x_iters + y_iters;
+    for (int i = 0; i < stages - 1; ++i) {
+      if (i < x_iters) request_x(stage0 + i * kStage);
+      else if (i < items) request_y(stage0 + i * kStage);
+      ad_copy_commit();
+    }
+    uint32_t at = 0, before = (stages - 1) * kStage;         // stages of item i and of item i - 1
+    const bool mine = mw * 16 < rows;                        // the warp has tokens
+    float acc[NTH][4];
+#pragma unroll
+    for (int h = 0; h < NTH; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[h][e] = 0.f;
+    T* op[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) op[i] = out + (long long)list[min(row0 + 8 * i, rows - 1)] * a.out_stride + cta * kCols + col + q * P;
+    // ---- first product.  (Ranks beyond r are multiplied too: whatever their rows of A hold goes into results nobody reads.)
+#pragma unroll 1
+    for (int i = 0; i < x_iters; ++i) {
+      ad_copy_wait(stages - 2);
+      __syncthreads();
+      if (i + stages - 1 < x_iters) request_x(stage0 + before);
+      else if (i + stages - 1 < items) request_y(stage0 + before);
+      ad_copy_commit();
+      const uint32_t st = stage0 + at;
+      before = at;
+      at = at + kStage == stages * kStage ? 0u : at + kStage;
+      if (!mine || (cta + i * C) * kCols >= a.d) continue;
+      if constexpr (kMatrixX) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {                        // 16 columns
+          uint32_t p[4];
+          ad_ldmatrix(p, (st + from_x) ^ (s * 32));
+          if constexpr (NTH == 1) {
+            uint32_t w[2];
+            ad_ldmatrix(w, (st + from_a) ^ (s * 32));
+            mma_bf16_16x8x16(acc[0], p[0], p[1], p[2], p[3], w[0], w[1]);
+          } else {
+#pragma unroll
+            for (int h = 0; h + 1 < NTH; h += 2) {
+              uint32_t w[4];
+              ad_ldmatrix(w, ((st + from_a) ^ (s * 32)) + h * 2048);
+              mma_bf16_16x8x16(acc[h], p[0], p[1], p[2], p[3], w[0], w[1]);
+              mma_bf16_16x8x16(acc[h + 1], p[0], p[1], p[2], p[3], w[2], w[3]);
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          uint4 p, p8;
+          if constexpr (kXPiece == 16) {
+            p = ad_lds((st + from_x) ^ (s * 64));
+            p8 = ad_lds(((st + from_x) ^ (s * 64)) + 8 * kXRow);
+          } else {
+            p = ad_lds8((st + from_x) ^ (s * 32));
+            p8 = ad_lds8(((st + from_x) ^ (s * 32)) + 8 * kXRow);
+          }
+#pragma unroll
+          for (int h = 0; h < NTH; ++h) ad_step(acc[h], p, p8, ad_lds(((st + from_a) ^ (s * 64)) + h * 2048), T());
+        }
+      }
+    }
+    ad_copy_wait(stages - 2);
+    __syncthreads();
+    {
+      // ---- u = scale * A x: the CTAs' parts are added in their order
+      const float sc = a.scale != nullptr ? a.scale[adapter] : 1.f;
+      if (C == 1) {
+        if (mine) {
+          float f[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) f[e] = a.x_scales != nullptr ? sc * a.x_scales[list[min(row0 + 8 * e, rows - 1)]] : sc;
+#pragma unroll
+          for (int h = 0; h < NTH; ++h) {
+            if ((nh * NTH + h) * 8 >= r)                     // ranks that A does not have
+              acc[h][0] = acc[h][1] = acc[h][2] = acc[h][3] = 0.f;
+            T* p = reinterpret_cast<T*>(us + row0 * kUPitch) + (nh * NTH + h) * 8 + 2 * q;
+            ad_store_u2(p, acc[h][0] * f[0], acc[h][1] * f[0]);
+            ad_store_u2(reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(p) + 8 * kUPitch), acc[h][2] * f[1], acc[h][3] * f[1]);
+          }
+        }
+      } else {
+        float* part = reinterpret_cast<float*>(smem + before);           // the stage just multiplied
+        if (mine) {
+#pragma unroll
+          for (int h = 0; h < NTH; ++h) {
+            float* p = part + row0 * RP + (nh * NTH + h) * 8 + 2 * q;
+            ad_store_u2(p, acc[h][0], acc[h][1]);
+            ad_store_u2(p + 8 * RP, acc[h][2], acc[h][3]);
+          }
+        }
+        cluster_arrive();
+        cluster_wait();
+        for (int k = tid * 4; k < rows * RP; k += kAdThreads * 4) {
+          const int t = k / RP, j = k % RP;
+          float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (j < r) {                                       // (ranks that A does not have: zeros)
+            s = ld_cluster4(part + k, 0);
+#pragma unroll
+            for (int c = 1; c < kAdMaxCtas; ++c) {
+              if (c >= C) break;
+              const float4 v = ld_cluster4(part + k, c);
+              s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+          }
+          const float f = a.x_scales != nullptr ? sc * a.x_scales[list[t]] : sc;
+          ad_store_u(reinterpret_cast<T*>(us + t * kUPitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
+        }
+        cluster_arrive();
+        cluster_wait();                                      // the stage is free again
+      }
+      __syncthreads();
+    }
+    // ---- second product: out = y + u B, two units of four lanes' pieces of columns
+    int c0 = cta * kCols;
+#pragma unroll 1
+    for (int i = x_iters; i < items; ++i) {
+      if (i > x_iters) {
+        ad_copy_wait(stages - 2);
+        __syncthreads();
+      }
+      if (i + stages - 1 < items) request_y(stage0 + before);
+      ad_copy_commit();
+      const uint32_t st = stage0 + at;
+      before = at;
+      at = at + kStage == stages * kStage ? 0u : at + kStage;
+      if (mine && c0 < a.n) {
+        float d[2][NT][4];
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int h = 0; h < NT; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[v][h][e] = 0.f;
+        if constexpr (kMatrixB) {
+#pragma unroll
+          for (int k = 0; k < RP / 16; ++k) {
+            uint32_t p[4];
+            ad_ldmatrix(p, from_u + k * 32);
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+#pragma unroll
+              for (int h = 0; h < NT; h += 2) {
+                uint32_t w[4];
+                ad_ldmatrix(w, ((st + from_b) ^ (k * 32)) + (v * 4 * P + 2 * h) * kBRow);
+                mma_bf16_16x8x16(d[v][h], p[0], p[1], p[2], p[3], w[0], w[1]);
+                mma_bf16_16x8x16(d[v][h + 1], p[0], p[1], p[2], p[3], w[2], w[3]);
+              }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < kBPieces; k += 4) {
+            const uint4 p = ad_lds(from_u + k * 16), p8 = ad_lds(from_u + 8 * kUPitch + k * 16);
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+#pragma unroll
+              for (int h = 0; h < NT; ++h)
+                ad_step(d[v][h], p, p8, ad_lds(((st + from_b) ^ (k * 16 ^ ad_swap_b(v * 4 * P, kBPieces) << 4)) + (v * 4 * P + 2 * h) * kBRow), T());
+          }
+        }
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          if (c0 + col + v * 4 * P + q * P >= a.n) continue;
+          uint4 y0, y8;
+          ad_zero(y0);
+          ad_zero(y8);
+          if (y != nullptr) {
+            y0 = ad_lds((st + from_y) ^ (v * 64));
+            y8 = ad_lds(((st + from_y) ^ (v * 64)) + 8 * 256);
+          }
+          if (row0 < rows) *reinterpret_cast<uint4*>(op[0] + v * 4 * P) = ad_finish(y0, d[v], 0, T());
+          if (row0 + 8 < rows) *reinterpret_cast<uint4*>(op[1] + v * 4 * P) = ad_finish(y8, d[v], 2, T());
+        }
+      }
+      op[0] += C * kCols;
+      op[1] += C * kCols;
+      c0 += C * kCols;
+    }
+    ad_copy_wait(0);
+  }
 }
 
 // Most tiles that T tokens on `count` adapters can make.
-inline int ad_max_tiles(int T, int count) { return T / kAdTile + (T < count + 1 ? T : count + 1); }
+inline int ad_max_tiles(int T, int count) { return T / kAdTM + (T < count + 1 ? T : count + 1); }
 constexpr int kAdMaxClusters = 2048;
 
 template <typename X, typename T>
 inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st, bool pdl) {
-  int tiles = a.T;
-  if (a.T > kAdDirect) {
-    const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(kAdPlanThreads), 0, st, pdl, a, kAdTile);
-    if (e != cudaSuccess) return e;
-    tiles = ad_max_tiles(a.T, a.count);
+  const int elem = (int)sizeof(T);
+  if (a.T <= kAdDirect) {
+    a.ctas = 1;
+    while (a.ctas < kAdMaxCtas && a.T * a.ctas < 2 * sm_count) a.ctas *= 2;
+    auto go = [&](auto kernel) {
+      return launch_cluster(kernel, a.ctas, dim3(a.ctas * a.T), dim3(kAdThreads), ad_smem_bytes(a.r, elem), st, pdl, a);
+    };
+    return ad_rtw(a.r) == 1 ? go(adapters_few_kernel<X, T, 1>) : ad_rtw(a.r) == 2 ? go(adapters_few_kernel<X, T, 2>)
+                                                                                  : go(adapters_few_kernel<X, T, 4>);
   }
-  // CTAs per cluster: as many as it takes to fill the chip
+  const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(kAdPlanThreads), 0, st, pdl, a, kAdTM);
+  if (e != cudaSuccess) return e;
+  const int tiles = ad_max_tiles(a.T, a.count), rp = ad_rank_up(a.r), stages = ad_stages(rp, elem);
   a.ctas = 1;
-  while (a.ctas < kAdMaxCtas && tiles * a.ctas < 3 * sm_count) a.ctas *= 2;
+  while (a.ctas < kAdMaxCtas && tiles * a.ctas < sm_count + sm_count / 2) a.ctas *= 2;
   const dim3 grid(a.ctas * (tiles < kAdMaxClusters ? tiles : kAdMaxClusters));
   auto go = [&](auto kernel) {
-    return launch_cluster(kernel, a.ctas, grid, dim3(kAdThreads), ad_smem_bytes(a.r, (int)sizeof(T)), st, pdl, a);
+    return launch_cluster(kernel, a.ctas, grid, dim3(kAdThreads), stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem), st, pdl, a, stages);
   };
-  return ad_rtw(a.r) == 1 ? go(adapters_kernel<X, T, 1>) : ad_rtw(a.r) == 2 ? go(adapters_kernel<X, T, 2>) : go(adapters_kernel<X, T, 4>);
+  return rp == 16 ? go(adapters_tile_kernel<X, T, 16>) : rp == 32 ? go(adapters_tile_kernel<X, T, 32>)
+       : rp == 64 ? go(adapters_tile_kernel<X, T, 64>) : go(adapters_tile_kernel<X, T, 128>);
 }
 // Raises the kernels' limit of dynamic shared memory where the default does not do.
+template <typename X, typename T>
 inline cudaError_t adapters_set_limits() {
   cudaError_t e = cudaSuccess;
-  auto raise = [&](auto kernel, int elem) {
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ad_smem_bytes(kAdMaxRank, elem));
+  auto raise = [&](auto kernel, int bytes) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  raise(adapters_kernel<float, float, 4>, 4);
-  raise(adapters_kernel<bf16, bf16, 4>, 2);
-  raise(adapters_kernel<__nv_fp8_e4m3, bf16, 4>, 2);
+  raise(adapters_few_kernel<X, T, 4>, ad_smem_bytes(kAdMaxRank, (int)sizeof(T)));
+  raise(adapters_tile_kernel<X, T, 16>, 224 * 1024);
+  raise(adapters_tile_kernel<X, T, 32>, 224 * 1024);
+  raise(adapters_tile_kernel<X, T, 64>, 224 * 1024);
+  raise(adapters_tile_kernel<X, T, 128>, 224 * 1024);
   return e;
 }
 

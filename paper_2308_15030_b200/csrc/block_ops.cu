@@ -149,7 +149,8 @@ int32_t swapmoe_adapters_create(swapmoe_adapters_t** out, const swapmoe_adapters
   b->tiles = reinterpret_cast<AdapterTile*>(b->ws);
   b->n_tiles = reinterpret_cast<int32_t*>(b->ws + tiles);
   b->perm = reinterpret_cast<int32_t*>(b->ws + tiles + 256);
-  if (adapters_set_limits() != cudaSuccess) {
+  const cudaError_t limits = c.dtype == SWAPMOE_F32 ? adapters_set_limits<float, float>() : adapters_set_limits<bf16, bf16>();
+  if (limits != cudaSuccess || (c.dtype == SWAPMOE_BF16 && adapters_set_limits<__nv_fp8_e4m3, bf16>() != cudaSuccess)) {
     cudaGetLastError();
     swapmoe_adapters_destroy(b);
     return SWAPMOE_ERR_CUDA;
