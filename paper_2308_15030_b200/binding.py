@@ -196,27 +196,6 @@ def _invalid(where: str, what: str) -> SwapMoEError:
     return SwapMoEError(-1, "%s: %s" % (where, what))
 
 
-def _dtype_of(t, where: str) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
-    raise _invalid(where, "float32 or bfloat16 rows expected, got %s" % t.dtype)
-
-
-def _row_stride(t, n_rows: int, width: int, dtype, device, where: str, name: str) -> int:
-    """Stride of the rows of a CUDA tensor [>= n_rows, width] of `dtype` on `device` whose rows are contiguous."""
-    if t.dtype != dtype or t.device != device or t.dim() != 2:
-        raise _invalid(where, "%s: a 2-d %s tensor on %s expected, got %d-d %s on %s" % (
-            name, dtype, device, t.dim(), t.dtype, t.device))
-    rows, w = t.shape
-    if rows < n_rows or w != width or (width > 1 and t.stride(1) != 1):
-        raise _invalid(where, "%s: [%d, %d] with contiguous rows expected, got %s, strides %s" % (
-            name, n_rows, width, tuple(t.shape), t.stride()))
-    return t.stride(0) if rows > 1 else max(width, t.stride(0))
-
-
 def _vector(t, n: int, dtype, device, where: str, name: str) -> int:
     if t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
         raise _invalid(where, "%s: %d contiguous values of %s on %s expected, got %s of %s on %s" % (
@@ -224,16 +203,32 @@ def _vector(t, n: int, dtype, device, where: str, name: str) -> int:
     return t.data_ptr()
 
 
-def _enqueue(where: str, device, stream, fn, *args) -> None:
-    """Calls fn(*args, stream) with `device` current; without a stream on the device's current one."""
-    import torch
-    if device.type != "cuda":
-        raise _invalid(where, "CUDA tensors expected, got %s" % device)
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            _check(fn(*args, _stream_ptr(stream)), where)
-    else:
-        _check(fn(*args, _stream_ptr(stream)), where)
+def _fail(status: int, where: str, text) -> None:
+    raise SwapMoEError(status, where) if text is None else SwapMoEError(status, "%s: %s" % (where, text))
+
+
+_marshal = None
+
+
+def marshal():
+    """The extension that checks and passes the arguments of the calls below (csrc/marshal.c; built if needed)."""
+    global _marshal
+    if _marshal is None:
+        import importlib.util
+        import torch
+        path = _build.MARSHAL if os.path.exists(_build.MARSHAL) and os.environ.get("SWAPMOE_NO_REBUILD") \
+            else _build.build_marshal()
+        spec = importlib.util.spec_from_file_location("paper_2308_15030_b200._marshal", path)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        L = lib()
+        m.init(_fail, tuple(ctypes.cast(f, ctypes.c_void_p).value for f in
+                            (L.swapmoe_rms_norm, L.swapmoe_route, L.swapmoe_adapters_forward)),
+               (torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.int32),
+               (torch._C._cuda_getDevice, torch._C._cuda_setDevice, torch._C._cuda_getCurrentRawStream)
+               if hasattr(torch._C, "_cuda_getCurrentRawStream") else (None, None, None))
+        _marshal = m
+    return _marshal
 
 
 def rms_norm(x, weight, eps: float, out=None, residual=None, residual_out=None, out8=None, scales=None, group: int = 0,
@@ -245,33 +240,7 @@ def rms_norm(x, weight, eps: float, out=None, residual=None, residual_out=None, 
     ``group`` columns (32, 64, 128 or 256; scales [T, ceil(d / group)]).  ``residual`` may be float32 beside bfloat16
     rows.  Rows may be strided; residual_out may be residual or x, out may be x.
     """
-    import torch
-    where = "swapmoe_rms_norm"
-    if x.dim() != 2:
-        raise _invalid(where, "x: [T, d] expected, got %s" % (tuple(x.shape),))
-    T, d = x.shape
-    dev, dtype = x.device, _dtype_of(x, where)
-    rdtype = dtype if residual is None else _dtype_of(residual, where)
-    rt = None if residual is None else residual.dtype
-    if residual_out is not None and residual is None:
-        raise _invalid(where, "residual_out without residual")
-    if (out8 is None) != (scales is None):
-        raise _invalid(where, "out8 and scales go together")
-    n_scales = -(-d // group) if group > 0 else 1
-    if scales is not None and scales.dim() == 1 and n_scales == 1:
-        scales = scales.unsqueeze(1)
-    a = RmsNormArgs(
-        x.data_ptr(), None if residual is None else residual.data_ptr(), _vector(weight, d, x.dtype, dev, where, "weight"),
-        None if residual_out is None else residual_out.data_ptr(), None if out is None else out.data_ptr(),
-        None if out8 is None else out8.data_ptr(), None if scales is None else scales.data_ptr(),
-        _row_stride(x, T, d, x.dtype, dev, where, "x"),
-        0 if residual is None else _row_stride(residual, T, d, rt, dev, where, "residual"),
-        0 if residual_out is None else _row_stride(residual_out, T, d, rt, dev, where, "residual_out"),
-        0 if out is None else _row_stride(out, T, d, x.dtype, dev, where, "out"),
-        0 if out8 is None else _row_stride(out8, T, d, torch.float8_e4m3fn, dev, where, "out8"),
-        0 if scales is None else _row_stride(scales, T, n_scales, torch.float32, dev, where, "scales"),
-        T, d, dtype, rdtype, int(group), eps)
-    _enqueue(where, dev, stream, lib().swapmoe_rms_norm, ctypes.byref(a))
+    (_marshal or marshal()).rms_norm(x, weight, eps, out, residual, residual_out, out8, scales, group, stream)
 
 
 def route(gate: Gate, logits, experts, weights, bias=None, expert_to_slot=None, slots=None, stream=None) -> None:
@@ -281,20 +250,7 @@ def route(gate: Gate, logits, experts, weights, bias=None, expert_to_slot=None, 
     added to the scores for the choice only.  With ``expert_to_slot`` [E] int32 (-1 = not resident) only resident experts are
     chosen and ``slots`` [T, top_k] int32 receives their entries.
     """
-    import torch
-    where = "swapmoe_route"
-    if logits.dim() != 2 or experts.dim() != 2:
-        raise _invalid(where, "logits [T, E] and experts [T, top_k] expected")
-    (T, E), k, dev = logits.shape, experts.shape[1], logits.device
-    stride = _row_stride(logits, T, E, torch.float32, dev, where, "logits")
-    if (expert_to_slot is None) != (slots is None):
-        raise _invalid(where, "expert_to_slot and slots go together")
-    _enqueue(where, dev, stream, lib().swapmoe_route, ctypes.byref(gate), logits.data_ptr(), stride,
-             None if bias is None else _vector(bias, E, torch.float32, dev, where, "bias"),
-             None if expert_to_slot is None else _vector(expert_to_slot, E, torch.int32, dev, where, "expert_to_slot"),
-             T, E, k, _vector(experts, T * k, torch.int32, dev, where, "experts"),
-             _vector(weights, T * k, torch.float32, dev, where, "weights"),
-             None if slots is None else _vector(slots, T * k, torch.int32, dev, where, "slots"))
+    (_marshal or marshal()).route(gate, logits, experts, weights, bias, expert_to_slot, slots, stream)
 
 
 class AdapterBank:
@@ -337,16 +293,9 @@ class AdapterBank:
     def forward(self, x, ids, y, out, x_scales=None, stream=None) -> None:
         """x [T, d_in] in the bank's dtype, or torch.float8_e4m3fn with x_scales [T] float32; ids [T] int32; y [T, d_out] or
         None (zeros); out [T, d_out], may be y.  Rows may be strided."""
-        import torch
-        c, where, dev = self.cfg, "swapmoe_adapters_forward", self._device
-        T = x.shape[0]
-        _enqueue(where, dev, stream, lib().swapmoe_adapters_forward, self._h, x.data_ptr(),
-                 _row_stride(x, T, c.d_in, self._dtype if x_scales is None else torch.float8_e4m3fn, dev, where, "x"),
-                 None if x_scales is None else _vector(x_scales, T, torch.float32, dev, where, "x_scales"),
-                 _vector(ids, T, torch.int32, dev, where, "ids"),
-                 None if y is None else y.data_ptr(),
-                 0 if y is None else _row_stride(y, T, c.d_out, self._dtype, dev, where, "y"), out.data_ptr(),
-                 _row_stride(out, T, c.d_out, self._dtype, dev, where, "out"), T)
+        c = self.cfg
+        (_marshal or marshal()).adapters_forward(self._h.value, self._device.index, self._dtype, c.d_in, c.d_out, x, ids, y, out,
+                                                 x_scales, stream)
 
 
 class Layer:

@@ -4,10 +4,13 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libswapmoe.so")
+MARSHAL_SRC = os.path.join(CSRC, "marshal.c")
+MARSHAL = os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 TRACE_LIB = os.path.join(_HERE, "libswapmoe_trace.so")
 SOURCES = ["api.cu", "route_static.cu", "block_ops.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -47,5 +50,18 @@ def build(force: bool = False, verbose: bool = False, trace: bool = False) -> st
     return LIB
 
 
+def build_marshal(force: bool = False) -> str:
+    """Compile the CPython extension that marshals the hot calls' arguments (gcc), if missing or older than its sources."""
+    sources = [MARSHAL_SRC, os.path.join(os.path.dirname(_HERE), "include", "swapmoe.h")]
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(map(os.path.getmtime, sources)):
+        return MARSHAL
+    tmp = MARSHAL + ".tmp.%d" % os.getpid()
+    subprocess.run(["gcc", "-O2", "-std=c11", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"], "-o", tmp, MARSHAL_SRC],
+                   check=True)
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 if __name__ == "__main__":
+    print(build_marshal(force=True))
     print(build(force=True, verbose="-v" in sys.argv, trace="--trace" in sys.argv))
