@@ -122,7 +122,7 @@ int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits, int64_t s
   a.logits = logits; a.bias = bias; a.expert_to_slot = expert_to_slot;
   a.experts = experts; a.weights = weights; a.slots = slots;
   a.stride = stride; a.T = T; a.E = E; a.k = top_k;
-  return launched(route_groups_launch(a, static_cast<cudaStream_t>(stream), true));
+  return launched(route_groups_launch(a, current_sm_count(), static_cast<cudaStream_t>(stream), true));
 }
 
 int32_t swapmoe_adapters_create(swapmoe_adapters_t** out, const swapmoe_adapters_config_t* cfg) {

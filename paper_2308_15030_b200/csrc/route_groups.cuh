@@ -7,6 +7,10 @@
 // A warp routes a token; lane l holds the experts l * N ... l * N + N - 1, so the order of lanes is that of indices and a tie goes to
 // the lowest lane.  The order of the choices is that of 64-bit scores: of thousands of tokens some have two experts closer than
 // fp32 tells apart.  Without a bias, and with groups valued by their best expert, it is that of the logits themselves.
+//
+// Bound by instructions, not by bytes (a row is 4 E bytes): so scores are fp32, and only a token whose choice hangs on a gap that is
+// not clear of their error is routed again in 64 bits (about one in 200; with 64 bits for all of them 16384 x 256 took 60 us).  Each lane sorts its
+// experts once, with their places in the keys' last bits; then a choice is one warp reduction, one vote and a shift of the winner's list.
 #pragma once
 #include <math_constants.h>
 
@@ -58,11 +62,14 @@ __device__ __forceinline__ float warp_max(float v) {
 __device__ __forceinline__ float exp_below(float l, float m) { return l == m ? 1.f : expf(l - m); }
 
 // The experts chosen for one token by a warp: lane j < k returns the j-th one's index, or -1 where the allowed ones ran out.
-// l: logits of the lane's experts (NaN replaced by -infinity), allow: which of them may be chosen, s_choice: E doubles of the warp's own.
+// row: logits, allow: which of the lane's experts may be chosen, s_choice: E doubles of the warp's own.  In 64 bits, out of line.
 template <int N>
-__device__ __forceinline__ int route_choose(const RouteGate& g, const float (&l)[N], const float* bias, uint32_t allow, int E, int k,
-                                            double* s_choice) {
+static __device__ __noinline__ int route_choose_exact(const RouteGate& g, const float* row, const float* bias, uint32_t allow, int E,
+                                                      int k, double* s_choice) {
   const int lane = threadIdx.x & 31, e0 = lane * N;
+  float l[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) l[i] = e0 + i < E ? fmaxf(row[e0 + i], -CUDART_INF_F) : -CUDART_INF_F;
   unsigned long long key[N];
   const bool groups = g.n_groups > 1;
   const bool by_score = bias != nullptr || (groups && g.group_top > 1);
@@ -157,6 +164,202 @@ __device__ __forceinline__ int route_choose(const RouteGate& g, const float (&l)
   return mine;
 }
 
+// ----------------------------------------------------------------------------- fp32, with a check of the gaps
+__host__ __device__ constexpr int route_pow2(int n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : n <= 8 ? 8 : 16; }
+
+// Descending order of M = 2^m keys (Batcher's odd-even merge sort: 19 exchanges for eight, 63 for sixteen).
+template <int M>
+__device__ __forceinline__ void sort_keys(uint32_t (&k)[M]) {
+#pragma unroll
+  for (int p = 1; p < M; p *= 2)
+#pragma unroll
+    for (int h = p; h >= 1; h /= 2)
+#pragma unroll
+      for (int j = h % p; j + h < M; j += 2 * h)
+#pragma unroll
+        for (int i = 0; i < h; ++i)
+          if (i + j + h < M && (i + j) / (2 * p) == (i + j + h) / (2 * p)) {
+            const uint32_t x = k[i + j], y = k[i + j + h];
+            k[i + j] = max(x, y);
+            k[i + j + h] = min(x, y);
+          }
+}
+
+// What a warp keeps for all its tokens: which of the lane's experts may be chosen, and how groups lie on the lanes.
+struct RouteLane {
+  uint32_t allow;
+  int have;                  // aligned groups: allowed experts of the lane's group
+};
+
+// Lanes per group where groups are whole runs of 2^i lanes, else 0.
+__host__ __device__ constexpr int route_group_lanes(int group_size, int n) {
+  const int lanes = group_size % n == 0 ? group_size / n : 0;
+  return lanes > 0 && (lanes & (lanes - 1)) == 0 && lanes <= 32 ? lanes : 0;
+}
+
+template <int N>
+__device__ __forceinline__ RouteLane route_lane(const RouteGate& g, const int32_t* expert_to_slot, int E) {
+  const int lane = threadIdx.x & 31;
+  RouteLane r;
+  r.allow = 0u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = lane * N + i;
+    if (e < E && (expert_to_slot == nullptr || expert_to_slot[e] >= 0)) r.allow |= 1u << i;
+  }
+  r.have = __popc(r.allow);
+  const int lanes = route_group_lanes(g.group_size, N);
+  for (int o = 1; o < lanes; o <<= 1) r.have += __shfl_xor_sync(0xffffffffu, r.have, o);
+  return r;
+}
+
+// As route_choose_exact, from the lane's logits l (NaN replaced by -infinity) and biases b.  *clear: no gap that the choice hangs on is
+// within the error of what was compared; if not, the result is not to be used.
+template <int N>
+__device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float (&l)[N], const float (&b)[N], bool with_bias,
+                                                 const RouteLane& rl, int E, int k, float* s_choice, bool* clear) {
+  constexpr int M = route_pow2(N);
+  constexpr uint32_t kPlace = M - 1;                        // bits of a key that hold the expert's place (first places larger)
+  const int lane = threadIdx.x & 31, e0 = lane * N;
+  const bool groups = g.n_groups > 1 && g.topk_groups < g.n_groups;
+  const bool by_score = with_bias || (g.n_groups > 1 && g.group_top > 1);
+  float c[N], error = 0.f;                                  // error: bound on a choice's, but for its own rounding
+  if (by_score) {
+    if (g.score == SWAPMOE_SCORE_SOFTMAX) {
+      float m = -CUDART_INF_F, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) m = fmaxf(m, (rl.allow >> i) & 1u ? l[i] : -CUDART_INF_F);
+      m = warp_max(m);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        c[i] = (rl.allow >> i) & 1u ? (l[i] == m ? 1.f : __expf(l[i] - m)) : 0.f;
+        sum += c[i];
+      }
+      const float inv = 1.f / warp_sum(sum);
+#pragma unroll
+      for (int i = 0; i < N; ++i) c[i] *= inv;
+      // exponentials: (2 + 1.2 |x|) 2^-23 of themselves, that is 1.5e-7 of the largest score (1 / sum) where it counts; sums of up to 21
+      // steps, reciprocal and product: 24 x 2^-24 of the score
+      error = 2e-6f * inv;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) c[i] = __fdividef(1.f, 1.f + __expf(-l[i]));
+      // s (1 - s) (2 + 1.2 |x|) 2^-23 <= 1e-7 from the exponential, three roundings of at most 2^-23 each
+      error = 5e-7f;
+    }
+    if (with_bias)
+#pragma unroll
+      for (int i = 0; i < N; ++i) c[i] += b[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = l[i];
+  }
+  uint32_t key[M];
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    key[i] = 0u;
+    if (i < N && ((rl.allow >> (i < N ? i : 0)) & 1u)) {
+      const float v = fmaxf(c[i < N ? i : 0], -CUDART_INF_F);          // NaN (of a bias) as -infinity
+      const uint32_t u = __float_as_uint(v);
+      key[i] = ((u & 0x80000000u ? ~u : u | 0x80000000u) & ~kPlace) | (kPlace - i);
+    }
+  }
+  auto value_of = [&](uint32_t q) { return gate_key_value(q & ~kPlace); };
+  constexpr float kCut = 2.f * M * 0x1p-23f;                // what the places cost a pair of keys, and the roundings, relative
+  float gap = CUDART_INF_F, first = 0.f, last = 0.f, group_gap = CUDART_INF_F, group_size = 0.f;
+  const int lanes = groups ? route_group_lanes(g.group_size, N) : 0;
+  if (groups && lanes == 0) {
+    // groups that do not lie on whole runs of lanes: lane q values group q from shared memory
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (e0 + i < E) s_choice[e0 + i] = (rl.allow >> i) & 1u ? fmaxf(c[i], -CUDART_INF_F) : CUDART_NAN_F;
+    __syncwarp();
+  }
+  if (lanes > 0) sort_keys<M>(key);
+  if (groups) {
+    float v1 = -CUDART_INF_F, v2 = -CUDART_INF_F;
+    int have = rl.have;
+    if (lanes > 0) {
+      v1 = key[0] ? value_of(key[0]) : -CUDART_INF_F;
+      if (M > 1) v2 = key[M > 1 ? 1 : 0] ? value_of(key[M > 1 ? 1 : 0]) : -CUDART_INF_F;
+      for (int o = 1; o < lanes; o <<= 1) {
+        const float w1 = __shfl_xor_sync(0xffffffffu, v1, o), w2 = __shfl_xor_sync(0xffffffffu, v2, o);
+        v2 = fmaxf(fminf(v1, w1), fmaxf(v2, w2));
+        v1 = fmaxf(v1, w1);
+      }
+      if (e0 >= E) have = 0;
+    } else {
+      have = 0;
+      if (lane < g.n_groups)
+        for (int i = 0; i < g.group_size; ++i) {
+          const float v = s_choice[lane * g.group_size + i];
+          if (v != v) continue;
+          ++have;
+          v2 = fmaxf(v2, fminf(v1, v));
+          v1 = fmaxf(v1, v);
+        }
+    }
+    const float value = g.group_top > 1 && have > 1 ? v1 + v2 : v1;
+    // (the error of a sum goes by its terms)
+    group_size = __uint_as_float(__reduce_max_sync(0xffffffffu, have == 0 ? 0u
+        : __float_as_uint(fmaxf(fabsf(v1), g.group_top > 1 && have > 1 ? fabsf(v2) : 0.f))));
+    uint32_t gk = 0u;
+    if (have > 0) {
+      const uint32_t u = __float_as_uint(value + 0.f);
+      gk = u & 0x80000000u ? ~u : u | 0x80000000u;
+    }
+    uint32_t kept = 0u;                                     // bit per group, or per lane of aligned groups
+    float front = 0.f;
+    for (int taken = 0, pool = 0;; ++taken) {
+      const uint32_t best = __reduce_max_sync(0xffffffffu, gk);
+      if (best == 0u) break;
+      const float v = gate_key_value(best);
+      if (taken > 0) group_gap = fminf(group_gap, front - v);
+      front = v;
+      if (taken >= g.topk_groups && pool >= k) break;
+      const int winner = __ffs(__ballot_sync(0xffffffffu, gk == best)) - 1;
+      pool += __shfl_sync(0xffffffffu, have, winner);
+      const bool mine = lanes > 0 ? (lane & ~(lanes - 1)) == winner : lane == winner;
+      if (mine) gk = 0u;
+      kept |= __ballot_sync(0xffffffffu, mine);
+    }
+    if (lanes > 0) {
+      if (!((kept >> lane) & 1u))
+#pragma unroll
+        for (int i = 0; i < M; ++i) key[i] = 0u;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (!((kept >> (__umulhi(2u * (uint32_t)(e0 + i), g.group_magic) & 31u)) & 1u)) key[i] = 0u;
+    }
+  }
+  if (lanes == 0) sort_keys<M>(key);
+  int mine = -1;
+  float front = 0.f;
+  for (int j = 0;; ++j) {
+    const uint32_t top = __reduce_max_sync(0xffffffffu, key[0]);
+    if (top == 0u) break;
+    const float v = value_of(top);
+    if (j > 0) gap = fminf(gap, front - v);
+    else first = v;
+    last = front = v;
+    if (j == k) break;
+    const int winner = __ffs(__ballot_sync(0xffffffffu, key[0] == top)) - 1;
+    if (lane == j) mine = winner * N + (int)(kPlace - (top & kPlace));
+    if (lane == winner) {
+#pragma unroll
+      for (int i = 0; i + 1 < M; ++i) key[i] = key[i + 1];
+      key[M - 1] = 0u;
+    }
+  }
+  // (infinities and NaN fail the comparisons)
+  const float slack = 2.f * error + kCut * fmaxf(fabsf(first), fabsf(last));
+  const float group_slack = 4.f * error + 2.f * kCut * group_size;
+  *clear = gap > slack && slack < CUDART_INF_F && group_gap > group_slack && group_slack < CUDART_INF_F;
+  return mine;
+}
+
 // Weight of the chosen expert of every lane j < k (`chosen` < 0: none, weight 0) from its logit lc.
 template <int N>
 __device__ __forceinline__ float route_weight(const RouteGate& g, const float (&l)[N], uint32_t allow, int chosen, float lc) {
@@ -185,41 +388,88 @@ __device__ __forceinline__ float route_weight(const RouteGate& g, const float (&
   return chosen >= 0 ? w * g.scale : 0.f;
 }
 
+// One row's logits of the lane's experts, NaN as -infinity.  vec: rows start at multiples of 16 bytes and E is a multiple of N.
 template <int N>
-__global__ void __launch_bounds__(kRouteWarps * 32) route_groups_kernel(const RouteGroupsArgs a) {
-  __shared__ double s_choice[kRouteWarps][32 * N];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long token = (long long)blockIdx.x * kRouteWarps + warp;
-  pdl_wait();
-  pdl_trigger();
-  if (token >= a.T) return;
-  const float* row = a.logits + token * a.stride;
-  float l[N];
-  uint32_t allow = 0u;
+__device__ __forceinline__ void route_load(const float* row, int E, bool vec, float (&l)[N]) {
+  const int e0 = (threadIdx.x & 31) * N;
+  if constexpr (N % 4 == 0) {
+    if (vec) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int e = lane * N + i;
-    l[i] = -CUDART_INF_F;
-    if (e < a.E) {
-      l[i] = fmaxf(row[e], -CUDART_INF_F);
-      if (a.expert_to_slot == nullptr || a.expert_to_slot[e] >= 0) allow |= 1u << i;
+      for (int i = 0; i < N; i += 4) {
+        float4 v = make_float4(-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F);
+        if (e0 < E) v = *reinterpret_cast<const float4*>(row + e0 + i);
+        l[i] = v.x; l[i + 1] = v.y; l[i + 2] = v.z; l[i + 3] = v.w;
+      }
+      return;
     }
   }
-  const int e = route_choose<N>(a.gate, l, a.bias, allow, a.E, a.k, s_choice[warp]);
-  const float lc = e >= 0 ? fmaxf(row[e], -CUDART_INF_F) : -CUDART_INF_F;
-  const float w = route_weight<N>(a.gate, l, allow, e, lc);
-  if (lane < a.k) {
-    a.experts[token * a.k + lane] = e;
-    a.weights[token * a.k + lane] = w;
-    if (a.slots != nullptr) a.slots[token * a.k + lane] = e >= 0 ? a.expert_to_slot[e] : -1;
+#pragma unroll
+  for (int i = 0; i < N; ++i) l[i] = e0 + i < E ? row[e0 + i] : -CUDART_INF_F;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kRouteWarps * 32, N <= 8 ? 8 : 4) route_groups_kernel(const RouteGroupsArgs a, int vec) {
+  __shared__ double s_choice[kRouteWarps][32 * N];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_wait();
+  pdl_trigger();
+  long long token = (long long)blockIdx.x * kRouteWarps + warp;
+  if (token >= a.T) return;
+  const long long step = (long long)gridDim.x * kRouteWarps;
+  const float* row = a.logits + token * a.stride;
+  float l[N], next[N], b[N];
+  route_load<N>(row, a.E, vec, next);
+  const RouteLane rl = route_lane<N>(a.gate, a.expert_to_slot, a.E);
+#pragma unroll
+  for (int i = 0; i < N; ++i) b[i] = a.bias != nullptr && lane * N + i < a.E ? a.bias[lane * N + i] : 0.f;
+#pragma unroll 1
+  for (; token < a.T; token += step, row += step * a.stride) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) l[i] = fmaxf(next[i], -CUDART_INF_F);
+    if (token + step < a.T) route_load<N>(row + step * a.stride, a.E, vec, next);
+    bool clear;
+    int e = route_choose_fast<N>(a.gate, l, b, a.bias != nullptr, rl, a.E, a.k, reinterpret_cast<float*>(s_choice[warp]), &clear);
+    if (!clear) e = route_choose_exact<N>(a.gate, row, a.bias, rl.allow, a.E, a.k, s_choice[warp]);
+    const float lc = e >= 0 ? fmaxf(row[e], -CUDART_INF_F) : -CUDART_INF_F;
+    const float w = route_weight<N>(a.gate, l, rl.allow, e, lc);
+    if (lane < a.k) {
+      a.experts[token * a.k + lane] = e;
+      a.weights[token * a.k + lane] = w;
+      if (a.slots != nullptr) a.slots[token * a.k + lane] = e >= 0 ? a.expert_to_slot[e] : -1;
+    }
   }
 }
 
-inline cudaError_t route_groups_launch(const RouteGroupsArgs& a, cudaStream_t st, bool pdl) {
-  const dim3 grid((unsigned)((a.T + kRouteWarps - 1) / kRouteWarps)), block(kRouteWarps * 32);
-  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, block, 0, st, pdl, a); };
-  return a.E <= 32 ? go(route_groups_kernel<1>) : a.E <= 64 ? go(route_groups_kernel<2>) : a.E <= 128 ? go(route_groups_kernel<4>)
-       : a.E <= 256 ? go(route_groups_kernel<8>) : go(route_groups_kernel<16>);
+// Experts per lane: the fewest that hold E, or a few more where groups then lie on whole runs of lanes.
+constexpr int kRouteSizes[] = {1, 2, 3, 4, 5, 6, 8, 12, 16};
+inline int route_lane_experts(int E, int n_groups) {
+  int pick = 0;
+  for (int n : kRouteSizes) {
+    if (32 * n < E) continue;
+    if (pick == 0) pick = n;
+    if (n_groups > 1 && n <= 2 * pick && route_group_lanes(E / n_groups, n) > 0) return n;
+  }
+  return pick;
+}
+
+inline cudaError_t route_groups_launch(const RouteGroupsArgs& a, int sm_count, cudaStream_t st, bool pdl) {
+  const int n = route_lane_experts(a.E, a.gate.n_groups);
+  // every warp a token while they last; beyond what the chip holds at once they walk through several (the next row is on its way meanwhile)
+  const long long ctas = ((long long)a.T + kRouteWarps - 1) / kRouteWarps, most = (n <= 8 ? 8ll : 4ll) * (sm_count > 0 ? sm_count : 1);
+  const dim3 grid((unsigned)(ctas < most ? ctas : most)), block(kRouteWarps * 32);
+  const int vec = a.stride % 4 == 0 && reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && a.E % n == 0;
+  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, block, 0, st, pdl, a, vec); };
+  switch (n) {
+    case 1: return go(route_groups_kernel<1>);
+    case 2: return go(route_groups_kernel<2>);
+    case 3: return go(route_groups_kernel<3>);
+    case 4: return go(route_groups_kernel<4>);
+    case 5: return go(route_groups_kernel<5>);
+    case 6: return go(route_groups_kernel<6>);
+    case 8: return go(route_groups_kernel<8>);
+    case 12: return go(route_groups_kernel<12>);
+    default: return go(route_groups_kernel<16>);
+  }
 }
 
 }  // namespace swapmoe
