@@ -53,10 +53,8 @@ __device__ __forceinline__ unsigned long long warp_max_key(unsigned long long ke
   const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(key >> 32) == hi ? (uint32_t)key : 0u);
   return (unsigned long long)hi << 32 | lo;
 }
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
+__device__ __forceinline__ float warp_max(float v) {              // (not for NaN)
+  return gate_key_value(__reduce_max_sync(0xffffffffu, gate_key(v)));
 }
 // exp(l - m) for l <= m; 1 where both are the same infinity.
 __device__ __forceinline__ float exp_below(float l, float m) { return l == m ? 1.f : expf(l - m); }
@@ -188,8 +186,11 @@ __device__ __forceinline__ void sort_keys(uint32_t (&k)[M]) {
 // What a warp keeps for all its tokens: which of the lane's experts may be chosen, and how groups lie on the lanes.
 struct RouteLane {
   uint32_t allow;
+  bool all;                  // no table: every expert may be chosen
   int have;                  // aligned groups: allowed experts of the lane's group
 };
+
+__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
 // Lanes per group where groups are whole runs of 2^i lanes, else 0.
 __host__ __device__ constexpr int route_group_lanes(int group_size, int n) {
@@ -202,6 +203,7 @@ __device__ __forceinline__ RouteLane route_lane(const RouteGate& g, const int32_
   const int lane = threadIdx.x & 31;
   RouteLane r;
   r.allow = 0u;
+  r.all = expert_to_slot == nullptr;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int e = lane * N + i;
@@ -266,7 +268,8 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
   }
   auto value_of = [&](uint32_t q) { return gate_key_value(q & ~kPlace); };
   constexpr float kCut = 2.f * M * 0x1p-23f;                // what the places cost a pair of keys, and the roundings, relative
-  float gap = CUDART_INF_F, first = 0.f, last = 0.f, group_gap = CUDART_INF_F, group_size = 0.f;
+  float group_size = 0.f;
+  uint32_t group_at = 0u, choice_at = 0u;                   // lane i: key of the i-th group, of the i-th choice (0: none)
   const int lanes = groups ? route_group_lanes(g.group_size, N) : 0;
   if (groups && lanes == 0) {
     // groups that do not lie on whole runs of lanes: lane q values group q from shared memory
@@ -310,19 +313,19 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
       gk = u & 0x80000000u ? ~u : u | 0x80000000u;
     }
     uint32_t kept = 0u;                                     // bit per group, or per lane of aligned groups
-    float front = 0.f;
-    for (int taken = 0, pool = 0;; ++taken) {
+    const uint32_t run = lanes > 0 ? (lanes == 32 ? 0xffffffffu : (1u << lanes) - 1u) : 1u;
+    int taken = 0, pool = 0;
+#pragma unroll 1
+    for (;; ++taken) {
       const uint32_t best = __reduce_max_sync(0xffffffffu, gk);
-      if (best == 0u) break;
-      const float v = gate_key_value(best);
-      if (taken > 0) group_gap = fminf(group_gap, front - v);
-      front = v;
-      if (taken >= g.topk_groups && pool >= k) break;
+      if (lane == taken) group_at = best;
+      if (best == 0u || (taken >= g.topk_groups && pool >= k)) break;
       const int winner = __ffs(__ballot_sync(0xffffffffu, gk == best)) - 1;
-      pool += __shfl_sync(0xffffffffu, have, winner);
-      const bool mine = lanes > 0 ? (lane & ~(lanes - 1)) == winner : lane == winner;
-      if (mine) gk = 0u;
-      kept |= __ballot_sync(0xffffffffu, mine);
+      const uint32_t these = run << winner;
+      kept |= these;
+      if ((these >> lane) & 1u) gk = 0u;
+      // (without a table topk_groups groups hold k experts)
+      pool = rl.all ? k : pool + __shfl_sync(0xffffffffu, have, winner);
     }
     if (lanes > 0) {
       if (!((kept >> lane) & 1u))
@@ -336,27 +339,30 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
   }
   if (lanes == 0) sort_keys<M>(key);
   int mine = -1;
-  float front = 0.f;
-  for (int j = 0;; ++j) {
+#pragma unroll 1
+  for (int j = 0; j < k; ++j) {
     const uint32_t top = __reduce_max_sync(0xffffffffu, key[0]);
     if (top == 0u) break;
-    const float v = value_of(top);
-    if (j > 0) gap = fminf(gap, front - v);
-    else first = v;
-    last = front = v;
-    if (j == k) break;
     const int winner = __ffs(__ballot_sync(0xffffffffu, key[0] == top)) - 1;
-    if (lane == j) mine = winner * N + (int)(kPlace - (top & kPlace));
+    if (lane == j) { choice_at = top; mine = winner; }
     if (lane == winner) {
 #pragma unroll
       for (int i = 0; i + 1 < M; ++i) key[i] = key[i + 1];
       key[M - 1] = 0u;
     }
   }
-  // (infinities and NaN fail the comparisons)
-  const float slack = 2.f * error + kCut * fmaxf(fabsf(first), fabsf(last));
+  const uint32_t behind = __reduce_max_sync(0xffffffffu, key[0]);       // the best one that was not chosen
+  if (lane == k) choice_at = behind;
+  if (mine >= 0) mine = mine * N + (int)(kPlace - (choice_at & kPlace));
+  // the gaps between neighbours of the two lists, and the largest magnitude in them (infinities fail the comparison)
+  const uint32_t below = __shfl_down_sync(0xffffffffu, choice_at, 1), group_below = __shfl_down_sync(0xffffffffu, group_at, 1);
+  const float v = value_of(choice_at), w = gate_key_value(group_at);
+  const uint32_t size = __reduce_max_sync(0xffffffffu, choice_at != 0u ? magnitude_bits(v) : 0u);
+  const float slack = 2.f * error + kCut * __uint_as_float(size);
   const float group_slack = 4.f * error + 2.f * kCut * group_size;
-  *clear = gap > slack && slack < CUDART_INF_F && group_gap > group_slack && group_slack < CUDART_INF_F;
+  const bool near = (lane < k && below != 0u && !(v - value_of(below) > slack)) ||
+                    (lane < 31 && group_below != 0u && !(w - gate_key_value(group_below) > group_slack));
+  *clear = !__any_sync(0xffffffffu, near) && size < 0x7f800000u && group_size < CUDART_INF_F;
   return mine;
 }
 
@@ -368,11 +374,11 @@ __device__ __forceinline__ float route_weight(const RouteGate& g, const float (&
   if (g.renorm) {
     // s / sum of s from values relative to the largest chosen one: scores far below 1 keep their ratios
     const float m = warp_max(chosen >= 0 ? lc : low);
+    // (quotients by __fdividef: denominators are at least 0.5; where 1 + exp(-l) leaves its range, beyond 2^126, the score is 0)
     if (g.score == SWAPMOE_SCORE_SOFTMAX) w = exp_below(lc, m);
-    else w = m >= 0.f ? 1.f / (1.f + expf(-lc)) : exp_below(lc, m) / (1.f + expf(lc));
+    else w = m >= 0.f ? __fdividef(1.f, 1.f + expf(-lc)) : __fdividef(exp_below(lc, m), 1.f + expf(lc));
     w = chosen >= 0 ? w : 0.f;
-    const float sum = warp_sum(w);
-    w = w / sum;
+    w = __fdividef(w, warp_sum(w));
   } else if (g.score == SWAPMOE_SCORE_SOFTMAX) {
     float m = low;
 #pragma unroll
@@ -381,9 +387,9 @@ __device__ __forceinline__ float route_weight(const RouteGate& g, const float (&
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) sum += (allow >> i) & 1u ? exp_below(l[i], m) : 0.f;
-    w = exp_below(lc, m) / warp_sum(sum);
+    w = __fdividef(exp_below(lc, m), warp_sum(sum));
   } else {
-    w = 1.f / (1.f + expf(-lc));
+    w = __fdividef(1.f, 1.f + expf(-lc));
   }
   return chosen >= 0 ? w * g.scale : 0.f;
 }
