@@ -59,6 +59,12 @@ __device__ __forceinline__ float warp_max(float v) {              // (not for Na
 // exp(l - m) for l <= m; 1 where both are the same infinity.
 __device__ __forceinline__ float exp_below(float l, float m) { return l == m ? 1.f : expf(l - m); }
 
+// Lanes per group where groups are whole runs of 2^i lanes, else 0.
+__host__ __device__ constexpr int route_group_lanes(int group_size, int n) {
+  const int lanes = group_size % n == 0 ? group_size / n : 0;
+  return lanes > 0 && (lanes & (lanes - 1)) == 0 && lanes <= 32 ? lanes : 0;
+}
+
 // The experts chosen for one token by a warp: lane j < k returns the j-th one's index, or -1 where the allowed ones ran out.
 // row: logits, allow: which of the lane's experts may be chosen, s_choice: E doubles of the warp's own.  In 64 bits, out of line.
 template <int N>
@@ -107,27 +113,47 @@ static __device__ __noinline__ int route_choose_exact(const RouteGate& g, const 
 #pragma unroll
   for (int i = 0; i < N; ++i) key[i] = (allow >> i) & 1u ? choice_key(c[i]) : 0ull;
   if (groups) {
-    // lane g values group g
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (e0 + i < E) s_choice[e0 + i] = (allow >> i) & 1u ? c[i] : CUDART_NAN;      // NaN: not to be chosen
-    __syncwarp();
+    // lane g values group g: groups on whole runs of lanes from the lanes' two best choices, others from shared memory
     unsigned long long value = 0ull;
     int have = 0;
-    if (lane < g.n_groups) {
-      unsigned long long k1 = 0ull, k2 = 0ull;
-      double v1 = 0.0, v2 = 0.0;
-      for (int i = 0; i < g.group_size; ++i) {
-        const double v = s_choice[lane * g.group_size + i];
-        if (v != v) continue;
-        ++have;
-        const unsigned long long kv = choice_key(v);
-        if (kv > k1) { k2 = k1; v2 = v1; k1 = kv; v1 = v; }
-        else if (kv > k2) { k2 = kv; v2 = v; }
+    const int lanes = route_group_lanes(g.group_size, N);
+    double v1 = -CUDART_INF, v2 = -CUDART_INF;
+    if (lanes > 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if ((allow >> i) & 1u) {
+          const double v = c[i] == c[i] ? c[i] : -CUDART_INF;
+          v2 = fmax(v2, fmin(v1, v));
+          v1 = fmax(v1, v);
+          ++have;
+        }
+      for (int o = 1; o < lanes; o <<= 1) {
+        const double w1 = __shfl_xor_sync(0xffffffffu, v1, o), w2 = __shfl_xor_sync(0xffffffffu, v2, o);
+        have += __shfl_xor_sync(0xffffffffu, have, o);
+        v2 = fmax(fmin(v1, w1), fmax(v2, w2));
+        v1 = fmax(v1, w1);
       }
-      if (have > 0) value = choice_key(g.group_top > 1 && have > 1 ? v1 + v2 : v1);
+      const int from = min(lane * lanes, 31);
+      v1 = __shfl_sync(0xffffffffu, v1, from);
+      v2 = __shfl_sync(0xffffffffu, v2, from);
+      have = __shfl_sync(0xffffffffu, have, from);
+      if (lane >= g.n_groups) have = 0;
+    } else {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (e0 + i < E) s_choice[e0 + i] = !((allow >> i) & 1u) ? CUDART_NAN : c[i] == c[i] ? c[i] : -CUDART_INF;   // NaN: not to be chosen
+      __syncwarp();
+      if (lane < g.n_groups)
+        for (int i = 0; i < g.group_size; ++i) {
+          const double v = s_choice[lane * g.group_size + i];
+          if (v != v) continue;
+          ++have;
+          v2 = fmax(v2, fmin(v1, v));
+          v1 = fmax(v1, v);
+        }
     }
+    if (have > 0) value = choice_key(g.group_top > 1 && have > 1 ? v1 + v2 : v1);
     uint32_t kept = 0u;
     for (int taken = 0, pool = 0; taken < g.topk_groups || pool < k; ++taken) {
       const unsigned long long best = warp_max_key(value);
@@ -191,12 +217,6 @@ struct RouteLane {
 };
 
 __device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-
-// Lanes per group where groups are whole runs of 2^i lanes, else 0.
-__host__ __device__ constexpr int route_group_lanes(int group_size, int n) {
-  const int lanes = group_size % n == 0 ? group_size / n : 0;
-  return lanes > 0 && (lanes & (lanes - 1)) == 0 && lanes <= 32 ? lanes : 0;
-}
 
 template <int N>
 __device__ __forceinline__ RouteLane route_lane(const RouteGate& g, const int32_t* expert_to_slot, int E) {
@@ -313,19 +333,36 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
       gk = u & 0x80000000u ? ~u : u | 0x80000000u;
     }
     uint32_t kept = 0u;                                     // bit per group, or per lane of aligned groups
-    const uint32_t run = lanes > 0 ? (lanes == 32 ? 0xffffffffu : (1u << lanes) - 1u) : 1u;
-    int taken = 0, pool = 0;
+    if (rl.all) {
+      // topk_groups groups hold k experts: a group is kept if fewer than that many are worth more (equal ones: in front of it).
+      // Lane q ranks group q.
+      const uint32_t mine = lanes > 0 ? __shfl_sync(0xffffffffu, gk, min(lane * lanes, 31)) : gk;
+      int rank = 0;
+#pragma unroll 4
+      for (int q = 0; q < g.n_groups; ++q) {
+        const uint32_t other = __shfl_sync(0xffffffffu, mine, q);
+        rank += other > mine || (other == mine && q < lane);
+      }
+      const bool in = lane < g.n_groups && rank < g.topk_groups;
+      const uint32_t in_mask = __ballot_sync(0xffffffffu, in);
+      kept = lanes > 0 ? __ballot_sync(0xffffffffu, (in_mask >> (lane / max(lanes, 1))) & 1u) : in_mask;
+      // only the border between the two kinds matters: the least of the kept ones and the best of the others
+      const uint32_t least = ~__reduce_max_sync(0xffffffffu, in ? ~mine : 0u);
+      const uint32_t best = __reduce_max_sync(0xffffffffu, !in && lane < g.n_groups ? mine : 0u);
+      group_at = lane == 0 ? least : lane == 1 ? best : 0u;
+    } else {
+      const uint32_t run = lanes > 0 ? (lanes == 32 ? 0xffffffffu : (1u << lanes) - 1u) : 1u;
 #pragma unroll 1
-    for (;; ++taken) {
-      const uint32_t best = __reduce_max_sync(0xffffffffu, gk);
-      if (lane == taken) group_at = best;
-      if (best == 0u || (taken >= g.topk_groups && pool >= k)) break;
-      const int winner = __ffs(__ballot_sync(0xffffffffu, gk == best)) - 1;
-      const uint32_t these = run << winner;
-      kept |= these;
-      if ((these >> lane) & 1u) gk = 0u;
-      // (without a table topk_groups groups hold k experts)
-      pool = rl.all ? k : pool + __shfl_sync(0xffffffffu, have, winner);
+      for (int taken = 0, pool = 0;; ++taken) {
+        const uint32_t best = __reduce_max_sync(0xffffffffu, gk);
+        if (lane == taken) group_at = best;
+        if (best == 0u || (taken >= g.topk_groups && pool >= k)) break;
+        const int winner = __ffs(__ballot_sync(0xffffffffu, gk == best)) - 1;
+        const uint32_t these = run << winner;
+        kept |= these;
+        if ((these >> lane) & 1u) gk = 0u;
+        pool += __shfl_sync(0xffffffffu, have, winner);
+      }
     }
     if (lanes > 0) {
       if (!((kept >> lane) & 1u))
