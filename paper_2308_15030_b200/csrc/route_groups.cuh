@@ -451,7 +451,7 @@ __device__ __forceinline__ void route_load(const float* row, int E, bool vec, fl
 }
 
 template <int N>
-__global__ void __launch_bounds__(kRouteWarps * 32, N <= 8 ? 8 : 4) route_groups_kernel(const RouteGroupsArgs a, int vec) {
+__global__ void __launch_bounds__(kRouteWarps * 32, N <= 8 ? 8 : 4) route_groups_kernel(const __grid_constant__ RouteGroupsArgs a, int vec) {
   __shared__ double s_choice[kRouteWarps][32 * N];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
