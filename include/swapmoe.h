@@ -392,7 +392,8 @@ int32_t swapmoe_route_static(const void* x_dev, const void* Wr_dev, const int32_
  * the same stride (and type); other overlaps are not allowed.  Nothing behind column d or row n_rows is written.  Work is
  * enqueued on `stream` of the CURRENT device; no allocation, no synchronisation, no state: calls may run side by side.
  * Errors: INVALID_ARG (null or misaligned pointer, bad dtype, stride or group, residual_out without residual, out8
- * without scales, no output at all), UNSUPPORTED (d > 16384), CUDA.  n_rows = 0 is a no-op. */
+ * without scales, no output at all), UNSUPPORTED (d > SWAPMOE_NORM_MAX_WIDTH), CUDA.  n_rows = 0 is a no-op. */
+#define SWAPMOE_NORM_MAX_WIDTH 16384
 typedef struct {
   const void* x;            /* [n_rows, d] dtype                                                    */
   const void* residual;     /* [n_rows, d] residual_dtype, or NULL                                  */
@@ -471,6 +472,28 @@ int32_t swapmoe_adapters_set_weights(swapmoe_adapters_t* bank, const void* A_dev
 int32_t swapmoe_adapters_forward(swapmoe_adapters_t* bank, const void* x_dev, int64_t x_stride, const float* x_scales_dev,
                                  const int32_t* ids_dev, const void* y_dev, int64_t y_stride, void* out_dev,
                                  int64_t out_stride, int32_t n_tokens, void* stream);
+
+/* Whether a bank can serve n_tokens rows of these widths and dtype: OK, or what its forward would refuse them with. */
+int32_t swapmoe_adapters_check(const swapmoe_adapters_t* bank, int32_t d_in, int32_t d_out, int32_t dtype, int32_t n_tokens);
+
+/* A layer's own gate: later forwards of the layer (all forms) route by `gate` over the router's logits instead of the
+ * softmax gate of its configuration (whose renorm_topk then has no effect): both selections, over all experts (Eq. 1)
+ * and over the resident ones (Masked Gating), and the gate values.  bias_dev [E] fp32 or NULL, not copied.  gate = NULL
+ * returns to the configuration's gate.  One more kernel per forward; decode steps run on the general kernels.  Host
+ * state only: takes effect for forwards enqueued after the call.  Errors: INVALID_ARG. */
+int32_t swapmoe_set_gate(swapmoe_layer_t* layer, const swapmoe_gate_t* gate, const float* bias_dev);
+
+/* The norm of the pre-norm block around a layer: weight_dev [d_model] in the layer's dtype, not copied.  Allocates the rows
+ * behind the norm (max_tokens * d_model values) on the first call.  Errors: INVALID_ARG, UNSUPPORTED, NO_MEMORY. */
+int32_t swapmoe_set_norm(swapmoe_layer_t* layer, const void* weight_dev, float eps);
+
+/* A pre-norm block: residual += x (rounded to the layer's dtype); n = norm(residual before rounding) * weight;
+ * out = layer(n), plus scale * B (A n) of each token's adapter.  residual_dev [n_tokens, d_model] is updated in place; NULL:
+ * n = norm(x).  adapters and ids_dev [n_tokens] both or neither; the bank has d_in = d_out = d_model and the layer's
+ * dtype.  Nothing is enqueued if the call is refused.  No two of x, residual and out may overlap.  Errors: as
+ * swapmoe_forward, and NOT_READY without a norm or without the bank's weights, INVALID_ARG for a bank of another shape. */
+int32_t swapmoe_forward_block(swapmoe_layer_t* layer, const void* x_dev, void* residual_dev, void* out_dev, int32_t n_tokens,
+                              swapmoe_adapters_t* adapters, const int32_t* ids_dev, void* stream);
 
 const char* swapmoe_status_string(int32_t status);
 

@@ -41,6 +41,7 @@ EXPORTS = [
     "swapmoe_read_scores_async", "swapmoe_read_decode_prefetch",
     "swapmoe_rms_norm", "swapmoe_route",
     "swapmoe_adapters_create", "swapmoe_adapters_destroy", "swapmoe_adapters_set_weights", "swapmoe_adapters_forward",
+    "swapmoe_adapters_check", "swapmoe_set_gate", "swapmoe_set_norm", "swapmoe_forward_block",
 ]
 
 
@@ -131,6 +132,10 @@ def lib() -> ctypes.CDLL:
         L.swapmoe_adapters_destroy.argtypes = [vp]
         L.swapmoe_adapters_set_weights.argtypes = [vp, vp, vp, vp]
         L.swapmoe_adapters_forward.argtypes = [vp, vp, i64, vp, vp, vp, i64, vp, i64, i32, vp]
+        L.swapmoe_adapters_check.argtypes = [vp, i32, i32, i32, i32]
+        L.swapmoe_set_gate.argtypes = [vp, ctypes.POINTER(Gate), vp]
+        L.swapmoe_set_norm.argtypes = [vp, vp, ctypes.c_float]
+        L.swapmoe_forward_block.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp]
         L.swapmoe_rms_norm.argtypes = [ctypes.POINTER(RmsNormArgs), vp]
         L.swapmoe_status_string.argtypes = [i32]
         L.swapmoe_status_string.restype = ctypes.c_char_p
@@ -344,7 +349,40 @@ class Layer:
     def set_gemm_path(self, path: int) -> None:
         _check(lib().swapmoe_set_gemm_path(self._h, int(path)), "swapmoe_set_gemm_path")
 
+    def set_gate(self, gate: Optional[Gate], bias=None) -> None:
+        """Later forwards route by ``gate`` (None: by the layer's configuration); ``bias`` [E] float32, not copied."""
+        import torch
+        pb = None if bias is None else _vector(bias, self.cfg.E, torch.float32, bias.device, "swapmoe_set_gate", "bias")
+        if bias is not None and not bias.is_cuda:
+            raise _invalid("swapmoe_set_gate", "bias: a CUDA tensor expected")
+        _check(lib().swapmoe_set_gate(self._h, None if gate is None else ctypes.byref(gate), pb), "swapmoe_set_gate")
+        self._keep["gate_bias"] = bias
+
+    def set_norm(self, weight, eps: float) -> None:
+        """The norm in front of the layer in forward_block: ``weight`` [d_model] in the layer's dtype, not copied."""
+        import torch
+        dt = torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
+        if not weight.is_cuda:
+            raise _invalid("swapmoe_set_norm", "weight: a CUDA tensor expected")
+        pw = _vector(weight, self.cfg.d_model, dt, weight.device, "swapmoe_set_norm", "weight")
+        _check(lib().swapmoe_set_norm(self._h, pw, eps), "swapmoe_set_norm")
+        self._keep["norm"] = weight
+
     # -- hot path
+    def forward_block(self, x, residual, out, adapters: Optional[AdapterBank] = None, ids=None, n_tokens: Optional[int] = None,
+                      stream=None) -> None:
+        """The pre-norm block around the layer: residual += x (None: no residual); out = layer(norm(residual)), plus each
+        token's adapter from ``adapters`` by ``ids`` [T] int32 (negative: none)."""
+        import torch
+        T = int(x.shape[0]) if n_tokens is None else int(n_tokens)
+        if ids is not None:
+            _vector(ids, T, torch.int32, x.device, "swapmoe_forward_block", "ids")
+        self.last_T = T
+        _check(lib().swapmoe_forward_block(
+            self._h, x.data_ptr(), None if residual is None else residual.data_ptr(), out.data_ptr(), T,
+            None if adapters is None else adapters._h, None if ids is None else ids.data_ptr(), _stream_ptr(stream)),
+            "swapmoe_forward_block")
+
     def forward(self, x, out, n_tokens: Optional[int] = None, stream=None) -> None:
         T = int(x.shape[0]) if n_tokens is None else int(n_tokens)
         self.last_T = T

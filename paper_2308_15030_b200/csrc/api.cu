@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -20,6 +21,7 @@
 #include "gemm_tc_f32_pair.cuh"
 #include "gemm_tc_ffn.cuh"
 #include "gemm_tc_small.cuh"
+#include "layer_gate.cuh"
 #include "permute.cuh"
 #include "router_gate.cuh"
 #include "router_tc.cuh"
@@ -52,6 +54,12 @@ struct swapmoe_layer {
   void *xp, *h, *x_stage, *out_stage;
   // host state
   const void *Wr, *arena_in, *arena_out;
+  bool own_gate;               // swapmoe_set_gate: routing by `gate` in place of the router kernels' own
+  RouteGate gate;
+  const float* gate_bias;
+  const void* norm_weight;     // swapmoe_set_norm, or nullptr
+  float norm_eps;
+  void* x_norm;                // [max_tokens, d_model] rows behind the norm (allocated by swapmoe_set_norm)
   bool router_set, resident_set;
   int32_t h_s2e[kMaxSlots], h_phys[kMaxSlots];
   int32_t last_T;
@@ -185,7 +193,7 @@ int32_t forward_impl(swapmoe_layer* L, const void* x, const float* ext_logits, v
   const swapmoe_config_t& c = L->cfg;
   const bool pdl = L->use_pdl && L->stage_events == nullptr;
   const int rerun = L->rerun_gemm;          // 1 / 2: only that grouped GEMM, on the state the last forward left
-  if (L->decode_path && T <= kDecMaxTokens && T * c.top_k <= L->decode_max_pairs && c.dtype == SWAPMOE_BF16) {
+  if (L->decode_path && !L->own_gate && T <= kDecMaxTokens && T * c.top_k <= L->decode_max_pairs && c.dtype == SWAPMOE_BF16) {
     if (rerun) return SWAPMOE_ERR_UNSUPPORTED;   // the one-launch kernel has no GEMM launch of its own
     // a handful of tokens: routing, both expert products and the combine in one launch
     DecodeArgs da;
@@ -223,7 +231,7 @@ int32_t forward_impl(swapmoe_layer* L, const void* x, const float* ext_logits, v
   // fp32 layers: eight-token CTAs of the split-TF32 mma router while they fit one wave of CTAs
   const bool small_f32 = L->small_router_f32 && ext_logits == nullptr && T <= kRsTok * std::min(L->sm_count, 256);
   if (small_f32) tok_tile = kRsTok;
-  const int n_cta = (T + tok_tile - 1) / tok_tile;
+  int n_cta = (T + tok_tile - 1) / tok_tile;
   const int n_pairs = T * c.top_k;
   const bool use_tc = tc_selected(L->gemm_path, c, T);
   // weight tiles per token tile of the grouped GEMMs on CTA pairs (0: one CTA per 128-row tile)
@@ -254,11 +262,11 @@ int32_t forward_impl(swapmoe_layer* L, const void* x, const float* ext_logits, v
   // Up to 256 router CTAs the router only leaves its per-CTA histograms and the permute kernel sums them itself
   // (every CTA its own base counts, one CTA the Eq. (1) partials); beyond that the last router CTA to finish scans
   // (re-reading all rows in every permute CTA would then cost more than its serial walk).
-  const bool own_scan = n_cta <= 256;
+  bool own_scan = n_cta <= 256;
   sa.cta_base = own_scan ? nullptr : L->cta_base; sa.count = L->count; sa.offset = L->offset;
   sa.pad_offset = L->pad_offset; sa.tiles = L->tiles; sa.n_tiles = L->n_tiles; sa.imp = L->imp;
   sa.cta_cnt = L->cta_cnt; sa.cta_mimp = L->cta_mimp; sa.s2e = L->s2e; sa.cnt = L->cnt; sa.mimp = L->mimp;
-  sa.ticket = own_scan ? nullptr : L->ticket;
+  sa.ticket = own_scan || L->own_gate ? nullptr : L->ticket;   // (with a gate of its own the layer's counts come from that)
   sa.touched = L->touched;
   sa.n_cta = n_cta; sa.K = c.K; sa.E = c.E; sa.tile_rows = tile_rows;
   // token tiles for CTA pairs: one list where the two GEMMs have the same number of weight tiles, else one each
@@ -331,6 +339,18 @@ int32_t forward_impl(swapmoe_layer* L, const void* x, const float* ext_logits, v
       return SWAPMOE_ERR_CUDA;
   }
   if (!rerun) L->launches++;
+  if (L->own_gate) {
+    tok_tile = layer_gate_tok(T);
+    n_cta = (T + tok_tile - 1) / tok_tile;
+    own_scan = n_cta <= 256;
+    sa.cta_base = own_scan ? nullptr : L->cta_base;
+    sa.ticket = own_scan ? nullptr : L->ticket;
+    sa.n_cta = n_cta;
+    if (!rerun) {
+      if (layer_gate_launch(ra, L->gate, L->gate_bias, tok_tile, st, pdl) != cudaSuccess) return SWAPMOE_ERR_CUDA;
+      L->launches++;
+    }
+  }
   mark(L, 1, st);   // (stage 1, the scan, has no launch of its own: it runs in the permute kernel, or for very large
                     // grids and swapmoe_route_static in the router's last CTA)
 
@@ -741,6 +761,7 @@ int32_t swapmoe_destroy(swapmoe_layer_t* L) {
   if (L->ev_out) cudaEventDestroy(L->ev_out);
   if (L->ev_load) cudaEventDestroy(L->ev_load);
   cudaFree(L->ws_base);
+  if (L->x_norm) cudaFree(L->x_norm);
   delete L;
   return SWAPMOE_OK;
 }
@@ -802,6 +823,64 @@ int32_t swapmoe_set_resident(swapmoe_layer_t* L, const int32_t* s2e, const int32
   L->arena_out = arena_out;
   L->resident_set = true;
   return check_launch();
+}
+
+int32_t swapmoe_set_gate(swapmoe_layer_t* L, const swapmoe_gate_t* gate, const float* bias_dev) {
+  if (!L || (reinterpret_cast<uintptr_t>(bias_dev) & 3)) return SWAPMOE_ERR_INVALID_ARG;
+  if (!gate) {
+    if (bias_dev) return SWAPMOE_ERR_INVALID_ARG;
+    L->own_gate = false;
+    return SWAPMOE_OK;
+  }
+  RouteGate g;
+  if (!route_gate_from(*gate, L->cfg.E, L->cfg.top_k, &g)) return SWAPMOE_ERR_INVALID_ARG;
+  L->gate = g;
+  L->gate_bias = bias_dev;
+  L->own_gate = true;
+  return SWAPMOE_OK;
+}
+
+int32_t swapmoe_set_norm(swapmoe_layer_t* L, const void* weight_dev, float eps) {
+  if (!L || !weight_dev || reinterpret_cast<uintptr_t>(weight_dev) % L->elem || !(eps >= 0.f) || !std::isfinite(eps))
+    return SWAPMOE_ERR_INVALID_ARG;
+  if (L->cfg.d_model > SWAPMOE_NORM_MAX_WIDTH) return SWAPMOE_ERR_UNSUPPORTED;
+  if (!L->x_norm && !cuda_ok(cudaMalloc(&L->x_norm, (size_t)L->cfg.max_tokens * L->cfg.d_model * L->elem))) {
+    cudaGetLastError();
+    L->x_norm = nullptr;
+    return SWAPMOE_ERR_NO_MEMORY;
+  }
+  L->norm_weight = weight_dev;
+  L->norm_eps = eps;
+  return SWAPMOE_OK;
+}
+
+int32_t swapmoe_forward_block(swapmoe_layer_t* L, const void* x, void* residual, void* out, int32_t T, swapmoe_adapters_t* adapters,
+                              const int32_t* ids, void* stream) {
+  if (!L || T < 0 || (adapters == nullptr) != (ids == nullptr)) return SWAPMOE_ERR_INVALID_ARG;
+  if (T == 0) { L->last_T = 0; return SWAPMOE_OK; }
+  const swapmoe_config_t& c = L->cfg;
+  if (!x || !out || ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(residual) | reinterpret_cast<uintptr_t>(out)) & 15) ||
+      (reinterpret_cast<uintptr_t>(ids) & 3))
+    return SWAPMOE_ERR_INVALID_ARG;
+  if (!L->router_set || !L->resident_set || !L->norm_weight) return SWAPMOE_ERR_NOT_READY;
+  if (T > c.max_tokens) return SWAPMOE_ERR_TOO_MANY_TOKENS;
+  if (adapters) {                              // everything that its forward refuses, before anything is enqueued
+    const int32_t rc = swapmoe_adapters_check(adapters, c.d_model, c.d_model, c.dtype, T);
+    if (rc != SWAPMOE_OK) return rc;
+  }
+  swapmoe_rms_norm_t n;
+  std::memset(&n, 0, sizeof(n));
+  n.x = x; n.residual = residual; n.residual_out = residual; n.weight = L->norm_weight; n.out = L->x_norm;
+  n.x_stride = n.residual_stride = n.residual_out_stride = n.out_stride = c.d_model;
+  n.n_rows = T; n.d = c.d_model; n.dtype = n.residual_dtype = c.dtype; n.eps = L->norm_eps;
+  int32_t rc = swapmoe_rms_norm(&n, stream);
+  if (rc != SWAPMOE_OK) return rc;
+  L->launches++;
+  rc = forward_checked(L, L->x_norm, nullptr, out, T, stream);
+  if (rc != SWAPMOE_OK || !adapters) return rc;
+  rc = swapmoe_adapters_forward(adapters, L->x_norm, c.d_model, nullptr, ids, out, c.d_model, out, c.d_model, T, stream);
+  if (rc == SWAPMOE_OK) L->launches++;
+  return rc;
 }
 
 int32_t swapmoe_forward(swapmoe_layer_t* L, const void* x, void* out, int32_t T, void* stream) {

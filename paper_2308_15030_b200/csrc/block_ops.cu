@@ -14,6 +14,8 @@
 
 using namespace swapmoe;
 
+static_assert(SWAPMOE_NORM_MAX_WIDTH == kNormMaxWidth, "the header's limit");
+
 struct swapmoe_adapters {
   swapmoe_adapters_config_t cfg;
   int sm_count;
@@ -45,19 +47,6 @@ int32_t launched(cudaError_t e) {
 // Whether rows of `elem`-byte values at p, `stride` values apart, all start on multiples of `bytes`.
 bool rows_aligned(const void* p, long long stride, size_t elem, size_t bytes) {
   return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (size_t)stride * elem % bytes == 0;
-}
-
-// Checks a gate for layers of E experts and top_k of them per token.
-bool gate_from(const swapmoe_gate_t& g, int E, int top_k, RouteGate* out) {
-  if (g.score != SWAPMOE_SCORE_SOFTMAX && g.score != SWAPMOE_SCORE_SIGMOID) return false;
-  if (g.n_groups < 1 || g.n_groups > kRouteMaxGroups || g.n_groups > E || E % g.n_groups) return false;
-  if (g.topk_groups < 1 || g.topk_groups > g.n_groups || g.topk_groups * (E / g.n_groups) < top_k) return false;
-  if ((g.group_top != 1 && g.group_top != 2) || (g.renorm != 0 && g.renorm != 1) || !std::isfinite(g.scale)) return false;
-  out->score = g.score; out->n_groups = g.n_groups; out->topk_groups = g.topk_groups; out->group_top = g.group_top;
-  out->renorm = g.renorm; out->scale = g.scale;
-  out->group_size = E / g.n_groups;
-  out->group_magic = (uint32_t)((0x80000000ull + out->group_size - 1) / out->group_size);
-  return true;
 }
 
 bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
@@ -114,7 +103,7 @@ int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits, int64_t s
   RouteGroupsArgs a;
   if (!gate || T < 0 || E < 1 || top_k < 1 || top_k > E || stride < E) return SWAPMOE_ERR_INVALID_ARG;
   if (E > kRouteMaxE || top_k > kRouteMaxTopK) return SWAPMOE_ERR_UNSUPPORTED;
-  if (!gate_from(*gate, E, top_k, &a.gate)) return SWAPMOE_ERR_INVALID_ARG;
+  if (!route_gate_from(*gate, E, top_k, &a.gate)) return SWAPMOE_ERR_INVALID_ARG;
   if (T == 0) return SWAPMOE_OK;
   if (!logits || !experts || !weights || (expert_to_slot == nullptr) != (slots == nullptr)) return SWAPMOE_ERR_INVALID_ARG;
   for (const void* p : {(const void*)logits, (const void*)bias, (const void*)expert_to_slot, (const void*)experts, (const void*)weights, (const void*)slots})
@@ -170,6 +159,12 @@ int32_t swapmoe_adapters_set_weights(swapmoe_adapters_t* b, const void* A, const
   if (!b || !A || !B || misaligned(A, 16) || misaligned(B, 16) || misaligned(scale, 4)) return SWAPMOE_ERR_INVALID_ARG;
   b->A = A; b->B = B; b->scale = scale;
   return SWAPMOE_OK;
+}
+
+int32_t swapmoe_adapters_check(const swapmoe_adapters_t* b, int32_t d_in, int32_t d_out, int32_t dtype, int32_t T) {
+  if (!b || T < 0 || b->cfg.d_in != d_in || b->cfg.d_out != d_out || b->cfg.dtype != dtype) return SWAPMOE_ERR_INVALID_ARG;
+  if (!b->A) return SWAPMOE_ERR_NOT_READY;
+  return T > b->cfg.max_tokens ? SWAPMOE_ERR_TOO_MANY_TOKENS : SWAPMOE_OK;
 }
 
 int32_t swapmoe_adapters_forward(swapmoe_adapters_t* b, const void* x, int64_t x_stride, const float* x_scales, const int32_t* ids,

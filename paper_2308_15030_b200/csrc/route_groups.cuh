@@ -14,6 +14,8 @@
 #pragma once
 #include <math_constants.h>
 
+#include <cmath>
+
 #include "../../include/swapmoe.h"
 #include "common.cuh"
 #include "launch.cuh"
@@ -29,6 +31,19 @@ struct RouteGate {
   int group_size;
   uint32_t group_magic;      // e / group_size = 2 e * group_magic >> 32 for the indices that occur
 };
+
+// Checks a gate for layers of E experts and top_k of them per token.
+inline bool route_gate_from(const swapmoe_gate_t& g, int E, int top_k, RouteGate* out) {
+  if (g.score != SWAPMOE_SCORE_SOFTMAX && g.score != SWAPMOE_SCORE_SIGMOID) return false;
+  if (g.n_groups < 1 || g.n_groups > kRouteMaxGroups || g.n_groups > E || E % g.n_groups) return false;
+  if (g.topk_groups < 1 || g.topk_groups > g.n_groups || g.topk_groups * (E / g.n_groups) < top_k) return false;
+  if ((g.group_top != 1 && g.group_top != 2) || (g.renorm != 0 && g.renorm != 1) || !std::isfinite(g.scale)) return false;
+  out->score = g.score; out->n_groups = g.n_groups; out->topk_groups = g.topk_groups; out->group_top = g.group_top;
+  out->renorm = g.renorm; out->scale = g.scale;
+  out->group_size = E / g.n_groups;
+  out->group_magic = (uint32_t)((0x80000000ull + out->group_size - 1) / out->group_size);
+  return true;
+}
 
 struct RouteGroupsArgs {
   const float* logits;

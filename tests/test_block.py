@@ -1,0 +1,247 @@
+"""A layer with a gate of its own, and the pre-norm block: norm, router, experts and adapters run together."""
+import numpy as np
+import pytest
+
+from paper_2308_15030_b200 import binding, inputs as I
+from paper_2308_15030_b200.binding import Gate
+
+
+# ------------------------------------------------------------------ refusals (host checks, no GPU needed)
+def test_null_handles():
+    import ctypes
+    L = binding.lib()
+    g = Gate()
+    assert L.swapmoe_set_gate(None, ctypes.byref(g), None) == -1
+    assert L.swapmoe_set_norm(None, 256, 1e-6) == -1
+    assert L.swapmoe_forward_block(None, 256, 256, 256, 1, None, None, None) == -1
+    assert L.swapmoe_adapters_check(None, 64, 64, 1, 1) == -1
+
+
+# ------------------------------------------------------------------ on the GPU
+def _expected(case, midx, mgate, slot):
+    """out in 64 bits from a routing: gate-weighted sum of the experts' FFN, hidden values rounded as the layer stores them."""
+    cfg = case.cfg
+    x = case.x.astype(np.float64)
+    out = np.zeros((case.T, cfg.d))
+    for s in range(cfg.K):
+        a_in, a_out = (a[case.phys[s]].astype(np.float64) for a in (case.a_in, case.a_out))
+        for j in range(cfg.k):
+            t = np.nonzero(slot[:, j] == s)[0]
+            if t.size == 0:
+                continue
+            if cfg.act == I.ACT_SWIGLU:
+                u = x[t] @ a_in[0].T
+                h = u / (1 + np.exp(-u)) * (x[t] @ a_in[1].T)
+            else:
+                h = np.maximum(x[t] @ a_in[0].T, 0)
+            h = I.store_round(h.astype(np.float32), cfg.dtype).astype(np.float64)
+            out[t] += mgate[t, j, None].astype(np.float64) * (h @ a_out.T)
+    return out
+
+
+def _case(T, E, k, K, dtype=I.BF16, act=I.ACT_RELU, d=128, f=256, max_tokens=None):
+    from harness import Case
+    cfg = I.LayerConfig("block", dtype, T=T, d=d, f=f, E=E, k=k, K=K, act=act, renorm=0, seed=7)
+    rng = np.random.default_rng(E + K)
+    return Case(cfg, s2e=rng.permutation(E)[:K], max_tokens=max_tokens)
+
+
+GATES = [Gate("sigmoid", 8, 4, 2, True, 2.5), Gate("softmax", 4, 2, 1, False, 16.0), Gate("sigmoid")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gate", range(len(GATES)))
+@pytest.mark.parametrize("T,E,k,K,dtype,act", [(1, 64, 2, 9, I.BF16, I.ACT_RELU), (5, 64, 1, 16, I.BF16, I.ACT_RELU),
+                                               (64, 256, 4, 33, I.BF16, I.ACT_SWIGLU), (100, 160, 3, 20, I.F32, I.ACT_RELU),
+                                               (4097, 64, 2, 12, I.BF16, I.ACT_RELU), (8300, 16, 1, 5, I.BF16, I.ACT_RELU),
+                                               (9000, 16, 2, 5, I.F32, I.ACT_SWIGLU)])
+def test_gate_of_its_own(T, E, k, K, dtype, act, gate):
+    import torch
+    import oracle
+    from harness import TOL_IMP_REL, TOL_OUT
+    from test_route_groups import REL, TINY, reference
+    g = GATES[gate]
+    case = _case(T, E, k, K, dtype, act)
+    L = case.layer
+    bias = np.random.default_rng(1).normal(0, 0.1, E).astype(np.float32) if g.score == 1 else None
+    L.set_gate(g, None if bias is None else torch.from_numpy(bias).cuda())
+    out = case.run()
+    assert L.device_status() == (0, 0)
+    lg = L.tap("logits")
+    table = np.full(E, -1, np.int32)
+    table[case.s2e] = np.arange(K)
+    args = (k, "sigmoid" if g.score else "softmax", g.n_groups, g.topk_groups, g.group_top, g.renorm, g.scale, bias)
+    ue, uw, _ = reference(lg, *args)
+    me, mw, ms = reference(lg, *args, table)
+    assert np.array_equal(L.tap("uidx"), ue) and np.array_equal(L.tap("midx"), me) and np.array_equal(L.tap("slot"), ms)
+    for name, w in (("ugate", uw), ("mgate", mw)):
+        assert np.all(np.abs(L.tap(name) - w) <= REL * np.abs(w) + TINY), name
+    count, offset, perm, inv = oracle.permute(ms.astype(np.int32), K)
+    for name, want in (("count", count), ("offset", offset), ("perm", perm), ("inv", inv)):
+        assert np.array_equal(L.tap(name), want.reshape(L.tap(name).shape)), name
+    xn = np.linalg.norm(case.x.astype(np.float64), axis=1)[:, None]
+    imp, cnt, mimp = np.zeros(E), np.zeros(E), np.zeros(E)
+    np.add.at(imp, ue, xn * np.abs(uw) * case.enorm[ue])
+    np.add.at(cnt, ue, 1)
+    np.add.at(mimp, me, xn * np.abs(mw) * case.enorm[me])
+    assert np.max(np.abs(L.read_importance() - imp)) <= TOL_IMP_REL * imp.max()
+    assert np.array_equal(L.read_score("count"), cnt)
+    assert np.max(np.abs(L.read_score("eq1_masked") - mimp)) <= TOL_IMP_REL * mimp.max()
+    ref = _expected(case, me, mw, ms)
+    assert np.max(np.abs(out - ref)) <= TOL_OUT[dtype] * np.max(np.abs(ref))
+    assert np.array_equal(case.run(), out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [2, 300])
+def test_back_to_the_configurations_gate(T):
+    case = _case(T, 32, 2, 8)
+    L = case.layer
+    first = case.run()
+    names = ("uidx", "midx", "slot", "ugate", "mgate", "perm")
+    taps = {n: L.tap(n) for n in names}
+    L.set_gate(Gate("softmax"))                              # the configuration's gate, by the other kernel
+    out = case.run()
+    for n in names[:3]:
+        assert np.array_equal(L.tap(n), taps[n]), n
+    for n in names[3:5]:
+        assert np.max(np.abs(L.tap(n) - taps[n])) <= 1e-6, n
+    assert np.max(np.abs(out - first)) <= 2e-2 * np.max(np.abs(first))
+    L.set_gate(Gate("sigmoid", 4, 2, 2, True))
+    assert not np.array_equal(case.run(), first)
+    L.set_gate(None)
+    assert np.array_equal(case.run(), first)
+
+
+def _block_inputs(case, dtype):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(case.T)
+    dt = torch.bfloat16 if dtype == I.BF16 else torch.float32
+    T, d = case.T, case.cfg.d
+    x = torch.empty(T, d, device="cuda").normal_(generator=gen).to(dt)
+    r = torch.empty(T, d, device="cuda").normal_(0, 2, generator=gen).to(dt)
+    w = torch.empty(d, device="cuda").normal_(1, 0.2, generator=gen).to(dt)
+    A = torch.empty(5, 16, d, device="cuda").normal_(0, d ** -0.5, generator=gen).to(dt)
+    B = torch.empty(5, d, 16, device="cuda").normal_(0, 0.25, generator=gen).to(dt)
+    sc = torch.empty(5, device="cuda").uniform_(0.5, 1.5, generator=gen)
+    ids = torch.randint(-1, 5, (T,), device="cuda", generator=gen).to(torch.int32)
+    bank = binding.AdapterBank(5, d, d, 16, dtype, max_tokens=T)
+    bank.set_weights(A, B, sc)
+    return x, r, w, bank, ids
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [I.BF16, I.F32])
+@pytest.mark.parametrize("own_gate", [False, True])
+@pytest.mark.parametrize("T", [1, 3, 40, 500])
+def test_block_is_its_parts(T, own_gate, dtype):
+    import torch
+    case = _case(T, 64, 2, 12, dtype)
+    L = case.layer
+    if own_gate:
+        L.set_gate(Gate("sigmoid", 8, 4, 2, True, 2.5))
+    x, r, w, bank, ids = _block_inputs(case, dtype)
+    n, r1, want = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    binding.rms_norm(x, w, 1e-5, out=n, residual=r, residual_out=r1)
+    L.forward(n, want)
+    bank.forward(n, ids, want, want)
+    L.set_norm(w, 1e-5)
+    r2, out = r.clone(), torch.empty_like(x)
+    L.forward_block(x, r2, out, bank, ids)
+    torch.cuda.synchronize()
+    assert torch.equal(r2, r1) and torch.equal(out, want)
+    # without adapters, without a residual
+    binding.rms_norm(x, w, 1e-5, out=n)
+    L.forward(n, want)
+    L.forward_block(x, None, out)
+    assert torch.equal(out, want)
+    assert L.device_status() == (0, 0)
+
+
+@pytest.mark.gpu
+def test_block_captured_and_on_another_stream():
+    import torch
+    case = _case(48, 64, 2, 12)
+    L = case.layer
+    L.set_gate(Gate("sigmoid", 8, 4, 2, True, 2.5))
+    x, r, w, bank, ids = _block_inputs(case, I.BF16)
+    L.set_norm(w, 1e-5)
+    r1, want = r.clone(), torch.empty_like(x)
+    L.forward_block(x, r1, want, bank, ids)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    r2, out = r.clone(), torch.empty_like(x)
+    side.wait_stream(torch.cuda.current_stream())
+    L.forward_block(x, r2, out, bank, ids, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want) and torch.equal(r2, r1)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        L.forward_block(x, r2, out, bank, ids)
+        L.forward_block(out, r2, torch.empty_like(out), bank, ids)
+    r2.copy_(r)
+    out.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+def test_block_refusals():
+    import torch
+    case = _case(8, 64, 2, 12)
+    L, lib = case.layer, binding.lib()
+    x, r, w, bank, ids = _block_inputs(case, I.BF16)
+    out = torch.full_like(x, 3.0)
+
+    def status(*a, **k):
+        with pytest.raises(binding.SwapMoEError) as e:
+            L.forward_block(*a, **k)
+        return e.value.status
+    assert status(x, r, out) == -2                             # no norm yet
+    L.set_norm(w, 1e-5)
+    for bad in (w[:64], w.float(), w.cpu()):
+        with pytest.raises(binding.SwapMoEError):
+            L.set_norm(bad, 1e-5)
+    for eps in (-1.0, float("nan"), float("inf")):
+        with pytest.raises(binding.SwapMoEError):
+            L.set_norm(w, eps)
+    assert status(x, r, out, bank) == -1 and status(x, r, out, None, ids) == -1
+    assert status(x, r, out, bank, ids.long()) == -1
+    assert status(x, r, out, n_tokens=9) == -3
+    small = binding.AdapterBank(5, 128, 128, 16, binding.BF16, max_tokens=4)
+    assert status(x, r, out, small, ids) == -2                 # no weights
+    other = binding.AdapterBank(5, 128, 64, 16, binding.BF16, max_tokens=8)
+    assert status(x, r, out, other, ids) == -1
+    keep = r.clone()
+    torch.cuda.synchronize()
+    assert bool((out == 3).all()) and torch.equal(r, keep)     # refused calls enqueue nothing
+    L.forward_block(x, r, out, n_tokens=0)
+    for g, b in ((Gate("softmax", 7), None), (Gate("softmax", 64, 1), None), (None, torch.zeros(64, device="cuda")),
+                 (Gate(), torch.zeros(63, device="cuda")), (Gate(), torch.zeros(64))):
+        with pytest.raises(binding.SwapMoEError) as e:
+            L.set_gate(g, b)
+        assert e.value.status == -1
+
+
+@pytest.mark.gpu
+def test_decode_stack_over_layers_with_gates_of_their_own():
+    import torch
+    from paper_2308_15030_b200.decode import DecodeStack, LayerState
+    cases = [_case(6, 32, 2, 8) for _ in range(2)]
+    states = []
+    for c in cases:
+        c.layer.set_gate(Gate("sigmoid", 4, 2, 2, True))
+        host = [torch.empty((32,) + tuple(a.shape[1:]), dtype=torch.bfloat16).pin_memory() for a in (c.d_in, c.d_out_w)]
+        states.append(LayerState(c.layer, np.asarray(c.s2e, np.int32), c.phys, [], c.d_in, c.d_out_w, host[0], host[1], enorm=c.enorm))
+    x = torch.stack([c.d_x for c in cases])
+    want = []
+    for c in cases:
+        o = torch.empty_like(c.d_x)
+        c.layer.forward(c.d_x, o)
+        want.append(o)
+    out = torch.empty_like(x)
+    stack = DecodeStack(states, frequency=100, graph_buffers=(torch.empty_like(x), out))
+    stack.step_graph(x)
+    torch.cuda.synchronize()
+    assert torch.equal(out, torch.stack(want))
