@@ -46,46 +46,61 @@ struct AdapterArgs {
 
 // ----------------------------------------------------------------------------- plan
 constexpr int kAdPlanThreads = 1024;
+constexpr int kAdPlanIds = 8;              // tokens whose ids a thread keeps
 
 // Groups the tokens by adapter and cuts the groups into tiles of at most `tile_rows`.  One CTA: counts per adapter, their
 // exclusive scans, then every token takes a place in its group.  (Which place is left to the order of atomics; a row's result does
-// not depend on it.)
+// not depend on it.)  A chain of latencies: ids are read once, in one go, runs of one adapter cost one atomic per warp.
 __global__ void __launch_bounds__(kAdPlanThreads) adapters_plan_kernel(const AdapterArgs a, int tile_rows) {
   __shared__ int32_t s_cursor[kAdMaxCount + 1];
   __shared__ int32_t s_warp[2][32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
+  const int groups = a.count + 1;                           // the last one: tokens without an adapter
+  for (int g = tid; g < groups; g += threads) s_cursor[g] = 0;
   pdl_wait();
   pdl_trigger();
-  const int groups = a.count + 1;                           // the last one: tokens without an adapter
-  for (int g = tid; g < groups; g += kAdPlanThreads) s_cursor[g] = 0;
-  __syncthreads();
   auto group_of = [&](int t) {
+    if (t >= a.T) return -1;
     const int id = a.ids[t];
     return id < 0 || id >= a.count ? a.count : id;
   };
-  for (int t0 = warp * 32; t0 < a.T; t0 += kAdPlanThreads) {
-    const int g = t0 + lane < a.T ? group_of(t0 + lane) : -1;
-    const uint32_t same = __match_any_sync(0xffffffffu, g);  // runs of one adapter: one atomic per warp
+  int kept[kAdPlanIds];
+#pragma unroll
+  for (int i = 0; i < kAdPlanIds; ++i) kept[i] = group_of(tid + i * threads);
+  __syncthreads();
+  auto count = [&](int g) {
+    const uint32_t same = __match_any_sync(0xffffffffu, g);
     if (g >= 0 && __ffs(same) - 1 == lane) atomicAdd(&s_cursor[g], __popc(same));
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < kAdPlanIds; ++i)
+    if (i * threads < a.T) count(kept[i]);
+  for (int t0 = kAdPlanIds * threads; t0 < a.T; t0 += threads) count(group_of(t0 + tid));
   __syncthreads();
   // thread i owns groups i * per ... : sums, scan over the threads, then first rows and tiles of its groups
-  const int per = (groups + kAdPlanThreads - 1) / kAdPlanThreads, g0 = tid * per;
+  const int per = (groups + threads - 1) / threads, g0 = tid * per;
   int rows = 0, tiles = 0;
   for (int g = g0; g < min(groups, g0 + per); ++g) {
     rows += s_cursor[g];
     tiles += (s_cursor[g] + tile_rows - 1) / tile_rows;
   }
-  int row_incl = rows, tile_incl = tiles;
+  auto scan = [&](int& u, int& v) {                         // inclusive, over the lanes
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, row_incl, o), v = __shfl_up_sync(0xffffffffu, tile_incl, o);
-    if (lane >= o) { row_incl += u; tile_incl += v; }
-  }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, u, o), y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) { u += x; v += y; }
+    }
+  };
+  int row_incl = rows, tile_incl = tiles;
+  scan(row_incl, tile_incl);
   if (lane == 31) { s_warp[0][warp] = row_incl; s_warp[1][warp] = tile_incl; }
   __syncthreads();
-  int row = row_incl - rows, tile = tile_incl - tiles;
-  for (int w = 0; w < warp; ++w) { row += s_warp[0][w]; tile += s_warp[1][w]; }
+  int row_base = lane < threads / 32 ? s_warp[0][lane] : 0, tile_base = lane < threads / 32 ? s_warp[1][lane] : 0;
+  scan(row_base, tile_base);
+  const int row_front = __shfl_sync(0xffffffffu, row_base, max(warp - 1, 0)), tile_front = __shfl_sync(0xffffffffu, tile_base, max(warp - 1, 0));
+  const int all_tiles = __shfl_sync(0xffffffffu, tile_base, 31);
+  int row = row_incl - rows + (warp > 0 ? row_front : 0), tile = tile_incl - tiles + (warp > 0 ? tile_front : 0);
+  if (tid == 0) *a.n_tiles = all_tiles;
   for (int g = g0; g < min(groups, g0 + per); ++g) {
     const int n = s_cursor[g], cut = (n + tile_rows - 1) / tile_rows;
     const int each = cut > 0 ? (n + cut - 1) / cut : 0;     // tiles of equal height
@@ -95,17 +110,19 @@ __global__ void __launch_bounds__(kAdPlanThreads) adapters_plan_kernel(const Ada
     row += n;
     tile += cut;
   }
-  if (tid == kAdPlanThreads - 1) *a.n_tiles = tile;
   __syncthreads();
-  for (int t0 = warp * 32; t0 < a.T; t0 += kAdPlanThreads) {
-    const int t = t0 + lane, g = t < a.T ? group_of(t) : -1;
+  auto place = [&](int g, int t) {
     const uint32_t same = __match_any_sync(0xffffffffu, g);
     const int leader = __ffs(same) - 1;
     int base = 0;
     if (g >= 0 && leader == lane) base = atomicAdd(&s_cursor[g], __popc(same));
     base = __shfl_sync(0xffffffffu, base, leader);
     if (g >= 0) a.perm[base + __popc(same & ((1u << lane) - 1))] = t;
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < kAdPlanIds; ++i)
+    if (i * threads < a.T) place(kept[i], tid + i * threads);
+  for (int t0 = kAdPlanIds * threads; t0 < a.T; t0 += threads) place(group_of(t0 + tid), t0 + tid);
 }
 
 // ----------------------------------------------------------------------------- fragments and products
@@ -580,17 +597,34 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const Adap
     __syncthreads();                                         // the tile in front is done with the list and the stages
     if (tid < rows) list[tid] = a.perm[td.first + tid];
     __syncthreads();
-    if (adapter < 0) {                                       // no adapter: rows of y as they are
-      const int pieces = rows * 16;
-      for (int i = cta; i < y_chunks; i += C) {
-        for (int p = tid; p < pieces; p += kAdThreads) {
-          const int t = p >> 4, c = i * kCols + (p & 15) * P;
-          if (c >= a.n) continue;
-          uint4 v;
-          ad_zero(v);
-          if (y != nullptr) v = *reinterpret_cast<const uint4*>(y + (long long)list[t] * a.y_stride + c);
-          *reinterpret_cast<uint4*>(out + (long long)list[t] * a.out_stride + c) = v;
-        }
+    if (adapter < 0) {                                       // no adapter: rows of y as they are, two chunks at a time
+      if (y == out && a.y_stride == a.out_stride) continue;
+      constexpr int kRows = kAdTM / 16;
+      const T* from[kRows];
+      T* to[kRows];
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        const long long t = list[min(crow + 16 * k, rows - 1)];
+        from[k] = y + t * a.y_stride + cpiece * P;
+        to[k] = out + t * a.out_stride + cpiece * P;
+      }
+      for (int c = cta * kCols; c < a.n; c += 2 * C * kCols) {
+        uint4 v[2][kRows];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < kRows; ++k) {
+            ad_zero(v[h][k]);
+            const int at = c + h * C * kCols;
+            if (y != nullptr && at + cpiece * P < a.n && crow + 16 * k < rows) v[h][k] = *reinterpret_cast<const uint4*>(from[k] + at);
+          }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < kRows; ++k) {
+            const int at = c + h * C * kCols;
+            if (at + cpiece * P < a.n && crow + 16 * k < rows) *reinterpret_cast<uint4*>(to[k] + at) = v[h][k];
+          }
       }
       continue;
     }
@@ -845,16 +879,20 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
   const int elem = (int)sizeof(T);
   if (a.T <= kAdDirect) {
     a.ctas = 1;
-    while (a.ctas < kAdMaxCtas && a.T * a.ctas < 2 * sm_count) a.ctas *= 2;
+    // CTAs per cluster: until every SM has one or a CTA's warps one step each.  us, 61 tokens of 4096 with 64 adapters of rank 16:
+    // 1 CTA 17.8, 2 13.5, 4 9.2, 8 11.7; one token of 1024: 6.0, 4.8, 4.2, 4.5.
+    while (a.ctas < kAdMaxCtas && a.T * a.ctas < sm_count && a.ctas * kAdWarps * (64 / elem) < (a.d > a.n ? a.d : a.n)) a.ctas *= 2;
     auto go = [&](auto kernel) {
       return launch_cluster(kernel, a.ctas, dim3(a.ctas * a.T), dim3(kAdThreads), ad_smem_bytes(a.r, elem), st, pdl, a);
     };
     return ad_rtw(a.r) == 1 ? go(adapters_few_kernel<X, T, 1>) : ad_rtw(a.r) == 2 ? go(adapters_few_kernel<X, T, 2>)
                                                                                   : go(adapters_few_kernel<X, T, 4>);
   }
-  const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(kAdPlanThreads), 0, st, pdl, a, kAdTM);
+  const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(a.T <= 2048 ? 256 : kAdPlanThreads), 0, st, pdl, a, kAdTM);
   if (e != cudaSuccess) return e;
   const int tiles = ad_max_tiles(a.T, a.count), rp = ad_rank_up(a.r), stages = ad_stages(rp, elem);
+  // us, 8192 tokens of 4096 at rank 64: 1 CTA 100, 2 64, 8 106 (two CTAs fit an SM, a second round costs as much as the first); 1531
+  // of 768 -> 2240 in fp32 at rank 8: 2 45, 4 27, 8 20.
   a.ctas = 1;
   while (a.ctas < kAdMaxCtas && tiles * a.ctas < sm_count + sm_count / 2) a.ctas *= 2;
   const dim3 grid(a.ctas * (tiles < kAdMaxClusters ? tiles : kAdMaxClusters));
