@@ -3,10 +3,11 @@
 // y as rows of the layer's dtype, as e4m3 rows with scales (q = y / s, s = max |y| / 448 over a row or a group of columns), or both.
 // The norm is taken of the sum before it is rounded, in fp32; every output is rounded once.
 //
-// Bound by HBM: each row is read once, kept in registers between the sum of squares and the scaling, and written once.  A team
-// of warps holds a row, eight columns per lane and chunk of 256.  y is computed as (h w) s: multiplying by the row's positive
-// factor keeps the order of magnitudes, so the largest |y| of a row is the largest |h w| times s to the last bit and is found in
-// the same exchange between the warps as the sum of squares.
+// Bound by HBM, and next to it by instructions: each row is read once, kept in registers between the sum of squares and the scaling,
+// and written once.  A team of warps holds a row, eight columns per lane and chunk of 256; fp32 arithmetic goes two values at a
+// time (f32x2).  Where 8-bit rows have one scale y is computed as (h w) s: multiplying by the row's positive factor keeps the order
+// of magnitudes, so the largest |y| of a row is the largest |h w| times s to the last bit and is found in the same exchange
+// between the warps as the sum of squares.
 #pragma once
 #include <cuda_fp8.h>
 #include <math_constants.h>
@@ -83,23 +84,49 @@ __device__ __forceinline__ void norm_store8_e4m3(uint8_t* row, int c0, int lane,
       if (c0 + i * 32 + lane < d) row[c0 + i * 32 + lane] = (uint8_t)pack_e4m3x2(v[i], 0.f);
   }
 }
-// Magnitudes as integers: their order is that of the values, with NaN above infinity.
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-
-// Scale of the largest magnitude, and its reciprocal (0 for a row or group of zeros, whose 8-bit values are zeros).
-__device__ __forceinline__ float norm_scale(float largest, float* inverse) {
-  const float s = largest > 0.f ? fmaxf(largest / kE4m3Max, kNormMinScale) : largest;     // NaN stays NaN
-  *inverse = s > 0.f ? 1.f / s : s;
-  return s;
+// Two products, sums at a time.
+__device__ __forceinline__ void mul2(float& a, float& b, float c, float d) {
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+__device__ __forceinline__ void add2(float& a, float& b, float c, float d) {
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+__device__ __forceinline__ void square2(float& a, float& b, float c, float d) {      // a += c c, b += d d
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n fma.rn.f32x2 x, y, y, x;\n mov.b64 {%0, %1}, x;\n}"
+      : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+// The largest of m, |a|, |b|; NaN if one of them is.
+__device__ __forceinline__ float max_magnitude(float m, float a, float b) {
+  asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return m;
+}
+__device__ __forceinline__ float largest8(const float (&v)[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) m = max_magnitude(m, v[i], v[i + 1]);
+  return m;
+}
+// (values that are not negative, infinities and NaN among them, are ordered as their bits)
+__device__ __forceinline__ float warp_largest(float m) {
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m) & 0x7fffffffu));
 }
 
-// T: rows and weight; R: the residual's rows; kChunks: chunks per warp.
-template <typename T, typename R, int kChunks, bool kVec>
-__global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const RmsNormArgs a) {
-  __shared__ float s_sum[kNormMaxWarps];
-  __shared__ uint32_t s_max[kNormMaxWarps];
+// Scale of the largest magnitude, and its reciprocal (0 for a row or group of zeros, whose 8-bit values are zeros; NaN for NaN).
+__device__ __forceinline__ float norm_scale(float largest, float* inverse) {
+  const float s = largest == 0.f ? 0.f : largest * (1.f / kE4m3Max);
+  const float t = s < kNormMinScale ? kNormMinScale : s;                // NaN stays NaN
+  *inverse = __fdividef(1.f, t);                                       // (t is below 2^119)
+  return largest == 0.f ? 0.f : t;
+}
+
+// T: rows and weight; R: the residual's rows; kChunks: chunks per warp; kRow8: 8-bit rows with one scale each.
+template <typename T, typename R, int kChunks, bool kVec, bool kRow8>
+__global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __grid_constant__ RmsNormArgs a) {
+  __shared__ float s_sum[kNormMaxWarps], s_max[kNormMaxWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int team = warp / a.warps_per_row, wr = warp - team * a.warps_per_row;
+  const int team = warp / a.warps_per_row, wr = warp - team * a.warps_per_row, team0 = team * a.warps_per_row;
   const long long row = (long long)blockIdx.x * a.rows_per_cta + team;
   const bool active = row < a.T;
   const int d = active ? a.d : 0;        // a team without a row computes on zeros and stores nothing
@@ -116,7 +143,7 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const RmsN
 #pragma unroll
     for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] += p[j][i];
+      for (int i = 0; i < 8; i += 2) add2(h[j][i], h[j][i + 1], p[j][i], p[j][i + 1]);
     if (a.residual_out != nullptr) {
       R* ro = static_cast<R*>(a.residual_out) + row * a.residual_out_stride;
 #pragma unroll
@@ -124,142 +151,140 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const RmsN
     }
   }
   if (a.out == nullptr && a.out8 == nullptr) return;                  // the same for the whole grid
-  float sum = 0.f;
-  uint32_t most = 0u;
+  float sum = 0.f, sum1 = 0.f, most = 0.f;
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
     norm_load8<kVec>(static_cast<const T*>(a.weight), (wr + j * a.warps_per_row) * kNormChunk, lane, d, p[j]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sum = fmaf(h[j][i], h[j][i], sum);
-      p[j][i] *= h[j][i];
-      most = max(most, magnitude(p[j][i]));
+    for (int i = 0; i < 8; i += 2) square2(sum, sum1, h[j][i], h[j][i + 1]);
+    if constexpr (kRow8) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        mul2(p[j][i], p[j][i + 1], h[j][i], h[j][i + 1]);             // h w
+        most = max_magnitude(most, p[j][i], p[j][i + 1]);
+      }
     }
   }
-  sum = warp_sum(sum);
-  most = __reduce_max_sync(0xffffffffu, most);
-  if (lane == 0) { s_sum[warp] = sum; s_max[warp] = most; }
+  sum = warp_sum(sum + sum1);
+  if constexpr (kRow8) most = warp_largest(most);
+  if (lane == 0) {
+    s_sum[warp] = sum;
+    if constexpr (kRow8) s_max[warp] = most;
+  }
   // squares that leave the range of fp32 (rows of 1e18 and more, or below 1e-15 with next to no eps), infinities, NaN
-  const bool rare = !(sum < 1e36f) || most >= 0x7f800000u || (sum < 1e-28f && a.eps < 1e-25f);
+  const bool rare = !(sum < 1e36f) || (kRow8 && !(most < 3e38f)) || (sum < 1e-28f && a.eps < 1e-25f);
   const bool slow = __syncthreads_or(rare) != 0;
-  float total = 0.f;
-  uint32_t largest = 0u;
+  float total = 0.f, largest = 0.f;
   for (int w = 0; w < a.warps_per_row; ++w) {
-    total += s_sum[team * a.warps_per_row + w];
-    largest = max(largest, s_max[team * a.warps_per_row + w]);
+    total += s_sum[team0 + w];
+    if constexpr (kRow8) largest = fmaxf(largest, s_max[team0 + w]);
   }
   float s = rsqrtf(total / (float)a.d + a.eps);
   if (slow) {
     // the same with the row divided by its largest magnitude m: h / sqrt(mean(h^2) + eps) = (h / m) / sqrt(mean((h / m)^2) + eps / m^2)
-    most = 0u;
+    auto over_team = [&](float v, bool add) {
+      __syncthreads();
+      if (lane == 0) s_sum[warp] = v;
+      __syncthreads();
+      float t = s_sum[team0];
+      for (int w = 1; w < a.warps_per_row; ++w) t = add ? t + s_sum[team0 + w] : max_magnitude(t, s_sum[team0 + w], 0.f);
+      return t;
+    };
+    most = 0.f;
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) most = max_magnitude(most, largest8(h[j]), 0.f);
+    const float m = over_team(warp_largest(most), false);
+    const bool scaled = m > 0.f && m < CUDART_INF_F;
+    sum = 0.f;
+    most = 0.f;
 #pragma unroll
     for (int j = 0; j < kChunks; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) most = max(most, magnitude(h[j][i]));
-    most = __reduce_max_sync(0xffffffffu, most);
-    __syncthreads();
-    if (lane == 0) s_max[warp] = most;
-    __syncthreads();
-    for (int w = 0; w < a.warps_per_row; ++w) most = max(most, s_max[team * a.warps_per_row + w]);
-    const float m = __uint_as_float(most);
-    const bool scaled = most > 0u && most < 0x7f800000u;
-    sum = 0.f;
-    most = 0u;
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-      norm_load8<kVec>(static_cast<const T*>(a.weight), (wr + j * a.warps_per_row) * kNormChunk, lane, d, p[j]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (scaled) h[j][i] /= m;
         sum = fmaf(h[j][i], h[j][i], sum);
       }
-    }
-    sum = warp_sum(sum);
-    __syncthreads();
-    if (lane == 0) s_sum[warp] = sum;
-    __syncthreads();
-    total = 0.f;
-    for (int w = 0; w < a.warps_per_row; ++w) total += s_sum[team * a.warps_per_row + w];
+    total = over_team(warp_sum(sum), true);
     s = rsqrtf(total / (float)a.d + (scaled ? a.eps / m / m : a.eps));
-    // the row's factor goes into the products at once: an infinity among them would be none behind it
+    if constexpr (kRow8) {
+      // the row's factor goes into the products at once: an infinity among them would be none behind it
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j)
+      for (int j = 0; j < kChunks; ++j) {
+        norm_load8<kVec>(static_cast<const T*>(a.weight), (wr + j * a.warps_per_row) * kNormChunk, lane, d, p[j]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[j][i] *= h[j][i] * s;
-        most = max(most, magnitude(p[j][i]));
+        for (int i = 0; i < 8; ++i) p[j][i] *= h[j][i] * s;
+        most = max_magnitude(most, largest8(p[j]), 0.f);
       }
-    s = 1.f;
-    most = __reduce_max_sync(0xffffffffu, most);
-    __syncthreads();
-    if (lane == 0) s_max[warp] = most;
-    __syncthreads();
-    largest = 0u;
-    for (int w = 0; w < a.warps_per_row; ++w) largest = max(largest, s_max[team * a.warps_per_row + w]);
+      s = 1.f;
+      largest = over_team(warp_largest(most), false);
+    }
   }
+  float (&y)[kChunks][8] = kRow8 ? p : h;
 #pragma unroll
   for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[j][i] *= s;
+    for (int i = 0; i < 8; i += 2) {
+      mul2(y[j][i], y[j][i + 1], s, s);
+      if constexpr (!kRow8) mul2(y[j][i], y[j][i + 1], p[j][i], p[j][i + 1]);
+    }
   if (a.out != nullptr) {
     T* o = static_cast<T*>(a.out) + row * a.out_stride;
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) norm_store8<kVec>(o, (wr + j * a.warps_per_row) * kNormChunk, lane, d, p[j]);
+    for (int j = 0; j < kChunks; ++j) norm_store8<kVec>(o, (wr + j * a.warps_per_row) * kNormChunk, lane, d, y[j]);
   }
   if (a.out8 == nullptr) return;
   uint8_t* q = a.out8 + row * a.out8_stride;
   float* sc = a.scales + row * a.scales_stride;
-  if (a.group == 0) {
+  if constexpr (kRow8) {
     float inv;
-    const float scale = norm_scale(__uint_as_float(largest) * s, &inv);
+    const float scale = norm_scale(largest * s, &inv);
     if (active && wr == 0 && lane == 0) sc[0] = scale;
 #pragma unroll
     for (int j = 0; j < kChunks; ++j) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[j][i] *= inv;
-      norm_store8_e4m3<kVec>(q, (wr + j * a.warps_per_row) * kNormChunk, lane, d, p[j]);
+      for (int i = 0; i < 8; i += 2) mul2(y[j][i], y[j][i + 1], inv, inv);
+      norm_store8_e4m3<kVec>(q, (wr + j * a.warps_per_row) * kNormChunk, lane, d, y[j]);
     }
-    return;
-  }
+  } else {
+    const int shift = 31 - __clz(a.group);
 #pragma unroll
-  for (int j = 0; j < kChunks; ++j) {
-    const int c0 = (wr + j * a.warps_per_row) * kNormChunk;
-    if constexpr (kVec) {
-      // a group is group / 8 neighbouring lanes
-      uint32_t m = 0u;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, magnitude(p[j][i]));
-      for (int o = a.group >> 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-      float inv;
-      const float scale = norm_scale(__uint_as_float(m), &inv);
-      const int c = c0 + lane * 8;
-      if (c < d && (c & (a.group - 1)) == 0) sc[c / a.group] = scale;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[j][i] *= inv;
-    } else {
-      // a group is group / 32 of the lanes' columns, over all lanes
-      uint32_t m[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m[i] = __reduce_max_sync(0xffffffffu, magnitude(p[j][i]));
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1)
-        if (a.group >= 64 * o) {
-          uint32_t t[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) t[i] = max(m[i], m[i ^ o]);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) m[i] = t[i];
-        }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
+    for (int j = 0; j < kChunks; ++j) {
+      const int c0 = (wr + j * a.warps_per_row) * kNormChunk;
+      if constexpr (kVec) {
+        // a group is group / 8 neighbouring lanes
+        float m = largest8(y[j]);
+        for (int o = a.group >> 4; o > 0; o >>= 1) m = max_magnitude(m, __shfl_xor_sync(0xffffffffu, m, o), 0.f);
         float inv;
-        const float scale = norm_scale(__uint_as_float(m[i]), &inv);
-        const int c = c0 + i * 32;
-        if (lane == 0 && c < d && (c & (a.group - 1)) == 0) sc[c / a.group] = scale;
-        p[j][i] *= inv;
+        const float scale = norm_scale(m, &inv);
+        const int c = c0 + lane * 8;
+        if (c < d && (c & (a.group - 1)) == 0) sc[c >> shift] = scale;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) mul2(y[j][i], y[j][i + 1], inv, inv);
+      } else {
+        // a group is group / 32 of the lanes' columns, over all lanes
+        float m[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = warp_largest(y[j][i]);
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1)
+          if (a.group >= 64 * o) {
+            float t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = max_magnitude(m[i], m[i ^ o], 0.f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[i] = t[i];
+          }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float inv;
+          const float scale = norm_scale(m[i], &inv);
+          const int c = c0 + i * 32;
+          if (lane == 0 && c < d && (c & (a.group - 1)) == 0) sc[c >> shift] = scale;
+          y[j][i] *= inv;
+        }
       }
+      norm_store8_e4m3<kVec>(q, c0, lane, d, y[j]);
     }
-    norm_store8_e4m3<kVec>(q, c0, lane, d, p[j]);
   }
 }
 
@@ -273,8 +298,11 @@ inline cudaError_t rms_norm_launch_typed(RmsNormArgs a, bool vec, int sm_count, 
   a.rows_per_cta = few || a.warps_per_row >= 8 ? 1 : 8 / a.warps_per_row;
   const dim3 grid((unsigned)((a.T + a.rows_per_cta - 1) / a.rows_per_cta)), block(32 * a.warps_per_row * a.rows_per_cta);
   auto go = [&](auto kernel) { return launch_kernel(kernel, grid, block, 0, st, pdl, a); };
-  if (vec) return per_warp == 1 ? go(rms_norm_kernel<T, R, 1, true>) : go(rms_norm_kernel<T, R, 2, true>);
-  return per_warp == 1 ? go(rms_norm_kernel<T, R, 1, false>) : go(rms_norm_kernel<T, R, 2, false>);
+  const bool row8 = a.out8 != nullptr && a.group == 0;
+  if (vec && row8) return few ? go(rms_norm_kernel<T, R, 1, true, true>) : go(rms_norm_kernel<T, R, 2, true, true>);
+  if (vec) return few ? go(rms_norm_kernel<T, R, 1, true, false>) : go(rms_norm_kernel<T, R, 2, true, false>);
+  if (row8) return few ? go(rms_norm_kernel<T, R, 1, false, true>) : go(rms_norm_kernel<T, R, 2, false, true>);
+  return few ? go(rms_norm_kernel<T, R, 1, false, false>) : go(rms_norm_kernel<T, R, 2, false, false>);
 }
 
 }  // namespace swapmoe
