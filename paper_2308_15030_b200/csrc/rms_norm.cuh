@@ -32,7 +32,7 @@ struct RmsNormArgs {
   float* scales;
   long long x_stride, residual_stride, residual_out_stride, out_stride, out8_stride, scales_stride;   // elements
   int T, d, group;                       // group: columns per scale (0: one scale per row)
-  float eps;
+  float eps, per_column;                 // per_column: 1 / d
   int warps_per_row, rows_per_cta;
 };
 
@@ -47,8 +47,15 @@ template <bool kVec, typename T>
 __device__ __forceinline__ void norm_load8(const T* row, int c0, int lane, int d, float (&v)[8]) {
   if constexpr (kVec) {
     if (c0 + lane * 8 < d) {
-      load4(row + c0 + lane * 8, v);
-      load4(row + c0 + lane * 8 + 4, v + 4);
+      if constexpr (sizeof(T) == 2) {
+        const uint4 u = *reinterpret_cast<const uint4*>(row + c0 + lane * 8);
+        const uint32_t q[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(q[i] << 16); v[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u); }
+      } else {
+        load4(row + c0 + lane * 8, v);
+        load4(row + c0 + lane * 8 + 4, v + 4);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = 0.f;
@@ -124,9 +131,9 @@ __device__ __forceinline__ float norm_scale(float largest, float* inverse) {
 // T: rows and weight; R: the residual's rows; kChunks: chunks per warp; kRow8: 8-bit rows with one scale each.
 template <typename T, typename R, int kChunks, bool kVec, bool kRow8>
 __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __grid_constant__ RmsNormArgs a) {
-  __shared__ float s_sum[kNormMaxWarps], s_max[kNormMaxWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int team = warp / a.warps_per_row, wr = warp - team * a.warps_per_row, team0 = team * a.warps_per_row;
+  __shared__ __align__(16) float s_sum[kNormMaxWarps], s_max[kNormMaxWarps];
+  const int lane = threadIdx.x & 31, wr = threadIdx.x >> 5, team = threadIdx.y;       // a team per row: blockDim.x threads
+  const int team0 = team * a.warps_per_row, warp = team0 + wr;
   const long long row = (long long)blockIdx.x * a.rows_per_cta + team;
   const bool active = row < a.T;
   const int d = active ? a.d : 0;        // a team without a row computes on zeros and stores nothing
@@ -175,11 +182,20 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
   const bool rare = !(sum < 1e36f) || (kRow8 && !(most < 3e38f)) || (sum < 1e-28f && a.eps < 1e-25f);
   const bool slow = __syncthreads_or(rare) != 0;
   float total = 0.f, largest = 0.f;
-  for (int w = 0; w < a.warps_per_row; ++w) {
+  int w = 0;
+  for (; w + 4 <= a.warps_per_row && team0 % 4 == 0; w += 4) {
+    const float4 t = *reinterpret_cast<const float4*>(s_sum + team0 + w);
+    total += (t.x + t.y) + (t.z + t.w);
+    if constexpr (kRow8) {
+      const float4 m = *reinterpret_cast<const float4*>(s_max + team0 + w);
+      largest = fmaxf(largest, fmaxf(fmaxf(m.x, m.y), fmaxf(m.z, m.w)));
+    }
+  }
+  for (; w < a.warps_per_row; ++w) {
     total += s_sum[team0 + w];
     if constexpr (kRow8) largest = fmaxf(largest, s_max[team0 + w]);
   }
-  float s = rsqrtf(total / (float)a.d + a.eps);
+  float s = rsqrtf(total * a.per_column + a.eps);
   if (slow) {
     // the same with the row divided by its largest magnitude m: h / sqrt(mean(h^2) + eps) = (h / m) / sqrt(mean((h / m)^2) + eps / m^2)
     auto over_team = [&](float v, bool add) {
@@ -205,7 +221,7 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
         sum = fmaf(h[j][i], h[j][i], sum);
       }
     total = over_team(warp_sum(sum), true);
-    s = rsqrtf(total / (float)a.d + (scaled ? a.eps / m / m : a.eps));
+    s = rsqrtf(total * a.per_column + (scaled ? a.eps / m / m : a.eps));
     if constexpr (kRow8) {
       // the row's factor goes into the products at once: an infinity among them would be none behind it
 #pragma unroll
@@ -296,7 +312,8 @@ inline cudaError_t rms_norm_launch_typed(RmsNormArgs a, bool vec, int sm_count, 
   const int per_warp = few ? 1 : 2;
   a.warps_per_row = (chunks + per_warp - 1) / per_warp;
   a.rows_per_cta = few || a.warps_per_row >= 8 ? 1 : 8 / a.warps_per_row;
-  const dim3 grid((unsigned)((a.T + a.rows_per_cta - 1) / a.rows_per_cta)), block(32 * a.warps_per_row * a.rows_per_cta);
+  const dim3 grid((unsigned)((a.T + a.rows_per_cta - 1) / a.rows_per_cta)), block(32 * a.warps_per_row, a.rows_per_cta);
+  a.per_column = 1.f / (float)a.d;
   auto go = [&](auto kernel) { return launch_kernel(kernel, grid, block, 0, st, pdl, a); };
   const bool row8 = a.out8 != nullptr && a.group == 0;
   if (vec && row8) return few ? go(rms_norm_kernel<T, R, 1, true, true>) : go(rms_norm_kernel<T, R, 2, true, true>);
