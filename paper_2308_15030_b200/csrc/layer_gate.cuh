@@ -9,6 +9,8 @@
 
 namespace swapmoe {
 
+static_assert(kMaxE <= 256, "experts per lane of layer_gate_launch");
+
 constexpr int kLayerGateWarps = 8, kLayerGateThreads = kLayerGateWarps * 32, kLayerGateTok = 32;
 
 // a: the router's arguments with the scan of this kernel's CTAs; tok: tokens per CTA (8, 16 or 32).  A warp routes tok / 8 tokens.
@@ -16,13 +18,14 @@ template <int N>
 __global__ void __launch_bounds__(kLayerGateThreads) layer_gate_kernel(const __grid_constant__ RouterArgs a,
                                                                         const __grid_constant__ RouteGate gate, const float* bias, int tok) {
   __shared__ double s_choice[kLayerGateWarps][32 * N];
+  __shared__ __align__(16) uint32_t s_list[kLayerGateWarps][32 * route_pow2(N) + 64];
   __shared__ __align__(16) int s_e[kLayerGateTok * kMaxTopK], s_s[kLayerGateTok * kMaxTopK];      // expert, slot per pair
   __shared__ __align__(16) float s_t[kLayerGateTok * kMaxTopK], s_m[kLayerGateTok * kMaxTopK];    // Eq. (1) terms of both routings
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = a.E, k = a.k;
   pdl_wait();
   pdl_trigger();
   const int tok0 = blockIdx.x * tok;
-  const RouteLane any = route_lane<N>(gate, nullptr, E), resident = route_lane<N>(gate, a.e2s, E);
+  const RouteLane<N> any = route_lane<N>(gate, nullptr, E), resident = route_lane<N>(gate, a.e2s, E);
   float b[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) b[i] = bias != nullptr && lane * N + i < E ? bias[lane * N + i] : 0.f;
@@ -41,9 +44,10 @@ __global__ void __launch_bounds__(kLayerGateThreads) layer_gate_kernel(const __g
     for (int i = 0; i < N; ++i) l[i] = fmaxf(l[i], -CUDART_INF_F);
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
-      const RouteLane& rl = pass == 0 ? any : resident;
+      RouteLane<N> rl = any;
+      if (pass == 1) rl = resident;
       bool clear;
-      int e = route_choose_fast<N>(gate, l, b, bias != nullptr, rl, E, k, reinterpret_cast<float*>(s_choice[warp]), &clear);
+      int e = route_choose_fast<N>(gate, l, b, bias != nullptr, rl, E, k, row, bias, reinterpret_cast<float*>(s_choice[warp]), s_list[warp], &clear);
       if (!clear) e = route_choose_exact<N>(gate, row, bias, rl.allow, E, k, s_choice[warp]);
       const float w = route_weight<N>(gate, l, rl.allow, e, e >= 0 ? fmaxf(row[e], -CUDART_INF_F) : -CUDART_INF_F);
       if (lane < k) {
@@ -104,8 +108,7 @@ inline cudaError_t layer_gate_launch(const RouterArgs& a, const RouteGate& gate,
     case 5: return go(layer_gate_kernel<5>);
     case 6: return go(layer_gate_kernel<6>);
     case 8: return go(layer_gate_kernel<8>);
-    case 12: return go(layer_gate_kernel<12>);
-    default: return go(layer_gate_kernel<16>);
+    default: return go(layer_gate_kernel<12>);       // (up to 256 experts: no more than twelve per lane)
   }
 }
 

@@ -8,9 +8,11 @@
 // the lowest lane.  The order of the choices is that of 64-bit scores: of thousands of tokens some have two experts closer than
 // fp32 tells apart.  Without a bias, and with groups valued by their best expert, it is that of the logits themselves.
 //
-// Bound by instructions, not by bytes (a row is 4 E bytes): so scores are fp32, and only a token whose choice hangs on a gap that is
-// not clear of their error is routed again in 64 bits (about one in 200; with 64 bits for all of them 16384 x 256 took 60 us).  Each lane sorts its
-// experts once, with their places in the keys' last bits; then a choice is one warp reduction, one vote and a shift of the winner's list.
+// Bound by instructions, not by bytes (a row is 4 E bytes; 16384 x 256 with eight groups, a bias and top-8: 24.8 us, 2.8 of bytes,
+// about 1000 instructions per token): so scores are fp32, and where a choice hangs on a gap that is not clear of their error the
+// experts or groups in doubt are compared in 64 bits, a lane each; only what that cannot settle is routed again with all scores in
+// 64 bits (one token's worth of that takes some 10 us on its own; with 64 bits for all tokens 60 us).  Each lane sorts its experts
+// once, with their places in the keys' last bits; then a choice is one warp reduction, one vote and a step down the winner's list.
 #pragma once
 #include <math_constants.h>
 
@@ -204,6 +206,18 @@ static __device__ __noinline__ int route_choose_exact(const RouteGate& g, const 
 }
 
 // ----------------------------------------------------------------------------- fp32, with a check of the gaps
+// 2^x and 1 / x by the hardware's approximations (errors 2^-22 and 2^-23), denormal results as 0.
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float fast_reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 __host__ __device__ constexpr int route_pow2(int n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : n <= 8 ? 8 : 16; }
 
 // Descending order of M = 2^m keys (Batcher's odd-even merge sort: 19 exchanges for eight, 63 for sixteen).
@@ -224,9 +238,12 @@ __device__ __forceinline__ void sort_keys(uint32_t (&k)[M]) {
           }
 }
 
-// What a warp keeps for all its tokens: which of the lane's experts may be chosen, and how groups lie on the lanes.
+// What a warp keeps for all its tokens: which of the lane's experts may be chosen (bits, and masks of their keys), and how many of
+// the lane's group.
+template <int N>
 struct RouteLane {
   uint32_t allow;
+  uint32_t mask[N];
   bool all;                  // no table: every expert may be chosen
   int have;                  // aligned groups: allowed experts of the lane's group
 };
@@ -234,15 +251,17 @@ struct RouteLane {
 __device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
 template <int N>
-__device__ __forceinline__ RouteLane route_lane(const RouteGate& g, const int32_t* expert_to_slot, int E) {
+__device__ __forceinline__ RouteLane<N> route_lane(const RouteGate& g, const int32_t* expert_to_slot, int E) {
   const int lane = threadIdx.x & 31;
-  RouteLane r;
+  RouteLane<N> r;
   r.allow = 0u;
   r.all = expert_to_slot == nullptr;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int e = lane * N + i;
-    if (e < E && (expert_to_slot == nullptr || expert_to_slot[e] >= 0)) r.allow |= 1u << i;
+    const bool may = e < E && (expert_to_slot == nullptr || expert_to_slot[e] >= 0);
+    r.allow |= (may ? 1u : 0u) << i;
+    r.mask[i] = may ? 0xffffffffu : 0u;
   }
   r.have = __popc(r.allow);
   const int lanes = route_group_lanes(g.group_size, N);
@@ -250,11 +269,12 @@ __device__ __forceinline__ RouteLane route_lane(const RouteGate& g, const int32_
   return r;
 }
 
-// As route_choose_exact, from the lane's logits l (NaN replaced by -infinity) and biases b.  *clear: no gap that the choice hangs on is
-// within the error of what was compared; if not, the result is not to be used.
+// As route_choose_exact, from the lane's logits l (NaN replaced by -infinity) and biases b.  s_list: 32 M + 64 words of the warp's own.  *clear: no gap that the
+// choice hangs on is within the error of what was compared; if not, the result is not to be used.
 template <int N>
 __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float (&l)[N], const float (&b)[N], bool with_bias,
-                                                 const RouteLane& rl, int E, int k, float* s_choice, bool* clear) {
+                                                 const RouteLane<N>& rl, int E, int k, const float* row, const float* bias, float* s_choice,
+                                                 uint32_t* s_list, bool* clear) {
   constexpr int M = route_pow2(N);
   constexpr uint32_t kPlace = M - 1;                        // bits of a key that hold the expert's place (first places larger)
   const int lane = threadIdx.x & 31, e0 = lane * N;
@@ -269,19 +289,19 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
       m = warp_max(m);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        c[i] = (rl.allow >> i) & 1u ? (l[i] == m ? 1.f : __expf(l[i] - m)) : 0.f;
+        c[i] = (rl.allow >> i) & 1u ? (l[i] == m ? 1.f : fast_exp2((l[i] - m) * 1.44269504f)) : 0.f;
         sum += c[i];
       }
       const float inv = 1.f / warp_sum(sum);
 #pragma unroll
       for (int i = 0; i < N; ++i) c[i] *= inv;
-      // exponentials: (2 + 1.2 |x|) 2^-23 of themselves, that is 1.5e-7 of the largest score (1 / sum) where it counts; sums of up to 21
+      // exponentials: (2 + |x|) 2^-22 of themselves, that is 5e-7 of the largest score (1 / sum) where it counts; sums of up to 21
       // steps, reciprocal and product: 24 x 2^-24 of the score
       error = 2e-6f * inv;
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) c[i] = __fdividef(1.f, 1.f + __expf(-l[i]));
-      // s (1 - s) (2 + 1.2 |x|) 2^-23 <= 1e-7 from the exponential, three roundings of at most 2^-23 each
+      for (int i = 0; i < N; ++i) c[i] = fast_reciprocal(1.f + fast_exp2(l[i] * -1.44269504f));
+      // exponential: |x| 2^-23 from its argument and 2^-22 of itself, times s (1 - s): below 2e-7; two roundings and the reciprocal's 2^-23
       error = 5e-7f;
     }
     if (with_bias)
@@ -289,16 +309,15 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
       for (int i = 0; i < N; ++i) c[i] += b[i];
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) c[i] = l[i];
+    for (int i = 0; i < N; ++i) c[i] = l[i] + 0.f;                      // (-0 becomes +0)
   }
   uint32_t key[M];
 #pragma unroll
   for (int i = 0; i < M; ++i) {
     key[i] = 0u;
-    if (i < N && ((rl.allow >> (i < N ? i : 0)) & 1u)) {
-      const float v = fmaxf(c[i < N ? i : 0], -CUDART_INF_F);          // NaN (of a bias) as -infinity
-      const uint32_t u = __float_as_uint(v);
-      key[i] = ((u & 0x80000000u ? ~u : u | 0x80000000u) & ~kPlace) | (kPlace - i);
+    if (i < N) {
+      const uint32_t u = __float_as_uint(fmaxf(c[i < N ? i : 0], -CUDART_INF_F));         // NaN (of a bias) as -infinity
+      key[i] = (((u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) & ~kPlace) | (kPlace - i)) & rl.mask[i < N ? i : 0];
     }
   }
   auto value_of = [&](uint32_t q) { return gate_key_value(q & ~kPlace); };
@@ -379,6 +398,45 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
         pool += __shfl_sync(0xffffffffu, have, winner);
       }
     }
+    {
+      // groups closer than the error allows: the lanes' two best experts in 64 bits, if no third one can matter, and the groups again
+      const uint32_t group_below = __shfl_down_sync(0xffffffffu, group_at, 1);
+      const float slack = 4.f * error + 2.f * kCut * group_size;
+      const bool near = lane < 31 && group_below != 0u && !(gate_key_value(group_at) - gate_key_value(group_below) > slack);
+      if (__any_sync(0xffffffffu, near) && lanes > 0 && group_size < CUDART_INF_F && !(by_score && g.score == SWAPMOE_SCORE_SOFTMAX)) {
+        const bool third = M > 2 && key[M > 2 ? 2 : 0] != 0u && !(v2 - value_of(key[M > 2 ? 2 : 0]) > slack);
+        if (!__any_sync(0xffffffffu, third)) {
+          double w1 = -CUDART_INF, w2 = -CUDART_INF;
+#pragma unroll 1
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t q = i == 0 ? key[0] : M > 1 ? key[M > 1 ? 1 : 0] : 0u;
+            if (q == 0u) continue;
+            const int e = e0 + (int)(kPlace - (q & kPlace));
+            double x = (double)fmaxf(row[e], -CUDART_INF_F);
+            if (by_score) x = 1.0 / (1.0 + exp(-x)) + (bias != nullptr ? (double)bias[e] : 0.0);
+            w2 = fmax(w2, fmin(w1, x));
+            w1 = fmax(w1, x);
+          }
+          for (int o = 1; o < lanes; o <<= 1) {
+            const double u1 = __shfl_xor_sync(0xffffffffu, w1, o), u2 = __shfl_xor_sync(0xffffffffu, w2, o);
+            w2 = fmax(fmin(w1, u1), fmax(w2, u2));
+            w1 = fmax(w1, u1);
+          }
+          unsigned long long exact = have > 0 ? choice_key(g.group_top > 1 && have > 1 ? w1 + w2 : w1) : 0ull;
+          kept = 0u;
+          for (int taken = 0, pool = 0; taken < g.topk_groups || pool < k; ++taken) {
+            const unsigned long long best = warp_max_key(exact);
+            if (best == 0ull) break;
+            const int winner = __ffs(__ballot_sync(0xffffffffu, exact == best)) - 1;
+            const bool in = (lane & ~(lanes - 1)) == winner;
+            kept |= __ballot_sync(0xffffffffu, in);
+            pool += __shfl_sync(0xffffffffu, have, winner);
+            if (in) exact = 0ull;
+          }
+          group_at = 0u;                                    // settled
+        }
+      }
+    }
     if (lanes > 0) {
       if (!((kept >> lane) & 1u))
 #pragma unroll
@@ -390,20 +448,27 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
     }
   }
   if (lanes == 0) sort_keys<M>(key);
-  int mine = -1;
+  // the lists' heads in registers, what is behind them in shared memory: the winner reads its next one
+  uint32_t* const list = s_list + lane * M;
+  __syncwarp();
+  if constexpr (M >= 4) {
+#pragma unroll
+    for (int i = 0; i < M; i += 4) *reinterpret_cast<uint4*>(list + i) = make_uint4(key[i], key[i + 1], key[i + 2], key[i + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < M; ++i) list[i] = key[i];
+  }
+  int mine = -1, at = 0;
+  uint32_t head = key[0];
 #pragma unroll 1
   for (int j = 0; j < k; ++j) {
-    const uint32_t top = __reduce_max_sync(0xffffffffu, key[0]);
+    const uint32_t top = __reduce_max_sync(0xffffffffu, head);
     if (top == 0u) break;
-    const int winner = __ffs(__ballot_sync(0xffffffffu, key[0] == top)) - 1;
+    const int winner = __ffs(__ballot_sync(0xffffffffu, head == top)) - 1;
     if (lane == j) { choice_at = top; mine = winner; }
-    if (lane == winner) {
-#pragma unroll
-      for (int i = 0; i + 1 < M; ++i) key[i] = key[i + 1];
-      key[M - 1] = 0u;
-    }
+    if (lane == winner) head = ++at < M ? list[at] : 0u;
   }
-  const uint32_t behind = __reduce_max_sync(0xffffffffu, key[0]);       // the best one that was not chosen
+  const uint32_t behind = __reduce_max_sync(0xffffffffu, head);       // the best one that was not chosen
   if (lane == k) choice_at = behind;
   if (mine >= 0) mine = mine * N + (int)(kPlace - (choice_at & kPlace));
   // the gaps between neighbours of the two lists, and the largest magnitude in them (infinities fail the comparison)
@@ -412,9 +477,36 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
   const uint32_t size = __reduce_max_sync(0xffffffffu, choice_at != 0u ? magnitude_bits(v) : 0u);
   const float slack = 2.f * error + kCut * __uint_as_float(size);
   const float group_slack = 4.f * error + 2.f * kCut * group_size;
-  const bool near = (lane < k && below != 0u && !(v - value_of(below) > slack)) ||
-                    (lane < 31 && group_below != 0u && !(w - gate_key_value(group_below) > group_slack));
-  *clear = !__any_sync(0xffffffffu, near) && size < 0x7f800000u && group_size < CUDART_INF_F;
+  const bool finite = size < 0x7f800000u && group_size < CUDART_INF_F;
+  const bool near_group = lane < 31 && group_below != 0u && !(w - gate_key_value(group_below) > group_slack);
+  const bool near = lane < k && below != 0u && !(v - value_of(below) > slack);
+  *clear = !__any_sync(0xffffffffu, near || near_group) && finite;
+  if (*clear || __any_sync(0xffffffffu, near_group) || !finite || (by_score && g.score == SWAPMOE_SCORE_SOFTMAX)) return mine;
+  // Only the order within the list is in doubt, if the best one that was not chosen is clear of the next one: then 64-bit values of
+  // the list's k + 1 experts settle it, a lane each.
+  const int winner = __ffs(__ballot_sync(0xffffffffu, head == behind)) - 1;
+  if (lane == winner) head = ++at < M ? list[at] : 0u;
+  const uint32_t next = __reduce_max_sync(0xffffffffu, head);
+  if (behind != 0u && next != 0u && !(value_of(behind) - value_of(next) > slack)) return mine;
+  if (lane == k) mine = behind != 0u ? winner * N + (int)(kPlace - (behind & kPlace)) : -1;
+  unsigned long long exact = 0ull;
+  if (lane <= k && mine >= 0) {
+    const double x = (double)fmaxf(row[mine], -CUDART_INF_F);
+    exact = choice_key(!by_score ? x : 1.0 / (1.0 + exp(-x)) + (bias != nullptr ? (double)bias[mine] : 0.0));
+  }
+  int rank = 0;
+  for (int i = 0; i <= k; ++i) {
+    const unsigned long long other = __shfl_sync(0xffffffffu, exact, i);
+    const int e = __shfl_sync(0xffffffffu, mine, i);
+    rank += other > exact || (other == exact && e < mine && other != 0ull);
+  }
+  __syncwarp();
+  if (lane <= k) s_list[exact != 0ull ? rank : 32 + lane] = (uint32_t)mine;      // (places of those that do not exist: nobody's)
+  const int chosen = __popc(__ballot_sync(0xffffffffu, lane <= k && exact != 0ull));
+  __syncwarp();
+  mine = lane < min(k, chosen) ? (int)s_list[lane] : -1;
+  __syncwarp();
+  *clear = true;
   return mine;
 }
 
@@ -468,6 +560,7 @@ __device__ __forceinline__ void route_load(const float* row, int E, bool vec, fl
 template <int N>
 __global__ void __launch_bounds__(kRouteWarps * 32, N <= 8 ? 8 : 4) route_groups_kernel(const __grid_constant__ RouteGroupsArgs a, int vec) {
   __shared__ double s_choice[kRouteWarps][32 * N];
+  __shared__ __align__(16) uint32_t s_list[kRouteWarps][32 * route_pow2(N) + 64];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
@@ -477,23 +570,43 @@ __global__ void __launch_bounds__(kRouteWarps * 32, N <= 8 ? 8 : 4) route_groups
   const float* row = a.logits + token * a.stride;
   float l[N], next[N], b[N];
   route_load<N>(row, a.E, vec, next);
-  const RouteLane rl = route_lane<N>(a.gate, a.expert_to_slot, a.E);
+  const RouteLane<N> rl = route_lane<N>(a.gate, a.expert_to_slot, a.E);
 #pragma unroll
   for (int i = 0; i < N; ++i) b[i] = a.bias != nullptr && lane * N + i < a.E ? a.bias[lane * N + i] : 0.f;
-#pragma unroll 1
-  for (; token < a.T; token += step, row += step * a.stride) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) l[i] = fmaxf(next[i], -CUDART_INF_F);
-    if (token + step < a.T) route_load<N>(row + step * a.stride, a.E, vec, next);
-    bool clear;
-    int e = route_choose_fast<N>(a.gate, l, b, a.bias != nullptr, rl, a.E, a.k, reinterpret_cast<float*>(s_choice[warp]), &clear);
-    if (!clear) e = route_choose_exact<N>(a.gate, row, a.bias, rl.allow, a.E, a.k, s_choice[warp]);
-    const float lc = e >= 0 ? fmaxf(row[e], -CUDART_INF_F) : -CUDART_INF_F;
-    const float w = route_weight<N>(a.gate, l, rl.allow, e, lc);
+  auto write = [&](long long t, int e, float w) {
     if (lane < a.k) {
-      a.experts[token * a.k + lane] = e;
-      a.weights[token * a.k + lane] = w;
-      if (a.slots != nullptr) a.slots[token * a.k + lane] = e >= 0 ? a.expert_to_slot[e] : -1;
+      a.experts[t * a.k + lane] = e;
+      a.weights[t * a.k + lane] = w;
+      if (a.slots != nullptr) a.slots[t * a.k + lane] = e >= 0 ? a.expert_to_slot[e] : -1;
+    }
+  };
+  auto logit = [&](const float* r, int e) { return e >= 0 ? fmaxf(r[e], -CUDART_INF_F) : -CUDART_INF_F; };
+  // Tokens that need 64 bits throughout are noted and routed behind the others, 64 tokens at a time: a call in the loop over the tokens, whatever it
+  // calls, makes that spill (16384 x 256: 30 us).
+#pragma unroll 1
+  while (token < a.T) {
+    const long long first = token;
+    unsigned long long unclear = 0ull;
+#pragma unroll 1
+    for (int i = 0; i < 64 && token < a.T; ++i, token += step, row += step * a.stride) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) l[j] = fmaxf(next[j], -CUDART_INF_F);
+      if (token + step < a.T) route_load<N>(row + step * a.stride, a.E, vec, next);
+      bool clear;
+      const int e = route_choose_fast<N>(a.gate, l, b, a.bias != nullptr, rl, a.E, a.k, row, a.bias, reinterpret_cast<float*>(s_choice[warp]),
+                                         s_list[warp], &clear);
+      if (!clear) { unclear |= 1ull << i; continue; }
+      write(token, e, route_weight<N>(a.gate, l, rl.allow, e, logit(row, e)));
+    }
+#pragma unroll 1
+    for (; unclear != 0ull; unclear &= unclear - 1) {
+      const long long t = first + (__ffsll((long long)unclear) - 1) * step;
+      const float* r = a.logits + t * a.stride;
+      const int e = route_choose_exact<N>(a.gate, r, a.bias, rl.allow, a.E, a.k, s_choice[warp]);
+      route_load<N>(r, a.E, false, l);
+#pragma unroll
+      for (int j = 0; j < N; ++j) l[j] = fmaxf(l[j], -CUDART_INF_F);
+      write(t, e, route_weight<N>(a.gate, l, rl.allow, e, logit(r, e)));
     }
   }
 }
