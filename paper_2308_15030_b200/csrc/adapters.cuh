@@ -538,6 +538,86 @@ __device__ __forceinline__ void ad_ldmatrix(uint32_t (&v)[2], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(at));
 }
 
+// Tile `which` of the plan that adapters_plan_kernel would make, found by a CTA for itself, for up to kAdHere tokens: rows and adapter
+// in ctl (no rows: there is no such tile), tokens in list.  Tokens of a group are taken in their order, so that all CTAs agree.
+// scratch: count + 1 + 96 words.
+constexpr int kAdHere = kAdPlanIds * kAdThreads;
+__device__ __forceinline__ void ad_tile_here(const AdapterArgs& a, int which, int32_t* scratch, int32_t* list, int32_t* ctl) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, groups = a.count + 1;
+  int32_t *cursor = scratch, *front = scratch + groups, *per_warp = front + 64;
+  int kept[kAdPlanIds];
+#pragma unroll
+  for (int i = 0; i < kAdPlanIds; ++i) {
+    const int t = tid + i * kAdThreads;
+    kept[i] = -1;
+    if (t < a.T) {
+      const int id = a.ids[t];
+      kept[i] = id < 0 || id >= a.count ? a.count : id;
+    }
+  }
+  for (int g = tid; g < groups; g += kAdThreads) cursor[g] = 0;
+  if (tid == 0) ctl[0] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kAdPlanIds; ++i) {
+    if (i * kAdThreads >= a.T) break;
+    const uint32_t same = __match_any_sync(0xffffffffu, kept[i]);
+    if (kept[i] >= 0 && __ffs(same) - 1 == lane) atomicAdd(&cursor[kept[i]], __popc(same));
+  }
+  __syncthreads();
+  const int per = (groups + kAdThreads - 1) / kAdThreads, g0 = tid * per;
+  int tiles = 0;
+  for (int g = g0; g < min(groups, g0 + per); ++g) tiles += (cursor[g] + kAdTM - 1) / kAdTM;
+  int incl = tiles;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) per_warp[warp] = incl;
+  __syncthreads();
+  int tile = incl - tiles;
+  for (int w = 0; w < warp; ++w) tile += per_warp[w];
+  for (int g = g0; g < min(groups, g0 + per); ++g) {
+    const int n = cursor[g], cut = (n + kAdTM - 1) / kAdTM;
+    if (which >= tile && which < tile + cut) {
+      const int each = (n + cut - 1) / cut;
+      ctl[2] = (which - tile) * each;                        // first place in the group
+      ctl[1] = g;
+      ctl[0] = min(each, n - ctl[2]);
+    }
+    tile += cut;
+  }
+  __syncthreads();
+  const int rows = ctl[0], group = ctl[1], first = ctl[2];
+  if (rows == 0) return;
+#pragma unroll
+  for (int i = 0; i < kAdPlanIds; ++i) {
+    const uint32_t m = __ballot_sync(0xffffffffu, kept[i] == group);
+    if (lane == 0) front[i * kAdWarps + warp] = __popc(m);
+  }
+  __syncthreads();
+  if (warp == 0) {                                           // exclusive scan of the 64 counts, in the tokens' order
+    const int u = front[2 * lane], v = front[2 * lane + 1];
+    int sum = u + v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int w = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += w;
+    }
+    front[2 * lane] = sum - u - v;
+    front[2 * lane + 1] = sum - v;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kAdPlanIds; ++i) {
+    const uint32_t m = __ballot_sync(0xffffffffu, kept[i] == group);
+    const int at = front[i * kAdWarps + warp] + __popc(m & ((1u << lane) - 1)) - first;
+    if (kept[i] == group && at >= 0 && at < rows) list[at] = tid + i * kAdThreads;
+  }
+  __syncthreads();
+}
+
 // Tiles of up to 64 tokens from the plan; a cluster takes a tile and deals its chunks of x, then of y, out to its CTAs.  The
 // chunks of both products run through one ring of stages, so the first of y and B are on their way while x is still multiplied; one
 // barrier per chunk.  Warp w multiplies 16 tokens (w % 4) by half the ranks, then by half the chunk's columns of out.
@@ -545,7 +625,7 @@ __device__ __forceinline__ void ad_ldmatrix(uint32_t (&v)[2], uint32_t at) {
 // itself: 8192 x 4096 at rank 64 80 us, constants 67).  bf16 operands come by ldmatrix, whose four registers are an operand as it is;
 // from two rows' 16-byte pieces it has to be put together, which took more instructions than the products.
 template <typename X, typename T, int RP>
-__global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const AdapterArgs a, int stages) {
+__global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __grid_constant__ AdapterArgs a, int stages, int here) {
   constexpr int kElem = (int)sizeof(T), P = 16 / kElem, NT = P / 2;
   constexpr int kCols = kAdChunk / kElem;                    // columns of a chunk
   constexpr int kXPiece = sizeof(X) == 1 ? 8 : 16;           // bytes of a lane's piece of x: P values
@@ -586,17 +666,27 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const Adap
   const uint32_t from_y = row0 * 256 + (((col / P + q) ^ ad_swap(g)) << 4);
   pdl_wait();
   pdl_trigger();
-  const int n_tiles = *a.n_tiles;
+  int n_tiles = cluster + 1;                                 // `here`: a tile for every cluster
+  if (here) ad_tile_here(a, cluster, reinterpret_cast<int32_t*>(smem), list, list + kAdTM);
+  else n_tiles = *a.n_tiles;
   const X* x = static_cast<const X*>(a.x);
   const T* y = static_cast<const T*>(a.y);
   T* out = static_cast<T*>(a.out);
 #pragma unroll 1
   for (int tile = cluster; tile < n_tiles; tile += n_clusters) {
-    const AdapterTile td = a.tiles[tile];
-    const int rows = td.rows, adapter = td.adapter;
-    __syncthreads();                                         // the tile in front is done with the list and the stages
-    if (tid < rows) list[tid] = a.perm[td.first + tid];
-    __syncthreads();
+    int rows, adapter;
+    if (here) {
+      rows = list[kAdTM];
+      adapter = list[kAdTM + 1] < a.count ? list[kAdTM + 1] : -1;
+      if (rows == 0) break;                                  // the same for the whole cluster
+    } else {
+      const AdapterTile td = a.tiles[tile];
+      rows = td.rows;
+      adapter = td.adapter;
+      __syncthreads();                                       // the tile in front is done with the list and the stages
+      if (tid < rows) list[tid] = a.perm[td.first + tid];
+      __syncthreads();
+    }
     if (adapter < 0) {                                       // no adapter: rows of y as they are, two chunks at a time
       if (y == out && a.y_stride == a.out_stride) continue;
       constexpr int kRows = kAdTM / 16;
@@ -888,16 +978,21 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
     return ad_rtw(a.r) == 1 ? go(adapters_few_kernel<X, T, 1>) : ad_rtw(a.r) == 2 ? go(adapters_few_kernel<X, T, 2>)
                                                                                   : go(adapters_few_kernel<X, T, 4>);
   }
-  const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(a.T <= 2048 ? 256 : kAdPlanThreads), 0, st, pdl, a, kAdTM);
-  if (e != cudaSuccess) return e;
   const int tiles = ad_max_tiles(a.T, a.count), rp = ad_rank_up(a.r), stages = ad_stages(rp, elem);
   // us, 8192 tokens of 4096 at rank 64: 1 CTA 100, 2 64, 8 106 (two CTAs fit an SM, a second round costs as much as the first); 1531
   // of 768 -> 2240 in fp32 at rank 8: 2 45, 4 27, 8 20.
   a.ctas = 1;
   while (a.ctas < kAdMaxCtas && tiles * a.ctas < sm_count + sm_count / 2) a.ctas *= 2;
+  // A plan of its own per CTA where all CTAs run at once (later rounds would pay for it again): us, 1531 tokens, with the plan kernel
+  // 20.4, without 19.2.
+  const int here = a.T <= kAdHere && tiles * a.ctas <= 2 * sm_count;
+  if (!here) {
+    const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(a.T <= 2048 ? 256 : kAdPlanThreads), 0, st, pdl, a, kAdTM);
+    if (e != cudaSuccess) return e;
+  }
   const dim3 grid(a.ctas * (tiles < kAdMaxClusters ? tiles : kAdMaxClusters));
   auto go = [&](auto kernel) {
-    return launch_cluster(kernel, a.ctas, grid, dim3(kAdThreads), stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem), st, pdl, a, stages);
+    return launch_cluster(kernel, a.ctas, grid, dim3(kAdThreads), stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem), st, pdl, a, stages, here);
   };
   return rp == 16 ? go(adapters_tile_kernel<X, T, 16>) : rp == 32 ? go(adapters_tile_kernel<X, T, 32>)
        : rp == 64 ? go(adapters_tile_kernel<X, T, 64>) : go(adapters_tile_kernel<X, T, 128>);
