@@ -490,7 +490,12 @@ __host__ __device__ constexpr int ad_swap_b(int row, int pieces) {
 __host__ __device__ constexpr int ad_rank_up(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
 __host__ __device__ constexpr int ad_stage_bytes(int r) { return kAdTM * kAdChunk + kAdChunk * r; }
 __host__ __device__ constexpr int ad_tile_u_pitch(int r, int elem) { return elem == 2 ? r * 2 + 16 : ad_u_pitch(r, elem); }
-__host__ __device__ constexpr int ad_tile_rest(int r, int elem) { return kAdTM * ad_tile_u_pitch(r, elem) + kAdTM * 4 + 512; }
+// What lies behind the stages: rows of u, for small ranks the CTA's part of u (else it takes the stage that was multiplied last,
+// which is then not free before the other CTAs have read it), the list of tokens.
+__host__ __device__ constexpr bool ad_own_part(int r) { return r <= 32; }
+__host__ __device__ constexpr int ad_tile_rest(int r, int elem) {
+  return kAdTM * ad_tile_u_pitch(r, elem) + (ad_own_part(r) ? kAdTM * r * 4 : 0) + kAdTM * 4 + 512;
+}
 // Stages: as many as fit with two CTAs per SM, or, where that leaves fewer than three, with one.
 inline int ad_stages(int r, int elem) {
   const int two = (112 * 1024 - ad_tile_rest(r, elem)) / ad_stage_bytes(r);
@@ -640,7 +645,8 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 511) & ~static_cast<uintptr_t>(511));
   const int r = a.r;
   unsigned char* us = smem + stages * kStage;
-  int32_t* list = reinterpret_cast<int32_t*>(us + kAdTM * kUPitch);
+  float* own_part = reinterpret_cast<float*>(us + kAdTM * kUPitch);
+  int32_t* list = reinterpret_cast<int32_t*>(us + kAdTM * kUPitch + (ad_own_part(RP) ? kAdTM * RP * 4 : 0));
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, q = lane & 3;
   const int mw = warp & 3, nh = warp >> 2;
   const int C = a.ctas, cta = blockIdx.x % C, cluster = blockIdx.x / C, n_clusters = gridDim.x / C;
@@ -860,7 +866,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
           }
         }
       } else {
-        float* part = reinterpret_cast<float*>(smem + before);           // the stage just multiplied
+        float* part = ad_own_part(RP) ? own_part : reinterpret_cast<float*>(smem + before);   // (the stage just multiplied)
         if (mine) {
 #pragma unroll
           for (int h = 0; h < NTH; ++h) {
@@ -887,7 +893,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
           ad_store_u(reinterpret_cast<T*>(us + t * kUPitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
         }
         cluster_arrive();
-        cluster_wait();                                      // the stage is free again
+        if (!ad_own_part(RP)) cluster_wait();                // the stage is free again
       }
       __syncthreads();
     }
@@ -957,6 +963,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
       c0 += C * kCols;
     }
     ad_copy_wait(0);
+    if (ad_own_part(RP) && C > 1) cluster_wait();            // the others have read the CTA's part
   }
 }
 
@@ -981,18 +988,20 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
   const int tiles = ad_max_tiles(a.T, a.count), rp = ad_rank_up(a.r), stages = ad_stages(rp, elem);
   // us, 8192 tokens of 4096 at rank 64: 1 CTA 100, 2 64, 8 106 (two CTAs fit an SM, a second round costs as much as the first); 1531
   // of 768 -> 2240 in fp32 at rank 8: 2 45, 4 27, 8 20.
+  const int smem = stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem);
+  const int at_once = smem <= 112 * 1024 ? 2 * sm_count : sm_count;
   a.ctas = 1;
-  while (a.ctas < kAdMaxCtas && tiles * a.ctas < sm_count + sm_count / 2) a.ctas *= 2;
+  while (a.ctas < kAdMaxCtas && 4 * tiles * a.ctas < 3 * at_once) a.ctas *= 2;
   // A plan of its own per CTA where all CTAs run at once (later rounds would pay for it again): us, 1531 tokens, with the plan kernel
   // 20.4, without 19.2.
-  const int here = a.T <= kAdHere && tiles * a.ctas <= 2 * sm_count;
+  const int here = a.T <= kAdHere && tiles * a.ctas <= at_once;
   if (!here) {
     const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(a.T <= 2048 ? 256 : kAdPlanThreads), 0, st, pdl, a, kAdTM);
     if (e != cudaSuccess) return e;
   }
   const dim3 grid(a.ctas * (tiles < kAdMaxClusters ? tiles : kAdMaxClusters));
   auto go = [&](auto kernel) {
-    return launch_cluster(kernel, a.ctas, grid, dim3(kAdThreads), stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem), st, pdl, a, stages, here);
+    return launch_cluster(kernel, a.ctas, grid, dim3(kAdThreads), smem, st, pdl, a, stages, here);
   };
   return rp == 16 ? go(adapters_tile_kernel<X, T, 16>) : rp == 32 ? go(adapters_tile_kernel<X, T, 32>)
        : rp == 64 ? go(adapters_tile_kernel<X, T, 64>) : go(adapters_tile_kernel<X, T, 128>);
