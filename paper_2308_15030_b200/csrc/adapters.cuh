@@ -145,25 +145,39 @@ __device__ __forceinline__ void ad_split(uint32_t x, uint32_t& hi, uint32_t& lo)
   asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(__uint_as_float(x)));
   asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(__uint_as_float(x) - __uint_as_float(hi)));
 }
-// c += one step of 64 bytes: rows g and g + 8 of the left operand (pieces p, p8), row g of the right one (w).
-__device__ __forceinline__ void ad_step(float (&c)[4], const uint4& p, const uint4& p8, const uint4& w, bf16) {
-  mma_bf16_16x8x16(c, p.x, p8.x, p.y, p8.y, w.x, w.y);
-  mma_bf16_16x8x16(c, p.z, p8.z, p.w, p8.w, w.z, w.w);
+// The left operand of a step of 64 bytes: rows g and g + 8 (pieces p, p8); fp32 ones in their TF32 pieces, once for all column tiles.
+template <typename T> struct AdLeft;
+template <> struct AdLeft<bf16> {
+  uint4 p, p8;
+  __device__ __forceinline__ AdLeft(const uint4& a, const uint4& b) : p(a), p8(b) {}
+};
+template <> struct AdLeft<float> {
+  uint32_t h[8], l[8];                       // of the two mma: rows g, g + 8, g, g + 8
+  __device__ __forceinline__ AdLeft(const uint4& p, const uint4& p8) {
+    const uint32_t v[8] = {p.x, p8.x, p.y, p8.y, p.z, p8.z, p.w, p8.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ad_split(v[i], h[i], l[i]);
+  }
+};
+// c += one step: row g of the right operand (w).
+__device__ __forceinline__ void ad_step(float (&c)[4], const AdLeft<bf16>& a, const uint4& w) {
+  mma_bf16_16x8x16(c, a.p.x, a.p8.x, a.p.y, a.p8.y, w.x, w.y);
+  mma_bf16_16x8x16(c, a.p.z, a.p8.z, a.p.w, a.p8.w, w.z, w.w);
 }
-__device__ __forceinline__ void ad_step(float (&c)[4], const uint4& p, const uint4& p8, const uint4& w, float) {
+__device__ __forceinline__ void ad_step(float (&c)[4], const AdLeft<float>& a, const uint4& w) {
   // fp32 products as three of TF32 pieces (lo * lo is below 2^-22).  The tensor core's sums truncate, so a step's six are added
   // to c by an ordinary addition: over d_in 4096 in one accumulator they drift by 3e-5 of the result.
   float t[4] = {0.f, 0.f, 0.f, 0.f};
-  auto two = [&](uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    uint32_t h[6], l[6];
-    ad_split(a0, h[0], l[0]); ad_split(a1, h[1], l[1]); ad_split(a2, h[2], l[2]); ad_split(a3, h[3], l[3]);
-    ad_split(b0, h[4], l[4]); ad_split(b1, h[5], l[5]);
-    ad_mma_tf32(t, l[0], l[1], l[2], l[3], h[4], h[5]);
-    ad_mma_tf32(t, h[0], h[1], h[2], h[3], l[4], l[5]);
-    ad_mma_tf32(t, h[0], h[1], h[2], h[3], h[4], h[5]);
-  };
-  two(p.x, p8.x, p.y, p8.y, w.x, w.y);
-  two(p.z, p8.z, p.w, p8.w, w.z, w.w);
+  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t h0, l0, h1, l1;
+    ad_split(v[2 * i], h0, l0);
+    ad_split(v[2 * i + 1], h1, l1);
+    ad_mma_tf32(t, a.l[4 * i], a.l[4 * i + 1], a.l[4 * i + 2], a.l[4 * i + 3], h0, h1);
+    ad_mma_tf32(t, a.h[4 * i], a.h[4 * i + 1], a.h[4 * i + 2], a.h[4 * i + 3], l0, l1);
+    ad_mma_tf32(t, a.h[4 * i], a.h[4 * i + 1], a.h[4 * i + 2], a.h[4 * i + 3], h0, h1);
+  }
 #pragma unroll
   for (int e = 0; e < 4; ++e) c[e] += t[e];
 }
@@ -318,9 +332,9 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
 #pragma unroll
       for (int m = 0; m < kAdMT; ++m) {
         if (m > 0 && mt == 1) break;
-        const uint4 p = ad_operand(s.x[2 * m]), p8 = ad_operand(s.x[2 * m + 1]);
+        const AdLeft<T> left(ad_operand(s.x[2 * m]), ad_operand(s.x[2 * m + 1]));
 #pragma unroll
-        for (int h = 0; h < RTW; ++h) ad_step(acc[h][m], p, p8, s.w[h], T());
+        for (int h = 0; h < RTW; ++h) ad_step(acc[h][m], left, s.w[h]);
       }
     };
     const int step = C * slices * 4 * P;
@@ -452,8 +466,9 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
 #pragma unroll
         for (int m = 0; m < kAdMT; ++m) {
           if (m > 0 && mt == 1) break;
+          const AdLeft<T> left(p[2 * m], p[2 * m + 1]);
 #pragma unroll
-          for (int h = 0; h < NT; ++h) ad_step(acc[m][h], p[2 * m], p[2 * m + 1], w[h], T());
+          for (int h = 0; h < NT; ++h) ad_step(acc[m][h], left, w[h]);
         }
       };
       int k0 = 0;
@@ -841,8 +856,9 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
             p = ad_lds8((st + from_x) ^ (s * 32));
             p8 = ad_lds8(((st + from_x) ^ (s * 32)) + 8 * kXRow);
           }
+          const AdLeft<T> left(p, p8);
 #pragma unroll
-          for (int h = 0; h < NTH; ++h) ad_step(acc[h], p, p8, ad_lds(((st + from_a) ^ (s * 64)) + h * 2048), T());
+          for (int h = 0; h < NTH; ++h) ad_step(acc[h], left, ad_lds(((st + from_a) ^ (s * 64)) + h * 2048));
         }
       }
     }
@@ -936,12 +952,12 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
         } else {
 #pragma unroll
           for (int k = 0; k < kBPieces; k += 4) {
-            const uint4 p = ad_lds(from_u + k * 16), p8 = ad_lds(from_u + 8 * kUPitch + k * 16);
+            const AdLeft<T> left(ad_lds(from_u + k * 16), ad_lds(from_u + 8 * kUPitch + k * 16));
 #pragma unroll
             for (int v = 0; v < 2; ++v)
 #pragma unroll
               for (int h = 0; h < NT; ++h)
-                ad_step(d[v][h], p, p8, ad_lds(((st + from_b) ^ (k * 16 ^ ad_swap_b(v * 4 * P, kBPieces) << 4)) + (v * 4 * P + 2 * h) * kBRow), T());
+                ad_step(d[v][h], left, ad_lds(((st + from_b) ^ (k * 16 ^ ad_swap_b(v * 4 * P, kBPieces) << 4)) + (v * 4 * P + 2 * h) * kBRow));
           }
         }
 #pragma unroll
@@ -991,7 +1007,7 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
   const int smem = stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem);
   const int at_once = smem <= 112 * 1024 ? 2 * sm_count : sm_count;
   a.ctas = 1;
-  while (a.ctas < kAdMaxCtas && 4 * tiles * a.ctas < 3 * at_once) a.ctas *= 2;
+  while (a.ctas < kAdMaxCtas && 10 * tiles * a.ctas <= 6 * at_once) a.ctas *= 2;      // (`tiles` is an upper bound)
   // A plan of its own per CTA where all CTAs run at once (later rounds would pay for it again): us, 1531 tokens, with the plan kernel
   // 20.4, without 19.2.
   const int here = a.T <= kAdHere && tiles * a.ctas <= at_once;
