@@ -1,11 +1,13 @@
 /*
  * swapmoe.h - C ABI of the B200 (sm_100a) Virtual-Expert MoE-layer forward.
  *
- * The library runs ONE thing: the forward pass of a Mixture-of-Experts layer that
+ * The library runs the forward pass of a Mixture-of-Experts layer that
  * is restricted to a small resident set of experts ("Virtual Experts", SwapMoE,
  * arXiv 2308.15030, abstract and Section 3), plus the per-expert importance score
  * (Eq. 1) that decides which experts should be resident next, and the
- * asynchronous copy that brings a new expert into a spare slot (Section 3.2).
+ * asynchronous copy that brings a new expert into a spare slot (Section 3.2); and the
+ * operators around the experts of a served block: the norm in front of a layer, routing
+ * by groups of experts, and low-rank adapters of many requests beside it.
  *
  * Conventions that hold for every call
  *   - every function returns an int32 status: 0 = SWAPMOE_OK, negative = error
@@ -373,7 +375,8 @@ int32_t swapmoe_route_static(const void* x_dev, const void* Wr_dev, const int32_
                              int32_t* offset_dev, float* imp_dev, void* stream);
 
 /*
- * Operators around the experts of a served MoE block: the norm in front of a layer.  They need no layer object.
+ * Operators around the experts of a served MoE block.  They run beside any layer object, or without one; the block form of a
+ * layer's forward (swapmoe_forward_block) calls them all.
  */
 
 /* Root-mean-square norm of n_rows rows with the residual's addition, and an output in 8 bits with scales.  Per row
@@ -386,7 +389,7 @@ int32_t swapmoe_route_static(const void* x_dev, const void* Wr_dev, const int32_
  * The sum enters the norm unrounded; everything is computed in fp32 and holds over the whole range of fp32 (rows whose squares
  * leave it are normed by their largest magnitude).  A group of zeros has scale 0 and 8-bit zeros; other scales are at least
  * 2^-120.  A NaN in a row makes its y and its scales NaN; an infinity makes the row's finite columns 0 and itself NaN, as the
- * formula does.
+ * formula does (and so does a row of zeros with eps = 0: NaN).
  * Strides count elements; any start and stride that keep elements aligned are taken, and rows that start at multiples of 16
  * bytes (8 for out8) with d a multiple of 8 run fastest.  residual_out may be residual or x, and out may be x or residual, with
  * the same stride (and type); other overlaps are not allowed.  Nothing behind column d or row n_rows is written.  Work is

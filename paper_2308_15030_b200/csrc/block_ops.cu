@@ -123,7 +123,13 @@ int32_t swapmoe_adapters_create(swapmoe_adapters_t** out, const swapmoe_adapters
       c.rank > kAdMaxRank || c.max_tokens >= 1 << 24)
     return SWAPMOE_ERR_UNSUPPORTED;
   const int sms = current_sm_count();
-  if (sms == 0) return SWAPMOE_ERR_CUDA;
+  int dev = 0, major = 0;
+  if (sms == 0 || cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return SWAPMOE_ERR_CUDA;
+  }
+  if (major != 10) return SWAPMOE_ERR_UNSUPPORTED;       // kernels are built for sm_100a only
   swapmoe_adapters* b = new (std::nothrow) swapmoe_adapters();
   if (!b) return SWAPMOE_ERR_NO_MEMORY;
   b->cfg = c;

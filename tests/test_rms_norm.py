@@ -203,6 +203,43 @@ def test_in_place(d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 2500])
+def test_the_addition_alone_and_the_norm_over_x(T):
+    """Only residual_out; and the sum written over x while out goes elsewhere."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.empty(T, 512, device="cuda").normal_(generator=gen).bfloat16()
+    r = torch.empty(T, 512, device="cuda").normal_(generator=gen).bfloat16()
+    w = torch.ones(512, dtype=torch.bfloat16, device="cuda")
+    ro, o, o2 = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    binding.rms_norm(x, w, EPS, residual=r, residual_out=ro)
+    assert torch.equal(ro, (x.float() + r.float()).bfloat16())
+    binding.rms_norm(x, w, EPS, out=o, residual=r)
+    x2 = x.clone()
+    binding.rms_norm(x2, w, EPS, out=o2, residual=r, residual_out=x2)
+    assert torch.equal(x2, ro) and torch.equal(o2, o)
+
+
+@pytest.mark.gpu
+def test_weights_that_are_not_finite():
+    import torch
+    x = torch.ones(2, 256, device="cuda")
+    w = torch.ones(256, device="cuda")
+    w[3], w[70] = float("nan"), float("inf")
+    o, q = torch.empty_like(x), torch.empty(2, 256, dtype=torch.float8_e4m3fn, device="cuda")
+    for group in (0, 64):
+        s = torch.empty(2, 4 if group else 1, device="cuda")
+        binding.rms_norm(x, w, EPS, out=o, out8=q, scales=s, group=group)
+        assert bool(o[:, 3].isnan().all()) and bool(o[:, 70].isinf().all())
+        keep = torch.ones(256, dtype=torch.bool, device="cuda")
+        keep[3] = keep[70] = False
+        assert bool(((o[:, keep] - 1).abs() < 1e-5).all())
+        assert bool(s[:, 0].isnan().all())
+        if group:
+            assert bool(s[:, 1].isinf().all()) and bool((s[:, 2:] > 0).all()) and bool((q.float()[:, 128:] == 448).all())
+
+
+@pytest.mark.gpu
 def test_captured_and_on_another_stream():
     import torch
     gen = torch.Generator(device="cuda").manual_seed(1)
