@@ -6,7 +6,7 @@
 // per element of x and out, warp-level mma with tokens as mma rows.  One launch does both products: tokens of one adapter form
 // tiles, a cluster of 1 to 8 CTAs takes a tile and splits the columns of x, then those of out; the CTAs' parts of A x are
 // added through distributed shared memory, in a fixed order.  Two forms:
-//  - up to 64 tokens (adapters_few_kernel, tiles of 32): all operands go from global memory straight to the registers of the warp
+//  - up to 64 tokens (adapters_few_kernel, tiles of 16): all operands go from global memory straight to the registers of the warp
 //    that multiplies them, 64 contiguous bytes of eight rows per load; clusters find their tiles themselves.
 //  - more (adapters_tile_kernel, tiles of 64, a plan kernel in front that groups the tokens by adapter): x, A, y and B run through
 //    a ring in shared memory, so A and B are fetched once per 64 tokens and the loads run ahead of the products.
@@ -23,7 +23,7 @@ namespace swapmoe {
 constexpr int kAdMaxRank = 128, kAdMaxCount = 4096, kAdMaxWidth = 1 << 16;
 constexpr int kAdThreads = 256, kAdWarps = kAdThreads / 32;
 constexpr int kAdMaxCtas = 8;              // most CTAs per cluster
-constexpr int kAdTile = 32, kAdMT = kAdTile / 16;   // tokens of a tile; mma row tiles
+constexpr int kAdTile = 16;                // tokens of a tile: one mma row tile
 constexpr int kAdDirect = 64;              // up to this many tokens every cluster finds its tile itself
 
 struct AdapterTile { int32_t adapter, first, rows, pad; };   // tokens perm[first] ... perm[first + rows - 1]; adapter -1: none
@@ -237,8 +237,8 @@ __host__ __device__ constexpr int ad_u_pitch(int r, int elem) {
 __host__ __device__ constexpr int ad_part_bytes(int r) { return kAdWarps / ad_rank_warps(r, ad_rtw(r)) * kAdTile * r * 4; }
 __host__ __device__ constexpr int ad_smem_bytes(int r, int elem) { return ad_part_bytes(r) + kAdTile * ad_u_pitch(r, elem) + kAdTile * 4 + 16; }
 
-// The tile of cluster i without a plan: it has one if token i is the first, or the 32nd, ... of its adapter; then its tokens
-// are the next 32 of that adapter from i on.  By one warp; T <= 64: lane l holds tokens l and l + 32.
+// The tile of cluster i without a plan: it has one if token i is the first, or the 17th, ... of its adapter; then its tokens
+// are the next 16 of that adapter from i on.  By one warp; T <= 64: lane l holds tokens l and l + 32.
 __device__ __forceinline__ int ad_direct_tile(const AdapterArgs& a, int i, int32_t* list, int* adapter) {
   const int lane = threadIdx.x & 31;
   int id[2];
@@ -295,113 +295,114 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
   __syncthreads();
   const int rows = ctl[0], adapter = ctl[1];
   if (rows == 0) return;                         // the same for the whole cluster
-  const int mt = (rows + 15) >> 4;
   const bool work = adapter >= 0;
-  // the lane's rows: g + 8 i; a row that the tile does not have repeats its first one and is not stored
-  int token[2 * kAdMT];
+  // the lane's rows: g, g + 8; a row that the tile does not have repeats its first one and is not stored
+  int token[2];
 #pragma unroll
-  for (int i = 0; i < 2 * kAdMT; ++i) token[i] = list[g + 8 * i < rows ? g + 8 * i : 0];
+  for (int i = 0; i < 2; ++i) token[i] = list[g + 8 * i < rows ? g + 8 * i : 0];
   if (work) {
-    // ---- first product.  Rank tiles that the warp does not have repeat the last one and are not stored: no load of a full
-    // step has a condition of its own.
+    // ---- first product, kDepth steps on their way.  Rank tiles that the warp does not have repeat the last one and are not stored:
+    // no load of a full step has a condition of its own.
+    constexpr int kDepth = RTW <= 2 ? 4 : 2;
     const char* A = reinterpret_cast<const char*>(static_cast<const T*>(a.A) + (long long)adapter * r * a.d);
     const int slice = warp / rank_warps, rt0 = (warp % rank_warps) * RTW;
-    const char* xp[2 * kAdMT];
+    const char* xp[2];
 #pragma unroll
-    for (int i = 0; i < 2 * kAdMT; ++i)
-      xp[i] = reinterpret_cast<const char*>(x + (long long)token[i] * a.x_stride);
+    for (int i = 0; i < 2; ++i) xp[i] = reinterpret_cast<const char*>(x + (long long)token[i] * a.x_stride);
     uint32_t ap[RTW];
 #pragma unroll
     for (int h = 0; h < RTW; ++h) ap[h] = (uint32_t)((min(rt0 + h, rank_tiles - 1) * 8 + g) * a.d) * kElem;
-    float acc[RTW][kAdMT][4];
+    float acc[RTW][4];
 #pragma unroll
     for (int h = 0; h < RTW; ++h)
 #pragma unroll
-      for (int m = 0; m < kAdMT; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[h][m][e] = 0.f;
-    struct Step { XPiece x[2 * kAdMT]; uint4 w[RTW]; };
+      for (int e = 0; e < 4; ++e) acc[h][e] = 0.f;
+    struct Step { XPiece x[2]; uint4 w[RTW]; };
     auto load = [&](Step& s, uint32_t c) {     // c: the lane's first column
 #pragma unroll
-      for (int i = 0; i < 2 * kAdMT; ++i)
-        if (i < 2 || mt > 1) s.x[i] = *reinterpret_cast<const XPiece*>(xp[i] + c * (uint32_t)sizeof(X));
+      for (int i = 0; i < 2; ++i) s.x[i] = *reinterpret_cast<const XPiece*>(xp[i] + c * (uint32_t)sizeof(X));
 #pragma unroll
       for (int h = 0; h < RTW; ++h) s.w[h] = __ldg(reinterpret_cast<const uint4*>(A + (ap[h] + c * kElem)));
     };
     auto multiply = [&](const Step& s) {
+      const AdLeft<T> left(ad_operand(s.x[0]), ad_operand(s.x[1]));
 #pragma unroll
-      for (int m = 0; m < kAdMT; ++m) {
-        if (m > 0 && mt == 1) break;
-        const AdLeft<T> left(ad_operand(s.x[2 * m]), ad_operand(s.x[2 * m + 1]));
-#pragma unroll
-        for (int h = 0; h < RTW; ++h) ad_step(acc[h][m], left, s.w[h]);
-      }
+      for (int h = 0; h < RTW; ++h) ad_step(acc[h], left, s.w[h]);
     };
-    const int step = C * slices * 4 * P;
-    int c0 = (cta * slices + slice) * 4 * P;   // the step's first column
-    Step s0, s1;
-    if (c0 + 4 * P <= a.d) {
-      load(s0, c0 + q * P);
+    const int step = C * slices * 4 * P, first = (cta * slices + slice) * 4 * P;
+    const int n_full = first + 4 * P <= a.d ? (a.d - 4 * P - first) / step + 1 : 0;     // steps all of whose pieces exist
+    Step s[kDepth];
+#pragma unroll
+    for (int i = 0; i < kDepth; ++i)
+      if (i < n_full) load(s[i], first + i * step + q * P);
 #pragma unroll 1
-      while (true) {
-        c0 += step;
-        const bool more = c0 + 4 * P <= a.d;
-        if (more) load(s1, c0 + q * P);
-        multiply(s0);
-        if (!more) break;
-        c0 += step;
-        const bool again = c0 + 4 * P <= a.d;
-        if (again) load(s0, c0 + q * P);
-        multiply(s1);
-        if (!again) break;
+    for (int n = 0; n < n_full; n += kDepth) {
+#pragma unroll
+      for (int i = 0; i < kDepth; ++i) {
+        if (n + i >= n_full) break;
+        multiply(s[i]);
+        if (n + i + kDepth < n_full) load(s[i], first + (n + i + kDepth) * step + q * P);
       }
     }
-    if (c0 < a.d) {                            // the last step of the rows, not all of whose pieces exist
+    const int c0 = first + n_full * step;
+    if (c0 < a.d) {                            // the last step of the rows
 #pragma unroll
-      for (int i = 0; i < 2 * kAdMT; ++i) ad_zero(s0.x[i]);
+      for (int i = 0; i < 2; ++i) ad_zero(s[0].x[i]);
 #pragma unroll
-      for (int h = 0; h < RTW; ++h) ad_zero(s0.w[h]);
-      if (c0 + q * P < a.d) load(s0, c0 + q * P);
-      multiply(s0);
+      for (int h = 0; h < RTW; ++h) ad_zero(s[0].w[h]);
+      if (c0 + q * P < a.d) load(s[0], c0 + q * P);
+      multiply(s[0]);
     }
 #pragma unroll
     for (int h = 0; h < RTW; ++h) {
       if (rt0 + h >= rank_tiles) break;
-#pragma unroll
-      for (int m = 0; m < kAdMT; ++m) {
-        if (m >= mt) break;
-        float* p = part + (slice * kAdTile + m * 16 + g) * r + (rt0 + h) * 8 + 2 * q;
-        *reinterpret_cast<float2*>(p) = make_float2(acc[h][m][0], acc[h][m][1]);
-        *reinterpret_cast<float2*>(p + 8 * r) = make_float2(acc[h][m][2], acc[h][m][3]);
-      }
+      float* p = part + (slice * kAdTile + g) * r + (rt0 + h) * 8 + 2 * q;
+      *reinterpret_cast<float2*>(p) = make_float2(acc[h][0], acc[h][1]);
+      *reinterpret_cast<float2*>(p + 8 * r) = make_float2(acc[h][2], acc[h][3]);
     }
     __syncthreads();
   }
-  // ---- second product: the first unit's y is requested before the sums are exchanged
+  // ---- second product, two units at a time: y and the first step of B are requested before the sums are exchanged, and those of
+  // the next two units before this pair is stored
+  constexpr int kUnits = 2;
   const char* B = reinterpret_cast<const char*>(static_cast<const T*>(a.B) + (long long)(work ? adapter : 0) * a.n * r);
-  const int n_units = (a.n + 4 * P - 1) / (4 * P);
-  const char* yp[2 * kAdMT];
-  char* op[2 * kAdMT];
+  const int n_units = (a.n + 4 * P - 1) / (4 * P), stride = C * kAdWarps;
+  const char* yp[2];
+  char* op[2];
 #pragma unroll
-  for (int i = 0; i < 2 * kAdMT; ++i) {
+  for (int i = 0; i < 2; ++i) {
     yp[i] = reinterpret_cast<const char*>(y + (long long)token[i] * a.y_stride) + q * 16;
     op[i] = reinterpret_cast<char*>(out + (long long)token[i] * a.out_stride) + q * 16;
   }
-  uint4 yv[2 * kAdMT];
+  uint4 yv[kUnits][2], wb[kUnits][NT];
 #pragma unroll
-  for (int i = 0; i < 2 * kAdMT; ++i) ad_zero(yv[i]);
-  auto load_y = [&](int unit) {
+  for (int v = 0; v < kUnits; ++v)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ad_zero(yv[v][i]);
+  auto load_y = [&](uint4 (&d)[2], int unit) {
     if (y != nullptr && (unit * 4 + q) * P < a.n) {
 #pragma unroll
-      for (int i = 0; i < 2 * kAdMT; ++i)
-        if (i < 2 || mt > 1) yv[i] = *reinterpret_cast<const uint4*>(yp[i] + (uint32_t)unit * 64u);
+      for (int i = 0; i < 2; ++i) d[i] = *reinterpret_cast<const uint4*>(yp[i] + (uint32_t)unit * 64u);
     }
   };
   // lane's row of B in column tile h of a unit: P (g / 2) + 2 h + g % 2
   const int b_col = P * (g >> 1) + (g & 1);
   const uint32_t b_row = (uint32_t)(r * kElem);
+  auto load_b = [&](uint4 (&w)[NT], int unit, int k0) {
+    const int c = unit * 4 * P + b_col;
+#pragma unroll
+    for (int h = 0; h < NT; ++h) {
+      ad_zero(w[h]);
+      if (k0 + q * P < r && c + 2 * h < a.n)
+        w[h] = __ldg(reinterpret_cast<const uint4*>(B + ((uint32_t)(c + 2 * h) * b_row + k0 * kElem + q * 16)));
+    }
+  };
   int unit = cta * kAdWarps + warp;
-  load_y(unit);
+#pragma unroll
+  for (int v = 0; v < kUnits; ++v) {
+    load_y(yv[v], unit + v * stride);
+    if (work) load_b(wb[v], unit + v * stride, 0);
+  }
   if (work) {
     const float sc = a.scale != nullptr ? a.scale[adapter] : 1.f;
     const int total = rows * r;
@@ -437,53 +438,49 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
     }
     __syncthreads();                           // u is complete
   }
+  auto operand_u = [&](uint4& p, int row, int k0) {
+    ad_zero(p);
+    if (k0 + q * P < r) p = *reinterpret_cast<const uint4*>(us + row * u_pitch + k0 * kElem + q * 16);
+  };
 #pragma unroll 1
-  for (; unit < n_units; unit += C * kAdWarps) {
-    const int c0 = unit * 4 * P;
-    float acc[kAdMT][NT][4];
+  for (; unit < n_units; unit += kUnits * stride) {
+    uint4 res[kUnits][2];
 #pragma unroll
-    for (int m = 0; m < kAdMT; ++m)
+    for (int v = 0; v < kUnits; ++v) {
+      if (work) {
+        float acc[NT][4];
 #pragma unroll
-      for (int h = 0; h < NT; ++h)
+        for (int h = 0; h < NT; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[m][h][e] = 0.f;
-    if (work) {
-      const uint32_t first = (uint32_t)(c0 + b_col) * b_row + q * 16;
-      const bool all = c0 + 4 * P <= a.n;
-      auto products = [&](int k0, bool in) {
-        uint4 w[NT], p[2 * kAdMT];
+          for (int e = 0; e < 4; ++e) acc[h][e] = 0.f;
+        for (int k0 = 0; k0 < r; k0 += 4 * P) {
+          uint4 p, p8;
+          operand_u(p, g, k0);
+          operand_u(p8, g + 8, k0);
+          const AdLeft<T> left(p, p8);
+          if (k0 > 0) load_b(wb[v], unit + v * stride, k0);
 #pragma unroll
-        for (int h = 0; h < NT; ++h) {
-          ad_zero(w[h]);
-          if (in && (all || c0 + b_col + 2 * h < a.n))
-            w[h] = __ldg(reinterpret_cast<const uint4*>(B + (first + 2 * h * b_row + k0 * kElem)));
+          for (int h = 0; h < NT; ++h) ad_step(acc[h], left, wb[v][h]);
         }
 #pragma unroll
-        for (int i = 0; i < 2 * kAdMT; ++i) {
-          ad_zero(p[i]);
-          if (in && (i < 2 || mt > 1)) p[i] = *reinterpret_cast<const uint4*>(us + (8 * i + g) * u_pitch + k0 * kElem + q * 16);
-        }
+        for (int i = 0; i < 2; ++i) res[v][i] = ad_finish(yv[v][i], acc, 2 * i, T());
+      } else {
 #pragma unroll
-        for (int m = 0; m < kAdMT; ++m) {
-          if (m > 0 && mt == 1) break;
-          const AdLeft<T> left(p[2 * m], p[2 * m + 1]);
-#pragma unroll
-          for (int h = 0; h < NT; ++h) ad_step(acc[m][h], left, w[h]);
-        }
-      };
-      int k0 = 0;
-#pragma unroll 2
-      for (; k0 + 4 * P <= r; k0 += 4 * P) products(k0, true);
-      if (k0 < r) products(k0, k0 + q * P < r);
+        for (int i = 0; i < 2; ++i) res[v][i] = yv[v][i];
+      }
     }
-    uint4 res[2 * kAdMT];
 #pragma unroll
-    for (int i = 0; i < 2 * kAdMT; ++i) res[i] = work ? ad_finish(yv[i], acc[i >> 1], (i & 1) * 2, T()) : yv[i];
-    load_y(unit + C * kAdWarps);
-    if (c0 + q * P < a.n) {
+    for (int v = 0; v < kUnits; ++v) {
+      const int next = unit + (kUnits + v) * stride;
+      load_y(yv[v], next);
+      if (work && next < n_units) load_b(wb[v], next, 0);
+    }
 #pragma unroll
-      for (int i = 0; i < 2 * kAdMT; ++i)
-        if (g + 8 * i < rows) *reinterpret_cast<uint4*>(op[i] + (uint32_t)unit * 64u) = res[i];
+    for (int v = 0; v < kUnits; ++v) {
+      const int at = unit + v * stride;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if ((at * 4 + q) * P < a.n && g + 8 * i < rows) *reinterpret_cast<uint4*>(op[i] + (uint32_t)at * 64u) = res[v][i];
     }
   }
   if (C > 1 && work) cluster_wait();              // nobody leaves while others read its part
