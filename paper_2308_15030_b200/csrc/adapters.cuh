@@ -6,7 +6,7 @@
 // per element of x and out, warp-level mma with tokens as mma rows.  One launch does both products: tokens of one adapter form
 // tiles, a cluster of 1 to 8 CTAs takes a tile and splits the columns of x, then those of out; the CTAs' parts of A x are
 // added through distributed shared memory, in a fixed order.  Two forms:
-//  - up to 64 tokens (adapters_few_kernel, tiles of 16): all operands go from global memory straight to the registers of the warp
+//  - up to 128 tokens (adapters_few_kernel, tiles of 16): all operands go from global memory straight to the registers of the warp
 //    that multiplies them, 64 contiguous bytes of eight rows per load; clusters find their tiles themselves.
 //  - more (adapters_tile_kernel, tiles of 64, a plan kernel in front that groups the tokens by adapter): x, A, y and B run through
 //    a ring in shared memory, so A and B are fetched once per 64 tokens and the loads run ahead of the products.
@@ -24,7 +24,7 @@ constexpr int kAdMaxRank = 128, kAdMaxCount = 4096, kAdMaxWidth = 1 << 16;
 constexpr int kAdThreads = 256, kAdWarps = kAdThreads / 32;
 constexpr int kAdMaxCtas = 8;              // most CTAs per cluster
 constexpr int kAdTile = 16;                // tokens of a tile: one mma row tile
-constexpr int kAdDirect = 64;              // up to this many tokens every cluster finds its tile itself
+constexpr int kAdDirect = 128;             // up to this many tokens every cluster finds its tile itself
 
 struct AdapterTile { int32_t adapter, first, rows, pad; };   // tokens perm[first] ... perm[first + rows - 1]; adapter -1: none
 
@@ -238,29 +238,40 @@ __host__ __device__ constexpr int ad_part_bytes(int r) { return kAdWarps / ad_ra
 __host__ __device__ constexpr int ad_smem_bytes(int r, int elem) { return ad_part_bytes(r) + kAdTile * ad_u_pitch(r, elem) + kAdTile * 4 + 16; }
 
 // The tile of cluster i without a plan: it has one if token i is the first, or the 17th, ... of its adapter; then its tokens
-// are the next 16 of that adapter from i on.  By one warp; T <= 64: lane l holds tokens l and l + 32.
+// are the next 16 of that adapter from i on.  By one warp: lane l holds tokens l, l + 32, ...
 __device__ __forceinline__ int ad_direct_tile(const AdapterArgs& a, int i, int32_t* list, int* adapter) {
+  constexpr int kWords = kAdDirect / 32;
   const int lane = threadIdx.x & 31;
-  int id[2];
+  int id[kWords], mine = 0;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int t = lane + 32 * h;
-    id[h] = t < a.T ? a.ids[t] : -2;
-    if (t < a.T && (id[h] < 0 || id[h] >= a.count)) id[h] = -1;
+  for (int w = 0; w < kWords; ++w) {
+    const int t = lane + 32 * w;
+    id[w] = t < a.T ? a.ids[t] : -2;
+    if (t < a.T && (id[w] < 0 || id[w] >= a.count)) id[w] = -1;
   }
-  const int mine = __shfl_sync(0xffffffffu, i < 32 ? id[0] : id[1], i & 31);
-  const unsigned long long all = (unsigned long long)__ballot_sync(0xffffffffu, id[1] == mine) << 32 |
-                                 __ballot_sync(0xffffffffu, id[0] == mine);
-  const unsigned long long below = (1ull << i) - 1;
+#pragma unroll
+  for (int w = 0; w < kWords; ++w) {
+    const int v = __shfl_sync(0xffffffffu, id[w], i & 31);
+    if (w == i >> 5) mine = v;
+  }
   *adapter = mine;
-  if (__popcll(all & below) % kAdTile != 0) return 0;
-  const unsigned long long rest = all & ~below;
+  int before = 0, at = 0;                        // tokens of the adapter in front of i; from i on, in front of word w
+  uint32_t rest[kWords];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int t = lane + 32 * h, at = __popcll(rest & ((1ull << t) - 1));
-    if ((rest >> t) & 1 && at < kAdTile) list[at] = t;
+  for (int w = 0; w < kWords; ++w) {
+    const uint32_t same = __ballot_sync(0xffffffffu, id[w] == mine);
+    const uint32_t front = w < i >> 5 ? 0xffffffffu : w == i >> 5 ? (1u << (i & 31)) - 1 : 0u;
+    before += __popc(same & front);
+    rest[w] = same & ~front;
   }
-  return min(kAdTile, __popcll(rest));
+  if (before % kAdTile != 0) return 0;
+#pragma unroll
+  for (int w = 0; w < kWords; ++w) {
+    const int place = at + __popc(rest[w] & ((1u << lane) - 1));
+    if ((rest[w] >> lane) & 1 && place < kAdTile) list[place] = lane + 32 * w;
+    at += __popc(rest[w]);
+  }
+  return min(kAdTile, at);
 }
 
 // First product: the contraction is dealt out to the warps in steps of 64 bytes (two or four warps share x from rank 40 on), and their
@@ -990,7 +1001,7 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
   if (a.T <= kAdDirect) {
     a.ctas = 1;
     // CTAs per cluster: until every SM has one or a CTA's warps one step each.  us, 61 tokens of 4096 with 64 adapters of rank 16:
-    // 1 CTA 17.8, 2 13.5, 4 9.2, 8 11.7; one token of 1024: 6.0, 4.8, 4.2, 4.5.
+    // 1 CTA 13.4, 2 11.0, 4 8.1, 8 11.0; one token of 1024: 4.9, 4.2, 4.3, 4.7.
     while (a.ctas < kAdMaxCtas && a.T * a.ctas < sm_count && a.ctas * kAdWarps * (64 / elem) < (a.d > a.n ? a.d : a.n)) a.ctas *= 2;
     auto go = [&](auto kernel) {
       return launch_cluster(kernel, a.ctas, dim3(a.ctas * a.T), dim3(kAdThreads), ad_smem_bytes(a.r, elem), st, pdl, a);
@@ -999,8 +1010,8 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
                                                                                   : go(adapters_few_kernel<X, T, 4>);
   }
   const int tiles = ad_max_tiles(a.T, a.count), rp = ad_rank_up(a.r), stages = ad_stages(rp, elem);
-  // us, 8192 tokens of 4096 at rank 64: 1 CTA 100, 2 64, 8 106 (two CTAs fit an SM, a second round costs as much as the first); 1531
-  // of 768 -> 2240 in fp32 at rank 8: 2 45, 4 27, 8 20.
+  // us, 8192 tokens of 4096 at rank 64: 1 CTA 69, 2 60, 4 70, 8 106 (two CTAs fit an SM, a second round costs as much as the first);
+  // 1531 of 768 -> 2240 in fp32 at rank 8: 1 54, 2 31, 4 23, 8 19.
   const int smem = stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem);
   const int at_once = smem <= 112 * 1024 ? 2 * sm_count : sm_count;
   a.ctas = 1;
