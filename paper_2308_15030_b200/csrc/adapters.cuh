@@ -133,30 +133,28 @@ __device__ __forceinline__ void mma_bf16_16x8x16(float (&c)[4], uint32_t a0, uin
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void ad_mma_tf32(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                            uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+// Two fp32 values as three pairs of bf16 pieces, each rounded to nearest from what the ones in front left: 24 bits in all.
+__device__ __forceinline__ void ad_split(uint32_t x, uint32_t y, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  float a = __uint_as_float(x), b = __uint_as_float(y);
+  hi = pack_bf16x2(a, b);
+  a -= __uint_as_float(hi << 16);
+  b -= __uint_as_float(hi & 0xffff0000u);
+  mid = pack_bf16x2(a, b);
+  lo = pack_bf16x2(a - __uint_as_float(mid << 16), b - __uint_as_float(mid & 0xffff0000u));
 }
-// x = hi + lo, both TF32, each rounded to nearest: what is lost is below 2^-22 of x.
-__device__ __forceinline__ void ad_split(uint32_t x, uint32_t& hi, uint32_t& lo) {
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(__uint_as_float(x)));
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(__uint_as_float(x) - __uint_as_float(hi)));
-}
-// The left operand of a step of 64 bytes: rows g and g + 8 (pieces p, p8); fp32 ones in their TF32 pieces, once for all column tiles.
+// The left operand of a step of 64 bytes: rows g and g + 8 (pieces p, p8); fp32 ones in their bf16 pieces, once for all column tiles.
 template <typename T> struct AdLeft;
 template <> struct AdLeft<bf16> {
   uint4 p, p8;
   __device__ __forceinline__ AdLeft(const uint4& a, const uint4& b) : p(a), p8(b) {}
 };
 template <> struct AdLeft<float> {
-  uint32_t h[8], l[8];                       // of the two mma: rows g, g + 8, g, g + 8
+  uint32_t v[3][4];                          // pieces of a mma's operand
   __device__ __forceinline__ AdLeft(const uint4& p, const uint4& p8) {
-    const uint32_t v[8] = {p.x, p8.x, p.y, p8.y, p.z, p8.z, p.w, p8.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ad_split(v[i], h[i], l[i]);
+    ad_split(p.x, p.y, v[0][0], v[1][0], v[2][0]);
+    ad_split(p8.x, p8.y, v[0][1], v[1][1], v[2][1]);
+    ad_split(p.z, p.w, v[0][2], v[1][2], v[2][2]);
+    ad_split(p8.z, p8.w, v[0][3], v[1][3], v[2][3]);
   }
 };
 // c += one step: row g of the right operand (w).
@@ -165,19 +163,21 @@ __device__ __forceinline__ void ad_step(float (&c)[4], const AdLeft<bf16>& a, co
   mma_bf16_16x8x16(c, a.p.z, a.p8.z, a.p.w, a.p8.w, w.z, w.w);
 }
 __device__ __forceinline__ void ad_step(float (&c)[4], const AdLeft<float>& a, const uint4& w) {
-  // fp32 products as three of TF32 pieces (lo * lo is below 2^-22).  The tensor core's sums truncate, so a step's six are added
-  // to c by an ordinary addition: over d_in 4096 in one accumulator they drift by 3e-5 of the result.
+  // fp32 products as six of bf16 pieces, the small ones first (the others are below 2^-25 together).  Three products of TF32 pieces
+  // are as many mma, two steps of 8 in depth each, and slower: 1531 tokens of 1024 18.8 us with them and 17.8 so, 400 of 2048 at
+  // rank 128 75.3 and 72.1.  The tensor core's sums truncate, so a step's six are added to c by an ordinary addition: over d_in
+  // 4096 in one accumulator they drift by 3e-5 of the result.
+  uint32_t b[3][2];
+  ad_split(w.x, w.y, b[0][0], b[1][0], b[2][0]);
+  ad_split(w.z, w.w, b[0][1], b[1][1], b[2][1]);
   float t[4] = {0.f, 0.f, 0.f, 0.f};
-  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    uint32_t h0, l0, h1, l1;
-    ad_split(v[2 * i], h0, l0);
-    ad_split(v[2 * i + 1], h1, l1);
-    ad_mma_tf32(t, a.l[4 * i], a.l[4 * i + 1], a.l[4 * i + 2], a.l[4 * i + 3], h0, h1);
-    ad_mma_tf32(t, a.h[4 * i], a.h[4 * i + 1], a.h[4 * i + 2], a.h[4 * i + 3], l0, l1);
-    ad_mma_tf32(t, a.h[4 * i], a.h[4 * i + 1], a.h[4 * i + 2], a.h[4 * i + 3], h0, h1);
-  }
+  auto product = [&](int i, int j) { mma_bf16_16x8x16(t, a.v[i][0], a.v[i][1], a.v[i][2], a.v[i][3], b[j][0], b[j][1]); };
+  product(2, 0);
+  product(0, 2);
+  product(1, 1);
+  product(1, 0);
+  product(0, 1);
+  product(0, 0);
 #pragma unroll
   for (int e = 0; e < 4; ++e) c[e] += t[e];
 }
