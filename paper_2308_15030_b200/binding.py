@@ -372,16 +372,24 @@ class Layer:
     def forward_block(self, x, residual, out, adapters: Optional[AdapterBank] = None, ids=None, n_tokens: Optional[int] = None,
                       stream=None) -> None:
         """The pre-norm block around the layer: residual += x (None: no residual); out = layer(norm(residual)), plus each
-        token's adapter from ``adapters`` by ``ids`` [T] int32 (negative: none)."""
+        token's adapter from ``adapters`` by ``ids`` [T] int32 (negative: none).  Rows [T, d_model] of the layer's dtype,
+        contiguous, on one device."""
         import torch
+        where, dt = "swapmoe_forward_block", torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
         T = int(x.shape[0]) if n_tokens is None else int(n_tokens)
+        need = min(T, self.cfg.max_tokens) * self.cfg.d_model      # (more tokens than that: the library's refusal)
+        for name, t in (("x", x), ("residual", residual), ("out", out)):
+            if t is not None and (t.dtype != dt or not t.is_cuda or t.device != x.device or not t.is_contiguous() or t.numel() < need):
+                raise _invalid(where, "%s: %d contiguous rows of %d values of %s on %s expected, got %s of %s on %s" % (
+                    name, T, self.cfg.d_model, dt, x.device, tuple(t.shape), t.dtype, t.device))
         if ids is not None:
-            _vector(ids, T, torch.int32, x.device, "swapmoe_forward_block", "ids")
+            _vector(ids, T, torch.int32, x.device, where, "ids")
+        if adapters is not None and adapters._device != x.device:
+            raise _invalid(where, "adapters: a bank on %s, rows on %s" % (adapters._device, x.device))
         self.last_T = T
         _check(lib().swapmoe_forward_block(
             self._h, x.data_ptr(), None if residual is None else residual.data_ptr(), out.data_ptr(), T,
-            None if adapters is None else adapters._h, None if ids is None else ids.data_ptr(), _stream_ptr(stream)),
-            "swapmoe_forward_block")
+            None if adapters is None else adapters._h, None if ids is None else ids.data_ptr(), _stream_ptr(stream)), where)
 
     def forward(self, x, out, n_tokens: Optional[int] = None, stream=None) -> None:
         T = int(x.shape[0]) if n_tokens is None else int(n_tokens)

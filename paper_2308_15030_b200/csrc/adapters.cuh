@@ -164,7 +164,7 @@ __device__ __forceinline__ void ad_step(float (&c)[4], const AdLeft<bf16>& a, co
 }
 __device__ __forceinline__ void ad_step(float (&c)[4], const AdLeft<float>& a, const uint4& w) {
   // fp32 products as six of bf16 pieces, the small ones first (the others are below 2^-25 together).  Three products of TF32 pieces
-  // are as many mma, two steps of 8 in depth each, and slower: 1531 tokens of 1024 18.8 us with them and 17.8 so, 400 of 2048 at
+  // are as many mma, two steps of 8 in depth each, and slower: 1531 tokens of 768 -> 2240 18.8 us with them and 17.8 so, 400 of 2048 at
   // rank 128 75.3 and 72.1.  The tensor core's sums truncate, so a step's six are added to c by an ordinary addition: over d_in
   // 4096 in one accumulator they drift by 3e-5 of the result.
   uint32_t b[3][2];

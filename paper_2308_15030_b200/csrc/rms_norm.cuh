@@ -312,7 +312,7 @@ inline cudaError_t rms_norm_launch_typed(RmsNormArgs a, bool vec, int sm_count, 
   const int per_warp = few ? 1 : 2;
   a.warps_per_row = (chunks + per_warp - 1) / per_warp;
   a.rows_per_cta = few || a.warps_per_row >= 8 ? 1 : 8 / a.warps_per_row;
-  const dim3 grid((unsigned)((a.T + a.rows_per_cta - 1) / a.rows_per_cta)), block(32 * a.warps_per_row, a.rows_per_cta);
+  const dim3 grid((unsigned)(((long long)a.T + a.rows_per_cta - 1) / a.rows_per_cta)), block(32 * a.warps_per_row, a.rows_per_cta);
   a.per_column = 1.f / (float)a.d;
   auto go = [&](auto kernel) { return launch_kernel(kernel, grid, block, 0, st, pdl, a); };
   const bool row8 = a.out8 != nullptr && a.group == 0;

@@ -245,3 +245,21 @@ def test_decode_stack_over_layers_with_gates_of_their_own():
     stack.step_graph(x)
     torch.cuda.synchronize()
     assert torch.equal(out, torch.stack(want))
+
+
+@pytest.mark.gpu
+def test_block_refuses_rows_that_are_not_its_own():
+    import torch
+    case = _case(8, 64, 2, 12)
+    L = case.layer
+    x, r, w, bank, ids = _block_inputs(case, I.BF16)
+    L.set_norm(w, 1e-5)
+    out, keep = torch.full_like(x, 3.0), r.clone()
+    wide = torch.zeros(x.shape[0], 2 * x.shape[1], dtype=x.dtype, device="cuda")[:, :x.shape[1]]
+    for bad in (x.float(), x.cpu(), wide, x[:7]):
+        for args in ((bad, r, out), (x, bad, out), (x, r, bad)):
+            with pytest.raises(binding.SwapMoEError) as e:
+                L.forward_block(*args, n_tokens=8)
+            assert e.value.status == -1
+    torch.cuda.synchronize()
+    assert bool((out == 3).all()) and torch.equal(r, keep)
