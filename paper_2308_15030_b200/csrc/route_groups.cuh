@@ -320,7 +320,8 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
       key[i] = (((u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) & ~kPlace) | (kPlace - i)) & rl.mask[i < N ? i : 0];
     }
   }
-  auto value_of = [&](uint32_t q) { return gate_key_value(q & ~kPlace); };
+  // (without its place bits the key of -infinity is that of a NaN)
+  auto value_of = [&](uint32_t q) { return fmaxf(gate_key_value(q & ~kPlace), -CUDART_INF_F); };
   constexpr float kCut = 2.f * M * 0x1p-23f;                // what the places cost a pair of keys, and the roundings, relative
   float group_size = 0.f;
   uint32_t group_at = 0u, choice_at = 0u;                   // lane i: key of the i-th group, of the i-th choice (0: none)
@@ -357,10 +358,12 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
           v1 = fmaxf(v1, v);
         }
     }
-    const float value = g.group_top > 1 && have > 1 ? v1 + v2 : v1;
-    // (the error of a sum goes by its terms)
-    group_size = __uint_as_float(__reduce_max_sync(0xffffffffu, have == 0 ? 0u
-        : __float_as_uint(fmaxf(fabsf(v1), g.group_top > 1 && have > 1 ? fabsf(v2) : 0.f))));
+    const bool two = g.group_top > 1 && have > 1;
+    const float value = fmaxf(two ? v1 + v2 : v1, -CUDART_INF_F);             // inf - inf as -infinity
+    // The error of a sum goes by its terms.  Infinite ones have none: they are clear of finite values, and equal ones of each other
+    // never (inf - inf exceeds no slack).
+    auto magnitude = [](float v) { return fabsf(v) < CUDART_INF_F ? __float_as_uint(fabsf(v)) : 0u; };
+    group_size = __uint_as_float(__reduce_max_sync(0xffffffffu, have == 0 ? 0u : max(magnitude(v1), two ? magnitude(v2) : 0u)));
     uint32_t gk = 0u;
     if (have > 0) {
       const uint32_t u = __float_as_uint(value + 0.f);
@@ -403,7 +406,7 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
       const uint32_t group_below = __shfl_down_sync(0xffffffffu, group_at, 1);
       const float slack = 4.f * error + 2.f * kCut * group_size;
       const bool near = lane < 31 && group_below != 0u && !(gate_key_value(group_at) - gate_key_value(group_below) > slack);
-      if (__any_sync(0xffffffffu, near) && lanes > 0 && group_size < CUDART_INF_F && !(by_score && g.score == SWAPMOE_SCORE_SOFTMAX)) {
+      if (__any_sync(0xffffffffu, near) && lanes > 0 && !(by_score && g.score == SWAPMOE_SCORE_SOFTMAX)) {
         const bool third = M > 2 && key[M > 2 ? 2 : 0] != 0u && !(v2 - value_of(key[M > 2 ? 2 : 0]) > slack);
         if (!__any_sync(0xffffffffu, third)) {
           double w1 = -CUDART_INF, w2 = -CUDART_INF;
@@ -471,13 +474,13 @@ __device__ __forceinline__ int route_choose_fast(const RouteGate& g, const float
   const uint32_t behind = __reduce_max_sync(0xffffffffu, head);       // the best one that was not chosen
   if (lane == k) choice_at = behind;
   if (mine >= 0) mine = mine * N + (int)(kPlace - (choice_at & kPlace));
-  // the gaps between neighbours of the two lists, and the largest magnitude in them (infinities fail the comparison)
+  // the gaps between neighbours of the two lists, and the largest magnitude among the choices (an infinity there: 64 bits decide)
   const uint32_t below = __shfl_down_sync(0xffffffffu, choice_at, 1), group_below = __shfl_down_sync(0xffffffffu, group_at, 1);
   const float v = value_of(choice_at), w = gate_key_value(group_at);
   const uint32_t size = __reduce_max_sync(0xffffffffu, choice_at != 0u ? magnitude_bits(v) : 0u);
   const float slack = 2.f * error + kCut * __uint_as_float(size);
   const float group_slack = 4.f * error + 2.f * kCut * group_size;
-  const bool finite = size < 0x7f800000u && group_size < CUDART_INF_F;
+  const bool finite = size < 0x7f800000u;
   const bool near_group = lane < 31 && group_below != 0u && !(w - gate_key_value(group_below) > group_slack);
   const bool near = lane < k && below != 0u && !(v - value_of(below) > slack);
   *clear = !__any_sync(0xffffffffu, near || near_group) && finite;

@@ -263,3 +263,31 @@ def test_block_refuses_rows_that_are_not_its_own():
             assert e.value.status == -1
     torch.cuda.synchronize()
     assert bool((out == 3).all()) and torch.equal(r, keep)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E,G,tg,k", [(160, 8, 3, 4), (256, 8, 4, 4), (64, 4, 2, 3)])
+def test_gate_over_groups_at_minus_infinity(E, G, tg, k):
+    """Both selections of a layer with a gate of its own, logits and biases with groups switched off."""
+    import torch
+    from test_route_groups import REL, TINY, dead_biases, dead_logits, reference
+    rng = np.random.default_rng(E)
+    lg = dead_logits(rng, E, G)
+    K = 24
+    case = _case(len(lg), E, k, K)
+    L = case.layer
+    table = np.full(E, -1, np.int32)
+    table[case.s2e] = np.arange(K)
+    plain = rng.normal(0, 1.5, lg.shape).astype(np.float32)
+    runs = [(Gate("softmax", G, tg, 1, True), None, lg), (Gate("sigmoid", G, tg, 2, False, 2.5), None, lg)]
+    runs += [(Gate("sigmoid", G, tg, 2, True), bias, plain) for bias in dead_biases(rng, E, G)]
+    for g, bias, logits in runs:
+        L.set_gate(g, None if bias is None else torch.from_numpy(bias).cuda())
+        L.forward_from_logits(case.d_x, torch.from_numpy(logits).cuda(), case.d_out)
+        args = (k, "sigmoid" if g.score else "softmax", g.n_groups, g.topk_groups, g.group_top, g.renorm, g.scale, bias)
+        ue, uw, _ = reference(logits, *args)
+        me, mw, ms = reference(logits, *args, table)
+        assert np.array_equal(L.tap("uidx"), ue)
+        assert np.array_equal(L.tap("midx"), me) and np.array_equal(L.tap("slot"), ms)
+        for name, w in (("ugate", uw), ("mgate", mw)):
+            assert np.all(np.abs(L.tap(name) - w) <= REL * np.abs(w) + TINY), name

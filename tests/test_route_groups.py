@@ -257,3 +257,58 @@ def test_captured_and_many_tokens():
     for t in (0, 77, 4999):                                  # a token's choice does not hang on its batch
         binding.route(gate, lg[t:t + 1], *small)
         assert torch.equal(small[0][0], want[0][t]) and torch.equal(small[1][0], want[1][t])
+
+
+# ------------------------------------------------------------------ groups that -infinity switches off, several experts per lane
+DEAD_SHAPES = [(160, 8, 3, 6), (256, 8, 4, 8), (96, 4, 2, 4), (64, 4, 2, 8), (512, 16, 5, 8), (200, 5, 2, 4), (240, 15, 4, 5)]
+
+
+def dead_logits(rng, E, G, repeats=8):
+    """Rows with whole groups, all of a group but one, or experts at random at -infinity or NaN."""
+    size, rows = E // G, []
+    for _ in range(repeats):
+        l = rng.normal(0, 1.5, (9, E)).astype(np.float32)
+        l[0, :size] = -np.inf
+        l[1, (G - 1) * size:] = -np.inf
+        l[2, size:3 * size] = np.nan
+        l[3, size:2 * size], l[3, 3 * size:4 * size] = -np.inf, np.nan
+        l[4, :(G - 1) * size] = -np.inf
+        l[5, 2 * size + 1:3 * size] = -np.inf
+        l[6, 2 * size:3 * size - 1] = np.nan
+        l[7, rng.random(E) < 0.7] = -np.inf
+        l[8, :size] = -3.4028235e38
+        rows.append(l)
+    return np.concatenate(rows)
+
+
+def dead_biases(rng, E, G):
+    """Biases of -infinity over runs of experts: those of one lane, all but one of a group, a group, some at random."""
+    size, lane = E // G, -(-E // 32)
+    for off in (slice(lane, 2 * lane), slice(size + 1, 2 * size), slice(size, 2 * size), rng.random(E) < 0.4):
+        bias = rng.normal(0, 0.1, E).astype(np.float32)
+        bias[off] = -np.inf
+        yield bias
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("top", [1, 2])
+@pytest.mark.parametrize("E,G,tg,k", DEAD_SHAPES)
+def test_groups_at_minus_infinity(E, G, tg, k, top, score):
+    rng = np.random.default_rng(E + top)
+    logits = dead_logits(rng, E, G)
+    for renorm in (False, True):
+        _check(logits, k, (score, G, tg, top, renorm, 1.0))
+        _check(logits, k, (score, G, tg, top, renorm, 1.0), table=_table(rng, E, E // 2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("top", [1, 2])
+@pytest.mark.parametrize("E,G,tg,k", DEAD_SHAPES)
+def test_biases_of_minus_infinity(E, G, tg, k, top, score):
+    rng = np.random.default_rng(E + 7 * top)
+    logits = rng.normal(0, 1.5, (200, E)).astype(np.float32)
+    for bias in dead_biases(rng, E, G):
+        _check(logits, k, (score, G, tg, top, True, 1.0), bias)
+        _check(logits, k, (score, G, tg, top, False, 2.5), bias, _table(rng, E, 2 * E // 3))
