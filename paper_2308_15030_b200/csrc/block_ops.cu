@@ -68,19 +68,20 @@ int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* p, void* stream) {
     return SWAPMOE_ERR_INVALID_ARG;
   const size_t elem = p->dtype == SWAPMOE_BF16 ? 2 : 4, relem = p->residual_dtype == SWAPMOE_BF16 ? 2 : 4;
   const long long d = p->d, n_scales = p->group ? (d + p->group - 1) / p->group : 1;
-  struct { const void* p; long long stride, width; size_t elem, vec; } rows[] = {
-      {p->x, p->x_stride, d, elem, 16},
-      {p->residual, p->residual_stride, d, relem, 16},
-      {p->residual_out, p->residual_out_stride, d, relem, 16},
-      {p->out, p->out_stride, d, elem, 16},
-      {p->out8, p->out8_stride, d, 1, 8},
-      {p->scales, p->scales_stride, n_scales, 4, 4},
-      {p->weight, d, d, elem, 16}};
+  const int32_t n = p->n_rows;
+  struct { const void* p; int32_t n; long long stride, width; size_t elem, vec; } rows[] = {
+      {p->x, n, p->x_stride, d, elem, 16},
+      {p->residual, n, p->residual_stride, d, relem, 16},
+      {p->residual_out, n, p->residual_out_stride, d, relem, 16},
+      {p->out, n, p->out_stride, d, elem, 16},
+      {p->out8, n, p->out8_stride, d, 1, 8},
+      {p->scales, n, p->scales_stride, n_scales, 4, 4},
+      {p->weight, 1, d, d, elem, 16}};
   bool vec = d % 8 == 0;
   for (const auto& r : rows) {
     if (!r.p) continue;
     if (r.stride < r.width || reinterpret_cast<uintptr_t>(r.p) % r.elem) return SWAPMOE_ERR_INVALID_ARG;
-    vec = vec && rows_aligned(r.p, p->n_rows > 1 && r.p != p->weight ? r.stride : 0, r.elem, r.vec);
+    vec = vec && rows_aligned(r.p, r.n > 1 ? r.stride : 0, r.elem, r.vec);
   }
   RmsNormArgs a;
   a.x = p->x; a.residual = p->residual; a.weight = p->weight;

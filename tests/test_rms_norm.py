@@ -263,3 +263,19 @@ def test_captured_and_on_another_stream():
     binding.rms_norm(want, w, EPS, out=again)
     torch.cuda.synchronize()
     assert torch.equal(o, again)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [5, 900])
+@pytest.mark.parametrize("stride", [1000, 1003, 1005])
+def test_the_weight_is_the_first_row(stride, T, dtype):
+    """x and the weight begin at the same address; rows lie wherever the stride puts them."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(stride)
+    mem = torch.empty(T, stride, device="cuda").normal_(generator=gen).to(torch.float32 if dtype == "fp32" else torch.bfloat16)
+    x, w = mem[:, :1000], mem[0, :1000]
+    o = torch.empty(T, 1000, dtype=mem.dtype, device="cuda")
+    binding.rms_norm(x, w, EPS, out=o)
+    _, y, _ = _reference(x.double().cpu(), None, w.double().cpu(), EPS, None)
+    assert bool(((o.double().cpu() - y).abs() <= y.abs() * (40 * 2.0 ** -24 + HALF[dtype] * (dtype == "bf16")) * 1.01).all())
