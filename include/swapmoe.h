@@ -387,7 +387,8 @@ int32_t swapmoe_route_static(const void* x_dev, const void* Wr_dev, const int32_
  *   scales = max |y| / 448, out8 = y / scales, rounded to e4m3 (finite values saturate): one scale per row (group = 0) or
  *            per `group` consecutive columns (32, 64, 128 or 256; the last group may be shorter)
  * The sum enters the norm unrounded; everything is computed in fp32 and holds over the whole range of fp32 (rows whose squares
- * leave it are normed by their largest magnitude).  A group of zeros has scale 0 and 8-bit zeros; other scales are at least
+ * leave it are normed by the larger of their largest magnitude and sqrt(eps)); what stands in other rows changes no bit of a
+ * row.  A group of zeros has scale 0 and 8-bit zeros; other scales are at least
  * 2^-120.  A NaN in a row makes its y and its scales NaN; an infinity makes the row's finite columns 0 and itself NaN, as the
  * formula does (and so does a row of zeros with eps = 0: NaN).
  * Strides count elements; any start and stride that keep elements aligned are taken, and rows that start at multiples of 16

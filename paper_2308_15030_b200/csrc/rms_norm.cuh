@@ -197,7 +197,9 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
   }
   float s = rsqrtf(total * a.per_column + a.eps);
   if (slow) {
-    // the same with the row divided by its largest magnitude m: h / sqrt(mean(h^2) + eps) = (h / m) / sqrt(mean((h / m)^2) + eps / m^2)
+    // For the rows that are rare (a CTA's other rows keep what they have: a row hangs on itself) the same with the row divided by m, the
+    // larger one of its largest magnitude and sqrt(eps), so that neither square leaves the range:
+    // h / sqrt(mean(h^2) + eps) = (h / m) / sqrt(mean((h / m)^2) + eps / m^2)
     auto over_team = [&](float v, bool add) {
       __syncthreads();
       if (lane == 0) s_sum[warp] = v;
@@ -206,11 +208,13 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
       for (int w = 1; w < a.warps_per_row; ++w) t = add ? t + s_sum[team0 + w] : max_magnitude(t, s_sum[team0 + w], 0.f);
       return t;
     };
+    const bool mine = over_team(rare ? 1.f : 0.f, false) > 0.f;
     most = 0.f;
 #pragma unroll
     for (int j = 0; j < kChunks; ++j) most = max_magnitude(most, largest8(h[j]), 0.f);
-    const float m = over_team(warp_largest(most), false);
-    const bool scaled = m > 0.f && m < CUDART_INF_F;
+    const float top = over_team(warp_largest(most), false);
+    const bool scaled = mine && top > 0.f && top < CUDART_INF_F;
+    const float m = fmaxf(top, sqrtf(a.eps));
     sum = 0.f;
     most = 0.f;
 #pragma unroll
@@ -221,18 +225,22 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
         sum = fmaf(h[j][i], h[j][i], sum);
       }
     total = over_team(warp_sum(sum), true);
-    s = rsqrtf(total * a.per_column + (scaled ? a.eps / m / m : a.eps));
+    if (mine) s = rsqrtf(total * a.per_column + (scaled ? a.eps / m / m : a.eps));
     if constexpr (kRow8) {
       // the row's factor goes into the products at once: an infinity among them would be none behind it
+      if (mine)
 #pragma unroll
-      for (int j = 0; j < kChunks; ++j) {
-        norm_load8<kVec>(static_cast<const T*>(a.weight), (wr + j * a.warps_per_row) * kNormChunk, lane, d, p[j]);
+        for (int j = 0; j < kChunks; ++j) {
+          norm_load8<kVec>(static_cast<const T*>(a.weight), (wr + j * a.warps_per_row) * kNormChunk, lane, d, p[j]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[j][i] *= h[j][i] * s;
-        most = max_magnitude(most, largest8(p[j]), 0.f);
+          for (int i = 0; i < 8; ++i) p[j][i] *= h[j][i] * s;
+          most = max_magnitude(most, largest8(p[j]), 0.f);
+        }
+      const float t = over_team(warp_largest(most), false);
+      if (mine) {
+        s = 1.f;
+        largest = t;
       }
-      s = 1.f;
-      largest = over_team(warp_largest(most), false);
     }
   }
   float (&y)[kChunks][8] = kRow8 ? p : h;

@@ -279,3 +279,56 @@ def test_the_weight_is_the_first_row(stride, T, dtype):
     binding.rms_norm(x, w, EPS, out=o)
     _, y, _ = _reference(x.double().cpu(), None, w.double().cpu(), EPS, None)
     assert bool(((o.double().cpu() - y).abs() <= y.abs() * (40 * 2.0 ** -24 + HALF[dtype] * (dtype == "bf16")) * 1.01).all())
+
+
+# ------------------------------------------------------------------ rows beside rows, and the ends of fp32's range
+@pytest.mark.gpu
+@pytest.mark.parametrize("group", [None, 0, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,d", [(1500, 512), (700, 1000), (40, 2048)])
+def test_a_row_hangs_on_itself(T, d, dtype, group):
+    """NaN, infinities and huge values in some rows change no bit of the others, tiny ones among them."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    dt = torch.float32 if dtype == "fp32" else torch.bfloat16
+    x = torch.empty(T, d, device="cuda").normal_(generator=gen)
+    x[1::7] *= 1e-24
+    x[2::7] *= 1e-35
+    x = x.to(dt)
+    w = torch.empty(d, device="cuda").normal_(1.0, 0.3, generator=gen).to(dt)
+
+    def run(x):
+        o = torch.empty_like(x)
+        q = s = None
+        if group is not None:
+            q = torch.empty(T, d, dtype=torch.float8_e4m3fn, device="cuda")
+            s = torch.empty(T, -(-d // group) if group else 1, device="cuda")
+        binding.rms_norm(x, w, EPS, out=o, out8=q, scales=s, group=group or 0)
+        return [o] + ([] if q is None else [q.view(torch.uint8), s])
+    alone = run(x)
+    odd = x.clone()
+    at = torch.arange(0, T, 5, device="cuda")
+    odd[at[0::3], 3] = float("nan")
+    odd[at[1::3], 5] = float("inf")
+    odd[at[2::3]] = 3e30
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[at] = False
+    for a, b in zip(alone, run(odd)):
+        assert torch.equal(a[keep], b[keep])
+    _, y, _ = _reference(x.double().cpu(), None, w.double().cpu(), EPS, None)
+    # (fp32 arithmetic as in _check, rounded once; the type's smallest steps where y is below its normal numbers)
+    tol = y.abs() * (40 * 2.0 ** -24 + HALF[dtype] * (dtype == "bf16")) * 1.01 + (2.0 ** -134 if dtype == "bf16" else 2.0 ** -149)
+    assert bool(((alone[0].double().cpu() - y).abs() <= tol).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [500, 512])
+@pytest.mark.parametrize("eps", [2.0 ** -87, 2.0 ** -100, 2.0 ** -126])
+@pytest.mark.parametrize("size", [1e-17, 1e-28, 1e-33, 1e-36])
+def test_tiny_rows_beside_a_tiny_eps(size, eps, d, dtype):
+    """eps far above and far below the squares of rows that are themselves out of the squares' range."""
+    import torch
+    x = torch.linspace(-1.0, 1.0, d, device="cuda").repeat(4, 1) * size
+    for group in (None, 0, 128):
+        _check(4, d, dtype, residual=None, x_values=x, eps=eps, group=group)
