@@ -25,6 +25,8 @@ constexpr float kE4m3Max = 448.f;
 // fewer of the 8-bit type's values.)
 constexpr float kNormMinScale = 0x1p-120f;
 
+constexpr float kNormLift = 0x1p56f;
+
 struct RmsNormArgs {
   const void *x, *residual, *weight;
   void *residual_out, *out;
@@ -167,7 +169,9 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
     if constexpr (kRow8) {
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        mul2(p[j][i], p[j][i + 1], h[j][i], h[j][i + 1]);             // h w
+        float u = h[j][i], v = h[j][i + 1];
+        mul2(u, v, kNormLift, kNormLift);
+        mul2(p[j][i], p[j][i + 1], u, v);                             // h w 2^56
         most = max_magnitude(most, p[j][i], p[j][i + 1]);
       }
     }
@@ -195,7 +199,7 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
     total += s_sum[team0 + w];
     if constexpr (kRow8) largest = fmaxf(largest, s_max[team0 + w]);
   }
-  float s = rsqrtf(total * a.per_column + a.eps);
+  float s = rsqrtf(total * a.per_column + a.eps) * (kRow8 ? 1.f / kNormLift : 1.f);
   if (slow) {
     // For the rows that are rare (a CTA's other rows keep what they have: a row hangs on itself) the same with the row divided by m, the
     // larger one of its largest magnitude and sqrt(eps), so that neither square leaves the range:

@@ -332,3 +332,22 @@ def test_tiny_rows_beside_a_tiny_eps(size, eps, d, dtype):
     x = torch.linspace(-1.0, 1.0, d, device="cuda").repeat(4, 1) * size
     for group in (None, 0, 128):
         _check(4, d, dtype, residual=None, x_values=x, eps=eps, group=group)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size,weight", [(1e-14, 1e-26), (1e-12, 1e-27), (1e15, 1e20), (1e-10, 1e-28)])
+def test_products_with_the_weight_outside_fp32(size, weight):
+    """Rows with one 8-bit scale: h * weight leaves fp32's normal range, y does not."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty(50, 512, device="cuda").normal_(0.0, size, generator=gen)
+    w = torch.empty(512, device="cuda").normal_(1.0, 0.1, generator=gen) * weight
+    o, s = torch.empty_like(x), torch.empty(50, 1, device="cuda")
+    q = torch.empty(50, 512, dtype=torch.float8_e4m3fn, device="cuda")
+    binding.rms_norm(x, w, 0.0, out=o, out8=q, scales=s)
+    _, y, sc = _reference(x.double().cpu(), None, w.double().cpu(), 0.0, 0)
+    f32 = 40 * 2.0 ** -24
+    assert bool(((o.double().cpu() - y).abs() <= y.abs() * f32).all())
+    assert bool(((s.double().cpu() - sc).abs() <= sc * 2 * f32).all())
+    ideal = y / sc
+    assert bool(((q.float().double().cpu() - ideal).abs() <= torch.clamp(ideal.abs() * 2.0 ** -4, min=2.0 ** -10) * (1 + 1e-3)).all())
