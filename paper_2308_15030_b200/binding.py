@@ -313,6 +313,8 @@ class Layer:
                           spare_slots)
         self._h = ctypes.c_void_p()
         _check(lib().swapmoe_create(ctypes.byref(self._h), ctypes.byref(self.cfg)), "swapmoe_create")
+        import torch
+        self._device = torch.device("cuda", torch.cuda.current_device())
         self._keep = {}
         self.last_T = 0
 
@@ -349,23 +351,28 @@ class Layer:
     def set_gemm_path(self, path: int) -> None:
         _check(lib().swapmoe_set_gemm_path(self._h, int(path)), "swapmoe_set_gemm_path")
 
-    def set_gate(self, gate: Optional[Gate], bias=None) -> None:
-        """Later forwards route by ``gate`` (None: by the layer's configuration); ``bias`` [E] float32, not copied."""
+    def _current(self, where: str) -> None:
         import torch
-        pb = None if bias is None else _vector(bias, self.cfg.E, torch.float32, bias.device, "swapmoe_set_gate", "bias")
-        if bias is not None and not bias.is_cuda:
-            raise _invalid("swapmoe_set_gate", "bias: a CUDA tensor expected")
-        _check(lib().swapmoe_set_gate(self._h, None if gate is None else ctypes.byref(gate), pb), "swapmoe_set_gate")
+        now = torch.cuda.current_device()
+        if now != self._device.index:
+            raise _invalid(where, "the layer is on %s, the current device is cuda:%d" % (self._device, now))
+
+    def set_gate(self, gate: Optional[Gate], bias=None) -> None:
+        """Later forwards route by ``gate`` (None: by the layer's configuration); ``bias`` [E] float32 on the layer's device, not
+        copied."""
+        import torch
+        where = "swapmoe_set_gate"
+        pb = None if bias is None else _vector(bias, self.cfg.E, torch.float32, self._device, where, "bias")
+        _check(lib().swapmoe_set_gate(self._h, None if gate is None else ctypes.byref(gate), pb), where)
         self._keep["gate_bias"] = bias
 
     def set_norm(self, weight, eps: float) -> None:
-        """The norm in front of the layer in forward_block: ``weight`` [d_model] in the layer's dtype, not copied."""
+        """The norm in front of the layer in forward_block: ``weight`` [d_model] in the layer's dtype on its device, not copied."""
         import torch
-        dt = torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
-        if not weight.is_cuda:
-            raise _invalid("swapmoe_set_norm", "weight: a CUDA tensor expected")
-        pw = _vector(weight, self.cfg.d_model, dt, weight.device, "swapmoe_set_norm", "weight")
-        _check(lib().swapmoe_set_norm(self._h, pw, eps), "swapmoe_set_norm")
+        where, dt = "swapmoe_set_norm", torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
+        pw = _vector(weight, self.cfg.d_model, dt, self._device, where, "weight")
+        self._current(where)                                       # (the rows behind the norm are allocated there)
+        _check(lib().swapmoe_set_norm(self._h, pw, eps), where)
         self._keep["norm"] = weight
 
     # -- hot path
@@ -373,19 +380,20 @@ class Layer:
                       stream=None) -> None:
         """The pre-norm block around the layer: residual += x (None: no residual); out = layer(norm(residual)), plus each
         token's adapter from ``adapters`` by ``ids`` [T] int32 (negative: none).  Rows [T, d_model] of the layer's dtype,
-        contiguous, on one device."""
+        contiguous, on the layer's device, which has to be the current one."""
         import torch
         where, dt = "swapmoe_forward_block", torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
         T = int(x.shape[0]) if n_tokens is None else int(n_tokens)
         need = min(T, self.cfg.max_tokens) * self.cfg.d_model      # (more tokens than that: the library's refusal)
         for name, t in (("x", x), ("residual", residual), ("out", out)):
-            if t is not None and (t.dtype != dt or not t.is_cuda or t.device != x.device or not t.is_contiguous() or t.numel() < need):
+            if t is not None and (t.dtype != dt or t.device != self._device or not t.is_contiguous() or t.numel() < need):
                 raise _invalid(where, "%s: %d contiguous rows of %d values of %s on %s expected, got %s of %s on %s" % (
-                    name, T, self.cfg.d_model, dt, x.device, tuple(t.shape), t.dtype, t.device))
+                    name, T, self.cfg.d_model, dt, self._device, tuple(t.shape), t.dtype, t.device))
         if ids is not None:
-            _vector(ids, T, torch.int32, x.device, where, "ids")
-        if adapters is not None and adapters._device != x.device:
-            raise _invalid(where, "adapters: a bank on %s, rows on %s" % (adapters._device, x.device))
+            _vector(ids, T, torch.int32, self._device, where, "ids")
+        if adapters is not None and adapters._device != self._device:
+            raise _invalid(where, "adapters: a bank on %s, the layer on %s" % (adapters._device, self._device))
+        self._current(where)
         self.last_T = T
         _check(lib().swapmoe_forward_block(
             self._h, x.data_ptr(), None if residual is None else residual.data_ptr(), out.data_ptr(), T,

@@ -17,6 +17,75 @@ def test_null_handles():
     assert L.swapmoe_adapters_check(None, 64, 64, 1, 1) == -1
 
 
+class _Tensor:
+    """What the checks ask of a tensor; its address is never used, a refused call does not reach the library."""
+    def __init__(self, shape, dtype, device):
+        import torch
+        self.shape, self.dtype, self.device, self.is_cuda = shape, dtype, torch.device(device), device.startswith("cuda")
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 256
+
+
+def _stand_in(cls, device, **cfg):
+    import ctypes
+    import types
+    import torch
+    obj = object.__new__(cls)
+    obj._h, obj._device, obj._keep, obj.last_T = ctypes.c_void_p(), torch.device(device), {}, 0
+    obj.cfg = types.SimpleNamespace(**cfg)
+    return obj
+
+
+@pytest.mark.parametrize("current", [0, 1])
+def test_tensors_of_other_devices_are_refused(monkeypatch, current):
+    """A layer on cuda:1 and operands on cuda:0 or the CPU, or a call while another device is current: refused before the library."""
+    import torch
+    calls = []
+
+    class Library:
+        swapmoe_status_string = staticmethod(lambda status: b"refused")
+
+        def __getattr__(self, name):
+            return lambda *a: calls.append(name) or 0
+    monkeypatch.setattr(binding, "lib", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+    L = _stand_in(binding.Layer, "cuda:1", E=8, d_model=64, dtype=binding.BF16, max_tokens=4)
+    bank = _stand_in(binding.AdapterBank, "cuda:1")
+    far_bank = _stand_in(binding.AdapterBank, "cuda:0")
+    there = dict(x=_Tensor((4, 64), torch.bfloat16, "cuda:1"), residual=_Tensor((4, 64), torch.bfloat16, "cuda:1"),
+                 out=_Tensor((4, 64), torch.bfloat16, "cuda:1"), adapters=bank, ids=_Tensor((4,), torch.int32, "cuda:1"), stream=0)
+
+    def refused(f, *a, **kw):
+        with pytest.raises(binding.SwapMoEError) as e:
+            f(*a, **kw)
+        assert e.value.status == -1 and not calls
+    for device in ("cuda:0", "cpu"):
+        refused(L.set_gate, Gate(), _Tensor((8,), torch.float32, device))
+        refused(L.set_norm, _Tensor((64,), torch.bfloat16, device), 1e-6)
+        rows = {n: _Tensor((4, 64), torch.bfloat16, device) for n in ("x", "residual", "out")}
+        refused(L.forward_block, **dict(there, **rows))
+        for n, t in rows.items():
+            refused(L.forward_block, **dict(there, **{n: t}))
+        refused(L.forward_block, **dict(there, ids=_Tensor((4,), torch.int32, device)))
+    refused(L.forward_block, **dict(there, adapters=far_bank))
+    if current == 0:
+        refused(L.forward_block, **there)
+        refused(L.set_norm, _Tensor((64,), torch.bfloat16, "cuda:1"), 1e-6)
+    else:
+        L.forward_block(**there)
+        L.set_norm(_Tensor((64,), torch.bfloat16, "cuda:1"), 1e-6)
+        L.set_gate(Gate(), _Tensor((8,), torch.float32, "cuda:1"))
+        assert calls == ["swapmoe_forward_block", "swapmoe_set_norm", "swapmoe_set_gate"]
+        calls.clear()
+
+
 # ------------------------------------------------------------------ on the GPU
 def _expected(case, midx, mgate, slot):
     """out in 64 bits from a routing: gate-weighted sum of the experts' FFN, hidden values rounded as the layer stores them."""
