@@ -212,6 +212,16 @@ def _fail(status: int, where: str, text) -> None:
     raise SwapMoEError(status, where) if text is None else SwapMoEError(status, "%s: %s" % (where, text))
 
 
+def _device_functions():
+    """torch's current device, set device and current stream of a device as an address; the bare ones (a tenth of a us
+    each, a us through torch.cuda) where torch has them."""
+    import torch
+    names = ("_cuda_getDevice", "_cuda_setDevice", "_cuda_getCurrentRawStream")
+    if all(hasattr(torch._C, n) for n in names):
+        return tuple(getattr(torch._C, n) for n in names)
+    return torch.cuda.current_device, torch.cuda.set_device, lambda device: torch.cuda.current_stream(device).cuda_stream
+
+
 _marshal = None
 
 
@@ -230,8 +240,7 @@ def marshal():
         m.init(_fail, tuple(ctypes.cast(f, ctypes.c_void_p).value for f in
                             (L.swapmoe_rms_norm, L.swapmoe_route, L.swapmoe_adapters_forward)),
                (torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.int32),
-               (torch._C._cuda_getDevice, torch._C._cuda_setDevice, torch._C._cuda_getCurrentRawStream)
-               if hasattr(torch._C, "_cuda_getCurrentRawStream") else (None, None, None))
+               _device_functions())
         _marshal = m
     return _marshal
 

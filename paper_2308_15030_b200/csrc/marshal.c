@@ -190,13 +190,13 @@ static PyObject* end(const Call* c, long back, int32_t status) {
 
 /* rms_norm(x, weight, eps, out, residual, residual_out, out8, scales, group, stream) */
 static PyObject* py_rms_norm(PyObject* self, PyObject* const* v, Py_ssize_t n) {
+  if (n != 10) return PyErr_Format(PyExc_TypeError, "ten arguments expected");
   Call c = {"swapmoe_rms_norm", -1};
   swapmoe_rms_norm_t a = {0};
   PyObject *x = v[0], *weight = v[1], *out = v[3], *residual = v[4], *residual_out = v[5], *out8 = v[6], *scales = v[7];
   PyObject *dtype, *rdtype = NULL;
   int dims;
   int64_t size[2], stride[2], group;
-  if (n != 10) return PyErr_Format(PyExc_TypeError, "ten arguments expected");
   if (layer_type(&c, x, "x", &a.dtype, &dtype) || sizes(&c, x, "x", &dims, size, stride)) return NULL;
   if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x: [T, d] expected"); return NULL; }
   const int64_t T = size[0], d = size[1];
@@ -240,6 +240,7 @@ static PyObject* py_rms_norm(PyObject* self, PyObject* const* v, Py_ssize_t n) {
 
 /* route(gate, logits, experts, weights, bias, expert_to_slot, slots, stream) */
 static PyObject* py_route(PyObject* self, PyObject* const* v, Py_ssize_t n) {
+  if (n != 8) return PyErr_Format(PyExc_TypeError, "eight arguments expected");
   Call c = {"swapmoe_route", -1};
   PyObject *logits = v[1], *experts = v[2], *weights = v[3], *bias = v[4], *table = v[5], *slots = v[6];
   int dims;
@@ -249,7 +250,6 @@ static PyObject* py_route(PyObject* self, PyObject* const* v, Py_ssize_t n) {
   int32_t status;
   swapmoe_gate_t gate;
   Py_buffer buf;
-  if (n != 8) return PyErr_Format(PyExc_TypeError, "eight arguments expected");
   if (PyObject_GetBuffer(v[0], &buf, PyBUF_SIMPLE)) return NULL;
   const int fits = buf.len == (Py_ssize_t)sizeof(gate);
   if (fits) gate = *(const swapmoe_gate_t*)buf.buf;
@@ -275,6 +275,7 @@ static PyObject* py_route(PyObject* self, PyObject* const* v, Py_ssize_t n) {
 
 /* adapters_forward(handle, device, dtype, d_in, d_out, x, ids, y, out, x_scales, stream) */
 static PyObject* py_adapters_forward(PyObject* self, PyObject* const* v, Py_ssize_t n) {
+  if (n != 11) return PyErr_Format(PyExc_TypeError, "eleven arguments expected");
   Call c = {"swapmoe_adapters_forward", -1};
   PyObject *dtype = v[2], *x = v[5], *ids = v[6], *y = v[7], *out = v[8], *x_scales = v[9];
   int dims;
@@ -282,7 +283,6 @@ static PyObject* py_adapters_forward(PyObject* self, PyObject* const* v, Py_ssiz
   void *xp, *ip, *yp = NULL, *op, *sp = NULL, *st;
   long back;
   int32_t status;
-  if (n != 11) return PyErr_Format(PyExc_TypeError, "eleven arguments expected");
   if (integer(v[1], &device) || integer(v[3], &d_in) || integer(v[4], &d_out)) return NULL;
   void* bank = v[0] == Py_None ? NULL : PyLong_AsVoidPtr(v[0]);
   if (PyErr_Occurred() || sizes(&c, x, "x", &dims, size, stride)) return NULL;
