@@ -996,8 +996,9 @@ inline int ad_max_tiles(int T, int count) { return T / kAdTM + (T < count + 1 ? 
 constexpr int kAdMaxClusters = 2048;
 
 template <typename X, typename T>
-inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st, bool pdl) {
+inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st, bool pdl, int* kernels) {
   const int elem = (int)sizeof(T);
+  *kernels = 1;
   if (a.T <= kAdDirect) {
     a.ctas = 1;
     // CTAs per cluster: until every SM has one or a CTA's warps one step each.  us, 61 tokens of 4096 with 64 adapters of rank 16:
@@ -1022,6 +1023,7 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
   if (!here) {
     const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(a.T <= 2048 ? 256 : kAdPlanThreads), 0, st, pdl, a, kAdTM);
     if (e != cudaSuccess) return e;
+    *kernels = 2;
   }
   const dim3 grid(a.ctas * (tiles < kAdMaxClusters ? tiles : kAdMaxClusters));
   auto go = [&](auto kernel) {

@@ -21,6 +21,7 @@
 #include "gemm_tc_f32_pair.cuh"
 #include "gemm_tc_ffn.cuh"
 #include "gemm_tc_small.cuh"
+#include "block_ops.cuh"
 #include "layer_gate.cuh"
 #include "permute.cuh"
 #include "router_gate.cuh"
@@ -873,14 +874,11 @@ int32_t swapmoe_forward_block(swapmoe_layer_t* L, const void* x, void* residual,
   n.x = x; n.residual = residual; n.residual_out = residual; n.weight = L->norm_weight; n.out = L->x_norm;
   n.x_stride = n.residual_stride = n.residual_out_stride = n.out_stride = c.d_model;
   n.n_rows = T; n.d = c.d_model; n.dtype = n.residual_dtype = c.dtype; n.eps = L->norm_eps;
-  int32_t rc = swapmoe_rms_norm(&n, stream);
+  int32_t rc = rms_norm_run(&n, stream, &L->launches);
   if (rc != SWAPMOE_OK) return rc;
-  L->launches++;
   rc = forward_checked(L, L->x_norm, nullptr, out, T, stream);
   if (rc != SWAPMOE_OK || !adapters) return rc;
-  rc = swapmoe_adapters_forward(adapters, L->x_norm, c.d_model, nullptr, ids, out, c.d_model, out, c.d_model, T, stream);
-  if (rc == SWAPMOE_OK) L->launches++;
-  return rc;
+  return adapters_run(adapters, L->x_norm, c.d_model, nullptr, ids, out, c.d_model, out, c.d_model, T, stream, &L->launches);
 }
 
 int32_t swapmoe_forward(swapmoe_layer_t* L, const void* x, void* out, int32_t T, void* stream) {

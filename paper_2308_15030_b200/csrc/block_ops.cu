@@ -8,6 +8,7 @@
 #include <new>
 
 #include "adapters.cuh"
+#include "block_ops.cuh"
 #include "common.cuh"
 #include "rms_norm.cuh"
 #include "route_groups.cuh"
@@ -38,9 +39,10 @@ int current_sm_count() {
   return n;
 }
 
-int32_t launched(cudaError_t e) {
+int32_t launched(cudaError_t e, int kernels = 0, int64_t* launches = nullptr) {
   if (e == cudaSuccess) e = cudaGetLastError();
   else cudaGetLastError();
+  if (e == cudaSuccess && launches) *launches += kernels;
   return e == cudaSuccess ? SWAPMOE_OK : SWAPMOE_ERR_CUDA;
 }
 
@@ -53,9 +55,9 @@ bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t
 
 }  // namespace
 
-extern "C" {
+namespace swapmoe {
 
-int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* p, void* stream) {
+int32_t rms_norm_run(const swapmoe_rms_norm_t* p, void* stream, int64_t* launches) {
   if (!p || p->n_rows < 0 || p->d < 1) return SWAPMOE_ERR_INVALID_ARG;
   if (p->dtype != SWAPMOE_F32 && p->dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
   if (p->residual_dtype != p->dtype && p->residual_dtype != SWAPMOE_F32) return SWAPMOE_ERR_INVALID_ARG;
@@ -93,10 +95,43 @@ int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* p, void* stream) {
   a.warps_per_row = a.rows_per_cta = 1;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int sms = current_sm_count();
-  if (p->dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<float, float>(a, vec, sms, st, true));
-  if (p->residual_dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<bf16, float>(a, vec, sms, st, true));
-  return launched(rms_norm_launch_typed<bf16, bf16>(a, vec, sms, st, true));
+  if (p->dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<float, float>(a, vec, sms, st, true), 1, launches);
+  if (p->residual_dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<bf16, float>(a, vec, sms, st, true), 1, launches);
+  return launched(rms_norm_launch_typed<bf16, bf16>(a, vec, sms, st, true), 1, launches);
 }
+
+int32_t adapters_run(swapmoe_adapters_t* b, const void* x, int64_t x_stride, const float* x_scales, const int32_t* ids, const void* y,
+                     int64_t y_stride, void* out, int64_t out_stride, int32_t T, void* stream, int64_t* launches) {
+  if (!b || T < 0) return SWAPMOE_ERR_INVALID_ARG;
+  if (T == 0) return SWAPMOE_OK;
+  const swapmoe_adapters_config_t& c = b->cfg;
+  if (!x || !ids || !out || x_stride < c.d_in || out_stride < c.d_out || (y && y_stride < c.d_out)) return SWAPMOE_ERR_INVALID_ARG;
+  if (x_scales && c.dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
+  if (!b->A) return SWAPMOE_ERR_NOT_READY;
+  if (T > c.max_tokens) return SWAPMOE_ERR_TOO_MANY_TOKENS;
+  const size_t elem = c.dtype == SWAPMOE_BF16 ? 2 : 4;
+  const long long many = T > 1;
+  if (!rows_aligned(x, many * x_stride, x_scales ? 1 : elem, x_scales ? 8 : 16) || !rows_aligned(out, many * out_stride, elem, 16) ||
+      (y && !rows_aligned(y, many * y_stride, elem, 16)) || misaligned(ids, 4) || misaligned(x_scales, 4))
+    return SWAPMOE_ERR_INVALID_ARG;
+  AdapterArgs a;
+  a.x = x; a.x_scales = x_scales; a.ids = ids; a.y = y; a.out = out; a.A = b->A; a.B = b->B; a.scale = b->scale;
+  a.perm = b->perm; a.tiles = b->tiles; a.n_tiles = b->n_tiles; a.ctas = 1;
+  a.x_stride = x_stride; a.y_stride = y_stride; a.out_stride = out_stride;
+  a.T = T; a.d = c.d_in; a.n = c.d_out; a.r = c.rank; a.count = c.n_adapters;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int kernels = 0;
+  const cudaError_t e = c.dtype == SWAPMOE_F32 ? adapters_launch<float, float>(a, b->sm_count, st, true, &kernels)
+                        : x_scales             ? adapters_launch<__nv_fp8_e4m3, bf16>(a, b->sm_count, st, true, &kernels)
+                                               : adapters_launch<bf16, bf16>(a, b->sm_count, st, true, &kernels);
+  return launched(e, kernels, launches);
+}
+
+}  // namespace swapmoe
+
+extern "C" {
+
+int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* p, void* stream) { return rms_norm_run(p, stream, nullptr); }
 
 int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits, int64_t stride, const float* bias,
                       const int32_t* expert_to_slot, int32_t T, int32_t E, int32_t top_k, int32_t* experts, float* weights,
@@ -176,27 +211,7 @@ int32_t swapmoe_adapters_check(const swapmoe_adapters_t* b, int32_t d_in, int32_
 
 int32_t swapmoe_adapters_forward(swapmoe_adapters_t* b, const void* x, int64_t x_stride, const float* x_scales, const int32_t* ids,
                                  const void* y, int64_t y_stride, void* out, int64_t out_stride, int32_t T, void* stream) {
-  if (!b || T < 0) return SWAPMOE_ERR_INVALID_ARG;
-  if (T == 0) return SWAPMOE_OK;
-  const swapmoe_adapters_config_t& c = b->cfg;
-  if (!x || !ids || !out || x_stride < c.d_in || out_stride < c.d_out || (y && y_stride < c.d_out)) return SWAPMOE_ERR_INVALID_ARG;
-  if (x_scales && c.dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
-  if (!b->A) return SWAPMOE_ERR_NOT_READY;
-  if (T > c.max_tokens) return SWAPMOE_ERR_TOO_MANY_TOKENS;
-  const size_t elem = c.dtype == SWAPMOE_BF16 ? 2 : 4;
-  const long long many = T > 1;
-  if (!rows_aligned(x, many * x_stride, x_scales ? 1 : elem, x_scales ? 8 : 16) || !rows_aligned(out, many * out_stride, elem, 16) ||
-      (y && !rows_aligned(y, many * y_stride, elem, 16)) || misaligned(ids, 4) || misaligned(x_scales, 4))
-    return SWAPMOE_ERR_INVALID_ARG;
-  AdapterArgs a;
-  a.x = x; a.x_scales = x_scales; a.ids = ids; a.y = y; a.out = out; a.A = b->A; a.B = b->B; a.scale = b->scale;
-  a.perm = b->perm; a.tiles = b->tiles; a.n_tiles = b->n_tiles; a.ctas = 1;
-  a.x_stride = x_stride; a.y_stride = y_stride; a.out_stride = out_stride;
-  a.T = T; a.d = c.d_in; a.n = c.d_out; a.r = c.rank; a.count = c.n_adapters;
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (c.dtype == SWAPMOE_F32) return launched(adapters_launch<float, float>(a, b->sm_count, st, true));
-  if (x_scales) return launched(adapters_launch<__nv_fp8_e4m3, bf16>(a, b->sm_count, st, true));
-  return launched(adapters_launch<bf16, bf16>(a, b->sm_count, st, true));
+  return adapters_run(b, x, x_stride, x_scales, ids, y, y_stride, out, out_stride, T, stream, nullptr);
 }
 
 }  // extern "C"

@@ -360,3 +360,26 @@ def test_gate_over_groups_at_minus_infinity(E, G, tg, k):
         assert np.array_equal(L.tap("midx"), me) and np.array_equal(L.tap("slot"), ms)
         for name, w in (("ugate", uw), ("mgate", mw)):
             assert np.all(np.abs(L.tap(name) - w) <= REL * np.abs(w) + TINY), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,own", [(3, 1), (300, 1), (2100, 2)])
+def test_the_blocks_launches_are_counted(T, own):
+    """The norm is one kernel, the adapters one, or two where a kernel groups many tokens by adapter first."""
+    import torch
+    case = _case(T, 64, 2, 12)
+    L = case.layer
+    x, r, w, bank, ids = _block_inputs(case, I.BF16)
+    out = torch.empty_like(x)
+    L.set_norm(w, 1e-5)
+
+    def launches(f, *a):
+        before = L.launch_count
+        f(*a)
+        return L.launch_count - before
+    layer = launches(L.forward, x, out)
+    assert launches(L.forward_block, x, r, out) == layer + 1
+    assert launches(L.forward_block, x, r, out, bank, ids) == layer + 1 + own
+    with pytest.raises(binding.SwapMoEError):
+        L.forward_block(x, r, out, bank, ids.long())
+    assert launches(L.forward_block, x, r, out, None, None, 0) == 0
