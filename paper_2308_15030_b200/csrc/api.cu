@@ -554,9 +554,8 @@ int32_t swapmoe_create(swapmoe_layer_t** out, const swapmoe_config_t* cfg) {
   L->device = dev;
   L->sm_count = prop.multiProcessorCount;
   {
-    const char* env = std::getenv("SWAPMOE_PDL");      // SWAPMOE_PDL=0 launches every kernel fully serialised
-    L->use_pdl = !(env && env[0] == '0');
-    env = std::getenv("SWAPMOE_PERMUTE_GROUPS");        // CTAs per token tile of the permute kernel (0: automatic)
+    L->use_pdl = dependent_launch();
+    const char* env = std::getenv("SWAPMOE_PERMUTE_GROUPS");        // CTAs per token tile of the permute kernel (0: automatic)
     L->permute_groups = env ? std::atoi(env) : 0;
     env = std::getenv("SWAPMOE_ROUTER_TOK");            // force the router's token tile (32, 64 or 128)
     L->router_tok = env ? std::atoi(env) : 0;
@@ -874,11 +873,11 @@ int32_t swapmoe_forward_block(swapmoe_layer_t* L, const void* x, void* residual,
   n.x = x; n.residual = residual; n.residual_out = residual; n.weight = L->norm_weight; n.out = L->x_norm;
   n.x_stride = n.residual_stride = n.residual_out_stride = n.out_stride = c.d_model;
   n.n_rows = T; n.d = c.d_model; n.dtype = n.residual_dtype = c.dtype; n.eps = L->norm_eps;
-  int32_t rc = rms_norm_run(&n, stream, &L->launches);
+  int32_t rc = rms_norm_run(&n, stream, L->use_pdl, &L->launches);
   if (rc != SWAPMOE_OK) return rc;
   rc = forward_checked(L, L->x_norm, nullptr, out, T, stream);
   if (rc != SWAPMOE_OK || !adapters) return rc;
-  return adapters_run(adapters, L->x_norm, c.d_model, nullptr, ids, out, c.d_model, out, c.d_model, T, stream, &L->launches);
+  return adapters_run(adapters, L->x_norm, c.d_model, nullptr, ids, out, c.d_model, out, c.d_model, T, stream, L->use_pdl, &L->launches);
 }
 
 int32_t swapmoe_forward(swapmoe_layer_t* L, const void* x, void* out, int32_t T, void* stream) {

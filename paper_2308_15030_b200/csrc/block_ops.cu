@@ -46,6 +46,12 @@ int32_t launched(cudaError_t e, int kernels = 0, int64_t* launches = nullptr) {
   return e == cudaSuccess ? SWAPMOE_OK : SWAPMOE_ERR_CUDA;
 }
 
+// The choice of dependent launches where no layer has made one: that of the process, read once.
+bool standalone_pdl() {
+  static const bool pdl = dependent_launch();
+  return pdl;
+}
+
 // Whether rows of `elem`-byte values at p, `stride` values apart, all start on multiples of `bytes`.
 bool rows_aligned(const void* p, long long stride, size_t elem, size_t bytes) {
   return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (size_t)stride * elem % bytes == 0;
@@ -57,7 +63,7 @@ bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t
 
 namespace swapmoe {
 
-int32_t rms_norm_run(const swapmoe_rms_norm_t* p, void* stream, int64_t* launches) {
+int32_t rms_norm_run(const swapmoe_rms_norm_t* p, void* stream, bool pdl, int64_t* launches) {
   if (!p || p->n_rows < 0 || p->d < 1) return SWAPMOE_ERR_INVALID_ARG;
   if (p->dtype != SWAPMOE_F32 && p->dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
   if (p->residual_dtype != p->dtype && p->residual_dtype != SWAPMOE_F32) return SWAPMOE_ERR_INVALID_ARG;
@@ -95,13 +101,13 @@ int32_t rms_norm_run(const swapmoe_rms_norm_t* p, void* stream, int64_t* launche
   a.warps_per_row = a.rows_per_cta = 1;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int sms = current_sm_count();
-  if (p->dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<float, float>(a, vec, sms, st, true), 1, launches);
-  if (p->residual_dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<bf16, float>(a, vec, sms, st, true), 1, launches);
-  return launched(rms_norm_launch_typed<bf16, bf16>(a, vec, sms, st, true), 1, launches);
+  if (p->dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<float, float>(a, vec, sms, st, pdl), 1, launches);
+  if (p->residual_dtype == SWAPMOE_F32) return launched(rms_norm_launch_typed<bf16, float>(a, vec, sms, st, pdl), 1, launches);
+  return launched(rms_norm_launch_typed<bf16, bf16>(a, vec, sms, st, pdl), 1, launches);
 }
 
 int32_t adapters_run(swapmoe_adapters_t* b, const void* x, int64_t x_stride, const float* x_scales, const int32_t* ids, const void* y,
-                     int64_t y_stride, void* out, int64_t out_stride, int32_t T, void* stream, int64_t* launches) {
+                     int64_t y_stride, void* out, int64_t out_stride, int32_t T, void* stream, bool pdl, int64_t* launches) {
   if (!b || T < 0) return SWAPMOE_ERR_INVALID_ARG;
   if (T == 0) return SWAPMOE_OK;
   const swapmoe_adapters_config_t& c = b->cfg;
@@ -121,9 +127,9 @@ int32_t adapters_run(swapmoe_adapters_t* b, const void* x, int64_t x_stride, con
   a.T = T; a.d = c.d_in; a.n = c.d_out; a.r = c.rank; a.count = c.n_adapters;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   int kernels = 0;
-  const cudaError_t e = c.dtype == SWAPMOE_F32 ? adapters_launch<float, float>(a, b->sm_count, st, true, &kernels)
-                        : x_scales             ? adapters_launch<__nv_fp8_e4m3, bf16>(a, b->sm_count, st, true, &kernels)
-                                               : adapters_launch<bf16, bf16>(a, b->sm_count, st, true, &kernels);
+  const cudaError_t e = c.dtype == SWAPMOE_F32 ? adapters_launch<float, float>(a, b->sm_count, st, pdl, &kernels)
+                        : x_scales             ? adapters_launch<__nv_fp8_e4m3, bf16>(a, b->sm_count, st, pdl, &kernels)
+                                               : adapters_launch<bf16, bf16>(a, b->sm_count, st, pdl, &kernels);
   return launched(e, kernels, launches);
 }
 
@@ -131,7 +137,7 @@ int32_t adapters_run(swapmoe_adapters_t* b, const void* x, int64_t x_stride, con
 
 extern "C" {
 
-int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* p, void* stream) { return rms_norm_run(p, stream, nullptr); }
+int32_t swapmoe_rms_norm(const swapmoe_rms_norm_t* p, void* stream) { return rms_norm_run(p, stream, standalone_pdl(), nullptr); }
 
 int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits, int64_t stride, const float* bias,
                       const int32_t* expert_to_slot, int32_t T, int32_t E, int32_t top_k, int32_t* experts, float* weights,
@@ -147,7 +153,7 @@ int32_t swapmoe_route(const swapmoe_gate_t* gate, const float* logits, int64_t s
   a.logits = logits; a.bias = bias; a.expert_to_slot = expert_to_slot;
   a.experts = experts; a.weights = weights; a.slots = slots;
   a.stride = stride; a.T = T; a.E = E; a.k = top_k;
-  return launched(route_groups_launch(a, current_sm_count(), static_cast<cudaStream_t>(stream), true));
+  return launched(route_groups_launch(a, current_sm_count(), static_cast<cudaStream_t>(stream), standalone_pdl()));
 }
 
 int32_t swapmoe_adapters_create(swapmoe_adapters_t** out, const swapmoe_adapters_config_t* cfg) {
@@ -211,7 +217,7 @@ int32_t swapmoe_adapters_check(const swapmoe_adapters_t* b, int32_t d_in, int32_
 
 int32_t swapmoe_adapters_forward(swapmoe_adapters_t* b, const void* x, int64_t x_stride, const float* x_scales, const int32_t* ids,
                                  const void* y, int64_t y_stride, void* out, int64_t out_stride, int32_t T, void* stream) {
-  return adapters_run(b, x, x_stride, x_scales, ids, y, y_stride, out, out_stride, T, stream, nullptr);
+  return adapters_run(b, x, x_stride, x_scales, ids, y, y_stride, out, out_stride, T, stream, standalone_pdl(), nullptr);
 }
 
 }  // extern "C"

@@ -2,7 +2,15 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <cstdlib>
+
 namespace swapmoe {
+
+// SWAPMOE_PDL=0 launches every kernel fully serialised.
+inline bool dependent_launch() {
+  const char* env = std::getenv("SWAPMOE_PDL");
+  return !(env && env[0] == '0');
+}
 
 // Launch helper: programmatic dependent launch lets the kernel's prologue overlap the tail of
 // the kernel before it on the stream.

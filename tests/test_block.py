@@ -383,3 +383,69 @@ def test_the_blocks_launches_are_counted(T, own):
     with pytest.raises(binding.SwapMoEError):
         L.forward_block(x, r, out, bank, ids.long())
     assert launches(L.forward_block, x, r, out, None, None, 0) == 0
+
+
+DEPENDENT_EDGES = """
+import ctypes
+import sys
+sys.path[:0] = ["tests", "."]
+import torch
+from paper_2308_15030_b200 import binding, inputs as I
+from test_block import Gate, _block_inputs, _case
+
+
+class Edge(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_ubyte) for n in ("from_port", "to_port", "type")] + [("reserved", ctypes.c_ubyte * 5)]
+
+
+runtime = ctypes.CDLL(next(line.split()[-1] for line in open("/proc/self/maps") if "libcudart" in line))
+
+
+def edges(f):
+    f()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(g):
+        f()
+    h, n = ctypes.c_void_p(g.raw_cuda_graph()), ctypes.c_size_t(0)
+    assert runtime.cudaGraphGetEdges_v2(h, None, None, None, ctypes.byref(n)) == 0 and n.value > 0
+    ends, data = [(ctypes.c_void_p * n.value)() for _ in range(2)], (Edge * n.value)()
+    assert runtime.cudaGraphGetEdges_v2(h, ends[0], ends[1], data, ctypes.byref(n)) == 0
+    return sum(e.type == 1 for e in data)                    # cudaGraphDependencyTypeProgrammatic
+
+
+T = 2100
+case = _case(T, 64, 2, 12)
+L = case.layer
+x, r, w, bank, ids = _block_inputs(case, I.BF16)
+out = torch.empty_like(x)
+L.set_norm(w, 1e-5)
+lg, e, wt = torch.zeros(T, 64, device="cuda"), torch.empty(T, 2, dtype=torch.int32, device="cuda"), torch.empty(T, 2, device="cuda")
+
+
+def twice(f):
+    return lambda: (f(), f())
+
+
+got = [edges(twice(lambda: binding.rms_norm(x, w, 1e-5, out=out))), edges(twice(lambda: binding.route(Gate(), lg, e, wt))),
+       edges(twice(lambda: bank.forward(x, ids, x, out))), edges(lambda: L.forward_block(x, r, out, bank, ids))]
+print("EDGES", *got)
+"""
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("switch", ["0", "1"])
+def test_dependent_launches_follow_the_switch(switch):
+    """SWAPMOE_PDL=0: no kernel of these calls is launched before the one in front of it has ended."""
+    import os
+    import subprocess
+    import sys
+    import torch
+    if not hasattr(torch.cuda.CUDAGraph, "raw_cuda_graph"):
+        pytest.skip("no access to the captured graph")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", DEPENDENT_EDGES], cwd=root, env=dict(os.environ, SWAPMOE_PDL=switch),
+                         capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stderr[-2000:]
+    got = [int(v) for v in run.stdout.split("EDGES")[1].split()]
+    assert got == [0, 0, 0, 0] if switch == "0" else all(n > 0 for n in got), got
