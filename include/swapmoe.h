@@ -318,7 +318,7 @@ int32_t swapmoe_selftest_bounded_wait(swapmoe_layer_t* layer, int32_t limit_ms, 
 /* Number of kernels of this library launched by the layer so far (host counter). */
 int64_t swapmoe_launch_count(const swapmoe_layer_t* layer);
 
-/* Bytes of device workspace the layer allocated at create. */
+/* Bytes of device workspace the layer allocated at create, and in swapmoe_set_norm. */
 int64_t swapmoe_workspace_bytes(const swapmoe_layer_t* layer);
 
 /* Selects the grouped-GEMM implementation for later forwards (test / benchmark

@@ -844,10 +844,14 @@ int32_t swapmoe_set_norm(swapmoe_layer_t* L, const void* weight_dev, float eps) 
   if (!L || !weight_dev || reinterpret_cast<uintptr_t>(weight_dev) % L->elem || !(eps >= 0.f) || !std::isfinite(eps))
     return SWAPMOE_ERR_INVALID_ARG;
   if (L->cfg.d_model > SWAPMOE_NORM_MAX_WIDTH) return SWAPMOE_ERR_UNSUPPORTED;
-  if (!L->x_norm && !cuda_ok(cudaMalloc(&L->x_norm, (size_t)L->cfg.max_tokens * L->cfg.d_model * L->elem))) {
-    cudaGetLastError();
-    L->x_norm = nullptr;
-    return SWAPMOE_ERR_NO_MEMORY;
+  if (!L->x_norm) {
+    const size_t bytes = (size_t)L->cfg.max_tokens * L->cfg.d_model * L->elem;
+    if (!cuda_ok(cudaMalloc(&L->x_norm, bytes))) {
+      cudaGetLastError();
+      L->x_norm = nullptr;
+      return SWAPMOE_ERR_NO_MEMORY;
+    }
+    L->ws_bytes += bytes;
   }
   L->norm_weight = weight_dev;
   L->norm_eps = eps;

@@ -449,3 +449,16 @@ def test_dependent_launches_follow_the_switch(switch):
     assert run.returncode == 0, run.stderr[-2000:]
     got = [int(v) for v in run.stdout.split("EDGES")[1].split()]
     assert got == [0, 0, 0, 0] if switch == "0" else all(n > 0 for n in got), got
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,size", [(I.BF16, 2), (I.F32, 4)])
+def test_the_rows_behind_the_norm_count_as_workspace(dtype, size):
+    import torch
+    case = _case(8, 16, 2, 6, dtype, max_tokens=40)
+    L = case.layer
+    x, r, w, bank, ids = _block_inputs(case, dtype)
+    before = L.workspace_bytes
+    for _ in range(2):                                       # allocated once
+        L.set_norm(w, 1e-5)
+        assert L.workspace_bytes == before + 40 * 128 * size
