@@ -14,6 +14,7 @@
 // row: out is written from registers.
 #pragma once
 #include <cuda_fp8.h>
+#include <math_constants.h>
 
 #include "common.cuh"
 #include "launch.cuh"
@@ -213,6 +214,36 @@ __device__ __forceinline__ uint4 ad_finish(const uint4& y, const float (&c)[2][4
   return make_uint4(__float_as_uint(__uint_as_float(y.x) + c[0][e]), __float_as_uint(__uint_as_float(y.y) + c[0][e + 1]),
                     __float_as_uint(__uint_as_float(y.z) + c[1][e]), __float_as_uint(__uint_as_float(y.w) + c[1][e + 1]));
 }
+// Sums of bf16 pieces that are not finite say little: an infinity's second piece is inf - inf, and its products with the other side's
+// pieces cancel; so does a finite value beyond bf16's largest.  What such a sum belongs to is computed again by plain multiply-adds,
+// out of line (never taken with finite results; a row of NaN costs its tile some 10 us).
+template <int N>
+__device__ __forceinline__ bool ad_finite(const float (&c)[N][4], int e) {
+  float m = 0.f;
+#pragma unroll
+  for (int h = 0; h < N; ++h) m += fabsf(c[h][e]) + fabsf(c[h][e + 1]);
+  return m < CUDART_INF_F;
+}
+// Two neighbouring ranks of A x: x a row, w the first rank's row of A.
+static __device__ __noinline__ float2 ad_again_u(const float* x, const float* w, int d) {
+  float2 s = make_float2(0.f, 0.f);
+#pragma unroll 4
+  for (int c = 0; c < d; ++c) {
+    s.x = fmaf(x[c], w[c], s.x);
+    s.y = fmaf(x[c], w[d + c], s.y);
+  }
+  return s;
+}
+// 16 bytes of out: u a row of the low-rank side, w the first column's row of B.
+static __device__ __noinline__ uint4 ad_again_out(const float* u, const float* w, int r, uint4 y) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int j = 0; j < r; ++j)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) s[c] = fmaf(u[j], w[c * r + j], s[c]);
+  return make_uint4(__float_as_uint(__uint_as_float(y.x) + s[0]), __float_as_uint(__uint_as_float(y.y) + s[1]),
+                    __float_as_uint(__uint_as_float(y.z) + s[2]), __float_as_uint(__uint_as_float(y.w) + s[3]));
+}
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ float4 ld_cluster4(const float* mine, int cta) {        // the same place in that CTA's shared memory
@@ -281,6 +312,7 @@ __device__ __forceinline__ int ad_direct_tile(const AdapterArgs& a, int i, int32
 template <typename X, typename T, int RTW>
 __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const AdapterArgs a) {
   constexpr int kElem = (int)sizeof(T);
+  constexpr bool kAgain = kElem == 4;            // see ad_finite
   constexpr int P = 16 / kElem;                  // values of a lane's piece; a step or unit is 4 P values
   constexpr int NT = P / 2;                      // column tiles of a unit of out
   typedef typename AdPiece<X>::type XPiece;
@@ -419,6 +451,13 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
     const int total = rows * r;
     auto finish = [&](int i, float4 s) {
       const int t = i / r, j = i - t * r;
+      if constexpr (kAgain)
+        if (!(fabsf(s.x) + fabsf(s.y) + fabsf(s.z) + fabsf(s.w) < CUDART_INF_F)) {
+          const X* row = x + (long long)list[t] * a.x_stride;
+          const T* w = static_cast<const T*>(a.A) + ((long long)adapter * r + j) * a.d;
+          const float2 lo = ad_again_u(row, w, a.d), hi = ad_again_u(row, w + 2ll * a.d, a.d);
+          s = make_float4(lo.x, lo.y, hi.x, hi.y);
+        }
       float f = sc;
       if (a.x_scales != nullptr) f *= a.x_scales[list[t]];
       ad_store_u(reinterpret_cast<T*>(us + t * u_pitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
@@ -474,7 +513,15 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
           for (int h = 0; h < NT; ++h) ad_step(acc[h], left, wb[v][h]);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) res[v][i] = ad_finish(yv[v][i], acc, 2 * i, T());
+        for (int i = 0; i < 2; ++i) {
+          res[v][i] = ad_finish(yv[v][i], acc, 2 * i, T());
+          if constexpr (kAgain) {
+            const int c = ((unit + v * stride) * 4 + q) * P, row = g + 8 * i;
+            if (!ad_finite(acc, 2 * i) && c < a.n && row < rows)
+              res[v][i] = ad_again_out(reinterpret_cast<const T*>(us + row * u_pitch), reinterpret_cast<const T*>(B) + (long long)c * r, r,
+                                       yv[v][i]);
+          }
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i) res[v][i] = yv[v][i];
@@ -655,6 +702,7 @@ __device__ __forceinline__ void ad_tile_here(const AdapterArgs& a, int which, in
 template <typename X, typename T, int RP>
 __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __grid_constant__ AdapterArgs a, int stages, int here) {
   constexpr int kElem = (int)sizeof(T), P = 16 / kElem, NT = P / 2;
+  constexpr bool kAgain = kElem == 4;                        // see ad_finite
   constexpr int kCols = kAdChunk / kElem;                    // columns of a chunk
   constexpr int kXPiece = sizeof(X) == 1 ? 8 : 16;           // bytes of a lane's piece of x: P values
   constexpr int kXRow = 16 * kXPiece;                        // bytes of a row of a chunk of x
@@ -884,6 +932,16 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
           for (int h = 0; h < NTH; ++h) {
             if ((nh * NTH + h) * 8 >= r)                     // ranks that A does not have
               acc[h][0] = acc[h][1] = acc[h][2] = acc[h][3] = 0.f;
+            if constexpr (kAgain) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (!(fabsf(acc[h][2 * e]) + fabsf(acc[h][2 * e + 1]) < CUDART_INF_F) && row0 + 8 * e < rows) {
+                  const float2 u = ad_again_u(x + (long long)list[row0 + 8 * e] * a.x_stride,
+                                              static_cast<const T*>(a.A) + ((long long)adapter * r + (nh * NTH + h) * 8 + 2 * q) * a.d, a.d);
+                  acc[h][2 * e] = u.x;
+                  acc[h][2 * e + 1] = u.y;
+                }
+            }
             T* p = reinterpret_cast<T*>(us + row0 * kUPitch) + (nh * NTH + h) * 8 + 2 * q;
             ad_store_u2(p, acc[h][0] * f[0], acc[h][1] * f[0]);
             ad_store_u2(reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(p) + 8 * kUPitch), acc[h][2] * f[1], acc[h][3] * f[1]);
@@ -912,6 +970,13 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
               const float4 v = ld_cluster4(part + k, c);
               s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
+            if constexpr (kAgain)
+              if (!(fabsf(s.x) + fabsf(s.y) + fabsf(s.z) + fabsf(s.w) < CUDART_INF_F)) {
+                const X* row = x + (long long)list[t] * a.x_stride;
+                const T* w = static_cast<const T*>(a.A) + ((long long)adapter * r + j) * a.d;
+                const float2 lo = ad_again_u(row, w, a.d), hi = ad_again_u(row, w + 2ll * a.d, a.d);
+                s = make_float4(lo.x, lo.y, hi.x, hi.y);
+              }
           }
           const float f = a.x_scales != nullptr ? sc * a.x_scales[list[t]] : sc;
           ad_store_u(reinterpret_cast<T*>(us + t * kUPitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
@@ -978,8 +1043,16 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
             y0 = ad_lds((st + from_y) ^ (v * 64));
             y8 = ad_lds(((st + from_y) ^ (v * 64)) + 8 * 256);
           }
-          if (row0 < rows) *reinterpret_cast<uint4*>(op[0] + v * 4 * P) = ad_finish(y0, d[v], 0, T());
-          if (row0 + 8 < rows) *reinterpret_cast<uint4*>(op[1] + v * 4 * P) = ad_finish(y8, d[v], 2, T());
+          auto store = [&](T* to, int row, const uint4& yr, int e) {
+            uint4 o = ad_finish(yr, d[v], e, T());
+            if constexpr (kAgain)
+              if (!ad_finite(d[v], e))
+                o = ad_again_out(reinterpret_cast<const T*>(us + row * kUPitch),
+                                 static_cast<const T*>(a.B) + ((long long)adapter * a.n + c0 + col + v * 4 * P + q * P) * r, r, yr);
+            *reinterpret_cast<uint4*>(to + v * 4 * P) = o;
+          };
+          if (row0 < rows) store(op[0], row0, y0, 0);
+          if (row0 + 8 < rows) store(op[1], row0 + 8, y8, 2);
         }
       }
       op[0] += C * kCols;

@@ -227,3 +227,41 @@ def test_refusals_with_a_bank():
     f = binding.AdapterBank(2, 64, 64, 8, binding.F32, max_tokens=4)
     assert L.swapmoe_adapters_set_weights(f._h, A.data_ptr(), B.data_ptr(), None) == 0
     assert L.swapmoe_adapters_forward(f._h, x.data_ptr(), 64, ids.data_ptr(), ids.data_ptr(), None, 0, x.data_ptr(), 64, 1, None) == -1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,d,r", [(1, 64, 8), (20, 256, 16), (100, 512, 64), (700, 256, 16), (3000, 512, 64), (300, 1024, 128)])
+def test_infinities_and_the_largest_values(T, d, r, dtype):
+    """Infinities in x, A, B and y, and finite values beyond bf16's largest, give what the formula gives."""
+    import torch
+    n, count = 136, 4
+    x, y, _, A, B, scale, bank = _make(T, d, n, r, count, dtype, seed=T)
+    A[:, :, 5], A[:, :, 6], scale[:] = A[:, :, 5].abs() + 0.01, A[:, :, 6].abs() * 2.0 ** -20, scale.abs() + 0.1
+    B[:2] = B[:2].abs() + 0.01                         # adapters 0 and 1: infinities of one sign stay infinite
+    A[1, :, 9], B[1, 40], B[1, 41, 0] = float("inf"), float("inf"), float("-inf")
+    B[3, 50, 1], B[3, 51] = float("inf"), 0.0
+    ids = torch.arange(T, dtype=torch.int32, device="cuda") % (count + 1) - 1
+    ids[0] = 0
+    x[::3, 5] = float("inf")
+    x[1::7, 5] = float("-inf")
+    if dtype == "fp32":
+        x[2::3, 6] = 3.4e38                            # (bf16's largest is 3.39e38)
+        B[0, 60] *= 2.0 ** -120
+    y[::4, 7], y[1::4, 8] = float("inf"), float("nan")
+    bank.set_weights(A, B, scale)
+    for with_y in (True, False):
+        out = torch.empty_like(y)
+        bank.forward(x, ids, y if with_y else None, out)
+        want, slack = _reference(x, y if with_y else None, None, A, B, scale, ids, dtype)
+        if dtype == "fp32":
+            # bf16's smallest step is 2^-133: what three pieces leave of an operand below 2^-110 (the weights of B[0, 60]) is up to half
+            # of that, however small the operand; times the sum of |u|, which is at most that of |A| |x|
+            for a in range(count):
+                t = torch.nonzero(ids == a)[:, 0]
+                slack[t] += 2.0 ** -134 * (x[t].double().abs() @ A[a].double().abs().T * scale[a].double()).sum(1)[:, None]
+        want = torch.where(want.abs() > torch.finfo(y.dtype).max, want.sign() * float("inf"), want)
+        assert torch.equal(out.isnan(), want.isnan()) and torch.equal(out.isinf(), want.isinf())
+        infinite, finite = want.isinf(), want.isfinite()
+        assert torch.equal(out.double()[infinite], want[infinite])
+        assert bool(((out.double() - want).abs()[finite] <= slack[finite]).all())
