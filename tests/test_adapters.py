@@ -265,3 +265,61 @@ def test_infinities_and_the_largest_values(T, d, r, dtype):
         infinite, finite = want.isinf(), want.isfinite()
         assert torch.equal(out.double()[infinite], want[infinite])
         assert bool(((out.double() - want).abs()[finite] <= slack[finite]).all())
+
+
+# ------------------------------------------------------------------ what the pieces of the operands keep
+def _pieces(v, n):
+    """A float32 array as n bf16 pieces, each rounded to nearest from what the ones in front left."""
+    import torch
+    got, rest = [], torch.from_numpy(v)
+    for _ in range(n):
+        got.append(rest.bfloat16().double().numpy())
+        rest = rest - rest.bfloat16().float()
+    return got
+
+
+def _product(x, w, n, most):
+    """x w^T from n pieces each, of the products i, j those with i + j <= most; sums in 64 bits."""
+    xs, ws = _pieces(x, n), _pieces(w, n)
+    return sum(xs[i] @ ws[j].T for i in range(n) for j in range(n) if i + j <= most)
+
+
+def _rms_limit(d, r):
+    """Largest rms error of fp32 results relative to their rms, without y, for values of random signs.  A product of three pieces
+    each and six of their products is off by 2^-24 per operand and twice 2^-24 for those left out: 2^-22; the six truncations of a
+    step by 6 x 2^-23 of the step's sum, and steps of random signs add up as their results do: 16 x 2^-24 in all, for each of
+    the two products.  The n = d / 16 (r / 16) steps are added in fp32: 2^-24 of the sum so far each, sqrt(n / 2) of the result; 8 for
+    partial sums, scales and the last rounding."""
+    return (32 + (d / 32) ** 0.5 + (r / 32) ** 0.5 + 8) * 2.0 ** -24
+
+
+RMS_SHAPES = [(64, 8), (256, 16), (512, 64), (1024, 128), (4096, 16)]
+
+
+@pytest.mark.parametrize("d,r", RMS_SHAPES)
+def test_the_rms_limit_tells_three_pieces_from_two(d, r):
+    """Two pieces (or three without the products of the small ones) are beyond the limit, three pieces and six products within."""
+    rng = np.random.default_rng(d)
+    x, A, B = (rng.normal(0, 1, s).astype(np.float32) for s in ((40, d), (r, d), (96, r)))
+    u = x.astype(np.float64) @ A.T.astype(np.float64)
+    want = u @ B.T.astype(np.float64)
+
+    def error(n, most):
+        got = _product(_product(x, A, n, most).astype(np.float32), B, n, most)
+        return np.sqrt(np.mean((got - want) ** 2) / np.mean(want ** 2))
+    assert error(3, 2) < 0.2 * _rms_limit(d, r)
+    assert error(2, 1) > 1.2 * _rms_limit(d, r) and error(3, 1) > 1.2 * _rms_limit(d, r)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [7, 90, 400, 3000])
+@pytest.mark.parametrize("d,r", RMS_SHAPES)
+def test_fp32_banks_keep_24_bits(T, d, r):
+    import torch
+    n, count = 328, 3
+    x, y, _, A, B, scale, bank = _make(T, d, n, r, count, "fp32", seed=d + T)
+    ids = _ids(T, count, T, none=0.0)
+    out = torch.empty_like(y)
+    bank.forward(x, ids, None, out)
+    want, _ = _reference(x, None, None, A, B, scale, ids, "fp32")
+    assert float(((out.double() - want) ** 2).mean().sqrt() / (want ** 2).mean().sqrt()) <= _rms_limit(d, r)
