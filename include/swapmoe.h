@@ -469,8 +469,8 @@ int32_t swapmoe_adapters_set_weights(swapmoe_adapters_t* bank, const void* A_dev
 /* One pass.  x_dev [n_tokens, d_in] in dtype, or e4m3 bytes (bf16 banks only) with x_scales_dev [n_tokens] fp32, one scale per row;
  * ids_dev [n_tokens] int32, in any order: a negative id, or one that is not in the bank, means no adapter (out = y, to
  * the last bit).  y_dev [n_tokens, d_out] or NULL (zeros); out_dev may be y_dev with the same stride, otherwise nothing may
- * overlap out.  Row strides count elements; rows start at multiples of 16 bytes (e4m3: 8).  Sums are fp32 (bf16 banks round
- * A x * scale to bf16 once before B, results are rounded once; fp32 banks multiply 24 bits of values down to 2^-110, and
+ * overlap out.  Row strides count elements; rows start at multiples of 16 bytes (e4m3: 8).  Sums are fp32 (bf16 banks keep
+ * A x * scale to 2^-16 of itself, results are rounded once; fp32 banks multiply 24 bits of values down to 2^-110, and
  * to within 2^-134 below).  Infinities and NaN give what the formula gives.  The same call returns the same bits.  Work is enqueued on `stream`; no allocation, no synchronisation.  Errors: NOT_READY (no
  * weights), TOO_MANY_TOKENS, INVALID_ARG, CUDA.  n_tokens = 0 is a no-op. */
 int32_t swapmoe_adapters_forward(swapmoe_adapters_t* bank, const void* x_dev, int64_t x_stride, const float* x_scales_dev,

@@ -197,9 +197,26 @@ __device__ __forceinline__ uint4 ad_operand(const uint2& v) {
 }
 __device__ __forceinline__ void ad_zero(uint4& v) { v = make_uint4(0u, 0u, 0u, 0u); }
 __device__ __forceinline__ void ad_zero(uint2& v) { v = make_uint2(0u, 0u); }
-__device__ __forceinline__ void ad_store_u(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void ad_store_u(bf16* p, float4 v) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+// What lies between the products, u = scale * A x, is kept in fp32 (fp32 banks) or in two bf16 pieces, to 2^-16: rounded to one, it
+// alone brought as much error as the rounding of the results.  The first piece is cut off, not rounded, and the second one is never 0
+// where the first is not (2^-24 of it in place of a 0): pieces of one sign, whose products with an infinity of B are
+// infinities of one sign too.  An infinite u has two infinite pieces.  `lo`: bytes from the first piece to the second.
+__device__ __forceinline__ float ad_rest(float v, float first) {
+  const float rest = v - first;
+  return fabsf(rest) > 0.f ? rest : first * 0x1p-24f;
+}
+__device__ __forceinline__ void ad_pieces(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const uint32_t x = __float_as_uint(a) & 0xffff0000u, y = __float_as_uint(b) & 0xffff0000u;
+  hi = x >> 16 | y;
+  lo = pack_bf16x2(ad_rest(a, __uint_as_float(x)), ad_rest(b, __uint_as_float(y)));
+}
+__device__ __forceinline__ void ad_store_u(float* p, float4 v, int) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void ad_store_u(bf16* p, float4 v, int lo) {
+  uint2 h, l;
+  ad_pieces(v.x, v.y, h.x, l.x);
+  ad_pieces(v.z, v.w, h.y, l.y);
+  *reinterpret_cast<uint2*>(p) = h;
+  *reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(p) + lo) = l;
 }
 // Two neighbouring values of y, plus the sums, rounded once.
 __device__ __forceinline__ uint32_t ad_add2(uint32_t y, float d0, float d1) {
@@ -214,9 +231,9 @@ __device__ __forceinline__ uint4 ad_finish(const uint4& y, const float (&c)[2][4
   return make_uint4(__float_as_uint(__uint_as_float(y.x) + c[0][e]), __float_as_uint(__uint_as_float(y.y) + c[0][e + 1]),
                     __float_as_uint(__uint_as_float(y.z) + c[1][e]), __float_as_uint(__uint_as_float(y.w) + c[1][e + 1]));
 }
-// Sums of bf16 pieces that are not finite say little: an infinity's second piece is inf - inf, and its products with the other side's
-// pieces cancel; so does a finite value beyond bf16's largest.  What such a sum belongs to is computed again by plain multiply-adds,
-// out of line (never taken with finite results; a row of NaN costs its tile some 10 us).
+// fp32: sums of bf16 pieces that are not finite say little: an infinity's second piece is inf - inf, and a finite value beyond bf16's
+// largest has an infinite one.  What such a sum belongs to is computed again by plain multiply-adds, out of line (never taken
+// with finite results).
 template <int N>
 __device__ __forceinline__ bool ad_finite(const float (&c)[N][4], int e) {
   float m = 0.f;
@@ -266,7 +283,11 @@ __host__ __device__ constexpr int ad_u_pitch(int r, int elem) {
   return b % 128 == 0 ? b + 64 : b;
 }
 __host__ __device__ constexpr int ad_part_bytes(int r) { return kAdWarps / ad_rank_warps(r, ad_rtw(r)) * kAdTile * r * 4; }
-__host__ __device__ constexpr int ad_smem_bytes(int r, int elem) { return ad_part_bytes(r) + kAdTile * ad_u_pitch(r, elem) + kAdTile * 4 + 16; }
+// bf16 rows of u are two: the first pieces and the second ones.  Up to rank 16 both are halves of one row of 64 bytes, a step of the
+// second product, whose other operand then is B twice: no more products than for one piece.
+__host__ __device__ constexpr bool ad_u_halves(int r, int elem) { return elem == 2 && r <= 16; }
+__host__ __device__ constexpr int ad_u_bytes(int r, int elem) { return kAdTile * ad_u_pitch(r, elem) * (elem == 2 && !ad_u_halves(r, elem) ? 2 : 1); }
+__host__ __device__ constexpr int ad_smem_bytes(int r, int elem) { return ad_part_bytes(r) + ad_u_bytes(r, elem) + kAdTile * 4 + 16; }
 
 // The tile of cluster i without a plan: it has one if token i is the first, or the 17th, ... of its adapter; then its tokens
 // are the next 16 of that adapter from i on.  By one warp: lane l holds tokens l, l + 32, ...
@@ -312,7 +333,7 @@ __device__ __forceinline__ int ad_direct_tile(const AdapterArgs& a, int i, int32
 template <typename X, typename T, int RTW>
 __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const AdapterArgs a) {
   constexpr int kElem = (int)sizeof(T);
-  constexpr bool kAgain = kElem == 4;            // see ad_finite
+  constexpr bool kHalves = kElem == 2 && RTW <= 2;      // ad_u_halves of the ranks that come here
   constexpr int P = 16 / kElem;                  // values of a lane's piece; a step or unit is 4 P values
   constexpr int NT = P / 2;                      // column tiles of a unit of out
   typedef typename AdPiece<X>::type XPiece;
@@ -320,8 +341,8 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
   const int r = a.r, rank_tiles = r / 8, u_pitch = ad_u_pitch(r, kElem);
   const int rank_warps = ad_rank_warps(r, RTW), slices = kAdWarps / rank_warps;
   float* part = reinterpret_cast<float*>(smem);                                 // [slices][tile][r]
-  unsigned char* us = smem + ad_part_bytes(r);                                  // [tile] rows of u in T
-  int32_t* list = reinterpret_cast<int32_t*>(us + kAdTile * u_pitch);           // [tile] tokens
+  unsigned char* us = smem + ad_part_bytes(r);                                  // [tile] rows of u in T, and their second pieces
+  int32_t* list = reinterpret_cast<int32_t*>(us + ad_u_bytes(r, kElem));        // [tile] tokens
   volatile int* ctl = list + kAdTile;                                           // rows, adapter
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, q = lane & 3;
   const int C = a.ctas, cta = blockIdx.x % C;
@@ -431,13 +452,14 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
   // lane's row of B in column tile h of a unit: P (g / 2) + 2 h + g % 2
   const int b_col = P * (g >> 1) + (g & 1);
   const uint32_t b_row = (uint32_t)(r * kElem);
+  const int qr = kHalves ? q & 1 : q;            // the lane's piece of the ranks
   auto load_b = [&](uint4 (&w)[NT], int unit, int k0) {
     const int c = unit * 4 * P + b_col;
 #pragma unroll
     for (int h = 0; h < NT; ++h) {
       ad_zero(w[h]);
-      if (k0 + q * P < r && c + 2 * h < a.n)
-        w[h] = __ldg(reinterpret_cast<const uint4*>(B + ((uint32_t)(c + 2 * h) * b_row + k0 * kElem + q * 16)));
+      if (k0 + qr * P < r && c + 2 * h < a.n)
+        w[h] = __ldg(reinterpret_cast<const uint4*>(B + ((uint32_t)(c + 2 * h) * b_row + k0 * kElem + qr * 16)));
     }
   };
   int unit = cta * kAdWarps + warp;
@@ -451,7 +473,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
     const int total = rows * r;
     auto finish = [&](int i, float4 s) {
       const int t = i / r, j = i - t * r;
-      if constexpr (kAgain)
+      if constexpr (kElem == 4)
         if (!(fabsf(s.x) + fabsf(s.y) + fabsf(s.z) + fabsf(s.w) < CUDART_INF_F)) {
           const X* row = x + (long long)list[t] * a.x_stride;
           const T* w = static_cast<const T*>(a.A) + ((long long)adapter * r + j) * a.d;
@@ -460,7 +482,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
         }
       float f = sc;
       if (a.x_scales != nullptr) f *= a.x_scales[list[t]];
-      ad_store_u(reinterpret_cast<T*>(us + t * u_pitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
+      ad_store_u(reinterpret_cast<T*>(us + t * u_pitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f), kHalves ? 32 : kAdTile * u_pitch);
     };
     for (int i = tid * 4; i < total; i += kAdThreads * 4) {
       float4 s = *reinterpret_cast<const float4*>(part + i);
@@ -490,7 +512,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
   }
   auto operand_u = [&](uint4& p, int row, int k0) {
     ad_zero(p);
-    if (k0 + q * P < r) p = *reinterpret_cast<const uint4*>(us + row * u_pitch + k0 * kElem + q * 16);
+    if (k0 + qr * P < r) p = *reinterpret_cast<const uint4*>(us + row * u_pitch + k0 * kElem + q * 16);
   };
 #pragma unroll 1
   for (; unit < n_units; unit += kUnits * stride) {
@@ -509,13 +531,20 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_few_kernel(const Adapt
           operand_u(p8, g + 8, k0);
           const AdLeft<T> left(p, p8);
           if (k0 > 0) load_b(wb[v], unit + v * stride, k0);
+          if constexpr (kElem == 2 && !kHalves) {        // the second pieces first
+            operand_u(p, g + kAdTile, k0);
+            operand_u(p8, g + 8 + kAdTile, k0);
+            const AdLeft<T> rest(p, p8);
+#pragma unroll
+            for (int h = 0; h < NT; ++h) ad_step(acc[h], rest, wb[v][h]);
+          }
 #pragma unroll
           for (int h = 0; h < NT; ++h) ad_step(acc[h], left, wb[v][h]);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           res[v][i] = ad_finish(yv[v][i], acc, 2 * i, T());
-          if constexpr (kAgain) {
+          if constexpr (kElem == 4) {
             const int c = ((unit + v * stride) * 4 + q) * P, row = g + 8 * i;
             if (!ad_finite(acc, 2 * i) && c < a.n && row < rows)
               res[v][i] = ad_again_out(reinterpret_cast<const T*>(us + row * u_pitch), reinterpret_cast<const T*>(B) + (long long)c * r, r,
@@ -559,17 +588,20 @@ __host__ __device__ constexpr int ad_swap_b(int row, int pieces) {
 }
 __host__ __device__ constexpr int ad_rank_up(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
 __host__ __device__ constexpr int ad_stage_bytes(int r) { return kAdTM * kAdChunk + kAdChunk * r; }
-__host__ __device__ constexpr int ad_tile_u_pitch(int r, int elem) { return elem == 2 ? r * 2 + 16 : ad_u_pitch(r, elem); }
+// A row of u: bf16 ones are first pieces, then second pieces, which trade places as above, by ad_swap_u of the row.
+__host__ __device__ constexpr int ad_tile_u_pitch(int r, int elem) { return elem == 2 ? r * 4 : ad_u_pitch(r, elem); }
+__host__ __device__ constexpr int ad_swap_u(int row, int pitch) { return pitch == 64 ? row >> 1 & 3 : row & 7; }
 // What lies behind the stages: rows of u, for small ranks the CTA's part of u (else it takes the stage that was multiplied last,
 // which is then not free before the other CTAs have read it), the list of tokens.
 __host__ __device__ constexpr bool ad_own_part(int r) { return r <= 32; }
 __host__ __device__ constexpr int ad_tile_rest(int r, int elem) {
   return kAdTM * ad_tile_u_pitch(r, elem) + (ad_own_part(r) ? kAdTM * r * 4 : 0) + kAdTM * 4 + 512;
 }
-// Stages: as many as fit with two CTAs per SM, or, where that leaves fewer than three, with one.
+// Stages: as many as fit with two CTAs per SM (228 KB, of which each CTA costs 1), or, where that leaves fewer than three, with one.
+constexpr int kAdTwoBytes = 113 * 1024, kAdOneBytes = 227 * 1024;
 inline int ad_stages(int r, int elem) {
-  const int two = (112 * 1024 - ad_tile_rest(r, elem)) / ad_stage_bytes(r);
-  const int n = two >= 3 ? two : (224 * 1024 - ad_tile_rest(r, elem)) / ad_stage_bytes(r);
+  const int two = (kAdTwoBytes - ad_tile_rest(r, elem)) / ad_stage_bytes(r);
+  const int n = two >= 3 ? two : (kAdOneBytes - ad_tile_rest(r, elem)) / ad_stage_bytes(r);
   return n < kAdMaxStages ? n : kAdMaxStages;
 }
 template <int kBytes>
@@ -592,8 +624,13 @@ __device__ __forceinline__ void ad_copy_wait(int pending) {            // at mos
     default: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
   }
 }
-__device__ __forceinline__ void ad_store_u2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
-__device__ __forceinline__ void ad_store_u2(bf16* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(a, b); }
+__device__ __forceinline__ void ad_store_u2(float* p, float a, float b, int) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+__device__ __forceinline__ void ad_store_u2(bf16* p, float a, float b, int lo) {
+  uint32_t h, l;
+  ad_pieces(a, b, h, l);
+  *reinterpret_cast<uint32_t*>(p) = h;
+  *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(p) + lo) = l;
+}
 
 __device__ __forceinline__ uint4 ad_lds(uint32_t at) {
   uint4 v;
@@ -702,7 +739,6 @@ __device__ __forceinline__ void ad_tile_here(const AdapterArgs& a, int which, in
 template <typename X, typename T, int RP>
 __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __grid_constant__ AdapterArgs a, int stages, int here) {
   constexpr int kElem = (int)sizeof(T), P = 16 / kElem, NT = P / 2;
-  constexpr bool kAgain = kElem == 4;                        // see ad_finite
   constexpr int kCols = kAdChunk / kElem;                    // columns of a chunk
   constexpr int kXPiece = sizeof(X) == 1 ? 8 : 16;           // bytes of a lane's piece of x: P values
   constexpr int kXRow = 16 * kXPiece;                        // bytes of a row of a chunk of x
@@ -739,7 +775,12 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
                                          : (nh * NTH * 8 + g) * 256 + ((q ^ ad_swap(g)) << 4));
   const int b_row = kMatrixB ? 8 * (l8 >> 1) + 2 * l2 + (l8 & 1) : P * (g >> 1) + (g & 1);      // (in column tile 0 of unit 0)
   const uint32_t from_b = kW + (col + b_row) * kBRow + (((kMatrixB ? l1 : q) ^ ad_swap_b(b_row, kBPieces)) << 4);
-  const uint32_t from_u = us0 + (kMatrixB ? (mw * 16 + l8 + 8 * l1) * kUPitch + l2 * 16 : row0 * kUPitch + q * 16);
+  const uint32_t from_u = us0 + (kMatrixB ? (mw * 16 + l8 + 8 * l1) * kUPitch + ((l2 ^ ad_swap_u(l8, kUPitch)) << 4) : row0 * kUPitch + q * 16);
+  // ranks j, j + 1, ... of row t of u, and the bytes from there to the second pieces
+  auto u_at = [&](int t, int j) {
+    return reinterpret_cast<T*>(us + t * kUPitch + (kMatrixB ? (((j >> 3) ^ ad_swap_u(t, kUPitch)) << 4) + (j & 7) * 2 : j * 4));
+  };
+  auto u_lo = [&](int t, int j) { return (((j >> 3 ^ ad_swap_u(t, kUPitch)) & RP / 8) ? -1 : 1) * (RP * 2); };
   const uint32_t from_y = row0 * 256 + (((col / P + q) ^ ad_swap(g)) << 4);
   pdl_wait();
   pdl_trigger();
@@ -932,7 +973,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
           for (int h = 0; h < NTH; ++h) {
             if ((nh * NTH + h) * 8 >= r)                     // ranks that A does not have
               acc[h][0] = acc[h][1] = acc[h][2] = acc[h][3] = 0.f;
-            if constexpr (kAgain) {
+            if constexpr (kElem == 4) {
 #pragma unroll
               for (int e = 0; e < 2; ++e)
                 if (!(fabsf(acc[h][2 * e]) + fabsf(acc[h][2 * e + 1]) < CUDART_INF_F) && row0 + 8 * e < rows) {
@@ -942,9 +983,11 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
                   acc[h][2 * e + 1] = u.y;
                 }
             }
-            T* p = reinterpret_cast<T*>(us + row0 * kUPitch) + (nh * NTH + h) * 8 + 2 * q;
-            ad_store_u2(p, acc[h][0] * f[0], acc[h][1] * f[0]);
-            ad_store_u2(reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(p) + 8 * kUPitch), acc[h][2] * f[1], acc[h][3] * f[1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int t = row0 + 8 * e, j = (nh * NTH + h) * 8 + 2 * q;
+              ad_store_u2(u_at(t, j), acc[h][2 * e] * f[e], acc[h][2 * e + 1] * f[e], u_lo(t, j));
+            }
           }
         }
       } else {
@@ -953,8 +996,8 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
 #pragma unroll
           for (int h = 0; h < NTH; ++h) {
             float* p = part + row0 * RP + (nh * NTH + h) * 8 + 2 * q;
-            ad_store_u2(p, acc[h][0], acc[h][1]);
-            ad_store_u2(p + 8 * RP, acc[h][2], acc[h][3]);
+            *reinterpret_cast<float2*>(p) = make_float2(acc[h][0], acc[h][1]);
+            *reinterpret_cast<float2*>(p + 8 * RP) = make_float2(acc[h][2], acc[h][3]);
           }
         }
         cluster_arrive();
@@ -970,7 +1013,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
               const float4 v = ld_cluster4(part + k, c);
               s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
-            if constexpr (kAgain)
+            if constexpr (kElem == 4)
               if (!(fabsf(s.x) + fabsf(s.y) + fabsf(s.z) + fabsf(s.w) < CUDART_INF_F)) {
                 const X* row = x + (long long)list[t] * a.x_stride;
                 const T* w = static_cast<const T*>(a.A) + ((long long)adapter * r + j) * a.d;
@@ -979,7 +1022,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
               }
           }
           const float f = a.x_scales != nullptr ? sc * a.x_scales[list[t]] : sc;
-          ad_store_u(reinterpret_cast<T*>(us + t * kUPitch) + j, make_float4(s.x * f, s.y * f, s.z * f, s.w * f));
+          ad_store_u(u_at(t, j), make_float4(s.x * f, s.y * f, s.z * f, s.w * f), u_lo(t, j));
         }
         cluster_arrive();
         if (!ad_own_part(RP)) cluster_wait();                // the stage is free again
@@ -1010,17 +1053,24 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
         if constexpr (kMatrixB) {
 #pragma unroll
           for (int k = 0; k < RP / 16; ++k) {
-            uint32_t p[4];
-            ad_ldmatrix(p, from_u + k * 32);
+            uint32_t p[4], rest[4], w[2][2][4];
+            ad_ldmatrix(p, from_u ^ (k * 32));
+            ad_ldmatrix(rest, from_u ^ (RP * 2 + k * 32));
 #pragma unroll
             for (int v = 0; v < 2; ++v)
 #pragma unroll
-              for (int h = 0; h < NT; h += 2) {
-                uint32_t w[4];
-                ad_ldmatrix(w, ((st + from_b) ^ (k * 32)) + (v * 4 * P + 2 * h) * kBRow);
-                mma_bf16_16x8x16(d[v][h], p[0], p[1], p[2], p[3], w[0], w[1]);
-                mma_bf16_16x8x16(d[v][h + 1], p[0], p[1], p[2], p[3], w[2], w[3]);
-              }
+              for (int h = 0; h < 2; ++h) ad_ldmatrix(w[v][h], ((st + from_b) ^ (k * 32)) + (v * 4 * P + 4 * h) * kBRow);
+            // the second pieces first, eight products between two that add to the same sums (8192 tokens of 4096 at rank 64: two
+            // between 67.8 us, four 65.8, eight 64.6; one piece 59.9)
+            auto product = [&](const uint32_t (&u)[4]) {
+#pragma unroll
+              for (int v = 0; v < 2; ++v)
+#pragma unroll
+                for (int h = 0; h < NT; ++h)
+                  mma_bf16_16x8x16(d[v][h], u[0], u[1], u[2], u[3], w[v][h / 2][h % 2 * 2], w[v][h / 2][h % 2 * 2 + 1]);
+            };
+            product(rest);
+            product(p);
           }
         } else {
 #pragma unroll
@@ -1045,7 +1095,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
           }
           auto store = [&](T* to, int row, const uint4& yr, int e) {
             uint4 o = ad_finish(yr, d[v], e, T());
-            if constexpr (kAgain)
+            if constexpr (kElem == 4)
               if (!ad_finite(d[v], e))
                 o = ad_again_out(reinterpret_cast<const T*>(us + row * kUPitch),
                                  static_cast<const T*>(a.B) + ((long long)adapter * a.n + c0 + col + v * 4 * P + q * P) * r, r, yr);
@@ -1087,7 +1137,7 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
   // us, 8192 tokens of 4096 at rank 64: 1 CTA 69, 2 60, 4 70, 8 106 (two CTAs fit an SM, a second round costs as much as the first);
   // 1531 of 768 -> 2240 in fp32 at rank 8: 1 54, 2 31, 4 23, 8 19.
   const int smem = stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem);
-  const int at_once = smem <= 112 * 1024 ? 2 * sm_count : sm_count;
+  const int at_once = smem <= kAdTwoBytes ? 2 * sm_count : sm_count;
   a.ctas = 1;
   while (a.ctas < kAdMaxCtas && 10 * tiles * a.ctas <= 6 * at_once) a.ctas *= 2;      // (`tiles` is an upper bound)
   // A plan of its own per CTA where all CTAs run at once (later rounds would pay for it again): us, 1531 tokens, with the plan kernel
@@ -1113,10 +1163,10 @@ inline cudaError_t adapters_set_limits() {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
   raise(adapters_few_kernel<X, T, 4>, ad_smem_bytes(kAdMaxRank, (int)sizeof(T)));
-  raise(adapters_tile_kernel<X, T, 16>, 224 * 1024);
-  raise(adapters_tile_kernel<X, T, 32>, 224 * 1024);
-  raise(adapters_tile_kernel<X, T, 64>, 224 * 1024);
-  raise(adapters_tile_kernel<X, T, 128>, 224 * 1024);
+  raise(adapters_tile_kernel<X, T, 16>, kAdOneBytes);
+  raise(adapters_tile_kernel<X, T, 32>, kAdOneBytes);
+  raise(adapters_tile_kernel<X, T, 64>, kAdOneBytes);
+  raise(adapters_tile_kernel<X, T, 128>, kAdOneBytes);
   return e;
 }
 

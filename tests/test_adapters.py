@@ -323,3 +323,31 @@ def test_fp32_banks_keep_24_bits(T, d, r):
     bank.forward(x, ids, None, out)
     want, _ = _reference(x, None, None, A, B, scale, ids, "fp32")
     assert float(((out.double() - want) ** 2).mean().sqrt() / (want ** 2).mean().sqrt()) <= _rms_limit(d, r)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("T", [1, 20, 100, 700, 3000])
+@pytest.mark.parametrize("d,r", [(64, 8), (64, 16), (128, 24), (256, 32), (256, 40), (256, 64), (512, 128)])
+def test_bf16_banks_round_only_their_results(T, d, r, x8):
+    """What lies between the two products is kept in two bf16 pieces: no error of the type's size but the results' own."""
+    import torch
+    n, count = 264, 3
+    x, y, xs, A, B, scale, bank = _make(T, d, n, r, count, "bf16", x8, seed=r + T)
+    ids = _ids(T, count, T, none=0.0)
+    out = torch.empty_like(y)
+    for with_y in (False, True):
+        bank.forward(x, ids, y if with_y else None, out, x_scales=xs)
+        want, _ = _reference(x, y if with_y else None, xs, A, B, scale, ids, "bf16")
+        x64 = x.double() * (1.0 if xs is None else xs.double()[:, None])
+        slack = want.abs() * 2.0 ** -8
+        for a in range(count):
+            t = torch.nonzero(ids == a)[:, 0]
+            A64, B64, sc = A[a].double(), B[a].double(), abs(float(scale[a]))
+            u, um = (x64[t] @ A64.T).abs() * sc, x64[t].abs() @ A64.abs().T * sc
+            # products of bf16 are exact; truncating sums (2^-23 of the terms' magnitude per step of 16 and per merge of partial sums); the
+            # factors 2^-22; two pieces 2^-8 x 2^-8; their two products, summed the same way
+            eu = (d / 16 + 64) * 2.0 ** -23 * um + (2.0 ** -22 + 2.0 ** -16) * u
+            slack[t] += (eu + (2 * r / 16 + 8) * 2.0 ** -23 * u) @ B64.abs().T * 1.01
+        err = (out.double() - want).abs()
+        assert bool((err <= slack + 1e-30).all()), float((err / slack).max())
