@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
   float s = rsqrtf(total * a.per_column + a.eps) * (kRow8 ? 1.f / kNormLift : 1.f);
   if (slow) {
     // For the rows that are rare (a CTA's other rows keep what they have: a row hangs on itself) the same with the row divided by m, the
-    // larger one of its largest magnitude and sqrt(eps), so that neither square leaves the range:
+    // power of two below the larger one of its largest magnitude and sqrt(eps), so that neither square leaves the range:
     // h / sqrt(mean(h^2) + eps) = (h / m) / sqrt(mean((h / m)^2) + eps / m^2)
     auto over_team = [&](float v, bool add) {
       __syncthreads();
@@ -218,18 +218,20 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) rms_norm_kernel(const __gr
     for (int j = 0; j < kChunks; ++j) most = max_magnitude(most, largest8(h[j]), 0.f);
     const float top = over_team(warp_largest(most), false);
     const bool scaled = mine && top > 0.f && top < CUDART_INF_F;
-    const float m = fmaxf(top, sqrtf(a.eps));
+    const uint32_t exponent = __float_as_uint(fmaxf(top, sqrtf(a.eps))) >> 23;                  // (below 2^-126: m = 2^-127)
+    const float inverse_m = __uint_as_float(exponent < 254u ? (254u - exponent) << 23 : 0x400000u);
+    const float by = scaled ? inverse_m : 1.f;
     sum = 0.f;
     most = 0.f;
 #pragma unroll
     for (int j = 0; j < kChunks; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (scaled) h[j][i] /= m;
+        h[j][i] *= by;
         sum = fmaf(h[j][i], h[j][i], sum);
       }
     total = over_team(warp_sum(sum), true);
-    if (mine) s = rsqrtf(total * a.per_column + (scaled ? a.eps / m / m : a.eps));
+    if (mine) s = rsqrtf(total * a.per_column + a.eps * by * by);
     if constexpr (kRow8) {
       // the row's factor goes into the products at once: an infinity among them would be none behind it
       if (mine)
