@@ -6,7 +6,7 @@
 // per element of x and out, warp-level mma with tokens as mma rows.  One launch does both products: tokens of one adapter form
 // tiles, a cluster of 1 to 8 CTAs takes a tile and splits the columns of x, then those of out; the CTAs' parts of A x are
 // added through distributed shared memory, in a fixed order.  Two forms:
-//  - up to 128 tokens (adapters_few_kernel, tiles of 16): all operands go from global memory straight to the registers of the warp
+//  - up to 128 tokens (fp32 at high ranks: fewer; adapters_few_kernel, tiles of 16): all operands go from global memory straight to the registers of the warp
 //    that multiplies them, 64 contiguous bytes of eight rows per load; clusters find their tiles themselves.
 //  - more (adapters_tile_kernel, tiles of 64, a plan kernel in front that groups the tokens by adapter): x, A, y and B run through
 //    a ring in shared memory, so A and B are fetched once per 64 tokens and the loads run ahead of the products.
@@ -25,7 +25,7 @@ constexpr int kAdMaxRank = 128, kAdMaxCount = 4096, kAdMaxWidth = 1 << 16;
 constexpr int kAdThreads = 256, kAdWarps = kAdThreads / 32;
 constexpr int kAdMaxCtas = 8;              // most CTAs per cluster
 constexpr int kAdTile = 16;                // tokens of a tile: one mma row tile
-constexpr int kAdDirect = 128;             // up to this many tokens every cluster finds its tile itself
+constexpr int kAdDirect = 128;             // up to this many tokens every cluster finds its tile itself (see ad_direct_tokens)
 
 struct AdapterTile { int32_t adapter, first, rows, pad; };   // tokens perm[first] ... perm[first + rows - 1]; adapter -1: none
 
@@ -1118,11 +1118,20 @@ __global__ void __launch_bounds__(kAdThreads, 2) adapters_tile_kernel(const __gr
 inline int ad_max_tiles(int T, int count) { return T / kAdTM + (T < count + 1 ? T : count + 1); }
 constexpr int kAdMaxClusters = 2048;
 
+// Most tokens of adapters_few_kernel.  us for 100 tokens of 2048 with 12 adapters, in it and in adapters_tile_kernel, every token with an
+// adapter of its own / runs of 50: bf16 at rank 16 5.7 (65 tokens) and 8.0, 72 13.7 and 13.2 / 14.4 and 18.8, 128 16.5 and 13.2 / 16.7 and
+// 19.4; fp32 at rank 40 27.3 and 25.5 / 27.0 and 28.9, 64 30.1 and 25.1 / 30.5 and 28.4, 128 69.6 and 42.0 / 56.3 and 47.5.  fp32
+// at rank 64, 72 tokens (clusters of four, two of them per SM; beyond half the SMs there are only two CTAs in each) 19.9 and 24.9.
+template <typename T>
+inline int ad_direct_tokens(int r, int sm_count) {
+  return sizeof(T) == 4 && r > 40 && sm_count / 2 < kAdDirect ? sm_count / 2 : kAdDirect;
+}
+
 template <typename X, typename T>
 inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st, bool pdl, int* kernels) {
   const int elem = (int)sizeof(T);
   *kernels = 1;
-  if (a.T <= kAdDirect) {
+  if (a.T <= ad_direct_tokens<T>(a.r, sm_count)) {
     a.ctas = 1;
     // CTAs per cluster: until every SM has one or a CTA's warps one step each.  us, 61 tokens of 4096 with 64 adapters of rank 16:
     // 1 CTA 13.4, 2 11.0, 4 8.1, 8 11.0; one token of 1024: 4.9, 4.2, 4.3, 4.7.
