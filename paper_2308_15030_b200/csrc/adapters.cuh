@@ -6,8 +6,8 @@
 // per element of x and out, warp-level mma with tokens as mma rows.  One launch does both products: tokens of one adapter form
 // tiles, a cluster of 1 to 8 CTAs takes a tile and splits the columns of x, then those of out; the CTAs' parts of A x are
 // added through distributed shared memory, in a fixed order.  Two forms:
-//  - up to 128 tokens (fp32 at high ranks: fewer; adapters_few_kernel, tiles of 16): all operands go from global memory straight to the registers of the warp
-//    that multiplies them, 64 contiguous bytes of eight rows per load; clusters find their tiles themselves.
+//  - up to 128 tokens (fp32 at high ranks: fewer; adapters_few_kernel, tiles of 16): all operands go from global memory straight to
+//    the registers of the warp that multiplies them, 64 contiguous bytes of eight rows per load; clusters find their tiles themselves.
 //  - more (adapters_tile_kernel, tiles of 64, a plan kernel in front that groups the tokens by adapter): x, A, y and B run through
 //    a ring in shared memory, so A and B are fetched once per 64 tokens and the loads run ahead of the products.
 // In the second product the columns are dealt out to the mma's column tiles so that a lane's results are 16 contiguous bytes of a
@@ -1134,7 +1134,7 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
   if (a.T <= ad_direct_tokens<T>(a.r, sm_count)) {
     a.ctas = 1;
     // CTAs per cluster: until every SM has one or a CTA's warps one step each.  us, 61 tokens of 4096 with 64 adapters of rank 16:
-    // 1 CTA 13.4, 2 11.0, 4 8.1, 8 11.0; one token of 1024: 4.9, 4.2, 4.3, 4.7.
+    // 1 CTA 13.5, 2 11.1, 4 8.2, 8 11.2; one token of 1024: 5.0, 4.3, 4.4, 4.7.
     while (a.ctas < kAdMaxCtas && a.T * a.ctas < sm_count && a.ctas * kAdWarps * (64 / elem) < (a.d > a.n ? a.d : a.n)) a.ctas *= 2;
     auto go = [&](auto kernel) {
       return launch_cluster(kernel, a.ctas, dim3(a.ctas * a.T), dim3(kAdThreads), ad_smem_bytes(a.r, elem), st, pdl, a);
@@ -1143,14 +1143,14 @@ inline cudaError_t adapters_launch(AdapterArgs a, int sm_count, cudaStream_t st,
                                                                                   : go(adapters_few_kernel<X, T, 4>);
   }
   const int tiles = ad_max_tiles(a.T, a.count), rp = ad_rank_up(a.r), stages = ad_stages(rp, elem);
-  // us, 8192 tokens of 4096 at rank 64: 1 CTA 69, 2 60, 4 70, 8 106 (two CTAs fit an SM, a second round costs as much as the first);
-  // 1531 of 768 -> 2240 in fp32 at rank 8: 1 54, 2 31, 4 23, 8 19.
+  // us, 8192 tokens of 4096 at rank 64: 1 CTA 76, 2 64, 4 73, 8 109 (two CTAs fit an SM, a second round costs as much as the first);
+  // 1531 of 768 -> 2240 in fp32 at rank 8: 1 53, 2 31, 4 23, 8 18.
   const int smem = stages * ad_stage_bytes(rp) + ad_tile_rest(rp, elem);
   const int at_once = smem <= kAdTwoBytes ? 2 * sm_count : sm_count;
   a.ctas = 1;
   while (a.ctas < kAdMaxCtas && 10 * tiles * a.ctas <= 6 * at_once) a.ctas *= 2;      // (`tiles` is an upper bound)
   // A plan of its own per CTA where all CTAs run at once (later rounds would pay for it again): us, 1531 tokens, with the plan kernel
-  // 20.4, without 19.2.
+  // 20.2, without 18.4.
   const int here = a.T <= kAdHere && tiles * a.ctas <= at_once;
   if (!here) {
     const cudaError_t e = launch_kernel(adapters_plan_kernel, dim3(1), dim3(a.T <= 2048 ? 256 : kAdPlanThreads), 0, st, pdl, a, kAdTM);

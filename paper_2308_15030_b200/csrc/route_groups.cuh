@@ -8,7 +8,7 @@
 // the lowest lane.  The order of the choices is that of 64-bit scores: of thousands of tokens some have two experts closer than
 // fp32 tells apart.  Without a bias, and with groups valued by their best expert, it is that of the logits themselves.
 //
-// Bound by instructions, not by bytes (a row is 4 E bytes; 16384 x 256 with eight groups, a bias and top-8: 24.8 us, 2.8 of bytes,
+// Bound by instructions, not by bytes (a row is 4 E bytes; 16384 x 256 with eight groups, a bias and top-8: 25.2 us, 2.8 of bytes,
 // about 1000 instructions per token): so scores are fp32, and where a choice hangs on a gap that is not clear of their error the
 // experts or groups in doubt are compared in 64 bits, a lane each; only what that cannot settle is routed again with all scores in
 // 64 bits (one token's worth of that takes some 10 us on its own; with 64 bits for all tokens 60 us).  Each lane sorts its experts
@@ -584,8 +584,8 @@ __global__ void __launch_bounds__(kRouteWarps * 32, N <= 8 ? 8 : 4) route_groups
     }
   };
   auto logit = [&](const float* r, int e) { return e >= 0 ? fmaxf(r[e], -CUDART_INF_F) : -CUDART_INF_F; };
-  // Tokens that need 64 bits throughout are noted and routed behind the others, 64 tokens at a time: a call in the loop over the tokens, whatever it
-  // calls, makes that spill (16384 x 256: 30 us).
+  // Tokens that need 64 bits throughout are noted and routed behind the others, 64 tokens at a time: with a call in the loop over the tokens, whatever
+  // it calls, more registers spill (16384 x 256: 30 us, 25 so; at eight experts per lane 116 bytes are spilled even so).
 #pragma unroll 1
   while (token < a.T) {
     const long long first = token;
