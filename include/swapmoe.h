@@ -499,6 +499,123 @@ int32_t swapmoe_set_norm(swapmoe_layer_t* layer, const void* weight_dev, float e
 int32_t swapmoe_forward_block(swapmoe_layer_t* layer, const void* x_dev, void* residual_dev, void* out_dev, int32_t n_tokens,
                               swapmoe_adapters_t* adapters, const int32_t* ids_dev, void* stream);
 
+/*
+ * Operators in 8-bit integers, and the norms around a block.  As above: they run beside any layer object, work is enqueued on `stream`
+ * of the CURRENT device, nothing allocates or synchronises (but the create calls), and n = 0 rows is a no-op.
+ */
+
+/* The norms behind and in front of a block in one pass, with the block's gate and residual scale.  Per row
+ *   p = x * post_weight / sqrt(mean(x^2) + post_eps)      (p = x without a post_weight)
+ *   h = residual + scale * gate * p                       (no residual: 0; no gate: 1);  residual_out = h (rounded to residual_dtype)
+ *   y = h * weight / sqrt(mean(h^2) + eps);  out = y (rounded to dtype)
+ *   scales = max |y| / m, out8 = y / scales: e4m3 (m = 448) or integers (m = 127; nearest, ties to even), one scale per row (group =
+ *            0) or per `group` consecutive columns (32, 64, 128 or 256; the last group may be shorter)
+ * The gate is one row for all (gate_stride = 0) or a row of its own for each (gate_stride >= d).  Without a weight only residual_out is
+ * written (behind the last block).  Everything is computed in fp32; the ends of its range, zeros, infinities and NaN are as in
+ * swapmoe_rms_norm (integers of a NaN: 0).  Strides count elements; any start and stride that keep elements aligned are taken, and rows
+ * that start at multiples of 16 bytes (8 for out8) with d a multiple of 8 run fastest.  residual_out may be residual or x, and out may be x or
+ * residual, with the same stride (and type); other overlaps are not allowed.  Nothing behind column d or row n_rows is written.  Calls may
+ * run side by side.  Errors: INVALID_ARG (null or misaligned pointer, bad dtype, type8, stride, group, eps or scale, out or out8 without a
+ * weight, out8 without scales, no output at all), UNSUPPORTED (d > SWAPMOE_NORM_MAX_WIDTH), CUDA. */
+enum { SWAPMOE_E4M3 = 0, SWAPMOE_INT8 = 1 };
+typedef struct {
+  const void* x;            /* [n_rows, d] dtype: the block's output                                */
+  const void* residual;     /* [n_rows, d] residual_dtype, or NULL                                  */
+  const void* post_weight;  /* [d] dtype, or NULL                                                   */
+  const void* gate;         /* [d] or [n_rows, d] dtype, or NULL                                    */
+  const void* weight;       /* [d] dtype, or NULL                                                   */
+  void* residual_out;       /* [n_rows, d] residual_dtype, or NULL                                  */
+  void* out;                /* [n_rows, d] dtype, or NULL                                           */
+  void* out8;               /* [n_rows, d] bytes of type8, or NULL                                  */
+  float* scales;            /* [n_rows, ceil(d / group)] ([n_rows, 1] for group = 0), with out8     */
+  int64_t x_stride, residual_stride, gate_stride, residual_out_stride, out_stride, out8_stride, scales_stride;
+  int32_t n_rows, d;
+  int32_t dtype;            /* SWAPMOE_F32 or SWAPMOE_BF16                                          */
+  int32_t residual_dtype;   /* dtype, or SWAPMOE_F32                                                */
+  int32_t type8;            /* SWAPMOE_E4M3 or SWAPMOE_INT8                                         */
+  int32_t group;            /* columns per scale: 0 (the row), 32, 64, 128 or 256                   */
+  float eps, post_eps;      /* >= 0                                                                 */
+  float scale;              /* finite                                                               */
+} swapmoe_block_norm_t;
+int32_t swapmoe_block_norm(const swapmoe_block_norm_t* args, void* stream);
+
+/* Rows to 8-bit integers with a scale each:
+ *   y = x;  RELU: max(x, 0);  SWIGLU: silu(x[0 .. d)) * x[d .. 2 d)          (fp32)
+ *   scales = max |y| / 127,  out8 = y / scales, rounded to nearest, ties to even
+ * as fp32 division rounds both quotients.  A row of zeros has scale 0 and zeros; other scales are at least 2^-120.  A row with a NaN or an infinity has
+ * such a scale.  This is what swapmoe_matmul_scaled and the expert bank take as rows, and, one row per channel, as weights.
+ * Any start and stride that keep elements aligned are taken; aligned rows (16 bytes, out8 8) with d a multiple of 8 run fastest.  out8
+ * must not overlap x.  Calls may run side by side.  Errors: INVALID_ARG, UNSUPPORTED (d > SWAPMOE_QUANTIZE_MAX_WIDTH), CUDA. */
+#define SWAPMOE_QUANTIZE_MAX_WIDTH 32768
+enum { SWAPMOE_QUANTIZE_NONE = 0, SWAPMOE_QUANTIZE_RELU = 1, SWAPMOE_QUANTIZE_SWIGLU = 2 };
+typedef struct {
+  const void* x;            /* [n_rows, d] (SWIGLU: [n_rows, 2 d]) dtype                            */
+  void* out8;               /* [n_rows, d] int8                                                     */
+  float* scales;            /* [n_rows]                                                             */
+  int64_t x_stride, out8_stride;
+  int32_t n_rows, d;
+  int32_t dtype;            /* SWAPMOE_F32 or SWAPMOE_BF16                                          */
+  int32_t act;              /* SWAPMOE_QUANTIZE_...                                                 */
+} swapmoe_quantize_rows_t;
+int32_t swapmoe_quantize_rows(const swapmoe_quantize_rows_t* args, void* stream);
+
+/* A product of 8-bit integers with a scale for each token and each channel (the projection that adapters stand beside):
+ *   out[t, n] = x_scales[t] * w_scales[n] * sum_k x[t, k] * w[n, k] + bias[n]
+ * The sums are exact; scaling and bias are fp32, and the result is rounded once.  Rows of x and w start at multiples of 16 bytes (k
+ * itself is free); out takes any start and stride that keep elements aligned, and rows at multiples of 16 bytes leave fastest.  Nothing
+ * behind column n or row n_tokens is written; out must not overlap an input.  Calls may run side by side.  Every wait inside
+ * the kernels is bounded (swapmoe_matmul_status).  Errors: INVALID_ARG, UNSUPPORTED (k > SWAPMOE_MATMUL_MAX_K), CUDA. */
+#define SWAPMOE_MATMUL_MAX_K 131071
+typedef struct {
+  const void* x;            /* [n_tokens, k] int8                                                   */
+  const void* w;            /* [n, k] int8                                                          */
+  const float* x_scales;    /* [n_tokens]                                                           */
+  const float* w_scales;    /* [n]                                                                  */
+  const float* bias;        /* [n], or NULL                                                         */
+  void* out;                /* [n_tokens, n] dtype                                                  */
+  int64_t x_stride, w_stride, out_stride;
+  int32_t n_tokens, k, n;
+  int32_t dtype;            /* SWAPMOE_F32 or SWAPMOE_BF16                                          */
+} swapmoe_matmul_t;
+int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* args, void* stream);
+
+/* Waits for `stream` and returns the status word that the 8-bit products of this process keep on the CURRENT device: SWAPMOE_OK, or
+ * SWAPMOE_ERR_DEVICE_TIMEOUT if a bounded wait of swapmoe_matmul_scaled or of an expert bank gave up since the last call (*detail, may be NULL,
+ * names the wait).  The word is cleared. */
+int32_t swapmoe_matmul_status(int32_t* detail, void* stream);
+
+/* Experts in 8-bit integers behind a router (Section 2; half the bytes of a resident expert in bf16, and half of what a swap moves):
+ *   out[t] = sum_j weights[t, j] * E_slots[t, j](x[t]),   E_s(x) = W_out act(W_in x)
+ * x is int8 with a scale per row, the products are those of swapmoe_matmul_scaled, act(W_in x) is fp32 and goes to 8 bits by rows as
+ * swapmoe_quantize_rows does it, and the results are added in fp32 in the order of j.  slots and weights are what swapmoe_route writes: a slot that is
+ * negative, or not in the bank, is left out (a token without any has zeros); a slot may be named twice.
+ * Like a layer, a bank may be driven from one stream at a time (its workspace is used by every call, captured ones too), on its device. */
+typedef struct swapmoe_expert_bank swapmoe_expert_bank_t; /* opaque, owned by the library */
+typedef struct {
+  int32_t n_slots;          /* resident experts, 1 .. 256                                           */
+  int32_t d_model, d_ff;    /* multiples of 64, up to 32768                                         */
+  int32_t top_k;            /* choices of a token, 1 .. 16                                          */
+  int32_t dtype;            /* SWAPMOE_F32 or SWAPMOE_BF16: out                                     */
+  int32_t act;              /* SWAPMOE_ACT_RELU or SWAPMOE_ACT_SWIGLU                               */
+  int32_t max_tokens;       /* largest n_tokens of any forward; the workspace is sized for it       */
+} swapmoe_expert_bank_config_t;
+/* Allocates the bank's workspace on the CURRENT device.  *out is written only on success.  Errors: INVALID_ARG, UNSUPPORTED (sizes beyond
+ * the above; max_tokens * top_k of 2^24 and more), CUDA, NO_MEMORY. */
+int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_expert_bank_config_t* cfg);
+/* The caller must have synchronised the streams that used the bank.  NULL is accepted. */
+int32_t swapmoe_expert_bank_destroy(swapmoe_expert_bank_t* bank);
+/* w_in_dev [n_slots, nin, d_ff, d_model] int8 with in_scales_dev [n_slots, nin, d_ff], w_out_dev [n_slots, d_model, d_ff] int8 with
+ * out_scales_dev [n_slots, d_model] (nin = 2 for SwiGLU, else 1; matrices 16-byte aligned): device memory, not copied, so that an
+ * expert is swapped by writing its slot while no forward that uses it is in flight.  Takes effect for forwards enqueued after this call. */
+int32_t swapmoe_expert_bank_set_weights(swapmoe_expert_bank_t* bank, const void* w_in_dev, const float* in_scales_dev, const void* w_out_dev,
+                                        const float* out_scales_dev);
+/* One pass.  x_dev [n_tokens, d_model] int8 (rows at multiples of 16 bytes) with x_scales_dev [n_tokens]; slots_dev, weights_dev
+ * [n_tokens, top_k] int32, fp32; out_dev [n_tokens, d_model], rows of any stride.  The same call returns the same bits.  Errors:
+ * NOT_READY (no weights), TOO_MANY_TOKENS, INVALID_ARG (another device than the bank's among them), CUDA. */
+int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* bank, const void* x_dev, int64_t x_stride, const float* x_scales_dev,
+                                    const int32_t* slots_dev, const float* weights_dev, void* out_dev, int64_t out_stride,
+                                    int32_t n_tokens, void* stream);
+
 const char* swapmoe_status_string(int32_t status);
 
 #ifdef __cplusplus

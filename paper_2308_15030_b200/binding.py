@@ -42,6 +42,8 @@ EXPORTS = [
     "swapmoe_rms_norm", "swapmoe_route",
     "swapmoe_adapters_create", "swapmoe_adapters_destroy", "swapmoe_adapters_set_weights", "swapmoe_adapters_forward",
     "swapmoe_adapters_check", "swapmoe_set_gate", "swapmoe_set_norm", "swapmoe_forward_block",
+    "swapmoe_block_norm", "swapmoe_quantize_rows", "swapmoe_matmul_scaled", "swapmoe_matmul_status",
+    "swapmoe_expert_bank_create", "swapmoe_expert_bank_destroy", "swapmoe_expert_bank_set_weights", "swapmoe_expert_bank_forward",
 ]
 
 
@@ -68,6 +70,30 @@ class AdaptersConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_adapters", "d_in", "d_out", "rank", "dtype", "max_tokens")]
 
 
+class BlockNormArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "post_weight", "gate", "weight", "residual_out", "out", "out8", "scales")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "gate_stride", "residual_out_stride", "out_stride",
+                                              "out8_stride", "scales_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_rows", "d", "dtype", "residual_dtype", "type8", "group")] + \
+               [(n, ctypes.c_float) for n in ("eps", "post_eps", "scale")]
+
+
+class QuantizeRowsArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "out8", "scales")] + [(n, ctypes.c_int64) for n in ("x_stride", "out8_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_rows", "d", "dtype", "act")]
+
+
+class MatmulArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w", "x_scales", "w_scales", "bias", "out")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "w_stride", "out_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_tokens", "k", "n", "dtype")]
+
+
+class ExpertBankConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_slots", "d_model", "d_ff", "top_k", "dtype", "act", "max_tokens")]
+
+
+QUANTIZE_ACTS = {None: 0, "relu": 1, "swiglu": 2}
 SCORES = {"softmax": 0, "sigmoid": 1}
 
 
@@ -137,6 +163,14 @@ def lib() -> ctypes.CDLL:
         L.swapmoe_set_norm.argtypes = [vp, vp, ctypes.c_float]
         L.swapmoe_forward_block.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp]
         L.swapmoe_rms_norm.argtypes = [ctypes.POINTER(RmsNormArgs), vp]
+        L.swapmoe_block_norm.argtypes = [ctypes.POINTER(BlockNormArgs), vp]
+        L.swapmoe_quantize_rows.argtypes = [ctypes.POINTER(QuantizeRowsArgs), vp]
+        L.swapmoe_matmul_scaled.argtypes = [ctypes.POINTER(MatmulArgs), vp]
+        L.swapmoe_matmul_status.argtypes = [vp, vp]
+        L.swapmoe_expert_bank_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(ExpertBankConfig)]
+        L.swapmoe_expert_bank_destroy.argtypes = [vp]
+        L.swapmoe_expert_bank_set_weights.argtypes = [vp] * 5
+        L.swapmoe_expert_bank_forward.argtypes = [vp, vp, i64, vp, vp, vp, vp, i64, i32, vp]
         L.swapmoe_status_string.argtypes = [i32]
         L.swapmoe_status_string.restype = ctypes.c_char_p
         for n in EXPORTS:
@@ -238,8 +272,9 @@ def marshal():
         spec.loader.exec_module(m)
         L = lib()
         m.init(_fail, tuple(ctypes.cast(f, ctypes.c_void_p).value for f in
-                            (L.swapmoe_rms_norm, L.swapmoe_route, L.swapmoe_adapters_forward)),
-               (torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.int32),
+                            (L.swapmoe_rms_norm, L.swapmoe_route, L.swapmoe_adapters_forward, L.swapmoe_block_norm,
+                             L.swapmoe_quantize_rows, L.swapmoe_matmul_scaled, L.swapmoe_expert_bank_forward)),
+               (torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.int32, torch.int8),
                _device_functions())
         _marshal = m
     return _marshal
@@ -310,6 +345,97 @@ class AdapterBank:
         c = self.cfg
         (_marshal or marshal()).adapters_forward(self._h.value, self._device.index, self._dtype, c.d_in, c.d_out, x, ids, y, out,
                                                  x_scales, stream)
+
+
+def block_norm(x, residual, weight, eps: float, out=None, residual_out=None, post_weight=None, post_eps: Optional[float] = None,
+               gate=None, scale: float = 1.0, out8=None, scales=None, group: int = 0, stream=None) -> None:
+    """The norms behind and in front of a block in one pass: ``x`` [T, d], float32 or bfloat16, is a block's output.
+
+    p = x * post_weight / sqrt(mean(x^2) + post_eps) (x itself without ``post_weight``; ``post_eps`` None: ``eps``);
+    h = residual + scale * gate * p, ``gate`` [d] or [T, d]; residual_out = h; y = h * weight / sqrt(mean(h^2) + eps); out = y; and in
+    8 bits out8 = y / scales: torch.float8_e4m3fn (scales = max |y| / 448) or torch.int8 (max |y| / 127), per row (group = 0) or per
+    ``group`` columns (32, 64, 128 or 256).  ``residual`` may be float32 beside bfloat16 rows, or None; ``weight`` may be None where only
+    residual_out is wanted.  Rows may be strided; residual_out may be residual or x, out may be x.
+    """
+    (_marshal or marshal()).block_norm(x, residual, weight, eps, out, residual_out, post_weight, post_eps, gate, scale, out8, scales, group,
+                                       stream)
+
+
+def quantize_rows(x, out8, scales, act: Optional[str] = None, stream=None) -> None:
+    """Rows of ``x`` [T, d], float32 or bfloat16, to 8-bit integers ``out8`` [T, d] (torch.int8) with a scale each, ``scales`` [T]:
+    scales = max |y| / 127, out8 = round(y / scales).
+
+    y = x; with ``act`` "relu" y = max(x, 0); with "swiglu" y = silu(x[:, :d]) * x[:, d:] for ``x`` [T, 2 d].  Rows of x and out8
+    may be strided.  A weight matrix [N, K] becomes the operand of :func:`matmul_scaled` the same way.
+    """
+    code = QUANTIZE_ACTS.get(act)
+    if code is None:
+        raise _invalid("swapmoe_quantize_rows", "act %r, one of %s expected" % (act, list(QUANTIZE_ACTS)))
+    (_marshal or marshal()).quantize_rows(x, out8, scales, code, stream)
+
+
+def matmul_scaled(x8, x_scales, w8, w_scales, out, bias=None, stream=None) -> None:
+    """out[t, n] = x_scales[t] * w_scales[n] * sum_k x8[t, k] * w8[n, k] + bias[n], the sums exact.
+
+    ``x8`` [T, K] and ``w8`` [N, K] torch.int8, rows at multiples of 16 bytes; ``x_scales`` [T], ``w_scales`` [N] and ``bias`` [N]
+    (or None) float32; ``out`` [T, N] float32 or bfloat16, rows may be strided.
+    """
+    (_marshal or marshal()).matmul_scaled(x8, x_scales, w8, w_scales, out, bias, stream)
+
+
+def matmul_status(stream=None):
+    """(status, detail) of the 8-bit products on the current device since the last call: (0, 0), or what timed out."""
+    detail = ctypes.c_int32(0)
+    st = lib().swapmoe_matmul_status(ctypes.byref(detail), _stream_ptr(stream))
+    return int(st), int(detail.value)
+
+
+class ExpertBank:
+    """Experts in 8-bit integers behind a router (thin handle).
+
+    out[t] = sum_j weights[t, j] * E_slots[t, j](x[t]), E(x) = W_out act(W_in x); ``slots`` and ``weights`` as :func:`route` writes
+    them (a slot that is negative or not in the bank is left out).
+    """
+
+    def __init__(self, n_slots: int, d_model: int, d_ff: int, top_k: int, dtype: int, act: int = ACT_SWIGLU, max_tokens: int = 1):
+        self.cfg = ExpertBankConfig(n_slots, d_model, d_ff, top_k, dtype, act, max_tokens)
+        self._h = ctypes.c_void_p()
+        _check(lib().swapmoe_expert_bank_create(ctypes.byref(self._h), ctypes.byref(self.cfg)), "swapmoe_expert_bank_create")
+        import torch
+        self._dtype = torch.bfloat16 if dtype == BF16 else torch.float32
+        self._device = torch.device("cuda", torch.cuda.current_device())
+        self._keep = None
+
+    def close(self) -> None:
+        if self._h:
+            lib().swapmoe_expert_bank_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def set_weights(self, w_in, in_scales, w_out, out_scales) -> None:
+        """w_in [n_slots, nin, d_ff, d_model] torch.int8 (nin = 2 for SwiGLU, else 1) with in_scales [n_slots, nin, d_ff] float32, w_out
+        [n_slots, d_model, d_ff] with out_scales [n_slots, d_model]: CUDA tensors, not copied."""
+        import torch
+        c, where = self.cfg, "swapmoe_expert_bank_set_weights"
+        wide = c.n_slots * (2 if c.act == ACT_SWIGLU else 1) * c.d_ff
+        p = [_vector(w_in, wide * c.d_model, torch.int8, self._device, where, "w_in"),
+             _vector(in_scales, wide, torch.float32, self._device, where, "in_scales"),
+             _vector(w_out, c.n_slots * c.d_model * c.d_ff, torch.int8, self._device, where, "w_out"),
+             _vector(out_scales, c.n_slots * c.d_model, torch.float32, self._device, where, "out_scales")]
+        _check(lib().swapmoe_expert_bank_set_weights(self._h, *p), where)
+        self._keep = (w_in, in_scales, w_out, out_scales)
+
+    def forward(self, x8, x_scales, slots, weights, out, stream=None) -> None:
+        """x8 [T, d_model] torch.int8 (rows at multiples of 16 bytes) with x_scales [T] float32; slots [T, top_k] int32, weights
+        [T, top_k] float32; out [T, d_model] in the bank's dtype, rows may be strided."""
+        c = self.cfg
+        (_marshal or marshal()).experts_forward(self._h.value, self._device.index, self._dtype, c.d_model, c.top_k, x8, x_scales, slots,
+                                                weights, out, stream)
 
 
 class Layer:

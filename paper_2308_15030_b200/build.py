@@ -12,9 +12,9 @@ LIB = os.path.join(_HERE, "libswapmoe.so")
 MARSHAL_SRC = os.path.join(CSRC, "marshal.c")
 MARSHAL = os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 TRACE_LIB = os.path.join(_HERE, "libswapmoe_trace.so")
-SOURCES = ["api.cu", "route_static.cu", "block_ops.cu"]
+SOURCES = ["api.cu", "route_static.cu", "block_ops.cu", "int8_ops.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+              "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "--threads", "0",
               # beyond a certain size nvcc compresses the kernels' image by itself, and unpacking it costs a process's first
               # layer 6 ms (first swapmoe_create 19.7 ms packed, 14.2 not; 16 MB of file instead of 7)
               "--compress-mode=none"]

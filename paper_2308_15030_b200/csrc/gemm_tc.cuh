@@ -18,13 +18,10 @@
 #include "../../include/swapmoe.h"
 #include "common.cuh"
 #include "launch.cuh"
-#include "ptx.cuh"
+#include "tc_common.cuh"
 
 namespace swapmoe {
 
-constexpr int kTcBM = 128;   // rows per tile (TMEM lanes)
-constexpr int kTcBK = 64;    // bf16 elements per k-block = one 128-byte swizzle row
-constexpr int kTcUmmaK = 16;
 constexpr int kTcThreads = 256;
 constexpr int kTcSmemBudget = 200 * 1024;
 
@@ -52,16 +49,6 @@ struct TcGemmArgs {
   int32_t early_b;          // 1: the tile list is final when the CTAs start (see the kernel): weights are requested early
 };
 
-// Shared-memory operand descriptor: K-major tile whose rows are 128 bytes, written by
-// TMA with 128-byte swizzle; 8-row groups are 1024 bytes apart.
-__device__ __forceinline__ uint64_t make_kmajor_sw128_desc(uint32_t smem_addr) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);  // start address
-  d |= (uint64_t)(1024u >> 4) << 32;             // stride between 8-row groups
-  d |= (uint64_t)1 << 46;                        // descriptor version of this architecture
-  d |= (uint64_t)2 << 61;                        // 128-byte swizzle
-  return d;
-}
 // Instruction descriptor: bf16 x bf16 -> fp32, both operands K-major, M x N tile.
 __host__ __device__ constexpr uint32_t make_idesc_bf16(int M, int N) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -80,21 +67,6 @@ __global__ void bounded_wait_selftest_kernel(int32_t* status, int code, unsigned
   __syncthreads();
   if (threadIdx.x == 0) bounded_wait(&bar, 0u, &abort_flag, status, code, limit_ns);
   __syncthreads();
-}
-
-// Work item t -> (row tile, column tile).  Row tiles vary fastest inside a group of `group` row
-// tiles, column tiles next, groups last: the row tiles of a slot (which share weights) run side
-// by side, and for large problems the activations of one group stay in L2 while its column
-// tiles are walked (group >= n_row_tiles: one group).
-__device__ __forceinline__ void decode_tile(int t, int n_row_tiles, int n_col_tiles, int group, int* rt, int* ct) {
-  group = min(group, n_row_tiles);
-  const int per_group = group * n_col_tiles;
-  const int g = t / per_group;
-  const int r0 = g * group;
-  const int rows_here = min(group, n_row_tiles - r0);
-  const int u = t - g * per_group;
-  *ct = u / rows_here;
-  *rt = r0 + (u - *ct * rows_here);
 }
 
 // ----------------------------------------------------------------------------- epilogue stores
@@ -464,11 +436,6 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 }
 
 // ----------------------------------------------------------------------------- host side
-typedef CUresult (*PFN_encodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                    const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                    CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                    CUtensorMapFloatOOBfill);
-
 // Column-tile widths the kernels are built for.  Narrow tiles exist for small batches
 // (decode): with few row tiles, wide column tiles would leave most SMs without work.
 constexpr int kBn1Options[3] = {256, 128, 64};

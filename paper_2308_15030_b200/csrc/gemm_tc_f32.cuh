@@ -452,18 +452,6 @@ struct TcF32State {
   int only;                           // 0: both grouped GEMMs; 1 / 2: launch only GEMM-1 / GEMM-2 (measurement re-runs)
 };
 
-// The driver's tensor-map encoder (nullptr when it cannot be had).
-inline PFN_encodeTiled tc_get_encoder() {
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult qres;
-  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &qres) != cudaSuccess ||
-      qres != cudaDriverEntryPointSuccess) {
-    cudaGetLastError();
-    return nullptr;
-  }
-  return reinterpret_cast<PFN_encodeTiled>(fn);
-}
-
 // Which fp32 layers run here rather than on gemm_tf32x3_kernel.  Both leave about the same error, from different sources: two
 // bf16 pieces per operand drop 2^-17 of every product (6.3e-6 of the result whatever the widths), while the warp-level
 // kernel's products are good to 2^-20 but its tensor core truncates at each of the many small steps of its sums, which grows

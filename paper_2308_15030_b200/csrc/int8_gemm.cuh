@@ -1,0 +1,384 @@
+// Products of 8-bit integers on CTA pairs, with a scale for each token and each channel:
+//   C[t, n] = x_scales[t] * w_scales[n] * sum_k x8[t, k] * w8[n, k] (+ bias[n]).
+// The sums are exact (int32; |sum| <= 2^14 K, K < 2^17); an epilogue turns them to fp32, scales them and rounds the result once.
+//
+// Bound by the tensor cores for many tokens and by the weights' bytes for few.  As in the grouped GEMM of bf16 layers (gemm_tc_pair.cuh)
+// two SMs share a tile of 256 WEIGHT rows x up to 256 TOKENS through tcgen05 `cta_group::2`, here of kind::i8: a k-block is 128
+// columns, the same 128 bytes a row that 64 bf16 values take, for the same tensor clocks and twice the products.  Weights are the MMA's
+// rows, so tokens, whose number is ragged, are its columns, in steps of 32.  Roles in each CTA (384 threads): warp 0 = TMA
+// producer, warp 1 = MMA issuer (even CTA only), warp 2 = TMEM allocation, warps 4-11 = epilogue of the CTA's own 128 weight rows, which
+// overlaps the next tile's MMAs through two accumulators.  No load uses cluster multicast; every wait is bounded.
+#pragma once
+#include "launch.cuh"
+#include "pair_common.cuh"
+
+namespace swapmoe {
+
+constexpr int kI8BK = 128;                                    // columns of a k-block: one 128-byte swizzle row
+constexpr int kI8MaxK = (1 << 17) - 1;                        // 2^14 (2^17 - 1) < 2^31
+enum { kI8Bf16 = 0, kI8F32 = 1, kI8Relu = 2, kI8Swiglu = 3 };
+
+// A bounded wait of these kernels that gave up: flag and code of the wait, read by the host.
+static __device__ int32_t g_int8_status[2];
+
+struct I8GemmArgs {
+  void* C;                  // [rows, ldc]
+  const TileDesc* tiles;    // token tiles of the slots (nullptr: one matrix of T rows, tiles of `height` rows)
+  const int32_t* n_tiles;   // [0] their number, [1] what they hold at most
+  const float *x_scales, *w_scales, *bias;
+  long long ldc;
+  int32_t n_cols;           // columns of C
+  int32_t n_col_tiles;      // weight tiles per slot (256 rows; SwiGLU 128 of either matrix)
+  int32_t k_blocks;
+  int32_t w_rows;           // weight rows per slot
+  int32_t row_group;        // token tiles per scheduling group (see decode_tile)
+  int32_t T, height;        // height: multiple of 32, up to 256
+  int32_t direct;           // rows of C that the TMA unit cannot store: elements leave one by one
+};
+
+// Instruction descriptor: int8 x int8 -> int32, both operands K-major, M x N tile.
+__host__ __device__ constexpr uint32_t make_idesc_int8(int M, int N) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+namespace ptx {
+__device__ __forceinline__ void umma_int8_pair(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem_d),
+      "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+}  // namespace ptx
+
+// staging of an epilogue warp: a box of 32 tokens x 32 columns (SwiGLU 16)
+__host__ __device__ constexpr int int8_warp_bytes(int epi) { return epi == kI8F32 || epi == kI8Relu ? 4096 : 2048; }
+__host__ __device__ constexpr int int8_smem_bytes(int epi) { return kPairStageArea + 2048 + 8 * int8_warp_bytes(epi); }
+
+template <int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX128,
+                      const __grid_constant__ CUtensorMap tmX64, const __grid_constant__ CUtensorMap tmX32,
+                      const __grid_constant__ CUtensorMap tmX16, const __grid_constant__ CUtensorMap tmC,
+                      const __grid_constant__ I8GemmArgs a) {
+  constexpr bool kSwiglu = EPI == kI8Swiglu;
+  constexpr uint32_t kTmemCols = 2 * kPairTokens;             // two accumulator sets
+
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  unsigned char* sW = smem;                                   // [stages][128][128] int8
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kPairStageArea);
+  uint64_t* full = bars;                    // [stages]  used in the even CTA
+  uint64_t* empty = bars + kPairMaxStages;  // [stages]  one in each CTA (the commit reaches both)
+  uint64_t* acc_full = bars + 2 * kPairMaxStages;  // [2]  one in each CTA
+  uint64_t* acc_empty = acc_full + 2;       // [2]       used in the even CTA
+  uint64_t* tmem_ready = acc_empty + 2;     // used in the even CTA: the odd one has allocated its half
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tmem_ready + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int32_t* const status = g_int8_status;
+
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // warp-uniform
+  const uint32_t rank = ptx::cluster_ctarank();               // 0: issues the MMAs
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    ptx::mbar_init(tmem_ready, 1);
+    for (int s = 0; s < kPairMaxStages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
+    for (int b = 0; b < 2; ++b) { ptx::mbar_init(&acc_full[b], 1); ptx::mbar_init(&acc_empty[b], 16); }
+    *abort_flag = 0;
+    ptx::fence_barrier_init();
+    ptx::prefetch_tmap(&tmW);
+    ptx::prefetch_tmap(&tmX128);
+  }
+  // Operands and the list of tiles come from the kernels in front; tensor memory is taken only when those have let go of theirs, and
+  // the next kernel's CTAs are let in only when these have got it.
+  pdl_wait();
+  ptx::cluster_start_sync();                                  // both CTAs run and their barriers are initialised
+  uint32_t tmem_base = 0;
+  if (warp != 0 && warp != 3) {
+    if (warp == 2) {
+      ptx::tmem_alloc_pair(tmem_slot, kTmemCols);             // issued in both CTAs: one allocation for the pair
+      ptx::tmem_relinquish_pair();
+      if (rank == 1 && lane == 0) ptx::mbar_arrive_release_cluster(ptx::map_to_cta(ptx::smem_u32(tmem_ready), 0u));
+    }
+    ptx::tc_fence_before();
+    asm volatile("bar.sync 1, %0;" ::"n"(kPairThreads - 64) : "memory");
+    ptx::tc_fence_after();
+    tmem_base = *tmem_slot;
+    pdl_trigger();
+  }
+
+  // tokens of a tile in the MMA's columns; each CTA stages half of them
+  const bool listed = a.tiles != nullptr;
+  const int n_row_tiles = listed ? __ldcg(a.n_tiles) : (a.T + a.height - 1) / a.height;
+  const int max_tokens = listed ? __ldcg(a.n_tiles + 1) : a.height > 128 ? 256 : a.height > 64 ? 128 : 64;
+  auto tile_cols = [&](const TileDesc& td) { return listed ? (td.rows + kPairTokenStep - 1) & ~(kPairTokenStep - 1) : a.height; };
+  auto tile_at = [&](int rt) {
+    TileDesc td;
+    if (listed) {
+      const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.tiles + rt));
+      td.phys = raw.x; td.row0 = raw.y; td.rows = raw.z; td.slot = raw.w;
+    } else {
+      td.phys = td.slot = 0; td.row0 = rt * a.height; td.rows = min(a.height, a.T - td.row0);
+    }
+    return td;
+  };
+  const int total = n_row_tiles * a.n_col_tiles;
+  const int n_stages = pair_stages(max_tokens), x_bytes = max_tokens / 2 * kI8BK;
+  unsigned char* sX = smem + n_stages * kPairABytes;          // [stages][max_tokens / 2][128] int8
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer (both CTAs)
+    const uint32_t full0 = ptx::map_to_cta(ptx::smem_u32(full), 0u);
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int t = pair; t < total && ok; t += n_pairs) {
+      int rt, ct;
+      decode_tile(t, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct);
+      const TileDesc td = tile_at(rt);
+      const int cols = tile_cols(td), half = cols / 2;         // half: a multiple of 16, at most 128
+      const int xrow = td.row0 + (int)rank * half;
+      const uint32_t bytes = (uint32_t)(2 * kPairABytes + cols * kI8BK);
+      for (int kb = 0; kb < a.k_blocks; ++kb) {
+        ok = warp_wait<true>(&empty[stage], phase ^ 1u, abort_flag, status, 31);
+        if (!ok) break;
+        if (ptx::elect_one()) {
+          if (rank == 0) ptx::mbar_expect_tx(&full[stage], bytes);
+          const uint32_t bar = full0 + 8u * (uint32_t)stage;
+          unsigned char* dst = sX + stage * x_bytes;
+          if (kSwiglu)
+            ptx::tma_load_5d_pair(sW + stage * kPairABytes, &tmW, bar, kb * kI8BK, 0, 0, ct * 8 + (int)rank * 4, td.phys);
+          else
+            ptx::tma_load_2d_pair(sW + stage * kPairABytes, &tmW, bar, kb * kI8BK, td.phys * a.w_rows + ct * 2 * kTcBM + (int)rank * kTcBM);
+          if (half == 128) {
+            ptx::tma_load_2d_pair(dst, &tmX128, bar, kb * kI8BK, xrow);
+          } else {                                             // boxes of 64, 32 and 16 rows
+            if (half & 64) ptx::tma_load_2d_pair(dst, &tmX64, bar, kb * kI8BK, xrow);
+            if (half & 32) ptx::tma_load_2d_pair(dst + (half & 64) * 128, &tmX32, bar, kb * kI8BK, xrow + (half & 64));
+            if (half & 16) ptx::tma_load_2d_pair(dst + (half & 96) * 128, &tmX16, bar, kb * kI8BK, xrow + (half & 96));
+          }
+        }
+        __syncwarp();
+        if (++stage == n_stages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok) {
+      // Give copies that are still in flight time to land before shared memory is released.
+      const uint64_t t0 = ptx::globaltimer_ns();
+      while (ptx::globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      // ------------------------------------------------------------------ MMA issuer (even CTA, for the pair)
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = warp_wait<true>(tmem_ready, 0u, abort_flag, status, 35);
+      ptx::tc_fence_after();
+      for (int t = pair; t < total && ok; t += n_pairs) {
+        int rt, ct_unused;
+        decode_tile(t, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct_unused);
+        const uint32_t idesc = make_idesc_int8(2 * kTcBM, tile_cols(tile_at(rt)));
+        ok = warp_wait<true>(&acc_empty[acc], acc_phase ^ 1u, abort_flag, status, 32);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        const uint32_t tmem_d = tmem_base + (uint32_t)(acc * kPairTokens);
+        for (int kb = 0; kb < a.k_blocks; ++kb) {
+          ok = warp_wait<true>(&full[stage], phase, abort_flag, status, 33);
+          if (!ok) break;
+          ptx::tc_fence_after();
+          const uint64_t dw = make_kmajor_sw128_desc(ptx::smem_u32(sW + stage * kPairABytes));
+          const uint64_t dx = make_kmajor_sw128_desc(ptx::smem_u32(sX + stage * x_bytes));
+          if (ptx::elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)                        // 32 columns each
+              ptx::umma_int8_pair(tmem_d, dw + (uint64_t)(2 * k), dx + (uint64_t)(2 * k), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+            ptx::umma_commit_pair(&empty[stage]);   // frees the stage in both CTAs once these MMAs have read it
+            if (kb + 1 == a.k_blocks) ptx::umma_commit_pair(&acc_full[acc]);    // accumulator complete, in both CTAs
+          }
+          __syncwarp();
+          if (++stage == n_stages) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      }
+    }
+  } else if (warp >= 4) {
+    // -------------------------------------------------------------------- epilogue (own 128 weight rows)
+    const int q = warp & 3;                    // TMEM lane quarter this warp may read
+    const int part = (warp - 4) >> 2;          // two warps per quarter take turns with the chunks of 32 tokens
+    const int odd = lane & 1, hi = lane >> 4;
+    unsigned char* stg = smem + kPairStageArea + 1024 + (warp - 4) * int8_warp_bytes(EPI);
+    const uint32_t acc_empty0 = ptx::map_to_cta(ptx::smem_u32(acc_empty), 0u);
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;
+    for (int t = pair; t < total && ok; t += n_pairs) {
+      int rt, ct;
+      decode_tile(t, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct);
+      const TileDesc td = tile_at(rt);
+      // first of this warp's output columns (32; SwiGLU 16), and this lane's weight row
+      const int col0 = kSwiglu ? (ct * 8 + (int)rank * 4 + q) * 16 : ct * 2 * kTcBM + (int)rank * kTcBM + q * 32;
+      const int col = kSwiglu ? col0 + (lane & 15) : col0 + lane;
+      const bool col_ok = col0 < a.n_cols;
+      const int last = (td.rows - 1) >> 5;                   // the tile's last chunk
+      const int my_last = last - ((last ^ part) & 1);        // this warp's last one (-1: none)
+      // scales come while the tile's MMAs run, those of the tokens a chunk ahead
+      auto token_scale = [&](int c) {
+        const int token = 32 * c + lane;
+        return token < td.rows ? a.x_scales[td.row0 + token] : 0.f;
+      };
+      float w_scale = 0.f, bias = 0.f, next = token_scale(part);
+      if (col < a.n_cols) {
+        w_scale = kSwiglu ? a.w_scales[((size_t)td.phys * 2 + hi) * a.n_cols + col] : a.w_scales[(size_t)td.phys * a.w_rows + col];
+        if (!kSwiglu && a.bias != nullptr) bias = a.bias[col];
+      }
+      ok = warp_wait<true>(&acc_full[acc], acc_phase, abort_flag, status, 34);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * kPairTokens);
+      if (my_last < 0 && lane == 0) ptx::mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)acc);
+#pragma unroll 1
+      for (int c = part; c <= last; c += 2) {
+        const int t0 = 32 * c, left = td.rows - t0;          // valid tokens of this chunk (may exceed 32)
+        const float x_scale = next;
+        next = token_scale(c + 2);
+        uint32_t v[32];
+        __syncwarp();                                        // the tensor-memory load is one of the whole warp
+        ptx::tmem_ld32(taddr + (uint32_t)t0, v);
+        ptx::tmem_ld_wait();
+        if (c == my_last) {
+          // last read of this accumulator: one arrival per warp on the even CTA's barrier, 16 hand it back to the MMA issuer
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)acc);
+        }
+        if (!col_ok) continue;
+        float f[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          f[j] = (float)(int)v[j] * w_scale * __shfl_sync(0xffffffffu, x_scale, j);
+        if (kSwiglu) {
+          // lanes l and l + 16 hold the two products of hidden unit l & 15: the lower one finishes token 2 i, the upper one token 2 i + 1
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float v0 = f[2 * i], v1 = f[2 * i + 1];
+            const float r = __shfl_xor_sync(0xffffffffu, hi ? v0 : v1, 16);
+            const float x1 = hi ? r : v0, x3 = hi ? v1 : r;
+            f[i] = silu_from_exp(x1, __expf(-x1)) * x3;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            f[j] += bias;
+            if (EPI == kI8Relu) f[j] = f[j] < 0.f ? 0.f : f[j];                              // NaN stays NaN
+          }
+        }
+        if (a.direct) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (!kSwiglu && j < left && col < a.n_cols) {
+              const size_t at = (size_t)(td.row0 + t0 + j) * a.ldc + col;
+              if (EPI == kI8Bf16) static_cast<bf16*>(a.C)[at] = __float2bfloat16_rn(f[j]);
+              else static_cast<float*>(a.C)[at] = f[j];
+            }
+          continue;
+        }
+        // Boxes of 32 tokens leave through the TMA unit.  Rows of a listed tile up to the next multiple of 32 are stored with the valid
+        // ones: they lie in the slot's own segment, and nobody reads a row that no pair occupies.
+        if (lane == 0) ptx::tma_store_wait_read();
+        __syncwarp();
+        if (kSwiglu) {
+          float* w = reinterpret_cast<float*>(stg) + hi * 16 + (lane & 15);    // [32 tokens][16 units]
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[32 * i] = f[i];
+        } else if (EPI == kI8Bf16) {
+          // neighbouring lanes trade, so that each holds two output columns of one token
+          uint32_t* w = reinterpret_cast<uint32_t*>(stg) + odd * 16 + (lane >> 1);      // [32 tokens][32 columns]
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float r = __shfl_xor_sync(0xffffffffu, odd ? f[2 * i] : f[2 * i + 1], 1);
+            w[32 * i] = odd ? pack_bf16x2(r, f[2 * i + 1]) : pack_bf16x2(f[2 * i], r);
+          }
+        } else {
+          float* w = reinterpret_cast<float*>(stg) + lane;     // [32 tokens][32 columns]
+#pragma unroll
+          for (int j = 0; j < 32; ++j) w[32 * j] = f[j];
+        }
+        ptx::fence_proxy_async();                              // the staged box is read by the TMA unit
+        __syncwarp();
+        if (lane == 0) ptx::tma_store_2d(&tmC, stg, col0, td.row0 + t0);
+      }
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+    }
+    if (!a.direct && lane == 0) ptx::tma_store_wait_all();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync_all();       // neither CTA's shared memory, barriers or TMEM go away while the peer may touch them
+  if (warp == 2) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+  }
+}
+
+// ----------------------------------------------------------------------------- host side
+typedef void (*I8GemmKernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap,
+                             const CUtensorMap, const I8GemmArgs);
+
+inline I8GemmKernel int8_gemm_kernel(int epi) {
+  return epi == kI8Bf16 ? int8_gemm_pair_kernel<kI8Bf16> : epi == kI8F32 ? int8_gemm_pair_kernel<kI8F32>
+         : epi == kI8Relu ? int8_gemm_pair_kernel<kI8Relu> : int8_gemm_pair_kernel<kI8Swiglu>;
+}
+
+// View of a row-major matrix [rows, cols] with a box of box_cols x box_rows elements (type: unsigned bytes, bf16 or fp32).
+inline bool int8_encode_2d(PFN_encodeTiled enc, CUtensorMap* m, const void* base, CUtensorMapDataType type, uint64_t elem, uint64_t rows,
+                           uint64_t cols, uint64_t stride, uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {stride * elem};
+  const cuuint32_t box[2] = {box_cols, box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return enc(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+inline bool int8_encode_operand(PFN_encodeTiled enc, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t stride,
+                                uint32_t box_rows) {
+  return int8_encode_2d(enc, m, base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, cols, stride, kI8BK, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// Once per device and process: shared memory limits of the kernels; 0 or the number of CTA pairs that run at once.
+inline int int8_gemm_init(int sm_count) {
+  for (int epi = 0; epi < 4; ++epi)
+    if (cudaFuncSetAttribute(int8_gemm_kernel(epi), cudaFuncAttributeMaxDynamicSharedMemorySize, int8_smem_bytes(epi)) != cudaSuccess) {
+      cudaGetLastError();
+      return 0;
+    }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (sm_count / 2)); cfg.blockDim = dim3(kPairThreads); cfg.dynamicSmemBytes = int8_smem_bytes(kI8F32);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, int8_gemm_pair_kernel<kI8F32>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  return n < sm_count / 2 ? n : sm_count / 2;
+}
+
+// Rows of a token tile for T rows and n_col_tiles weight tiles on n_pairs pairs of CTAs: the height whose rounds of tiles cost least.  A
+// tile's k-block takes the longer of its tensor clocks (2 per token) and its loads (32 KB of weights per pair weigh like 112 tokens).
+inline int int8_tile_height(int T, int n_col_tiles, int n_pairs) {
+  int best = 256;
+  long long least = -1;
+  for (int h = 256; h >= 32; h -= 32) {
+    const long long tiles = (long long)((T + h - 1) / h) * n_col_tiles;
+    const long long cost = (tiles + n_pairs - 1) / n_pairs * (h > 112 ? h : 112);
+    if (least < 0 || cost < least) { least = cost; best = h; }
+  }
+  return best;
+}
+
+}  // namespace swapmoe

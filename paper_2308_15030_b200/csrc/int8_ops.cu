@@ -1,0 +1,409 @@
+// C ABI of the operators in 8-bit integers and of the norms around a block (see include/swapmoe.h): argument checks and launches.
+#include "../../include/swapmoe.h"
+
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <initializer_list>
+#include <mutex>
+#include <new>
+
+#include "block_norm.cuh"
+#include "block_ops.cuh"
+#include "common.cuh"
+#include "expert_bank.cuh"
+#include "int8_gemm.cuh"
+#include "quantize_rows.cuh"
+
+using namespace swapmoe;
+
+static_assert(SWAPMOE_NORM_MAX_WIDTH == kNormMaxWidth && SWAPMOE_QUANTIZE_MAX_WIDTH == kQuantMaxWidth, "the header's limits");
+static_assert(SWAPMOE_QUANTIZE_NONE == kQuantNone && SWAPMOE_QUANTIZE_RELU == kQuantRelu && SWAPMOE_QUANTIZE_SWIGLU == kQuantSwiglu, "the header's values");
+static_assert(SWAPMOE_MATMUL_MAX_K == kI8MaxK, "the header's limit");
+
+namespace {
+
+struct Device {
+  int id, sms, pairs;                     // SMs; CTA pairs that run at once
+};
+
+// The current device, its kernels' limits set once.
+int32_t current_device(Device* d) {
+  constexpr int kMany = 64;
+  static std::mutex lock;
+  static Device known[kMany];
+  static std::atomic<bool> ready[kMany];
+  int dev = 0, major = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    cudaGetLastError();
+    return SWAPMOE_ERR_CUDA;
+  }
+  if (dev < kMany && ready[dev].load(std::memory_order_acquire)) {
+    *d = known[dev];
+    return SWAPMOE_OK;
+  }
+  if (dev >= kMany || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return SWAPMOE_ERR_CUDA;
+  }
+  if (major != 10) return SWAPMOE_ERR_UNSUPPORTED;       // kernels are built for sm_100a only
+  std::lock_guard<std::mutex> hold(lock);
+  const int pairs = int8_gemm_init(sms);
+  if (pairs < 1) return SWAPMOE_ERR_CUDA;
+  known[dev] = Device{dev, sms, pairs};
+  ready[dev].store(true, std::memory_order_release);
+  *d = known[dev];
+  return SWAPMOE_OK;
+}
+
+PFN_encodeTiled encoder() {
+  static const PFN_encodeTiled enc = tc_get_encoder();
+  return enc;
+}
+
+int32_t launched(cudaError_t e, int kernels = 0, int64_t* launches = nullptr) {
+  if (e == cudaSuccess) e = cudaGetLastError();
+  else cudaGetLastError();
+  if (e == cudaSuccess && launches) *launches += kernels;
+  return e == cudaSuccess ? SWAPMOE_OK : SWAPMOE_ERR_CUDA;
+}
+
+// The choice of dependent launches where no layer has made one: that of the process, read once.
+bool standalone_pdl() {
+  static const bool pdl = dependent_launch();
+  return pdl;
+}
+
+bool misaligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+// Whether n rows of `elem`-byte values at p, `stride` values apart, all start on multiples of `bytes`.
+bool rows_aligned(const void* p, long long n, long long stride, size_t elem, size_t bytes) {
+  return !misaligned(p, bytes) && (n < 2 || (size_t)stride * elem % bytes == 0);
+}
+
+}  // namespace
+
+namespace swapmoe {
+
+int32_t block_norm_run(const swapmoe_block_norm_t* p, void* stream, bool pdl, int64_t* launches) {
+  if (!p || p->n_rows < 0 || p->d < 1) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->dtype != SWAPMOE_F32 && p->dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->residual_dtype != p->dtype && p->residual_dtype != SWAPMOE_F32) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->type8 != SWAPMOE_E4M3 && p->type8 != SWAPMOE_INT8) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->group != 0 && p->group != 32 && p->group != 64 && p->group != 128 && p->group != 256) return SWAPMOE_ERR_INVALID_ARG;
+  if (!(p->eps >= 0.f) || std::isinf(p->eps) || !(p->post_eps >= 0.f) || std::isinf(p->post_eps) || !std::isfinite(p->scale))
+    return SWAPMOE_ERR_INVALID_ARG;
+  if (p->d > kNormMaxWidth) return SWAPMOE_ERR_UNSUPPORTED;
+  if (p->n_rows == 0) return SWAPMOE_OK;
+  if (!p->x || (!p->out && !p->out8 && !p->residual_out) || ((p->out || p->out8) && !p->weight) || (p->out8 == nullptr) != (p->scales == nullptr))
+    return SWAPMOE_ERR_INVALID_ARG;
+  const size_t elem = p->dtype == SWAPMOE_BF16 ? 2 : 4, relem = p->residual_dtype == SWAPMOE_BF16 ? 2 : 4;
+  const long long d = p->d, n_scales = p->group ? (d + p->group - 1) / p->group : 1;
+  const int32_t n = p->n_rows;
+  struct { const void* p; int32_t n; long long stride, width; size_t elem, vec; } rows[] = {
+      {p->x, n, p->x_stride, d, elem, 16},
+      {p->residual, n, p->residual_stride, d, relem, 16},
+      {p->gate, p->gate_stride ? n : 1, p->gate_stride ? p->gate_stride : d, d, elem, 16},
+      {p->residual_out, n, p->residual_out_stride, d, relem, 16},
+      {p->out, n, p->out_stride, d, elem, 16},
+      {p->out8, n, p->out8_stride, d, 1, 8},
+      {p->scales, n, p->scales_stride, n_scales, 4, 4},
+      {p->weight, 1, d, d, elem, 16},
+      {p->post_weight, 1, d, d, elem, 16}};
+  bool vec = d % 8 == 0;
+  for (const auto& r : rows) {
+    if (!r.p) continue;
+    if (r.stride < r.width || misaligned(r.p, r.elem)) return SWAPMOE_ERR_INVALID_ARG;
+    vec = vec && rows_aligned(r.p, r.n, r.stride, r.elem, r.vec);
+  }
+  BlockNormArgs a;
+  a.x = p->x; a.residual = p->residual; a.post_weight = p->post_weight; a.gate = p->gate; a.weight = p->weight;
+  a.residual_out = p->residual_out; a.out = p->out; a.out8 = static_cast<uint8_t*>(p->out8); a.scales = p->scales;
+  a.x_stride = p->x_stride; a.residual_stride = p->residual_stride; a.gate_stride = p->gate_stride;
+  a.residual_out_stride = p->residual_out_stride; a.out_stride = p->out_stride; a.out8_stride = p->out8_stride;
+  a.scales_stride = p->scales_stride;
+  a.T = p->n_rows; a.d = p->d; a.group = p->group; a.int8 = p->type8 == SWAPMOE_INT8;
+  a.eps = p->eps; a.post_eps = p->post_eps; a.scale = p->scale;
+  a.warps_per_row = a.rows_per_cta = 1;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Device dev;
+  const int32_t rc = current_device(&dev);
+  if (rc != SWAPMOE_OK) return rc;
+  if (p->dtype == SWAPMOE_F32) return launched(block_norm_launch_typed<float, float>(a, vec, dev.sms, st, pdl), 1, launches);
+  if (p->residual_dtype == SWAPMOE_F32) return launched(block_norm_launch_typed<bf16, float>(a, vec, dev.sms, st, pdl), 1, launches);
+  return launched(block_norm_launch_typed<bf16, bf16>(a, vec, dev.sms, st, pdl), 1, launches);
+}
+
+}  // namespace swapmoe
+
+struct swapmoe_expert_bank {
+  swapmoe_expert_bank_config_t cfg;
+  Device dev;
+  char* ws;
+  long long max_rows;                      // rows of the pairs with the slots' padding
+  int8_t *rows8, *h8;
+  float *row_scales, *h, *h_scales, *y;
+  int32_t *row_pair, *pair_row, *counts, *cta_base, *n_tiles;
+  TileDesc* tiles;
+  const float *in_scales, *out_scales;
+  bool bound;
+  CUtensorMap map_in, map_out, map_x[4], map_h[4], map_h_out, map_y_out;
+};
+
+namespace {
+
+// A product of a whole matrix (matmul_scaled).
+int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t st, bool pdl) {
+  const PFN_encodeTiled enc = encoder();
+  if (!enc) return SWAPMOE_ERR_CUDA;
+  I8GemmArgs g = {};
+  g.C = p.out; g.x_scales = p.x_scales; g.w_scales = p.w_scales; g.bias = p.bias;
+  g.ldc = p.out_stride; g.n_cols = p.n; g.n_col_tiles = (p.n + 255) / 256; g.k_blocks = (p.k + kI8BK - 1) / kI8BK; g.w_rows = p.n;
+  g.T = p.n_tokens;
+  g.height = int8_tile_height(p.n_tokens, g.n_col_tiles, dev.pairs);
+  g.row_group = 1 << 30;
+  // Token rows of a group stay in L2 across its weight tiles: 20 MB of them (as in tc_gemm_pair)
+  if ((long long)p.n_tokens * p.k > (24ll << 20)) {
+    g.row_group = (int)((20ll << 20) / ((long long)g.height * p.k));
+    if (g.row_group < 4) g.row_group = 4;
+  }
+  const size_t elem = p.dtype == SWAPMOE_BF16 ? 2 : 4;
+  g.direct = !rows_aligned(p.out, 2, p.out_stride, elem, 16);
+  const long long xs = p.n_tokens > 1 ? p.x_stride : (p.k + 15) / 16 * 16, ws = p.n > 1 ? p.w_stride : (p.k + 15) / 16 * 16;
+  CUtensorMap mw, mx[4], mc;
+  if (!int8_encode_operand(enc, &mw, p.w, p.n, p.k, ws, 128)) return SWAPMOE_ERR_CUDA;
+  const int half = g.height / 2;
+  int have = -1;
+  for (int i = 0; i < 4; ++i)
+    if (half & (128 >> i)) {
+      if (!int8_encode_operand(enc, &mx[i], p.x, p.n_tokens, p.k, xs, 128 >> i)) return SWAPMOE_ERR_CUDA;
+      have = i;
+    }
+  for (int i = 0; i < 4; ++i)
+    if (!(half & (128 >> i))) mx[i] = mx[have];              // not used
+  if (g.direct) mc = mw;                                     // not used
+  else if (!int8_encode_2d(enc, &mc, p.out, p.dtype == SWAPMOE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, elem,
+                           p.n_tokens, p.n, p.out_stride, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE))
+    return SWAPMOE_ERR_CUDA;
+  const int epi = p.dtype == SWAPMOE_BF16 ? kI8Bf16 : kI8F32;
+  const long long work = (long long)((p.n_tokens + g.height - 1) / g.height) * g.n_col_tiles;
+  return launched(launch_kernel(int8_gemm_kernel(epi), dim3(2 * (work > dev.pairs ? dev.pairs : (int)work)), dim3(kPairThreads),
+                                int8_smem_bytes(epi), st, pdl, mw, mx[0], mx[1], mx[2], mx[3], mc, g));
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t swapmoe_block_norm(const swapmoe_block_norm_t* p, void* stream) { return block_norm_run(p, stream, standalone_pdl(), nullptr); }
+
+int32_t swapmoe_quantize_rows(const swapmoe_quantize_rows_t* p, void* stream) {
+  if (!p || p->n_rows < 0 || p->d < 1) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->dtype != SWAPMOE_F32 && p->dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->act != kQuantNone && p->act != kQuantRelu && p->act != kQuantSwiglu) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->d > kQuantMaxWidth) return SWAPMOE_ERR_UNSUPPORTED;
+  if (p->n_rows == 0) return SWAPMOE_OK;
+  const size_t elem = p->dtype == SWAPMOE_BF16 ? 2 : 4;
+  const long long width = p->act == kQuantSwiglu ? 2ll * p->d : p->d;
+  if (!p->x || !p->out8 || !p->scales || p->x_stride < width || p->out8_stride < p->d || misaligned(p->x, elem) || misaligned(p->scales, 4))
+    return SWAPMOE_ERR_INVALID_ARG;
+  QuantizeArgs a = {};
+  a.x = p->x; a.out8 = static_cast<uint8_t*>(p->out8); a.scales = p->scales; a.x_stride = p->x_stride; a.out8_stride = p->out8_stride;
+  a.T = p->n_rows; a.d = p->d; a.act = p->act;
+  const bool vec = p->d % 8 == 0 && rows_aligned(p->x, p->n_rows, p->x_stride, elem, 16) && rows_aligned(p->out8, p->n_rows, p->out8_stride, 1, 8);
+  Device dev;
+  const int32_t rc = current_device(&dev);
+  if (rc != SWAPMOE_OK) return rc;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return launched(p->dtype == SWAPMOE_F32 ? quantize_rows_launch<float>(a, vec, dev.sms, st, standalone_pdl())
+                                          : quantize_rows_launch<bf16>(a, vec, dev.sms, st, standalone_pdl()));
+}
+
+int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* p, void* stream) {
+  if (!p || p->n_tokens < 0 || p->k < 1 || p->n < 1) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->dtype != SWAPMOE_F32 && p->dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
+  if (p->k > kI8MaxK) return SWAPMOE_ERR_UNSUPPORTED;
+  if (p->n_tokens == 0) return SWAPMOE_OK;
+  const size_t elem = p->dtype == SWAPMOE_BF16 ? 2 : 4;
+  if (!p->x || !p->x_scales || !p->w || !p->w_scales || !p->out || p->x_stride < p->k || p->w_stride < p->k || p->out_stride < p->n)
+    return SWAPMOE_ERR_INVALID_ARG;
+  if (!rows_aligned(p->x, p->n_tokens, p->x_stride, 1, 16) || !rows_aligned(p->w, p->n, p->w_stride, 1, 16) || misaligned(p->out, elem) ||
+      misaligned(p->x_scales, 4) || misaligned(p->w_scales, 4) || misaligned(p->bias, 4))
+    return SWAPMOE_ERR_INVALID_ARG;
+  Device dev;
+  const int32_t rc = current_device(&dev);
+  if (rc != SWAPMOE_OK) return rc;
+  return matmul_pair(*p, dev, static_cast<cudaStream_t>(stream), standalone_pdl());
+}
+
+int32_t swapmoe_matmul_status(int32_t* detail, void* stream) {
+  int32_t s[2] = {0, 0};
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  static const int32_t zero[2] = {0, 0};
+  if (cudaMemcpyFromSymbolAsync(s, g_int8_status, sizeof(s), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess ||
+      (s[0] != 0 && cudaMemcpyToSymbolAsync(g_int8_status, zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st) != cudaSuccess)) {
+    cudaGetLastError();
+    return SWAPMOE_ERR_CUDA;
+  }
+  if (detail) *detail = s[1];
+  return s[0] ? SWAPMOE_ERR_DEVICE_TIMEOUT : SWAPMOE_OK;
+}
+
+int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_expert_bank_config_t* cfg) {
+  if (!out || !cfg) return SWAPMOE_ERR_INVALID_ARG;
+  const swapmoe_expert_bank_config_t c = *cfg;
+  if (c.n_slots < 1 || c.d_model < 1 || c.d_ff < 1 || c.top_k < 1 || c.max_tokens < 1) return SWAPMOE_ERR_INVALID_ARG;
+  if (c.dtype != SWAPMOE_F32 && c.dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
+  if (c.act != SWAPMOE_ACT_RELU && c.act != SWAPMOE_ACT_SWIGLU) return SWAPMOE_ERR_INVALID_ARG;
+  const int nin = c.act == SWAPMOE_ACT_SWIGLU ? 2 : 1;
+  if (c.n_slots > kBankMaxSlots || c.top_k > 16 || c.d_model % 64 || c.d_ff % 64 || c.d_model > kQuantMaxWidth || c.d_ff > kQuantMaxWidth ||
+      (long long)c.max_tokens * c.top_k >= 1 << 24 || (long long)c.n_slots * nin * c.d_ff >= 1ll << 31 || (long long)c.n_slots * c.d_model >= 1ll << 31)
+    return SWAPMOE_ERR_UNSUPPORTED;
+  Device dev;
+  const int32_t rc = current_device(&dev);
+  if (rc != SWAPMOE_OK) return rc;
+  const PFN_encodeTiled enc = encoder();
+  if (!enc) return SWAPMOE_ERR_CUDA;
+  swapmoe_expert_bank* b = new (std::nothrow) swapmoe_expert_bank();
+  if (!b) return SWAPMOE_ERR_NO_MEMORY;
+  b->cfg = c;
+  b->dev = dev;
+  const long long P = (long long)c.max_tokens * c.top_k, d = c.d_model, f = c.d_ff;
+  b->max_rows = (P + 31ll * (c.n_slots < P ? c.n_slots : P) + 31) / 32 * 32;
+  const size_t R = (size_t)b->max_rows;
+  // a slot's tiles: at most one for every 32 rows, 64 rows or more in each but the last
+  const size_t n_tiles = R / 32 + 32;
+  struct { void** p; size_t bytes; } parts[] = {
+      {reinterpret_cast<void**>(&b->rows8), R * d}, {reinterpret_cast<void**>(&b->h8), R * f},
+      {reinterpret_cast<void**>(&b->h), R * f * 4}, {reinterpret_cast<void**>(&b->y), R * d * 4},
+      {reinterpret_cast<void**>(&b->row_scales), R * 4}, {reinterpret_cast<void**>(&b->h_scales), R * 4},
+      {reinterpret_cast<void**>(&b->row_pair), R * 4}, {reinterpret_cast<void**>(&b->pair_row), (size_t)P * 4},
+      {reinterpret_cast<void**>(&b->counts), kBankMaxSlots * 4}, {reinterpret_cast<void**>(&b->cta_base), (size_t)kBankMaxCtas * c.n_slots * 4},
+      {reinterpret_cast<void**>(&b->n_tiles), 16}, {reinterpret_cast<void**>(&b->tiles), n_tiles * sizeof(TileDesc)}};
+  size_t bytes = 0;
+  for (auto& q : parts) bytes += (q.bytes + 255) / 256 * 256;
+  if (cudaMalloc(&b->ws, bytes) != cudaSuccess) {
+    cudaGetLastError();
+    delete b;
+    return SWAPMOE_ERR_NO_MEMORY;
+  }
+  char* at = b->ws;
+  for (auto& q : parts) {
+    *q.p = at;
+    at += (q.bytes + 255) / 256 * 256;
+  }
+  bool ok = cudaMemset(b->counts, 0, kBankMaxSlots * 4) == cudaSuccess;
+  for (int i = 0; i < 4; ++i)
+    ok = ok && int8_encode_operand(enc, &b->map_x[i], b->rows8, R, d, d, 128 >> i) && int8_encode_operand(enc, &b->map_h[i], b->h8, R, f, f, 128 >> i);
+  ok = ok && int8_encode_2d(enc, &b->map_h_out, b->h, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, f, f, nin == 2 ? 16 : 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE) &&
+       int8_encode_2d(enc, &b->map_y_out, b->y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, d, d, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
+  if (!ok) {
+    cudaGetLastError();
+    swapmoe_expert_bank_destroy(b);
+    return SWAPMOE_ERR_CUDA;
+  }
+  *out = b;
+  return SWAPMOE_OK;
+}
+
+int32_t swapmoe_expert_bank_destroy(swapmoe_expert_bank_t* b) {
+  if (!b) return SWAPMOE_OK;
+  cudaFree(b->ws);
+  delete b;
+  return SWAPMOE_OK;
+}
+
+int32_t swapmoe_expert_bank_set_weights(swapmoe_expert_bank_t* b, const void* w_in, const float* in_scales, const void* w_out,
+                                        const float* out_scales) {
+  if (!b || !w_in || !in_scales || !w_out || !out_scales || misaligned(w_in, 16) || misaligned(w_out, 16) || misaligned(in_scales, 4) ||
+      misaligned(out_scales, 4))
+    return SWAPMOE_ERR_INVALID_ARG;
+  const swapmoe_expert_bank_config_t& c = b->cfg;
+  const PFN_encodeTiled enc = encoder();
+  const cuuint64_t d = (cuuint64_t)c.d_model, f = (cuuint64_t)c.d_ff, S = (cuuint64_t)c.n_slots;
+  CUtensorMap in, outm;
+  if (c.act == SWAPMOE_ACT_SWIGLU) {
+    // sixteen rows of the first matrix, the same sixteen of the second, the next sixteen of the first ...
+    const cuuint64_t dims[5] = {d, 16, 2, f / 16, S};
+    const cuuint64_t strides[4] = {d, f * d, 16 * d, 2 * f * d};
+    const cuuint32_t box[5] = {(cuuint32_t)kI8BK, 16, 2, 4, 1};
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    if (enc(&in, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<void*>(w_in), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return SWAPMOE_ERR_CUDA;
+  } else if (!int8_encode_operand(enc, &in, w_in, S * f, d, d, 128)) {
+    return SWAPMOE_ERR_CUDA;
+  }
+  if (!int8_encode_operand(enc, &outm, w_out, S * d, f, f, 128)) return SWAPMOE_ERR_CUDA;
+  b->map_in = in; b->map_out = outm; b->in_scales = in_scales; b->out_scales = out_scales;
+  b->bound = true;
+  return SWAPMOE_OK;
+}
+
+int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int64_t x_stride, const float* x_scales, const int32_t* slots,
+                                    const float* weights, void* out, int64_t out_stride, int32_t T, void* stream) {
+  if (!b || T < 0) return SWAPMOE_ERR_INVALID_ARG;
+  if (T == 0) return SWAPMOE_OK;
+  const swapmoe_expert_bank_config_t& c = b->cfg;
+  if (!x || !x_scales || !slots || !weights || !out || x_stride < c.d_model || out_stride < c.d_model) return SWAPMOE_ERR_INVALID_ARG;
+  const size_t elem = c.dtype == SWAPMOE_BF16 ? 2 : 4;
+  if (!rows_aligned(x, T, x_stride, 1, 16) || misaligned(out, elem) || misaligned(x_scales, 4) || misaligned(slots, 4) || misaligned(weights, 4))
+    return SWAPMOE_ERR_INVALID_ARG;
+  if (!b->bound) return SWAPMOE_ERR_NOT_READY;
+  if (T > c.max_tokens) return SWAPMOE_ERR_TOO_MANY_TOKENS;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev != b->dev.id) {
+    cudaGetLastError();
+    return SWAPMOE_ERR_INVALID_ARG;
+  }
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool pdl = standalone_pdl(), swiglu = c.act == SWAPMOE_ACT_SWIGLU;
+  const int P = T * c.top_k, pairs = b->dev.pairs;
+  BankArgs a;
+  a.x8 = static_cast<const int8_t*>(x); a.x_scales = x_scales; a.slots = slots; a.weights = weights; a.rows8 = b->rows8; a.row_scales = b->row_scales;
+  a.row_pair = b->row_pair; a.pair_row = b->pair_row; a.counts = b->counts; a.cta_base = b->cta_base; a.tiles = b->tiles; a.n_tiles = b->n_tiles;
+  a.x_stride = x_stride; a.P = P; a.S = c.n_slots; a.k = c.top_k; a.d = c.d_model;
+  a.direct = P <= kBankDirectPairs;
+  // eight pairs a CTA (one per warp) where that makes no more CTAs than run at once
+  a.per_cta = (P + 2 * b->dev.sms - 1) / (2 * b->dev.sms);
+  if (a.per_cta < 8) a.per_cta = 8;
+  const int ctas = (P + a.per_cta - 1) / a.per_cta;
+  if (ctas > kBankMaxCtas) return SWAPMOE_ERR_UNSUPPORTED;
+  cudaError_t e = cudaSuccess;
+  if (!a.direct) e = launch_kernel(bank_count_kernel, dim3(ctas), dim3(kBankThreads), 0, st, pdl, a);
+  if (e == cudaSuccess) e = launch_kernel(bank_gather_kernel, dim3(ctas), dim3(kBankThreads), 0, st, pdl, a);
+
+  const long long rows = std::min<long long>(b->max_rows, (P + 31ll * std::min(P, c.n_slots) + 31) / 32 * 32);
+  const long long max_tiles = (P + 63) / 64 + std::min(P, c.n_slots);
+  I8GemmArgs g = {};
+  g.tiles = b->tiles; g.n_tiles = b->n_tiles; g.row_group = 1 << 30; g.height = 256;
+  g.C = b->h; g.x_scales = b->row_scales; g.w_scales = b->in_scales; g.ldc = c.d_ff; g.n_cols = c.d_ff;
+  g.n_col_tiles = (c.d_ff + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); g.k_blocks = (c.d_model + kI8BK - 1) / kI8BK; g.w_rows = c.d_ff;
+  int epi = swiglu ? kI8Swiglu : kI8Relu;
+  long long work = max_tiles * g.n_col_tiles;
+  if (e == cudaSuccess)
+    e = launch_kernel(int8_gemm_kernel(epi), dim3(2 * (unsigned)std::min<long long>(work, pairs)), dim3(kPairThreads), int8_smem_bytes(epi), st, pdl,
+                      b->map_in, b->map_x[0], b->map_x[1], b->map_x[2], b->map_x[3], b->map_h_out, g);
+  QuantizeArgs q = {};
+  q.x = b->h; q.out8 = reinterpret_cast<uint8_t*>(b->h8); q.scales = b->h_scales; q.row_pair = b->row_pair; q.n_rows = b->n_tiles + 2;
+  q.x_stride = q.out8_stride = c.d_ff; q.T = (int)rows; q.d = c.d_ff; q.act = kQuantNone;
+  if (e == cudaSuccess) e = quantize_rows_launch<float>(q, true, b->dev.sms, st, pdl);
+  g.C = b->y; g.x_scales = b->h_scales; g.w_scales = b->out_scales; g.ldc = c.d_model; g.n_cols = c.d_model;
+  g.n_col_tiles = (c.d_model + 255) / 256; g.k_blocks = (c.d_ff + kI8BK - 1) / kI8BK; g.w_rows = c.d_model;
+  work = max_tiles * g.n_col_tiles;
+  if (e == cudaSuccess)
+    e = launch_kernel(int8_gemm_kernel(kI8F32), dim3(2 * (unsigned)std::min<long long>(work, pairs)), dim3(kPairThreads), int8_smem_bytes(kI8F32), st,
+                      pdl, b->map_out, b->map_h[0], b->map_h[1], b->map_h[2], b->map_h[3], b->map_y_out, g);
+  BankCombineArgs m;
+  m.y = b->y; m.pair_row = b->pair_row; m.weights = weights; m.counts = b->counts; m.out = out; m.out_stride = out_stride;
+  m.T = T; m.k = c.top_k; m.d = c.d_model; m.S = c.n_slots; m.vec = rows_aligned(out, T, out_stride, elem, elem * 4);
+  const dim3 grid(T, (c.d_model + 1023) / 1024);
+  if (e == cudaSuccess)
+    e = c.dtype == SWAPMOE_BF16 ? launch_kernel(bank_combine_kernel<bf16>, grid, dim3(256), 0, st, pdl, m)
+                                : launch_kernel(bank_combine_kernel<float>, grid, dim3(256), 0, st, pdl, m);
+  return launched(e);
+}
+
+}  // extern "C"

@@ -1,5 +1,5 @@
-/* Argument marshalling of the calls that run once per layer and step (rms_norm, route, AdapterBank.forward), as a CPython
- * extension: checks of the tensors' types, devices, shapes and strides, the current stream, and the call into the C ABI.  The same in
+/* Argument marshalling of the calls that run once per layer and step (rms_norm, route, AdapterBank.forward, block_norm,
+ * quantize_rows, matmul_scaled, ExpertBank.forward), as a CPython extension: checks of the tensors' types, devices, shapes and strides, the current stream, and the call into the C ABI.  The same in
  * Python and ctypes takes 10 us of host time per call, longer than the kernels of a decode step.  No torch headers: tensors are
  * asked through their Python attributes.  The functions of the library come in as addresses (init). */
 #define PY_SSIZE_T_CLEAN
@@ -15,10 +15,20 @@ typedef int32_t (*route_fn)(const swapmoe_gate_t*, const float*, int64_t, const 
 typedef int32_t (*adapters_fn)(swapmoe_adapters_t*, const void*, int64_t, const float*, const int32_t*, const void*, int64_t, void*,
                                int64_t, int32_t, void*);
 
+typedef int32_t (*block_norm_fn)(const swapmoe_block_norm_t*, void*);
+typedef int32_t (*quantize_fn)(const swapmoe_quantize_rows_t*, void*);
+typedef int32_t (*matmul_fn)(const swapmoe_matmul_t*, void*);
+typedef int32_t (*experts_fn)(swapmoe_expert_bank_t*, const void*, int64_t, const float*, const int32_t*, const float*, void*, int64_t,
+                              int32_t, void*);
+
 static rms_norm_fn f_rms_norm;
 static route_fn f_route;
 static adapters_fn f_adapters;
-static PyObject *fail, *d_f32, *d_bf16, *d_e4m3, *d_i32;                      /* the error function, torch's types */
+static block_norm_fn f_block_norm;
+static quantize_fn f_quantize;
+static matmul_fn f_matmul;
+static experts_fn f_experts;
+static PyObject *fail, *d_f32, *d_bf16, *d_e4m3, *d_i32, *d_i8;                      /* the error function, torch's types */
 static PyObject *get_device_fn, *set_device_fn, *raw_stream_fn;               /* torch's current device and stream */
 static PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_is_contiguous, *s_cuda_stream, *s_numel;
 
@@ -300,16 +310,191 @@ static PyObject* py_adapters_forward(PyObject* self, PyObject* const* v, Py_ssiz
   return end(&c, back, status);
 }
 
+/* block_norm(x, residual, weight, eps, out, residual_out, post_weight, post_eps, gate, scale, out8, scales, group, stream) */
+static PyObject* py_block_norm(PyObject* self, PyObject* const* v, Py_ssize_t n) {
+  if (n != 14) return PyErr_Format(PyExc_TypeError, "fourteen arguments expected");
+  Call c = {"swapmoe_block_norm", -1};
+  swapmoe_block_norm_t a = {0};
+  PyObject *x = v[0], *residual = v[1], *weight = v[2], *out = v[4], *residual_out = v[5], *post_weight = v[6], *gate = v[8], *out8 = v[10],
+           *scales = v[11];
+  PyObject *dtype, *rdtype;
+  int dims;
+  int64_t size[2], stride[2], group;
+  if (layer_type(&c, x, "x", &a.dtype, &dtype) || sizes(&c, x, "x", &dims, size, stride)) return NULL;
+  if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x: [T, d] expected"); return NULL; }
+  const int64_t T = size[0], d = size[1];
+  if (integer(v[12], &group)) return NULL;
+  if (group < 0 || group > INT32_MAX) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "group: %lld", (long long)group); return NULL; }
+  const double eps = PyFloat_AsDouble(v[3]);
+  if (eps == -1.0 && PyErr_Occurred()) return NULL;
+  const double post_eps = v[7] == Py_None ? eps : PyFloat_AsDouble(v[7]);
+  if (post_eps == -1.0 && PyErr_Occurred()) return NULL;
+  const double scale = PyFloat_AsDouble(v[9]);
+  if (scale == -1.0 && PyErr_Occurred()) return NULL;
+  a.n_rows = (int32_t)T; a.d = (int32_t)d; a.group = (int32_t)group; a.eps = (float)eps; a.post_eps = (float)post_eps; a.scale = (float)scale;
+  a.residual_dtype = a.dtype;
+  void* p;
+  if (rows(&c, x, "x", dtype, T, d, &p, &a.x_stride)) return NULL;
+  a.x = p;
+  rdtype = dtype;
+  if (residual != Py_None) {
+    if (layer_type(&c, residual, "residual", &a.residual_dtype, &rdtype) ||
+        rows(&c, residual, "residual", rdtype, T, d, &p, &a.residual_stride))
+      return NULL;
+    a.residual = p;
+  } else if (residual_out != Py_None && layer_type(&c, residual_out, "residual_out", &a.residual_dtype, &rdtype)) {
+    return NULL;
+  }
+  if (weight != Py_None) {
+    if (vector(&c, weight, "weight", dtype, d, &p)) return NULL;
+    a.weight = p;
+  }
+  if (post_weight != Py_None) {
+    if (vector(&c, post_weight, "post_weight", dtype, d, &p)) return NULL;
+    a.post_weight = p;
+  }
+  if (gate != Py_None) {
+    if (sizes(&c, gate, "gate", &dims, size, stride)) return NULL;
+    if (dims == 1) {
+      if (vector(&c, gate, "gate", dtype, d, &p)) return NULL;
+    } else if (rows(&c, gate, "gate", dtype, T, d, &p, &a.gate_stride)) {
+      return NULL;
+    }
+    a.gate = p;
+  }
+  if (residual_out != Py_None && rows(&c, residual_out, "residual_out", rdtype, T, d, &a.residual_out, &a.residual_out_stride)) return NULL;
+  if (out != Py_None && rows(&c, out, "out", dtype, T, d, &a.out, &a.out_stride)) return NULL;
+  if ((out8 == Py_None) != (scales == Py_None)) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "out8 and scales go together"); return NULL; }
+  if (out8 != Py_None) {
+    PyObject* t = PyObject_GetAttr(out8, s_dtype);
+    if (!t) return NULL;
+    Py_DECREF(t);                                   /* (torch keeps its types) */
+    a.type8 = t == d_i8 ? SWAPMOE_INT8 : SWAPMOE_E4M3;
+    if (rows(&c, out8, "out8", t == d_i8 ? d_i8 : d_e4m3, T, d, &a.out8, &a.out8_stride) ||
+        rows(&c, scales, "scales", d_f32, T, group ? (d + group - 1) / group : 1, &p, &a.scales_stride))
+      return NULL;
+    a.scales = (float*)p;
+  }
+  void* st;
+  long back;
+  int32_t status;
+  if (begin(&c, v[13], &st, &back)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = f_block_norm(&a, st);
+  Py_END_ALLOW_THREADS
+  return end(&c, back, status);
+}
+
+/* quantize_rows(x, out8, scales, act, stream) */
+static PyObject* py_quantize_rows(PyObject* self, PyObject* const* v, Py_ssize_t n) {
+  if (n != 5) return PyErr_Format(PyExc_TypeError, "five arguments expected");
+  Call c = {"swapmoe_quantize_rows", -1};
+  swapmoe_quantize_rows_t a = {0};
+  PyObject *x = v[0], *out8 = v[1], *scales = v[2], *dtype;
+  int dims;
+  int64_t size[2], stride[2], act;
+  if (layer_type(&c, x, "x", &a.dtype, &dtype) || sizes(&c, x, "x", &dims, size, stride)) return NULL;
+  if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x: [T, d] expected"); return NULL; }
+  if (integer(v[3], &act)) return NULL;
+  const int64_t T = size[0], width = size[1], d = act == SWAPMOE_QUANTIZE_SWIGLU ? width / 2 : width;
+  if (act == SWAPMOE_QUANTIZE_SWIGLU && width % 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x: an even number of columns expected"); return NULL; }
+  a.n_rows = (int32_t)T; a.d = (int32_t)d; a.act = (int32_t)act;
+  void* p;
+  if (rows(&c, x, "x", dtype, T, width, &p, &a.x_stride)) return NULL;
+  a.x = p;
+  if (rows(&c, out8, "out8", d_i8, T, d, &a.out8, &a.out8_stride) || vector(&c, scales, "scales", d_f32, T, &p)) return NULL;
+  a.scales = (float*)p;
+  void* st;
+  long back;
+  int32_t status;
+  if (begin(&c, v[4], &st, &back)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = f_quantize(&a, st);
+  Py_END_ALLOW_THREADS
+  return end(&c, back, status);
+}
+
+/* matmul_scaled(x8, x_scales, w8, w_scales, out, bias, stream) */
+static PyObject* py_matmul_scaled(PyObject* self, PyObject* const* v, Py_ssize_t n) {
+  if (n != 7) return PyErr_Format(PyExc_TypeError, "seven arguments expected");
+  Call c = {"swapmoe_matmul_scaled", -1};
+  swapmoe_matmul_t a = {0};
+  PyObject *x = v[0], *w = v[2], *out = v[4], *dtype;
+  int dims;
+  int64_t xsize[2], wsize[2], stride[2];
+  if (sizes(&c, x, "x8", &dims, xsize, stride)) return NULL;
+  if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x8: [T, K] expected"); return NULL; }
+  if (sizes(&c, w, "w8", &dims, wsize, stride)) return NULL;
+  if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "w8: [N, K] expected"); return NULL; }
+  const int64_t T = xsize[0], K = xsize[1], N = wsize[0];
+  a.n_tokens = (int32_t)T; a.k = (int32_t)K; a.n = (int32_t)N;
+  void* p;
+  if (rows(&c, x, "x8", d_i8, T, K, &p, &a.x_stride)) return NULL;
+  a.x = p;
+  if (vector(&c, v[1], "x_scales", d_f32, T, &p)) return NULL;
+  a.x_scales = (const float*)p;
+  if (rows(&c, w, "w8", d_i8, N, K, &p, &a.w_stride)) return NULL;
+  a.w = p;
+  if (vector(&c, v[3], "w_scales", d_f32, N, &p)) return NULL;
+  a.w_scales = (const float*)p;
+  if (v[5] != Py_None) {
+    if (vector(&c, v[5], "bias", d_f32, N, &p)) return NULL;
+    a.bias = (const float*)p;
+  }
+  if (layer_type(&c, out, "out", &a.dtype, &dtype) || rows(&c, out, "out", dtype, T, N, &a.out, &a.out_stride)) return NULL;
+  void* st;
+  long back;
+  int32_t status;
+  if (begin(&c, v[6], &st, &back)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = f_matmul(&a, st);
+  Py_END_ALLOW_THREADS
+  return end(&c, back, status);
+}
+
+/* experts_forward(handle, device, dtype, d, top_k, x8, x_scales, slots, weights, out, stream) */
+static PyObject* py_experts_forward(PyObject* self, PyObject* const* v, Py_ssize_t n) {
+  if (n != 11) return PyErr_Format(PyExc_TypeError, "eleven arguments expected");
+  Call c = {"swapmoe_expert_bank_forward", -1};
+  PyObject *dtype = v[2], *x = v[5], *out = v[9];
+  int dims;
+  int64_t device, d, k, size[2], stride[2], xs, os;
+  void *xp, *xsp, *sp, *wp, *op, *st;
+  long back;
+  int32_t status;
+  if (integer(v[1], &device) || integer(v[3], &d) || integer(v[4], &k)) return NULL;
+  void* bank = v[0] == Py_None ? NULL : PyLong_AsVoidPtr(v[0]);
+  if (PyErr_Occurred() || sizes(&c, x, "x8", &dims, size, stride)) return NULL;
+  if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x8: [T, d_model] expected"); return NULL; }
+  const int64_t T = size[0];
+  c.device = (long)device;
+  if (rows(&c, x, "x8", d_i8, T, d, &xp, &xs) || vector(&c, v[6], "x_scales", d_f32, T, &xsp) || vector(&c, v[7], "slots", d_i32, T * k, &sp) ||
+      vector(&c, v[8], "weights", d_f32, T * k, &wp) || rows(&c, out, "out", dtype, T, d, &op, &os))
+    return NULL;
+  if (begin(&c, v[10], &st, &back)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = f_experts(bank, xp, xs, xsp, sp, wp, op, os, (int32_t)T, st);
+  Py_END_ALLOW_THREADS
+  return end(&c, back, status);
+}
+
 /* init(fail, (addresses of the library's functions), (torch's types), (torch's device and stream functions)) */
 static PyObject* py_init(PyObject* self, PyObject* args) {
-  PyObject *e, *a[3], *t[4], *d[3];
-  if (!PyArg_ParseTuple(args, "O(OOO)(OOOO)(OOO)", &e, &a[0], &a[1], &a[2], &t[0], &t[1], &t[2], &t[3], &d[0], &d[1], &d[2])) return NULL;
+  PyObject *e, *a[7], *t[5], *d[3];
+  if (!PyArg_ParseTuple(args, "O(OOOOOOO)(OOOOO)(OOO)", &e, &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &t[0], &t[1], &t[2], &t[3], &t[4],
+                        &d[0], &d[1], &d[2]))
+    return NULL;
   f_rms_norm = (rms_norm_fn)PyLong_AsVoidPtr(a[0]);
   f_route = (route_fn)PyLong_AsVoidPtr(a[1]);
   f_adapters = (adapters_fn)PyLong_AsVoidPtr(a[2]);
+  f_block_norm = (block_norm_fn)PyLong_AsVoidPtr(a[3]);
+  f_quantize = (quantize_fn)PyLong_AsVoidPtr(a[4]);
+  f_matmul = (matmul_fn)PyLong_AsVoidPtr(a[5]);
+  f_experts = (experts_fn)PyLong_AsVoidPtr(a[6]);
   if (PyErr_Occurred()) return NULL;
   fail = Py_NewRef(e);                              /* (kept for the life of the process, like the functions themselves) */
   d_f32 = Py_NewRef(t[0]); d_bf16 = Py_NewRef(t[1]); d_e4m3 = Py_NewRef(t[2]); d_i32 = Py_NewRef(t[3]);
+  d_i8 = Py_NewRef(t[4]);
   get_device_fn = Py_NewRef(d[0]); set_device_fn = Py_NewRef(d[1]); raw_stream_fn = Py_NewRef(d[2]);
   Py_RETURN_NONE;
 }
@@ -318,6 +503,10 @@ static PyMethodDef methods[] = {
     {"init", py_init, METH_VARARGS, NULL},
     {"rms_norm", (PyCFunction)(void (*)(void))py_rms_norm, METH_FASTCALL, NULL},
     {"route", (PyCFunction)(void (*)(void))py_route, METH_FASTCALL, NULL},
+    {"block_norm", (PyCFunction)(void (*)(void))py_block_norm, METH_FASTCALL, NULL},
+    {"quantize_rows", (PyCFunction)(void (*)(void))py_quantize_rows, METH_FASTCALL, NULL},
+    {"matmul_scaled", (PyCFunction)(void (*)(void))py_matmul_scaled, METH_FASTCALL, NULL},
+    {"experts_forward", (PyCFunction)(void (*)(void))py_experts_forward, METH_FASTCALL, NULL},
     {"adapters_forward", (PyCFunction)(void (*)(void))py_adapters_forward, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
