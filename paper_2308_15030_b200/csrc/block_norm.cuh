@@ -4,9 +4,10 @@
 // y as rows of the layer's dtype, in 8 bits (e4m3 or integers) with scales, or both.  All in fp32; every output is rounded once, and the
 // second norm is taken of the sum before it is rounded.
 //
-// Bound by HBM: each row is read once, kept in registers through both sums and written once.  A team of warps holds a row, eight
-// columns per lane and chunk of 256; the residual's loads go out with those of x, so that the first sum's exchange between the warps hides
-// behind them.  Where 8-bit rows have one scale, the largest |h w| of the row is found in the same exchange as the second sum: the
+// Bound by HBM, and next to it by the chain of a row: loads, an exchange between the warps for each sum, weights, stores.  A team of warps
+// holds a row, eight columns per lane and chunk of 256, and an SM as many teams as its registers hold: x and a bf16 residual stay packed until
+// they are added, which makes room for five CTAs of eight warps instead of four.  Where 8-bit rows have one scale, the largest |h w| of the
+// row is found in the same exchange as the second sum: the
 // largest |y| is that times the row's positive factor.
 #pragma once
 #include "rms_norm.cuh"
@@ -46,7 +47,7 @@ __device__ __forceinline__ void store8_int8(uint8_t* row, int c0, int lane, int 
 // Scale of the largest magnitude, and the factor that takes values to the 8-bit type (0 for zeros, NaN for NaN).
 __device__ __forceinline__ float scale8(float largest, float inverse_max, float* inverse) {
   const float s = largest * inverse_max, t = s < kNormMinScale ? kNormMinScale : s;         // NaN stays NaN
-  *inverse = __frcp_rn(t);
+  *inverse = __fdividef(1.f, t);                                       // (t is below 2^122)
   return largest == 0.f ? 0.f : t;
 }
 
@@ -70,7 +71,16 @@ struct NormTeam {
     }
     const bool any = __syncthreads_or(*rare) != 0;
     float t = 0.f, m = 0.f;
-    for (int w = 0; w < n; ++w) {
+    int w = 0;
+    for (; w + 4 <= n && first % 4 == 0; w += 4) {
+      const float4 u = *reinterpret_cast<const float4*>(s_sum + first + w);
+      t += (u.x + u.y) + (u.z + u.w);
+      if constexpr (kMax) {
+        const float4 v = *reinterpret_cast<const float4*>(s_max + first + w);
+        m = fmaxf(m, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+      }
+    }
+    for (; w < n; ++w) {
       t += s_sum[first + w];
       if constexpr (kMax) m = fmaxf(m, s_max[first + w]);
     }
@@ -86,35 +96,74 @@ struct NormTeam {
     for (int w = 1; w < n; ++w) t = add ? t + s_sum[first + w] : max_magnitude(t, s_sum[first + w], 0.f);
     return t;
   }
-  // The factor of a rare row (others keep theirs: a row hangs on itself): values are divided by m, the power of two below the larger one
-  // of their largest magnitude and sqrt(eps), so that neither square leaves the range:
+  // The factors of a rare row (others keep theirs: a row hangs on itself): values are multiplied by `by` first, the reciprocal of the power of
+  // two m below the larger one of their largest magnitude and sqrt(eps), so that neither square leaves the range:
   // v / sqrt(mean(v^2) + eps) = (v / m) / sqrt(mean((v / m)^2) + eps / m^2)
-  template <int kChunks>
-  __device__ __forceinline__ bool rescale(float (&v)[kChunks][8], bool rare, float eps, float per_column, float* s) const {
+  template <int kChunks, typename Values>
+  __device__ __forceinline__ bool rescale(Values values, bool rare, float eps, float per_column, float* by, float* s) const {
     const bool mine = over(rare ? 1.f : 0.f, false) > 0.f;
-    float most = 0.f;
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j) most = max_magnitude(most, largest8(v[j]), 0.f);
+    float most = 0.f, v[8];
+#pragma unroll 1
+    for (int j = 0; j < kChunks; ++j) {
+      values(j, v);
+      most = max_magnitude(most, largest8(v), 0.f);
+    }
     const float top = over(warp_largest(most), false);
     const uint32_t exponent = __float_as_uint(fmaxf(top, sqrtf(eps))) >> 23;                    // (below 2^-126: m = 2^-127)
-    const float by = mine && top > 0.f && top < CUDART_INF_F ? __uint_as_float(exponent < 254u ? (254u - exponent) << 23 : 0x400000u) : 1.f;
+    const float f = mine && top > 0.f && top < CUDART_INF_F ? __uint_as_float(exponent < 254u ? (254u - exponent) << 23 : 0x400000u) : 1.f;
     float sum = 0.f;
+#pragma unroll 1
+    for (int j = 0; j < kChunks; ++j) {
+      values(j, v);
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[j][i] *= by;
-        sum = fmaf(v[j][i], v[j][i], sum);
-      }
+      for (int i = 0; i < 8; ++i) sum = fmaf(v[i] * f, v[i] * f, sum);
+    }
     const float total = over(warp_sum(sum), true);
-    if (mine) *s = rsqrtf(total * per_column + eps * by * by);
+    if (mine) {
+      *by = f;
+      *s = rsqrtf(total * per_column + eps * f * f);
+    }
     return mine;
   }
 };
 
-// T: x, weights, gate, out; R: the residual's rows; kChunks: chunks per warp; kRow8: 8-bit rows with one scale each.
-template <typename T, typename R, int kChunks, bool kVec, bool kRow8>
-__global__ void __launch_bounds__(kNormMaxWarps * 32) block_norm_kernel(const __grid_constant__ BlockNormArgs a) {
+// Eight values of a row as they are stored.
+template <typename S> struct RowPiece;
+template <> struct RowPiece<float> {
+  float v[8];
+  template <bool kVec>
+  __device__ __forceinline__ void load(const float* row, int c0, int lane, int d) { norm_load8<kVec>(row, c0, lane, d, v); }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = v[i];
+  }
+};
+template <> struct RowPiece<bf16> {
+  uint32_t v[4];
+  template <bool kVec>
+  __device__ __forceinline__ void load(const bf16* row, int c0, int lane, int d) {
+    if constexpr (kVec) {
+      const uint4 u = c0 + lane * 8 < d ? *reinterpret_cast<const uint4*>(row + c0 + lane * 8) : make_uint4(0u, 0u, 0u, 0u);
+      v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+    } else {
+      const uint16_t* r = reinterpret_cast<const uint16_t*>(row);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = c0 + 2 * i * 32 + lane;
+        v[i] = (c < d ? r[c] : 0u) | (c + 32 < d ? (uint32_t)r[c + 32] << 16 : 0u);
+      }
+    }
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(v[i] << 16); f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+  }
+};
+
+// T: x, weights, gate, out; R: the residual's rows; kChunks: chunks per warp; kRow8: 8-bit rows with one scale each; kThreads, kCtas: most
+// threads of a CTA, CTAs that an SM is to hold.
+template <typename T, typename R, int kChunks, bool kVec, bool kRow8, int kThreads, int kCtas>
+__global__ void __launch_bounds__(kThreads, kCtas) block_norm_kernel(const __grid_constant__ BlockNormArgs a) {
   __shared__ __align__(16) float s_sum[kNormMaxWarps], s_max[kNormMaxWarps];
   const int lane = threadIdx.x & 31, wr = threadIdx.x >> 5, team = threadIdx.y;       // a team per row: blockDim.x threads
   const NormTeam tm = {s_sum, s_max, lane, team * a.warps_per_row + wr, team * a.warps_per_row, a.warps_per_row};
@@ -122,87 +171,113 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) block_norm_kernel(const __
   const bool active = row < a.T;
   const int d = active ? a.d : 0;        // a team without a row computes on zeros and stores nothing
   auto first = [&](int j) { return (wr + j * a.warps_per_row) * kNormChunk; };
-  float h[kChunks][8], p[kChunks][8], w[8];
+  RowPiece<T> x[kChunks];
+  RowPiece<R> r[kChunks];
+  float h[kChunks][8];
   pdl_wait();
   pdl_trigger();
-  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+  {
+    const T* xs = static_cast<const T*>(a.x) + row * a.x_stride;
+    const R* rs = static_cast<const R*>(a.residual) + row * a.residual_stride;
 #pragma unroll
-  for (int j = 0; j < kChunks; ++j) norm_load8<kVec>(x, first(j), lane, d, p[j]);
-  if (a.residual != nullptr) {
-    const R* r = static_cast<const R*>(a.residual) + row * a.residual_stride;
+    for (int j = 0; j < kChunks; ++j) x[j].template load<kVec>(xs, first(j), lane, d);
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) norm_load8<kVec>(r, first(j), lane, d, h[j]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] = 0.f;
+    for (int j = 0; j < kChunks; ++j) r[j].template load<kVec>(rs, first(j), lane, a.residual != nullptr ? d : 0);
   }
   bool rare;
-  float s = 1.f, none = 0.f;
+  float s = 1.f, by = 1.f, none = 0.f;
   if (a.post_weight != nullptr) {
     float sum = 0.f, sum1 = 0.f;
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j)
+    for (int j = 0; j < kChunks; ++j) {
+      float v[8];
+      x[j].get(v);
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) square2(sum, sum1, p[j][i], p[j][i + 1]);
+      for (int i = 0; i < 8; i += 2) square2(sum, sum1, v[i], v[i + 1]);
+    }
     sum += sum1;
     const bool slow = tm.exchange<false>(sum, none, false, a.post_eps, &rare);
     s = rsqrtf(sum * a.per_column + a.post_eps);
-    if (slow) tm.rescale<kChunks>(p, rare, a.post_eps, a.per_column, &s);
+    if (slow) {
+      auto block = [&](int j, float (&v)[8]) {
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-      norm_load8<kVec>(static_cast<const T*>(a.post_weight), first(j), lane, d, w);
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        mul2(p[j][i], p[j][i + 1], s, s);
-        mul2(p[j][i], p[j][i + 1], w[i], w[i + 1]);
-      }
+        for (int k = 0; k < kChunks; ++k)
+          if (k == j) x[k].get(v);
+      };
+      tm.rescale<kChunks>(block, rare, a.post_eps, a.per_column, &by, &s);
     }
   }
   const T* gate = static_cast<const T*>(a.gate) + row * a.gate_stride;
+  R* ro = static_cast<R*>(a.residual_out) + row * a.residual_out_stride;
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
+    float v[8], w[8];
+    x[j].get(v);
+    if (a.post_weight != nullptr) {
+      norm_load8<kVec>(static_cast<const T*>(a.post_weight), first(j), lane, d, w);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        mul2(v[i], v[i + 1], by, by);
+        mul2(v[i], v[i + 1], s, s);
+        mul2(v[i], v[i + 1], w[i], w[i + 1]);
+      }
+    }
     if (a.gate != nullptr) {
       norm_load8<kVec>(gate, first(j), lane, d, w);
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) mul2(p[j][i], p[j][i + 1], w[i], w[i + 1]);
+      for (int i = 0; i < 8; i += 2) mul2(v[i], v[i + 1], w[i], w[i + 1]);
     }
+    r[j].get(h[j]);
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      mul2(p[j][i], p[j][i + 1], a.scale, a.scale);
-      add2(h[j][i], h[j][i + 1], p[j][i], p[j][i + 1]);
+      mul2(v[i], v[i + 1], a.scale, a.scale);
+      add2(h[j][i], h[j][i + 1], v[i], v[i + 1]);
     }
-  }
-  if (a.residual_out != nullptr) {
-    R* ro = static_cast<R*>(a.residual_out) + row * a.residual_out_stride;
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j) norm_store8<kVec>(ro, first(j), lane, d, h[j]);
+    if (a.residual_out != nullptr) norm_store8<kVec>(ro, first(j), lane, d, h[j]);
   }
   if (a.out == nullptr && a.out8 == nullptr) return;                  // the same for the whole grid
   float sum = 0.f, sum1 = 0.f, most = 0.f;
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
-    norm_load8<kVec>(static_cast<const T*>(a.weight), first(j), lane, d, p[j]);
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      square2(sum, sum1, h[j][i], h[j][i + 1]);
-      if constexpr (kRow8) most = max_magnitude(most, h[j][i] * p[j][i], h[j][i + 1] * p[j][i + 1]);
+    for (int i = 0; i < 8; i += 2) square2(sum, sum1, h[j][i], h[j][i + 1]);
+    if constexpr (kRow8) {
+      float w[8];
+      norm_load8<kVec>(static_cast<const T*>(a.weight), first(j), lane, d, w);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) most = max_magnitude(most, h[j][i] * w[i], h[j][i + 1] * w[i + 1]);
     }
   }
   sum += sum1;
   const bool slow = tm.exchange<kRow8>(sum, most, true, a.eps, &rare);
   s = rsqrtf(sum * a.per_column + a.eps);
+  by = 1.f;
   float largest = most * s;
   bool mine = false;
-  if (slow) mine = tm.rescale<kChunks>(h, rare, a.eps, a.per_column, &s);
+  if (slow) {
+    auto stream = [&](int j, float (&v)[8]) {
 #pragma unroll
-  for (int j = 0; j < kChunks; ++j)
+      for (int k = 0; k < kChunks; ++k)
+        if (k == j)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = h[k][i];
+    };
+    mine = tm.rescale<kChunks>(stream, rare, a.eps, a.per_column, &by, &s);
+  }
+  T* o = static_cast<T*>(a.out) + row * a.out_stride;
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    float w[8];
+    norm_load8<kVec>(static_cast<const T*>(a.weight), first(j), lane, d, w);
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
+      if (slow) mul2(h[j][i], h[j][i + 1], by, by);
       mul2(h[j][i], h[j][i + 1], s, s);
-      mul2(h[j][i], h[j][i + 1], p[j][i], p[j][i + 1]);               // y
+      mul2(h[j][i], h[j][i + 1], w[i], w[i + 1]);                     // y
     }
+    if (a.out != nullptr) norm_store8<kVec>(o, first(j), lane, d, h[j]);
+  }
+  if (a.out8 == nullptr) return;
   if constexpr (kRow8) {
     if (slow) {
       most = 0.f;
@@ -212,12 +287,6 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) block_norm_kernel(const __
       if (mine) largest = t;
     }
   }
-  if (a.out != nullptr) {
-    T* o = static_cast<T*>(a.out) + row * a.out_stride;
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j) norm_store8<kVec>(o, first(j), lane, d, h[j]);
-  }
-  if (a.out8 == nullptr) return;
   uint8_t* q = a.out8 + row * a.out8_stride;
   float* sc = a.scales + row * a.scales_stride;
   const float inverse_max = a.int8 ? 1.f / kInt8Max : 1.f / kE4m3Max;
@@ -237,20 +306,28 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) block_norm_kernel(const __
     }
   } else {
     const int shift = 31 - __clz(a.group);
+    if constexpr (kVec) {
+      // a group is group / 8 neighbouring lanes; the chunks' exchanges go side by side
+      float m[kChunks];
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-      const int c0 = first(j);
-      if constexpr (kVec) {
-        // a group is group / 8 neighbouring lanes
-        float m = largest8(h[j]);
-        for (int o = a.group >> 4; o > 0; o >>= 1) m = max_magnitude(m, __shfl_xor_sync(0xffffffffu, m, o), 0.f);
+      for (int j = 0; j < kChunks; ++j) m[j] = largest8(h[j]);
+#pragma unroll 1
+      for (int o = a.group >> 4; o > 0; o >>= 1)
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) m[j] = max_magnitude(m[j], __shfl_xor_sync(0xffffffffu, m[j], o), 0.f);
+#pragma unroll
+      for (int j = 0; j < kChunks; ++j) {
         float inv;
-        const float scale = scale8(m, inverse_max, &inv);
-        const int c = c0 + lane * 8;
+        const float scale = scale8(m[j], inverse_max, &inv);
+        const int c = first(j) + lane * 8;
         if (c < d && (c & (a.group - 1)) == 0) sc[c >> shift] = scale;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) mul2(h[j][i], h[j][i + 1], inv, inv);
-      } else {
+        store(first(j), h[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kChunks; ++j) {
         // a group is group / 32 of the lanes' columns, over all lanes
         float m[8];
 #pragma unroll
@@ -268,12 +345,12 @@ __global__ void __launch_bounds__(kNormMaxWarps * 32) block_norm_kernel(const __
         for (int i = 0; i < 8; ++i) {
           float inv;
           const float scale = scale8(m[i], inverse_max, &inv);
-          const int c = c0 + i * 32;
+          const int c = first(j) + i * 32;
           if (lane == 0 && c < d && (c & (a.group - 1)) == 0) sc[c >> shift] = scale;
           h[j][i] *= inv;
         }
+        store(first(j), h[j]);
       }
-      store(c0, h[j]);
     }
   }
 }
@@ -290,10 +367,13 @@ inline cudaError_t block_norm_launch_typed(BlockNormArgs a, bool vec, int sm_cou
   a.per_column = 1.f / (float)a.d;
   auto go = [&](auto kernel) { return launch_kernel(kernel, grid, block, 0, st, pdl, a); };
   const bool row8 = a.out8 != nullptr && a.group == 0;
-  if (vec && row8) return few ? go(block_norm_kernel<T, R, 1, true, true>) : go(block_norm_kernel<T, R, 2, true, true>);
-  if (vec) return few ? go(block_norm_kernel<T, R, 1, true, false>) : go(block_norm_kernel<T, R, 2, true, false>);
-  if (row8) return few ? go(block_norm_kernel<T, R, 1, false, true>) : go(block_norm_kernel<T, R, 2, false, true>);
-  return few ? go(block_norm_kernel<T, R, 1, false, false>) : go(block_norm_kernel<T, R, 2, false, false>);
+  constexpr int kWide = 32 * kNormMaxWarps, kCtas = sizeof(T) == 2 ? 5 : 4;
+  if (vec && few) return row8 ? go(block_norm_kernel<T, R, 1, true, true, kWide, 1>) : go(block_norm_kernel<T, R, 1, true, false, kWide, 1>);
+  if (vec && a.warps_per_row <= 8)
+    return row8 ? go(block_norm_kernel<T, R, 2, true, true, 256, kCtas>) : go(block_norm_kernel<T, R, 2, true, false, 256, kCtas>);
+  if (vec) return row8 ? go(block_norm_kernel<T, R, 2, true, true, kWide, 1>) : go(block_norm_kernel<T, R, 2, true, false, kWide, 1>);
+  if (few) return row8 ? go(block_norm_kernel<T, R, 1, false, true, kWide, 1>) : go(block_norm_kernel<T, R, 1, false, false, kWide, 1>);
+  return row8 ? go(block_norm_kernel<T, R, 2, false, true, kWide, 1>) : go(block_norm_kernel<T, R, 2, false, false, kWide, 1>);
 }
 
 }  // namespace swapmoe

@@ -5,7 +5,7 @@
 // computed by itself and a token's choices are added in their order.
 //   count (more than kBankDirectPairs pairs only): pairs per slot, and every CTA's share of a slot
 //   gather: slot offsets, token tiles, rows of x8 with their scales to their places
-//   product, activation in fp32; rows to 8 bits (quantize_rows.cuh); product; combine.
+//   product, activation in fp32 with the rows' largest magnitudes; rows to 8 bits; product; combine.
 #pragma once
 #include "int8_gemm.cuh"
 #include "quantize_rows.cuh"
@@ -21,15 +21,15 @@ struct BankArgs {
   const int8_t* x8;
   const float* x_scales;
   const int32_t* slots;
-  const float* weights;
   int8_t* rows8;                // [rows, d]
   float* row_scales;
   int32_t *row_pair, *pair_row; // pair of a row (-1: none), row of a pair (-1: none)
+  int32_t* largest;             // [rows]
   int32_t *counts, *cta_base;   // [S] zero between calls; [CTAs, S]
   TileDesc* tiles;
   int32_t* n_tiles;             // [0] tiles, [1] most rows of one, [2] rows with the slots' padding
   long long x_stride;
-  int P, S, k, d, per_cta;      // pairs, pairs of a CTA
+  int P, S, k, d, per_cta;      // pairs, ..., pairs of a CTA
   int direct;
 };
 
@@ -54,12 +54,6 @@ __global__ void __launch_bounds__(kBankThreads) bank_count_kernel(const __grid_c
     a.cta_base[(size_t)blockIdx.x * a.S + s] = s_count[s] ? atomicAdd(&a.counts[s], s_count[s]) : 0;
 }
 
-// Token tiles of one slot: equal heights, multiples of 32, of at most `cap` rows.
-__device__ __forceinline__ int bank_tile_rows(int count, int cap) {
-  const int n = (count + cap - 1) / cap;
-  return n ? ((count + n - 1) / n + 31) & ~31 : 32;
-}
-
 __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_constant__ BankArgs a) {
   __shared__ int s_count[kBankMaxSlots], s_at[kBankMaxSlots], s_off[kBankMaxSlots];
   __shared__ int s_row[kBankThreads];
@@ -71,11 +65,13 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
   pdl_trigger();
   __syncthreads();
   if (a.direct) {
-    for (int p = threadIdx.x; p < a.P; p += kBankThreads) {
-      const int s = bank_slot(a, p);
-      if (s < 0) continue;
-      atomicAdd(&s_count[s], 1);
-      if (p < p0) atomicAdd(&s_at[s], 1);
+    for (int b = 0; b < a.P; b += kBankThreads) {
+      const int p = b + threadIdx.x, s = p < a.P ? bank_slot(a, p) : -1;
+      const unsigned same = __match_any_sync(0xffffffffu, s), front = __ballot_sync(0xffffffffu, p < p0);
+      if (s >= 0 && (same & ((1u << lane) - 1u)) == 0) {
+        atomicAdd(&s_count[s], __popc(same));
+        if (same & front) atomicAdd(&s_at[s], __popc(same & front));
+      }
     }
   } else {
     for (int s = threadIdx.x; s < a.S; s += kBankThreads) {
@@ -93,22 +89,23 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
     int row0 = 0, tile0 = 0;
     for (int s0 = 0; s0 < a.S; s0 += 32) {
       const int s = s0 + lane, count = s < a.S ? s_count[s] : 0;
-      const int padded = (count + 31) & ~31, n = (count + cap - 1) / cap, height = bank_tile_rows(count, cap);
-      const int used = (count + height - 1) / height;         // (heights are rounded up: the last tile may have become empty)
+      // a slot's rows in as few tiles as the cap allows, by 32 and as even as that can be
+      const int padded = (count + 31) & ~31, used = (count + cap - 1) / cap;
       int rows = padded, tiles = used;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int u = __shfl_up_sync(0xffffffffu, rows, o), v = __shfl_up_sync(0xffffffffu, tiles, o);
         if (lane >= o) { rows += u; tiles += v; }
       }
-      (void)n;
       const int off = row0 + rows - padded;
       if (s < a.S) s_off[s] = off;
       if (blockIdx.x == 0) {
-        for (int i = 0; i < used; ++i) {
+        for (int i = 0, at = 0; i < used; ++i) {
+          const int units = padded / 32, height = (units / used + (i < units % used ? 1 : 0)) * 32;
           TileDesc td;
-          td.phys = td.slot = s; td.row0 = off + i * height; td.rows = min(height, count - i * height);
+          td.phys = td.slot = s; td.row0 = off + at; td.rows = min(height, count - at);
           a.tiles[tile0 + tiles - used + i] = td;
+          at += height;
         }
         for (int r = count; r < padded; ++r) a.row_pair[off + r] = -1;
       }
@@ -126,6 +123,7 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
       if (s >= 0) {
         row = s_off[s] + atomicAdd(&s_at[s], 1);
         a.row_pair[row] = p;
+        a.largest[row] = 0;
         a.row_scales[row] = a.x_scales[p / a.k];
       }
       a.pair_row[p] = row;
@@ -137,9 +135,64 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
       if (to < 0) continue;
       const uint4* src = reinterpret_cast<const uint4*>(a.x8 + (size_t)((b + i) / a.k) * a.x_stride);
       uint4* dst = reinterpret_cast<uint4*>(a.rows8 + (size_t)to * a.d);
-      for (int c = lane; c < a.d / 16; c += 32) dst[c] = src[c];
+      const int quads = a.d / 16;
+      for (int c0 = lane; c0 < quads; c0 += 256) {
+        uint4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (c0 + 32 * u < quads) v[u] = src[c0 + 32 * u];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (c0 + 32 * u < quads) dst[c0 + 32 * u] = v[u];
+      }
     }
     __syncthreads();
+  }
+}
+
+// Hidden values to 8 bits by the rows' largest magnitudes, as quantize_rows does it: a warp per row and 128 kTurns columns, so that the values
+// are asked for together with what says whether the row holds a pair; or, where most rows would not (few pairs), per pair.
+struct BankQuantizeArgs {
+  const float* h;               // [rows, F]
+  const int32_t *largest, *row_pair, *pair_row, *n_tiles;
+  uint8_t* h8;
+  float* h_scales;
+  int F, parts;                 // parts of a row
+  int n;                        // rows, or pairs
+  int by_pair;
+};
+
+template <int kTurns>
+__global__ void __launch_bounds__(kBankThreads, kTurns == 8 ? 4 : 6) bank_quantize_kernel(const __grid_constant__ BankQuantizeArgs a) {
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31, unit = blockIdx.x * (kBankThreads / 32) + (threadIdx.x >> 5);
+  const int index = unit / a.parts, part = unit - index * a.parts;
+  if (index >= a.n) return;
+  const int row = a.by_pair ? __ldcg(a.pair_row + index) : index;
+  if (row < 0) return;
+  const int c0 = part * 128 * kTurns + 4 * lane;
+  const float* h = a.h + (size_t)row * a.F;
+  float4 v[kTurns];
+#pragma unroll
+  for (int u = 0; u < kTurns; ++u)
+    v[u] = c0 + 128 * u < a.F ? __ldcs(reinterpret_cast<const float4*>(h + c0 + 128 * u)) : make_float4(0.f, 0.f, 0.f, 0.f);
+  const float most = __int_as_float(__ldcg(a.largest + row));
+  if (!a.by_pair) {
+    const int rows = __ldcg(a.n_tiles + 2), pair = __ldcg(a.row_pair + row);
+    if (row >= rows || pair < 0) return;
+  }
+  const float divisor = quantize_divisor(most), inverse = __frcp_rn(divisor);
+  if (part == 0 && lane == 0) a.h_scales[row] = most == 0.f ? 0.f : divisor;
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.h8 + (size_t)row * a.F);
+#pragma unroll
+  for (int u = 0; u < kTurns; u += 2) {
+    float f[8] = {v[u].x, v[u].y, v[u].z, v[u].w, v[u + 1].x, v[u + 1].y, v[u + 1].z, v[u + 1].w};
+    uint32_t q[8];
+    quotients8(f, divisor, inverse, q);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (c0 + 128 * (u + i) < a.F) out[(c0 + 128 * (u + i)) / 4] = pack_bytes(q + 4 * i);
   }
 }
 
@@ -153,31 +206,62 @@ struct BankCombineArgs {
   int T, k, d, S, vec;
 };
 
-template <typename T>
+// A CTA per token: four columns a thread and turn, kTurns turns of kRows rows on their way at once.
+template <typename T, int kTurns, int kRows>
 __global__ void __launch_bounds__(256) bank_combine_kernel(const __grid_constant__ BankCombineArgs a) {
   pdl_wait();
   pdl_trigger();
-  if (blockIdx.x == 0 && blockIdx.y == 0)
+  const int t = blockIdx.x;
+  if (t == 0)
     for (int s = threadIdx.x; s < a.S; s += 256) a.counts[s] = 0;     // for the next call
-  const int t = blockIdx.x, c = (blockIdx.y * 256 + threadIdx.x) * 4;
-  if (c >= a.d) return;
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int j = 0; j < a.k; ++j) {
-    const int row = a.pair_row[t * a.k + j];
-    if (row < 0) continue;
-    const float w = a.weights[t * a.k + j];
-    float v[4];
-    load4(a.y + (size_t)row * a.d + c, v);
+  const int32_t* rows = a.pair_row + (size_t)t * a.k;
+  const float* weights = a.weights + (size_t)t * a.k;
+  for (int c0 = 4 * threadIdx.x; c0 < a.d; c0 += 1024 * kTurns) {
+    float acc[kTurns][4] = {};
+    for (int j0 = 0; j0 < a.k; j0 += kRows) {
+      float4 v[kRows][kTurns];
+      float w[kRows];
+      bool have[kRows];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = fmaf(w, v[i], acc[i]);
-  }
-  T* out = static_cast<T*>(a.out) + (size_t)t * a.out_stride + c;
-  if (a.vec) {
-    store4(out, acc);
-  } else {
+      for (int j = 0; j < kRows; ++j) {
+        const int row = j0 + j < a.k ? rows[j0 + j] : -1;
+        have[j] = row >= 0;
+        w[j] = have[j] ? weights[j0 + j] : 0.f;
+        const float* y = a.y + (size_t)max(row, 0) * a.d;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) norm_store(out + i, acc[i]);
+        for (int u = 0; u < kTurns; ++u)
+          if (have[j] && c0 + 1024 * u < a.d) v[j][u] = __ldcs(reinterpret_cast<const float4*>(y + c0 + 1024 * u));
+      }
+#pragma unroll
+      for (int j = 0; j < kRows; ++j)
+        if (have[j])
+#pragma unroll
+          for (int u = 0; u < kTurns; ++u) {
+            acc[u][0] = fmaf(w[j], v[j][u].x, acc[u][0]); acc[u][1] = fmaf(w[j], v[j][u].y, acc[u][1]);
+            acc[u][2] = fmaf(w[j], v[j][u].z, acc[u][2]); acc[u][3] = fmaf(w[j], v[j][u].w, acc[u][3]);
+          }
+    }
+    T* out = static_cast<T*>(a.out) + (size_t)t * a.out_stride;
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u) {
+      const int c = c0 + 1024 * u;
+      if (c >= a.d) continue;
+      if (a.vec) {
+        store4(out + c, acc[u]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) norm_store(out + c + i, acc[u][i]);
+      }
+    }
   }
+}
+
+template <typename T>
+inline cudaError_t bank_combine_launch(const BankCombineArgs& a, cudaStream_t st, bool pdl) {
+  const dim3 grid(a.T), block(256);
+  if (a.d <= 1024) return launch_kernel(bank_combine_kernel<T, 1, 4>, grid, block, 0, st, pdl, a);
+  if (a.d <= 2048) return launch_kernel(bank_combine_kernel<T, 2, 4>, grid, block, 0, st, pdl, a);
+  return launch_kernel(bank_combine_kernel<T, 4, 2>, grid, block, 0, st, pdl, a);
 }
 
 }  // namespace swapmoe

@@ -5,12 +5,14 @@
 // Bound by the tensor cores for many tokens and by the weights' bytes for few.  As in the grouped GEMM of bf16 layers (gemm_tc_pair.cuh)
 // two SMs share a tile of 256 WEIGHT rows x up to 256 TOKENS through tcgen05 `cta_group::2`, here of kind::i8: a k-block is 128
 // columns, the same 128 bytes a row that 64 bf16 values take, for the same tensor clocks and twice the products.  Weights are the MMA's
-// rows, so tokens, whose number is ragged, are its columns, in steps of 32.  Roles in each CTA (384 threads): warp 0 = TMA
-// producer, warp 1 = MMA issuer (even CTA only), warp 2 = TMEM allocation, warps 4-11 = epilogue of the CTA's own 128 weight rows, which
-// overlaps the next tile's MMAs through two accumulators.  No load uses cluster multicast; every wait is bounded.
+// rows, so tokens, whose number is ragged, are its columns, in steps of 32.  Roles in each CTA (640 threads): warp 0 = TMA
+// producer, warp 1 = MMA issuer (even CTA only), warp 2 = TMEM allocation, warps 4-19 = epilogue of the CTA's own 128 weight rows, which
+// overlaps the next tile's MMAs through two accumulators.  Sixteen warps, sixteen tokens at a time: what an epilogue does is a chain of
+// instructions that wait for one another, and with short contractions it sets the pace.  No load uses cluster multicast; every wait is bounded.
 #pragma once
 #include "launch.cuh"
 #include "pair_common.cuh"
+#include "rms_norm.cuh"
 
 namespace swapmoe {
 
@@ -34,6 +36,10 @@ struct I8GemmArgs {
   int32_t row_group;        // token tiles per scheduling group (see decode_tile)
   int32_t T, height;        // height: multiple of 32, up to 256
   int32_t direct;           // rows of C that the TMA unit cannot store: elements leave one by one
+  // 1: the kernel in front holds no tensor memory and has waited for all before it: pairs get ready while it runs.  2: and the list of
+  // tiles and the weights are older than it: the first boxes of weights are requested too.
+  int32_t early;
+  int32_t* largest;         // [rows] largest magnitude of a row of hidden values, as its bits (ReLU, SwiGLU: zero before)
 };
 
 // Instruction descriptor: int8 x int8 -> int32, both operands K-major, M x N tile.
@@ -42,6 +48,8 @@ __host__ __device__ constexpr uint32_t make_idesc_int8(int M, int N) {
 }
 
 namespace ptx {
+// All of this thread's stores but the last one have read their shared memory.
+__device__ __forceinline__ void tma_store_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void umma_int8_pair(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
@@ -51,12 +59,24 @@ __device__ __forceinline__ void umma_int8_pair(uint32_t tmem_d, uint64_t desc_a,
 }
 }  // namespace ptx
 
-// staging of an epilogue warp: a box of 32 tokens x 32 columns (SwiGLU 16)
-__host__ __device__ constexpr int int8_warp_bytes(int epi) { return epi == kI8F32 || epi == kI8Relu ? 4096 : 2048; }
-__host__ __device__ constexpr int int8_smem_bytes(int epi) { return kPairStageArea + 2048 + 8 * int8_warp_bytes(epi); }
+constexpr int kI8EpiWarps = 16;
+constexpr int kI8EpiParts = kI8EpiWarps / 4;                  // warps that share a quarter of tensor memory
+constexpr int kI8Chunk = 16;                                  // tokens an epilogue warp takes at once
+constexpr int kI8Threads = 128 + 32 * kI8EpiWarps;
+// staging of an epilogue warp: two boxes of 16 tokens x 32 columns (SwiGLU 16), so that one is filled while the other leaves
+__host__ __device__ constexpr int int8_box_bytes(int epi) { return epi == kI8F32 || epi == kI8Relu ? 2048 : 1024; }
+// the ring takes what that leaves: stages of 256 / 128 / 64 tokens 6 / 8 / 9, where boxes are of 2 KB 5 / 6 / 8
+__host__ __device__ constexpr int int8_ring_bytes(int epi) { return (int8_box_bytes(epi) == 2048 ? 5 : 6) * (kPairABytes + kPairBBytes); }
+__host__ __device__ constexpr int int8_stages(int epi, int max_tokens) {
+  return int8_box_bytes(epi) == 2048 ? (max_tokens > 128 ? 5 : max_tokens > 64 ? 6 : 8) : max_tokens > 128 ? 6 : max_tokens > 64 ? 8 : 9;
+}
+// ... and the scales of a warp's tokens
+__host__ __device__ constexpr int int8_smem_bytes(int epi) { return int8_ring_bytes(epi) + 2048 + kI8EpiWarps * (2 * int8_box_bytes(epi) + 4 * kI8Chunk); }
+static_assert(int8_smem_bytes(kI8F32) <= 227 * 1024 && int8_smem_bytes(kI8Bf16) <= 227 * 1024, "what a CTA may have");
+static_assert(int8_stages(kI8F32, 64) * (kPairABytes + 32 * kI8BK) <= int8_ring_bytes(kI8F32) && int8_stages(kI8Bf16, 64) <= kPairMaxStages, "stages fit");
 
 template <int EPI>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8Threads, 1)
 int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX128,
                       const __grid_constant__ CUtensorMap tmX64, const __grid_constant__ CUtensorMap tmX32,
                       const __grid_constant__ CUtensorMap tmX16, const __grid_constant__ CUtensorMap tmC,
@@ -68,7 +88,7 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   unsigned char* sW = smem;                                   // [stages][128][128] int8
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kPairStageArea);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + int8_ring_bytes(EPI));
   uint64_t* full = bars;                    // [stages]  used in the even CTA
   uint64_t* empty = bars + kPairMaxStages;  // [stages]  one in each CTA (the commit reaches both)
   uint64_t* acc_full = bars + 2 * kPairMaxStages;  // [2]  one in each CTA
@@ -85,7 +105,7 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   if (threadIdx.x == 0) {
     ptx::mbar_init(tmem_ready, 1);
     for (int s = 0; s < kPairMaxStages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { ptx::mbar_init(&acc_full[b], 1); ptx::mbar_init(&acc_empty[b], 16); }
+    for (int b = 0; b < 2; ++b) { ptx::mbar_init(&acc_full[b], 1); ptx::mbar_init(&acc_empty[b], 2 * kI8EpiWarps); }
     *abort_flag = 0;
     ptx::fence_barrier_init();
     ptx::prefetch_tmap(&tmW);
@@ -93,7 +113,7 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   }
   // Operands and the list of tiles come from the kernels in front; tensor memory is taken only when those have let go of theirs, and
   // the next kernel's CTAs are let in only when these have got it.
-  pdl_wait();
+  if (a.early == 0) pdl_wait();
   ptx::cluster_start_sync();                                  // both CTAs run and their barriers are initialised
   uint32_t tmem_base = 0;
   if (warp != 0 && warp != 3) {
@@ -103,11 +123,14 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       if (rank == 1 && lane == 0) ptx::mbar_arrive_release_cluster(ptx::map_to_cta(ptx::smem_u32(tmem_ready), 0u));
     }
     ptx::tc_fence_before();
-    asm volatile("bar.sync 1, %0;" ::"n"(kPairThreads - 64) : "memory");
+    asm volatile("bar.sync 1, %0;" ::"n"(kI8Threads - 64) : "memory");
     ptx::tc_fence_after();
     tmem_base = *tmem_slot;
+    if (a.early != 0) pdl_wait();
     pdl_trigger();
-  }
+  } else if (a.early == 1 || warp == 3) {
+    if (a.early != 0) pdl_wait();
+  }                                                           // (the producer of early weights waits behind them)
 
   // tokens of a tile in the MMA's columns; each CTA stages half of them
   const bool listed = a.tiles != nullptr;
@@ -116,7 +139,7 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   auto tile_cols = [&](const TileDesc& td) { return listed ? (td.rows + kPairTokenStep - 1) & ~(kPairTokenStep - 1) : a.height; };
   auto tile_at = [&](int rt) {
     TileDesc td;
-    if (listed) {
+    if (listed) {                                              // (the list holds one entry at least)
       const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.tiles + rt));
       td.phys = raw.x; td.row0 = raw.y; td.rows = raw.z; td.slot = raw.w;
     } else {
@@ -125,12 +148,41 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     return td;
   };
   const int total = n_row_tiles * a.n_col_tiles;
-  const int n_stages = pair_stages(max_tokens), x_bytes = max_tokens / 2 * kI8BK;
+  auto at_step = [&](int t) {                                  // the tile of step t (behind the last step: any)
+    int rt = 0, ct_unused = 0;
+    if (t < total) decode_tile(t, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct_unused);
+    return tile_at(rt);
+  };
+  const int n_stages = int8_stages(EPI, max_tokens), x_bytes = max_tokens / 2 * kI8BK;
   unsigned char* sX = smem + n_stages * kPairABytes;          // [stages][max_tokens / 2][128] int8
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (both CTAs)
     const uint32_t full0 = ptx::map_to_cta(ptx::smem_u32(full), 0u);
+    auto load_w = [&](int stage, int kb, int phys, int ct) {
+      const uint32_t bar = full0 + 8u * (uint32_t)stage;
+      if (kSwiglu)
+        ptx::tma_load_5d_pair(sW + stage * kPairABytes, &tmW, bar, kb * kI8BK, 0, 0, ct * 8 + (int)rank * 4, phys);
+      else
+        ptx::tma_load_2d_pair(sW + stage * kPairABytes, &tmW, bar, kb * kI8BK, phys * a.w_rows + ct * 2 * kTcBM + (int)rank * kTcBM);
+    };
+    int pre = 0;                                              // k-blocks of the first tile whose weights are on their way
+    if (a.early == 2) {
+      if (pair < total) {
+        int rt, ct;
+        decode_tile(pair, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct);
+        const TileDesc td = tile_at(rt);
+        pre = min(a.k_blocks, n_stages);
+        for (int kb = 0; kb < pre; ++kb) {
+          if (ptx::elect_one()) {
+            if (rank == 0) ptx::mbar_expect_tx(&full[kb], (uint32_t)(2 * kPairABytes + tile_cols(td) * kI8BK));
+            load_w(kb, kb, td.phys, ct);
+          }
+          __syncwarp();
+        }
+      }
+      pdl_wait();
+    }
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -142,16 +194,16 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       const int xrow = td.row0 + (int)rank * half;
       const uint32_t bytes = (uint32_t)(2 * kPairABytes + cols * kI8BK);
       for (int kb = 0; kb < a.k_blocks; ++kb) {
-        ok = warp_wait<true>(&empty[stage], phase ^ 1u, abort_flag, status, 31);
-        if (!ok) break;
+        const bool early = t == pair && kb < pre;              // armed and weights requested above
+        if (!early) {
+          ok = warp_wait<true>(&empty[stage], phase ^ 1u, abort_flag, status, 31);
+          if (!ok) break;
+        }
         if (ptx::elect_one()) {
-          if (rank == 0) ptx::mbar_expect_tx(&full[stage], bytes);
+          if (rank == 0 && !early) ptx::mbar_expect_tx(&full[stage], bytes);
           const uint32_t bar = full0 + 8u * (uint32_t)stage;
           unsigned char* dst = sX + stage * x_bytes;
-          if (kSwiglu)
-            ptx::tma_load_5d_pair(sW + stage * kPairABytes, &tmW, bar, kb * kI8BK, 0, 0, ct * 8 + (int)rank * 4, td.phys);
-          else
-            ptx::tma_load_2d_pair(sW + stage * kPairABytes, &tmW, bar, kb * kI8BK, td.phys * a.w_rows + ct * 2 * kTcBM + (int)rank * kTcBM);
+          if (!early) load_w(stage, kb, td.phys, ct);
           if (half == 128) {
             ptx::tma_load_2d_pair(dst, &tmX128, bar, kb * kI8BK, xrow);
           } else {                                             // boxes of 64, 32 and 16 rows
@@ -176,10 +228,10 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
       uint32_t phase = 0, acc_phase = 0;
       bool ok = warp_wait<true>(tmem_ready, 0u, abort_flag, status, 35);
       ptx::tc_fence_after();
+      TileDesc ahead = at_step(pair);                          // (a tile's descriptor comes while the one before it is multiplied)
       for (int t = pair; t < total && ok; t += n_pairs) {
-        int rt, ct_unused;
-        decode_tile(t, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct_unused);
-        const uint32_t idesc = make_idesc_int8(2 * kTcBM, tile_cols(tile_at(rt)));
+        const uint32_t idesc = make_idesc_int8(2 * kTcBM, tile_cols(ahead));
+        ahead = at_step(t + n_pairs);
         ok = warp_wait<true>(&acc_empty[acc], acc_phase ^ 1u, abort_flag, status, 32);
         if (!ok) break;
         ptx::tc_fence_after();
@@ -207,77 +259,110 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
   } else if (warp >= 4) {
     // -------------------------------------------------------------------- epilogue (own 128 weight rows)
     const int q = warp & 3;                    // TMEM lane quarter this warp may read
-    const int part = (warp - 4) >> 2;          // two warps per quarter take turns with the chunks of 32 tokens
+    const int part = (warp - 4) >> 2;          // the warps of a quarter take turns with the chunks of tokens
     const int odd = lane & 1, hi = lane >> 4;
-    unsigned char* stg = smem + kPairStageArea + 1024 + (warp - 4) * int8_warp_bytes(EPI);
+    constexpr int kBox = int8_box_bytes(EPI);
+    unsigned char* const stg0 = smem + int8_ring_bytes(EPI) + 1024 + (warp - 4) * 2 * kBox;
+    float* s_scale = reinterpret_cast<float*>(smem + int8_ring_bytes(EPI) + 1024 + 2 * kI8EpiWarps * kBox) + (warp - 4) * kI8Chunk;
+    int box = 0;                               // which of the two is filled next
     const uint32_t acc_empty0 = ptx::map_to_cta(ptx::smem_u32(acc_empty), 0u);
     int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
-    for (int t = pair; t < total && ok; t += n_pairs) {
-      int rt, ct;
-      decode_tile(t, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct);
-      const TileDesc td = tile_at(rt);
-      // first of this warp's output columns (32; SwiGLU 16), and this lane's weight row
-      const int col0 = kSwiglu ? (ct * 8 + (int)rank * 4 + q) * 16 : ct * 2 * kTcBM + (int)rank * kTcBM + q * 32;
-      const int col = kSwiglu ? col0 + (lane & 15) : col0 + lane;
-      const bool col_ok = col0 < a.n_cols;
-      const int last = (td.rows - 1) >> 5;                   // the tile's last chunk
-      const int my_last = last - ((last ^ part) & 1);        // this warp's last one (-1: none)
-      // scales come while the tile's MMAs run, those of the tokens a chunk ahead
-      auto token_scale = [&](int c) {
-        const int token = 32 * c + lane;
-        return token < td.rows ? a.x_scales[td.row0 + token] : 0.f;
-      };
-      float w_scale = 0.f, bias = 0.f, next = token_scale(part);
+    // What a tile needs from memory comes while the tiles before it are worked on: its descriptor two steps ahead, its scales one.
+    struct Scales { float w, bias, token; };
+    auto col_of = [&](int t, int* col0) {                      // first of this warp's output columns (32; SwiGLU 16), and this lane's
+      int rt = 0, ct = 0;
+      if (t < total) decode_tile(t, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct);
+      *col0 = kSwiglu ? (ct * 8 + (int)rank * 4 + q) * 16 : ct * 2 * kTcBM + (int)rank * kTcBM + q * 32;
+      return kSwiglu ? *col0 + (lane & 15) : *col0 + lane;
+    };
+    auto token_scale = [&](const TileDesc& td, int c) {
+      const int token = kI8Chunk * c + (lane & (kI8Chunk - 1));
+      return token < td.rows ? a.x_scales[td.row0 + token] : 0.f;
+    };
+    auto scales_of = [&](int t, const TileDesc& td) {
+      Scales s = {0.f, 0.f, 0.f};
+      int col0;
+      const int col = col_of(t, &col0);
+      if (t >= total) return s;
+      s.token = token_scale(td, part);
       if (col < a.n_cols) {
-        w_scale = kSwiglu ? a.w_scales[((size_t)td.phys * 2 + hi) * a.n_cols + col] : a.w_scales[(size_t)td.phys * a.w_rows + col];
-        if (!kSwiglu && a.bias != nullptr) bias = a.bias[col];
+        s.w = kSwiglu ? a.w_scales[((size_t)td.phys * 2 + hi) * a.n_cols + col] : a.w_scales[(size_t)td.phys * a.w_rows + col];
+        if (!kSwiglu && a.bias != nullptr) s.bias = a.bias[col];
       }
+      return s;
+    };
+    TileDesc td_next = at_step(pair), td_after = at_step(pair + n_pairs);
+    Scales s_next = scales_of(pair, td_next);
+    for (int t = pair; t < total && ok; t += n_pairs) {
+      const TileDesc td = td_next;
+      const float w_scale = s_next.w, bias = s_next.bias;
+      float next = s_next.token;                             // scales of the tokens, a chunk ahead
+      td_next = td_after;
+      td_after = at_step(t + 2 * n_pairs);
+      s_next = scales_of(t + n_pairs, td_next);
+      int col0;
+      const int col = col_of(t, &col0);
+      const bool col_ok = col0 < a.n_cols;
+      const int last = (td.rows - 1) / kI8Chunk;             // the tile's last chunk
+      const int my_last = part <= last ? last - (last - part) % kI8EpiParts : -1;              // this warp's last one (-1: none)
       ok = warp_wait<true>(&acc_full[acc], acc_phase, abort_flag, status, 34);
       if (!ok) break;
       ptx::tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * kPairTokens);
-      if (my_last < 0 && lane == 0) ptx::mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)acc);
+      auto release = [&]() {
+        // last read of this accumulator: one arrival per warp on the even CTA's barrier, all warps' hand it back to the MMA issuer
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)acc);
+      };
+      uint32_t v[kI8Chunk];
+      __syncwarp();                                          // the tensor-memory load is one of the whole warp
+      if (my_last < 0) release();
+      else ptx::tmem_ld16(taddr + (uint32_t)(kI8Chunk * part), v);
 #pragma unroll 1
-      for (int c = part; c <= last; c += 2) {
-        const int t0 = 32 * c, left = td.rows - t0;          // valid tokens of this chunk (may exceed 32)
-        const float x_scale = next;
-        next = token_scale(c + 2);
-        uint32_t v[32];
-        __syncwarp();                                        // the tensor-memory load is one of the whole warp
-        ptx::tmem_ld32(taddr + (uint32_t)t0, v);
+      for (int c = part; c <= last; c += kI8EpiParts) {
+        const int t0 = kI8Chunk * c, left = td.rows - t0;    // valid tokens of this chunk (may exceed its size)
+        __syncwarp();                                        // the scales of the chunk before have been read
+        if (lane < kI8Chunk) s_scale[lane] = next;
+        next = token_scale(td, c + kI8EpiParts);
         ptx::tmem_ld_wait();
-        if (c == my_last) {
-          // last read of this accumulator: one arrival per warp on the even CTA's barrier, 16 hand it back to the MMA issuer
-          ptx::tc_fence_before();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)acc);
-        }
-        if (!col_ok) continue;
-        float f[32];
+        float f[kI8Chunk];
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-          f[j] = (float)(int)v[j] * w_scale * __shfl_sync(0xffffffffu, x_scale, j);
+        for (int j = 0; j < kI8Chunk; ++j) f[j] = (float)(int)v[j];
+        __syncwarp();
+        // the next chunk comes out of tensor memory while this one is worked on
+        if (c == my_last) release();
+        else ptx::tmem_ld16(taddr + (uint32_t)(t0 + kI8Chunk * kI8EpiParts), v);
+        if (!col_ok) continue;
+#pragma unroll
+        for (int j = 0; j < kI8Chunk; j += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(s_scale + j);
+          mul2(f[j], f[j + 1], w_scale, w_scale);
+          mul2(f[j], f[j + 1], x.x, x.y);
+          mul2(f[j + 2], f[j + 3], w_scale, w_scale);
+          mul2(f[j + 2], f[j + 3], x.z, x.w);
+        }
         if (kSwiglu) {
           // lanes l and l + 16 hold the two products of hidden unit l & 15: the lower one finishes token 2 i, the upper one token 2 i + 1
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          for (int i = 0; i < kI8Chunk / 2; ++i) {
             const float v0 = f[2 * i], v1 = f[2 * i + 1];
             const float r = __shfl_xor_sync(0xffffffffu, hi ? v0 : v1, 16);
             const float x1 = hi ? r : v0, x3 = hi ? v1 : r;
-            f[i] = silu_from_exp(x1, __expf(-x1)) * x3;
+            f[i] = __fdividef(x1, 1.f + __expf(-x1)) * x3;   // (two steps of 2^-23 at most: what follows has 8 bits)
           }
         } else {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
+          for (int j = 0; j < kI8Chunk; ++j) {
             f[j] += bias;
             if (EPI == kI8Relu) f[j] = f[j] < 0.f ? 0.f : f[j];                              // NaN stays NaN
           }
         }
         if (a.direct) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
+          for (int j = 0; j < kI8Chunk; ++j)
             if (!kSwiglu && j < left && col < a.n_cols) {
               const size_t at = (size_t)(td.row0 + t0 + j) * a.ldc + col;
               if (EPI == kI8Bf16) static_cast<bf16*>(a.C)[at] = __float2bfloat16_rn(f[j]);
@@ -285,30 +370,45 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
             }
           continue;
         }
-        // Boxes of 32 tokens leave through the TMA unit.  Rows of a listed tile up to the next multiple of 32 are stored with the valid
+        // Boxes of 16 tokens leave through the TMA unit.  Rows of a listed tile up to the next multiple of 16 are stored with the valid
         // ones: they lie in the slot's own segment, and nobody reads a row that no pair occupies.
-        if (lane == 0) ptx::tma_store_wait_read();
+        unsigned char* const stg = stg0 + box * kBox;
+        box ^= 1;
+        if (lane == 0) ptx::tma_store_wait_read_but_one();     // the box before the last one has left
         __syncwarp();
         if (kSwiglu) {
-          float* w = reinterpret_cast<float*>(stg) + hi * 16 + (lane & 15);    // [32 tokens][16 units]
+          float* w = reinterpret_cast<float*>(stg) + hi * 16 + (lane & 15);    // [16 tokens][16 units]
 #pragma unroll
-          for (int i = 0; i < 16; ++i) w[32 * i] = f[i];
+          for (int i = 0; i < kI8Chunk / 2; ++i) w[32 * i] = f[i];
         } else if (EPI == kI8Bf16) {
           // neighbouring lanes trade, so that each holds two output columns of one token
-          uint32_t* w = reinterpret_cast<uint32_t*>(stg) + odd * 16 + (lane >> 1);      // [32 tokens][32 columns]
+          uint32_t* w = reinterpret_cast<uint32_t*>(stg) + odd * 16 + (lane >> 1);      // [16 tokens][32 columns]
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          for (int i = 0; i < kI8Chunk / 2; ++i) {
             const float r = __shfl_xor_sync(0xffffffffu, odd ? f[2 * i] : f[2 * i + 1], 1);
             w[32 * i] = odd ? pack_bf16x2(r, f[2 * i + 1]) : pack_bf16x2(f[2 * i], r);
           }
         } else {
-          float* w = reinterpret_cast<float*>(stg) + lane;     // [32 tokens][32 columns]
+          float* w = reinterpret_cast<float*>(stg) + lane;     // [16 tokens][32 columns]
 #pragma unroll
-          for (int j = 0; j < 32; ++j) w[32 * j] = f[j];
+          for (int j = 0; j < kI8Chunk; ++j) w[32 * j] = f[j];
         }
         ptx::fence_proxy_async();                              // the staged box is read by the TMA unit
         __syncwarp();
         if (lane == 0) ptx::tma_store_2d(&tmC, stg, col0, td.row0 + t0);
+        if (EPI == kI8Relu || kSwiglu) {
+          // two lanes take a token over the box's columns
+          constexpr int kQuads = kSwiglu ? 2 : 4;
+          const float4* row = reinterpret_cast<const float4*>(stg) + lane * kQuads;
+          float most = 0.f;
+#pragma unroll
+          for (int i = 0; i < kQuads; ++i) {
+            const float4 u = row[i];
+            most = max_magnitude(max_magnitude(most, u.x, u.y), u.z, u.w);
+          }
+          most = max_magnitude(most, __shfl_xor_sync(0xffffffffu, most, 1), 0.f);
+          if (odd == 0 && lane / 2 < left) atomicMax(a.largest + td.row0 + t0 + lane / 2, __float_as_int(most) & 0x7fffffff);
+        }
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
@@ -355,7 +455,7 @@ inline int int8_gemm_init(int sm_count) {
       return 0;
     }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * (sm_count / 2)); cfg.blockDim = dim3(kPairThreads); cfg.dynamicSmemBytes = int8_smem_bytes(kI8F32);
+  cfg.gridDim = dim3(2 * (sm_count / 2)); cfg.blockDim = dim3(kI8Threads); cfg.dynamicSmemBytes = int8_smem_bytes(kI8F32);
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;

@@ -15,12 +15,14 @@
 #include "common.cuh"
 #include "expert_bank.cuh"
 #include "int8_gemm.cuh"
+#include "int8_split.cuh"
+#include "int8_stream.cuh"
 #include "quantize_rows.cuh"
 
 using namespace swapmoe;
 
 static_assert(SWAPMOE_NORM_MAX_WIDTH == kNormMaxWidth && SWAPMOE_QUANTIZE_MAX_WIDTH == kQuantMaxWidth, "the header's limits");
-static_assert(SWAPMOE_QUANTIZE_NONE == kQuantNone && SWAPMOE_QUANTIZE_RELU == kQuantRelu && SWAPMOE_QUANTIZE_SWIGLU == kQuantSwiglu, "the header's values");
+static_assert((int)SWAPMOE_QUANTIZE_NONE == (int)kQuantNone && (int)SWAPMOE_QUANTIZE_RELU == (int)kQuantRelu && (int)SWAPMOE_QUANTIZE_SWIGLU == (int)kQuantSwiglu, "the header's values");
 static_assert(SWAPMOE_MATMUL_MAX_K == kI8MaxK, "the header's limit");
 
 namespace {
@@ -52,7 +54,11 @@ int32_t current_device(Device* d) {
   if (major != 10) return SWAPMOE_ERR_UNSUPPORTED;       // kernels are built for sm_100a only
   std::lock_guard<std::mutex> hold(lock);
   const int pairs = int8_gemm_init(sms);
-  if (pairs < 1) return SWAPMOE_ERR_CUDA;
+  if (pairs < 1 || cudaFuncSetAttribute(int8_split_kernel<bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitMaxSmem) != cudaSuccess ||
+      cudaFuncSetAttribute(int8_split_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitMaxSmem) != cudaSuccess) {
+    cudaGetLastError();
+    return SWAPMOE_ERR_CUDA;
+  }
   known[dev] = Device{dev, sms, pairs};
   ready[dev].store(true, std::memory_order_release);
   *d = known[dev];
@@ -144,9 +150,10 @@ struct swapmoe_expert_bank {
   char* ws;
   long long max_rows;                      // rows of the pairs with the slots' padding
   int8_t *rows8, *h8;
-  float *row_scales, *h, *h_scales, *y;
-  int32_t *row_pair, *pair_row, *counts, *cta_base, *n_tiles;
+  float *row_scales, *h, *h_scales, *y, *largest;
+  int32_t *row_pair, *pair_row, *row_largest, *counts, *cta_base, *n_tiles;
   TileDesc* tiles;
+  const int8_t *w_in, *w_out;
   const float *in_scales, *out_scales;
   bool bound;
   CUtensorMap map_in, map_out, map_x[4], map_h[4], map_h_out, map_y_out;
@@ -185,12 +192,66 @@ int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t s
     if (!(half & (128 >> i))) mx[i] = mx[have];              // not used
   if (g.direct) mc = mw;                                     // not used
   else if (!int8_encode_2d(enc, &mc, p.out, p.dtype == SWAPMOE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, elem,
-                           p.n_tokens, p.n, p.out_stride, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE))
+                           p.n_tokens, p.n, p.out_stride, 32, kI8Chunk, CU_TENSOR_MAP_SWIZZLE_NONE))
     return SWAPMOE_ERR_CUDA;
   const int epi = p.dtype == SWAPMOE_BF16 ? kI8Bf16 : kI8F32;
   const long long work = (long long)((p.n_tokens + g.height - 1) / g.height) * g.n_col_tiles;
-  return launched(launch_kernel(int8_gemm_kernel(epi), dim3(2 * (work > dev.pairs ? dev.pairs : (int)work)), dim3(kPairThreads),
+  return launched(launch_kernel(int8_gemm_kernel(epi), dim3(2 * (work > dev.pairs ? dev.pairs : (int)work)), dim3(kI8Threads),
                                 int8_smem_bytes(epi), st, pdl, mw, mx[0], mx[1], mx[2], mx[3], mc, g));
+}
+
+// The same for up to kSplitMaxTokens tokens, a cluster for each 128 rows of weights.
+int32_t matmul_split(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t st, bool pdl) {
+  const PFN_encodeTiled enc = encoder();
+  if (!enc) return SWAPMOE_ERR_CUDA;
+  I8SplitArgs g;
+  g.out = p.out; g.x_scales = p.x_scales; g.w_scales = p.w_scales; g.bias = p.bias; g.ldc = p.out_stride;
+  g.T = p.n_tokens; g.N = p.n; g.k_blocks = (p.k + kI8BK - 1) / kI8BK;
+  const int tiles = (p.n + kTcBM - 1) / kTcBM;
+  // One CTA an SM at most, with two k-blocks at least; a cluster of eight only where a quarter of the columns would leave half the SMs idle
+  // and still be sixteen k-blocks.  us at 1 / 2 / 4 / 8 CTAs, 16 and 64 tokens: 4096 x 4096 9.0 / 6.9 / 5.7 / 6.8 and 12.0 / 9.4 / 7.6 / 9.0;
+  // 4096 -> 1024 8.3 / 5.7 / 4.1 / 3.8 and 9.8 / 7.5 / 5.5 / 4.7; 1024 x 1024 3.6 / 3.3 / 2.9 / 3.4 and 4.9 / 5.1 / 4.2 / 4.3.
+  int cluster = 1;
+  while (cluster < 4 && 2 * cluster * tiles <= dev.sms && 4 * cluster <= g.k_blocks) cluster *= 2;
+  if (cluster == 4 && 16 * tiles <= dev.sms && g.k_blocks >= 32) cluster = 8;
+  const int step = std::max(16, 4 * cluster);
+  g.cols = (p.n_tokens + step - 1) / step * step;
+  g.share = (g.k_blocks + cluster - 1) / cluster;
+  const int stage = kSplitABytes + g.cols * kI8BK;
+  g.n_stages = std::max(1, std::min(std::min(g.share, kSplitMaxStages), kSplitRoom / stage));
+  const long long xs = p.n_tokens > 1 ? p.x_stride : (p.k + 15) / 16 * 16, ws = p.n > 1 ? p.w_stride : (p.k + 15) / 16 * 16;
+  CUtensorMap mw, mx;
+  if (!int8_encode_operand(enc, &mw, p.w, p.n, p.k, ws, 128) || !int8_encode_operand(enc, &mx, p.x, p.n_tokens, p.k, xs, g.cols)) return SWAPMOE_ERR_CUDA;
+  const size_t smem = 1024 + int8_split_area(g.cols, g.n_stages);
+  const dim3 grid(tiles * cluster), block(kSplitThreads);
+  return launched(p.dtype == SWAPMOE_BF16 ? launch_cluster(int8_split_kernel<bf16>, cluster, grid, block, smem, st, pdl, mw, mx, g)
+                                          : launch_cluster(int8_split_kernel<float>, cluster, grid, block, smem, st, pdl, mw, mx, g));
+}
+
+// The same for up to kStreamTokens tokens.
+int32_t matmul_stream(const swapmoe_matmul_t& p, cudaStream_t st, bool pdl) {
+  I8StreamArgs a;
+  a.x = static_cast<const int8_t*>(p.x); a.w = static_cast<const int8_t*>(p.w);
+  a.x_scales = p.x_scales; a.w_scales = p.w_scales; a.bias = p.bias; a.out = p.out;
+  a.x_stride = p.x_stride; a.w_stride = p.w_stride; a.out_stride = p.out_stride;
+  a.T = p.n_tokens; a.K = p.k; a.N = p.n;
+  const dim3 grid((p.n + 15) / 16), block(kStreamThreads);
+  return launched(p.dtype == SWAPMOE_BF16 ? launch_kernel(int8_stream_kernel<bf16>, grid, block, 0, st, pdl, a)
+                                          : launch_kernel(int8_stream_kernel<float>, grid, block, 0, st, pdl, a));
+}
+
+// Experts of few pairs.
+template <typename T, int kN>
+cudaError_t bank_stream(const BankStreamArgs& a, bool swiglu, int slots, cudaStream_t st, bool pdl) {
+  const dim3 grid(a.F / 16, slots), block(kStreamThreads);
+  const cudaError_t e = swiglu ? launch_kernel(bank_stream_in_kernel<true, kN>, grid, block, 0, st, pdl, a)
+                               : launch_kernel(bank_stream_in_kernel<false, kN>, grid, block, 0, st, pdl, a);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(bank_stream_out_kernel<T, kN>, dim3(a.d / 16), dim3(kBankOutThreads), 0, st, pdl, a);
+}
+template <typename T>
+cudaError_t bank_stream(const BankStreamArgs& a, bool swiglu, int slots, cudaStream_t st, bool pdl) {
+  return a.P <= 8 ? bank_stream<T, 1>(a, swiglu, slots, st, pdl) : bank_stream<T, 2>(a, swiglu, slots, st, pdl);
 }
 
 }  // namespace
@@ -235,7 +296,16 @@ int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* p, void* stream) {
   Device dev;
   const int32_t rc = current_device(&dev);
   if (rc != SWAPMOE_OK) return rc;
-  return matmul_pair(*p, dev, static_cast<cudaStream_t>(stream), standalone_pdl());
+  // Few tokens and a small matrix: the weights straight to registers.  Few tokens, or few tiles: the contraction shared.  us for 8 tokens,
+  // registers / shared: 1024 x 1024 2.2 / 3.0, 2048 x 2048 2.7 / 4, 4096 -> 1024 3.9 / 3.7, 4096 x 4096 6.2 / 5.7, 4096 -> 14336 15.8 / 11.9.
+  // Shared / CTA pairs at 32, 64, 96, 128 tokens: 4096 x 4096 6.1 / 9.9, 7.1 / 10.2, 8.4 / 10.5, 9.4 / 10.6; 1024 -> 4096 3.6 / 4.8, 4.3 / 5.1,
+  // 5.4 / 5.4, 6.4 / 5.4; 4096 -> 14336 12.5 / 12.5, 14.4 / 12.8, 16.2 / 13.1, 17.0 / 13.4.
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (p->n_tokens <= kStreamTokens && p->k <= 2048 && (long long)p->k * p->n <= 6ll << 20) return matmul_stream(*p, st, standalone_pdl());
+  const int tiles = (p->n + kTcBM - 1) / kTcBM;
+  const int shared = 4 * tiles <= dev.sms ? (p->k >= 2048 ? kSplitMaxTokens : 96) : 2 * tiles <= dev.sms ? 64 : 32;
+  if (p->n_tokens <= shared) return matmul_split(*p, dev, st, standalone_pdl());
+  return matmul_pair(*p, dev, st, standalone_pdl());
 }
 
 int32_t swapmoe_matmul_status(int32_t* detail, void* stream) {
@@ -279,7 +349,8 @@ int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_ex
       {reinterpret_cast<void**>(&b->rows8), R * d}, {reinterpret_cast<void**>(&b->h8), R * f},
       {reinterpret_cast<void**>(&b->h), R * f * 4}, {reinterpret_cast<void**>(&b->y), R * d * 4},
       {reinterpret_cast<void**>(&b->row_scales), R * 4}, {reinterpret_cast<void**>(&b->h_scales), R * 4},
-      {reinterpret_cast<void**>(&b->row_pair), R * 4}, {reinterpret_cast<void**>(&b->pair_row), (size_t)P * 4},
+      {reinterpret_cast<void**>(&b->row_pair), R * 4}, {reinterpret_cast<void**>(&b->row_largest), R * 4}, {reinterpret_cast<void**>(&b->pair_row), (size_t)P * 4},
+      {reinterpret_cast<void**>(&b->largest), (size_t)kStreamMaxPairs * (f / 16) * 4},
       {reinterpret_cast<void**>(&b->counts), kBankMaxSlots * 4}, {reinterpret_cast<void**>(&b->cta_base), (size_t)kBankMaxCtas * c.n_slots * 4},
       {reinterpret_cast<void**>(&b->n_tiles), 16}, {reinterpret_cast<void**>(&b->tiles), n_tiles * sizeof(TileDesc)}};
   size_t bytes = 0;
@@ -297,8 +368,8 @@ int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_ex
   bool ok = cudaMemset(b->counts, 0, kBankMaxSlots * 4) == cudaSuccess;
   for (int i = 0; i < 4; ++i)
     ok = ok && int8_encode_operand(enc, &b->map_x[i], b->rows8, R, d, d, 128 >> i) && int8_encode_operand(enc, &b->map_h[i], b->h8, R, f, f, 128 >> i);
-  ok = ok && int8_encode_2d(enc, &b->map_h_out, b->h, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, f, f, nin == 2 ? 16 : 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE) &&
-       int8_encode_2d(enc, &b->map_y_out, b->y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, d, d, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
+  ok = ok && int8_encode_2d(enc, &b->map_h_out, b->h, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, f, f, nin == 2 ? 16 : 32, kI8Chunk, CU_TENSOR_MAP_SWIZZLE_NONE) &&
+       int8_encode_2d(enc, &b->map_y_out, b->y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, d, d, 32, kI8Chunk, CU_TENSOR_MAP_SWIZZLE_NONE);
   if (!ok) {
     cudaGetLastError();
     swapmoe_expert_bank_destroy(b);
@@ -337,6 +408,7 @@ int32_t swapmoe_expert_bank_set_weights(swapmoe_expert_bank_t* b, const void* w_
     return SWAPMOE_ERR_CUDA;
   }
   if (!int8_encode_operand(enc, &outm, w_out, S * d, f, f, 128)) return SWAPMOE_ERR_CUDA;
+  b->w_in = static_cast<const int8_t*>(w_in); b->w_out = static_cast<const int8_t*>(w_out);
   b->map_in = in; b->map_out = outm; b->in_scales = in_scales; b->out_scales = out_scales;
   b->bound = true;
   return SWAPMOE_OK;
@@ -361,9 +433,20 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool pdl = standalone_pdl(), swiglu = c.act == SWAPMOE_ACT_SWIGLU;
   const int P = T * c.top_k, pairs = b->dev.pairs;
+  // Few pairs on small experts: two launches that take the weights straight to registers.  us, that form / the general one: 1024 x 512 top-4
+  // 4 pairs 6.9 / 17, 16 pairs 16.5 / 19; 2048 x 1024 4 pairs 12.6 / 18, 8 pairs 19.6 / 21; 1024 x 4096 2 pairs 16 / 17, 4 pairs 25.7 / 22.
+  if (P <= kStreamMaxPairs && 3ll * P * c.d_model * c.d_ff <= 25ll << 20) {
+    BankStreamArgs q;
+    q.x8 = static_cast<const int8_t*>(x); q.w_in = b->w_in; q.w_out = b->w_out; q.x_scales = x_scales; q.in_scales = b->in_scales;
+    q.out_scales = b->out_scales; q.weights = weights; q.slots = slots; q.h = b->h; q.largest = b->largest; q.out = out;
+    q.x_stride = x_stride; q.out_stride = out_stride; q.P = P; q.S = c.n_slots; q.k = c.top_k; q.d = c.d_model; q.F = c.d_ff; q.T = T;
+    const int most = std::min(P, c.n_slots);
+    return launched(c.dtype == SWAPMOE_BF16 ? bank_stream<bf16>(q, swiglu, most, st, pdl) : bank_stream<float>(q, swiglu, most, st, pdl));
+  }
   BankArgs a;
-  a.x8 = static_cast<const int8_t*>(x); a.x_scales = x_scales; a.slots = slots; a.weights = weights; a.rows8 = b->rows8; a.row_scales = b->row_scales;
-  a.row_pair = b->row_pair; a.pair_row = b->pair_row; a.counts = b->counts; a.cta_base = b->cta_base; a.tiles = b->tiles; a.n_tiles = b->n_tiles;
+  a.x8 = static_cast<const int8_t*>(x); a.x_scales = x_scales; a.slots = slots; a.rows8 = b->rows8; a.row_scales = b->row_scales;
+  a.row_pair = b->row_pair; a.pair_row = b->pair_row; a.largest = b->row_largest; a.counts = b->counts; a.cta_base = b->cta_base; a.tiles = b->tiles;
+  a.n_tiles = b->n_tiles;
   a.x_stride = x_stride; a.P = P; a.S = c.n_slots; a.k = c.top_k; a.d = c.d_model;
   a.direct = P <= kBankDirectPairs;
   // eight pairs a CTA (one per warp) where that makes no more CTAs than run at once
@@ -378,31 +461,33 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   const long long rows = std::min<long long>(b->max_rows, (P + 31ll * std::min(P, c.n_slots) + 31) / 32 * 32);
   const long long max_tiles = (P + 63) / 64 + std::min(P, c.n_slots);
   I8GemmArgs g = {};
-  g.tiles = b->tiles; g.n_tiles = b->n_tiles; g.row_group = 1 << 30; g.height = 256;
-  g.C = b->h; g.x_scales = b->row_scales; g.w_scales = b->in_scales; g.ldc = c.d_ff; g.n_cols = c.d_ff;
+  g.tiles = b->tiles; g.n_tiles = b->n_tiles; g.row_group = 1 << 30; g.height = 256; g.early = 1;
+  g.C = b->h; g.x_scales = b->row_scales; g.w_scales = b->in_scales; g.ldc = c.d_ff; g.n_cols = c.d_ff; g.largest = b->row_largest;
   g.n_col_tiles = (c.d_ff + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); g.k_blocks = (c.d_model + kI8BK - 1) / kI8BK; g.w_rows = c.d_ff;
-  int epi = swiglu ? kI8Swiglu : kI8Relu;
+  const int epi = swiglu ? kI8Swiglu : kI8Relu;
   long long work = max_tiles * g.n_col_tiles;
   if (e == cudaSuccess)
-    e = launch_kernel(int8_gemm_kernel(epi), dim3(2 * (unsigned)std::min<long long>(work, pairs)), dim3(kPairThreads), int8_smem_bytes(epi), st, pdl,
+    e = launch_kernel(int8_gemm_kernel(epi), dim3(2 * (unsigned)std::min<long long>(work, pairs)), dim3(kI8Threads), int8_smem_bytes(epi), st, pdl,
                       b->map_in, b->map_x[0], b->map_x[1], b->map_x[2], b->map_x[3], b->map_h_out, g);
-  QuantizeArgs q = {};
-  q.x = b->h; q.out8 = reinterpret_cast<uint8_t*>(b->h8); q.scales = b->h_scales; q.row_pair = b->row_pair; q.n_rows = b->n_tiles + 2;
-  q.x_stride = q.out8_stride = c.d_ff; q.T = (int)rows; q.d = c.d_ff; q.act = kQuantNone;
-  if (e == cudaSuccess) e = quantize_rows_launch<float>(q, true, b->dev.sms, st, pdl);
-  g.C = b->y; g.x_scales = b->h_scales; g.w_scales = b->out_scales; g.ldc = c.d_model; g.n_cols = c.d_model;
+  BankQuantizeArgs q;
+  q.h = b->h; q.largest = b->row_largest; q.row_pair = b->row_pair; q.pair_row = b->pair_row; q.n_tiles = b->n_tiles;
+  q.h8 = reinterpret_cast<uint8_t*>(b->h8); q.h_scales = b->h_scales;
+  const int turns = c.d_ff < 1024 ? 4 : 8;
+  q.F = c.d_ff; q.by_pair = P < rows / 2; q.n = q.by_pair ? P : (int)rows; q.parts = (c.d_ff + 128 * turns - 1) / (128 * turns);
+  const dim3 units((unsigned)(((long long)q.n * q.parts + kBankThreads / 32 - 1) / (kBankThreads / 32)));
+  if (e == cudaSuccess)
+    e = turns == 4 ? launch_kernel(bank_quantize_kernel<4>, units, dim3(kBankThreads), 0, st, pdl, q)
+                   : launch_kernel(bank_quantize_kernel<8>, units, dim3(kBankThreads), 0, st, pdl, q);
+  g.C = b->y; g.x_scales = b->h_scales; g.w_scales = b->out_scales; g.ldc = c.d_model; g.n_cols = c.d_model; g.largest = nullptr; g.early = 2;
   g.n_col_tiles = (c.d_model + 255) / 256; g.k_blocks = (c.d_ff + kI8BK - 1) / kI8BK; g.w_rows = c.d_model;
   work = max_tiles * g.n_col_tiles;
   if (e == cudaSuccess)
-    e = launch_kernel(int8_gemm_kernel(kI8F32), dim3(2 * (unsigned)std::min<long long>(work, pairs)), dim3(kPairThreads), int8_smem_bytes(kI8F32), st,
+    e = launch_kernel(int8_gemm_kernel(kI8F32), dim3(2 * (unsigned)std::min<long long>(work, pairs)), dim3(kI8Threads), int8_smem_bytes(kI8F32), st,
                       pdl, b->map_out, b->map_h[0], b->map_h[1], b->map_h[2], b->map_h[3], b->map_y_out, g);
   BankCombineArgs m;
   m.y = b->y; m.pair_row = b->pair_row; m.weights = weights; m.counts = b->counts; m.out = out; m.out_stride = out_stride;
-  m.T = T; m.k = c.top_k; m.d = c.d_model; m.S = c.n_slots; m.vec = rows_aligned(out, T, out_stride, elem, elem * 4);
-  const dim3 grid(T, (c.d_model + 1023) / 1024);
-  if (e == cudaSuccess)
-    e = c.dtype == SWAPMOE_BF16 ? launch_kernel(bank_combine_kernel<bf16>, grid, dim3(256), 0, st, pdl, m)
-                                : launch_kernel(bank_combine_kernel<float>, grid, dim3(256), 0, st, pdl, m);
+  m.T = T; m.k = c.top_k; m.d = c.d_model; m.S = c.n_slots; m.vec = rows_aligned(out, T, out_stride, elem, 4 * elem);
+  if (e == cudaSuccess) e = c.dtype == SWAPMOE_BF16 ? bank_combine_launch<bf16>(m, st, pdl) : bank_combine_launch<float>(m, st, pdl);
   return launched(e);
 }
 

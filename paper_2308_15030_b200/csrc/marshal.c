@@ -116,18 +116,24 @@ done:
   return rc;
 }
 
-/* At least n_rows rows of `width` contiguous values of `dtype`; a vector stands for rows of one value. */
-static int rows(Call* c, PyObject* t, const char* name, PyObject* dtype, int64_t n_rows, int64_t width, void** p, int64_t* row_stride) {
-  int dims;
-  int64_t size[2], stride[2];
-  if (type_is(c, t, name, dtype) || sizes(c, t, name, &dims, size, stride) || place(c, t, name, p)) return -1;
-  if (dims == 1) { size[1] = 1; stride[1] = 1; }
+/* At least n_rows rows of `width` contiguous values of `dtype`, whose shape and strides have been read; a vector stands for rows of one
+ * value. */
+static int rows_read(Call* c, PyObject* t, const char* name, PyObject* dtype, int dims, const int64_t given_size[2],
+                     const int64_t given_stride[2], int64_t n_rows, int64_t width, void** p, int64_t* row_stride) {
+  const int64_t size[2] = {given_size[0], dims == 1 ? 1 : given_size[1]}, stride[2] = {given_stride[0], dims == 1 ? 1 : given_stride[1]};
+  if (type_is(c, t, name, dtype) || place(c, t, name, p)) return -1;
   if ((dims == 1 && width != 1) || size[0] < n_rows || size[1] != width || (width > 1 && stride[1] != 1))
     return refuse(c, SWAPMOE_ERR_INVALID_ARG, "%s: [%lld, %lld] with contiguous rows expected, got [%lld, %lld], strides (%lld, %lld)",
                   name, (long long)n_rows, (long long)width, (long long)size[0], (long long)size[1], (long long)stride[0],
                   (long long)stride[1]);
   *row_stride = size[0] > 1 || stride[0] > width ? stride[0] : width;
   return 0;
+}
+static int rows(Call* c, PyObject* t, const char* name, PyObject* dtype, int64_t n_rows, int64_t width, void** p, int64_t* row_stride) {
+  int dims;
+  int64_t size[2], stride[2];
+  if (sizes(c, t, name, &dims, size, stride)) return -1;
+  return rows_read(c, t, name, dtype, dims, size, stride, n_rows, width, p, row_stride);
 }
 
 /* n contiguous values of `dtype`. */
@@ -334,7 +340,7 @@ static PyObject* py_block_norm(PyObject* self, PyObject* const* v, Py_ssize_t n)
   a.n_rows = (int32_t)T; a.d = (int32_t)d; a.group = (int32_t)group; a.eps = (float)eps; a.post_eps = (float)post_eps; a.scale = (float)scale;
   a.residual_dtype = a.dtype;
   void* p;
-  if (rows(&c, x, "x", dtype, T, d, &p, &a.x_stride)) return NULL;
+  if (rows_read(&c, x, "x", dtype, dims, size, stride, T, d, &p, &a.x_stride)) return NULL;
   a.x = p;
   rdtype = dtype;
   if (residual != Py_None) {
@@ -400,7 +406,7 @@ static PyObject* py_quantize_rows(PyObject* self, PyObject* const* v, Py_ssize_t
   if (act == SWAPMOE_QUANTIZE_SWIGLU && width % 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x: an even number of columns expected"); return NULL; }
   a.n_rows = (int32_t)T; a.d = (int32_t)d; a.act = (int32_t)act;
   void* p;
-  if (rows(&c, x, "x", dtype, T, width, &p, &a.x_stride)) return NULL;
+  if (rows_read(&c, x, "x", dtype, dims, size, stride, T, width, &p, &a.x_stride)) return NULL;
   a.x = p;
   if (rows(&c, out8, "out8", d_i8, T, d, &a.out8, &a.out8_stride) || vector(&c, scales, "scales", d_f32, T, &p)) return NULL;
   a.scales = (float*)p;
@@ -421,19 +427,19 @@ static PyObject* py_matmul_scaled(PyObject* self, PyObject* const* v, Py_ssize_t
   swapmoe_matmul_t a = {0};
   PyObject *x = v[0], *w = v[2], *out = v[4], *dtype;
   int dims;
-  int64_t xsize[2], wsize[2], stride[2];
-  if (sizes(&c, x, "x8", &dims, xsize, stride)) return NULL;
+  int64_t xsize[2], wsize[2], xstride[2], wstride[2];
+  if (sizes(&c, x, "x8", &dims, xsize, xstride)) return NULL;
   if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x8: [T, K] expected"); return NULL; }
-  if (sizes(&c, w, "w8", &dims, wsize, stride)) return NULL;
+  if (sizes(&c, w, "w8", &dims, wsize, wstride)) return NULL;
   if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "w8: [N, K] expected"); return NULL; }
   const int64_t T = xsize[0], K = xsize[1], N = wsize[0];
   a.n_tokens = (int32_t)T; a.k = (int32_t)K; a.n = (int32_t)N;
   void* p;
-  if (rows(&c, x, "x8", d_i8, T, K, &p, &a.x_stride)) return NULL;
+  if (rows_read(&c, x, "x8", d_i8, 2, xsize, xstride, T, K, &p, &a.x_stride)) return NULL;
   a.x = p;
   if (vector(&c, v[1], "x_scales", d_f32, T, &p)) return NULL;
   a.x_scales = (const float*)p;
-  if (rows(&c, w, "w8", d_i8, N, K, &p, &a.w_stride)) return NULL;
+  if (rows_read(&c, w, "w8", d_i8, 2, wsize, wstride, N, K, &p, &a.w_stride)) return NULL;
   a.w = p;
   if (vector(&c, v[3], "w_scales", d_f32, N, &p)) return NULL;
   a.w_scales = (const float*)p;
@@ -468,7 +474,7 @@ static PyObject* py_experts_forward(PyObject* self, PyObject* const* v, Py_ssize
   if (dims != 2) { refuse(&c, SWAPMOE_ERR_INVALID_ARG, "x8: [T, d_model] expected"); return NULL; }
   const int64_t T = size[0];
   c.device = (long)device;
-  if (rows(&c, x, "x8", d_i8, T, d, &xp, &xs) || vector(&c, v[6], "x_scales", d_f32, T, &xsp) || vector(&c, v[7], "slots", d_i32, T * k, &sp) ||
+  if (rows_read(&c, x, "x8", d_i8, 2, size, stride, T, d, &xp, &xs) || vector(&c, v[6], "x_scales", d_f32, T, &xsp) || vector(&c, v[7], "slots", d_i32, T * k, &sp) ||
       vector(&c, v[8], "weights", d_f32, T * k, &wp) || rows(&c, out, "out", dtype, T, d, &op, &os))
     return NULL;
   if (begin(&c, v[10], &st, &back)) return NULL;
