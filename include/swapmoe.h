@@ -491,8 +491,14 @@ int32_t swapmoe_set_gate(swapmoe_layer_t* layer, const swapmoe_gate_t* gate, con
  * behind the norm (max_tokens * d_model values) on the first call.  Errors: INVALID_ARG, UNSUPPORTED, NO_MEMORY. */
 int32_t swapmoe_set_norm(swapmoe_layer_t* layer, const void* weight_dev, float eps);
 
-/* A pre-norm block: residual += x (rounded to the layer's dtype); n = norm(residual before rounding) * weight;
- * out = layer(n), plus scale * B (A n) of each token's adapter.  residual_dev [n_tokens, d_model] is updated in place; NULL:
+/* The norm behind the block in front, with that block's gate and residual scale, for layers whose x is a block's output (sandwich
+ * norms): later swapmoe_forward_block calls add scale * gate * x * weight / sqrt(mean(x^2) + eps) to the residual instead of x, as
+ * swapmoe_block_norm does.  weight_dev, gate_dev [d_model] in the layer's dtype or NULL, not copied; both NULL with scale = 1 returns to the plain
+ * addition.  Host state only: takes effect for forwards enqueued after the call.  Errors: INVALID_ARG. */
+int32_t swapmoe_set_post_norm(swapmoe_layer_t* layer, const void* weight_dev, float eps, const void* gate_dev, float scale);
+
+/* A pre-norm block: residual += x (rounded to the layer's dtype; with swapmoe_set_post_norm what that says); n = norm(residual before
+ * rounding) * weight; out = layer(n), plus scale * B (A n) of each token's adapter.  residual_dev [n_tokens, d_model] is updated in place; NULL:
  * n = norm(x).  adapters and ids_dev [n_tokens] both or neither; the bank has d_in = d_out = d_model and the layer's
  * dtype.  Nothing is enqueued if the call is refused.  No two of x, residual and out may overlap.  Errors: as
  * swapmoe_forward, and NOT_READY without a norm or without the bank's weights, INVALID_ARG for a bank of another shape. */

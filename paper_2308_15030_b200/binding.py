@@ -41,7 +41,7 @@ EXPORTS = [
     "swapmoe_read_scores_async", "swapmoe_read_decode_prefetch",
     "swapmoe_rms_norm", "swapmoe_route",
     "swapmoe_adapters_create", "swapmoe_adapters_destroy", "swapmoe_adapters_set_weights", "swapmoe_adapters_forward",
-    "swapmoe_adapters_check", "swapmoe_set_gate", "swapmoe_set_norm", "swapmoe_forward_block",
+    "swapmoe_adapters_check", "swapmoe_set_gate", "swapmoe_set_norm", "swapmoe_set_post_norm", "swapmoe_forward_block",
     "swapmoe_block_norm", "swapmoe_quantize_rows", "swapmoe_matmul_scaled", "swapmoe_matmul_status",
     "swapmoe_expert_bank_create", "swapmoe_expert_bank_destroy", "swapmoe_expert_bank_set_weights", "swapmoe_expert_bank_forward",
 ]
@@ -161,6 +161,7 @@ def lib() -> ctypes.CDLL:
         L.swapmoe_adapters_check.argtypes = [vp, i32, i32, i32, i32]
         L.swapmoe_set_gate.argtypes = [vp, ctypes.POINTER(Gate), vp]
         L.swapmoe_set_norm.argtypes = [vp, vp, ctypes.c_float]
+        L.swapmoe_set_post_norm.argtypes = [vp, vp, ctypes.c_float, vp, ctypes.c_float]
         L.swapmoe_forward_block.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp]
         L.swapmoe_rms_norm.argtypes = [ctypes.POINTER(RmsNormArgs), vp]
         L.swapmoe_block_norm.argtypes = [ctypes.POINTER(BlockNormArgs), vp]
@@ -510,10 +511,21 @@ class Layer:
         _check(lib().swapmoe_set_norm(self._h, pw, eps), where)
         self._keep["norm"] = weight
 
+    def set_post_norm(self, weight=None, eps: float = 1e-6, gate=None, scale: float = 1.0) -> None:
+        """For layers whose x is a block's output: forward_block then adds scale * gate * norm(x) to the residual instead of x, with the norm's
+        ``weight`` [d_model] (None: x itself) and ``gate`` [d_model] (None: 1) in the layer's dtype on its device, not copied.  Without
+        arguments: the plain addition again."""
+        import torch
+        where, dt = "swapmoe_set_post_norm", torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
+        pw = None if weight is None else _vector(weight, self.cfg.d_model, dt, self._device, where, "weight")
+        pg = None if gate is None else _vector(gate, self.cfg.d_model, dt, self._device, where, "gate")
+        _check(lib().swapmoe_set_post_norm(self._h, pw, eps, pg, scale), where)
+        self._keep["post_norm"] = (weight, gate)
+
     # -- hot path
     def forward_block(self, x, residual, out, adapters: Optional[AdapterBank] = None, ids=None, n_tokens: Optional[int] = None,
                       stream=None) -> None:
-        """The pre-norm block around the layer: residual += x (None: no residual); out = layer(norm(residual)), plus each
+        """The pre-norm block around the layer: residual += x (None: no residual; set_post_norm: x normed, gated and scaled); out = layer(norm(residual)), plus each
         token's adapter from ``adapters`` by ``ids`` [T] int32 (negative: none).  Rows [T, d_model] of the layer's dtype,
         contiguous, on the layer's device, which has to be the current one."""
         import torch

@@ -60,6 +60,9 @@ struct swapmoe_layer {
   const float* gate_bias;
   const void* norm_weight;     // swapmoe_set_norm, or nullptr
   float norm_eps;
+  bool post_norm;              // swapmoe_set_post_norm has given what follows
+  const void *post_weight, *post_gate;
+  float post_eps, post_scale;
   void* x_norm;                // [max_tokens, d_model] rows behind the norm (allocated by swapmoe_set_norm)
   bool router_set, resident_set;
   int32_t h_s2e[kMaxSlots], h_phys[kMaxSlots];
@@ -858,6 +861,15 @@ int32_t swapmoe_set_norm(swapmoe_layer_t* L, const void* weight_dev, float eps) 
   return SWAPMOE_OK;
 }
 
+int32_t swapmoe_set_post_norm(swapmoe_layer_t* L, const void* weight_dev, float eps, const void* gate_dev, float scale) {
+  if (!L || (weight_dev && (reinterpret_cast<uintptr_t>(weight_dev) % L->elem || !(eps >= 0.f) || !std::isfinite(eps))) ||
+      reinterpret_cast<uintptr_t>(gate_dev) % L->elem || !std::isfinite(scale))
+    return SWAPMOE_ERR_INVALID_ARG;
+  L->post_norm = weight_dev != nullptr || gate_dev != nullptr || scale != 1.f;
+  L->post_weight = weight_dev; L->post_gate = gate_dev; L->post_eps = weight_dev ? eps : 0.f; L->post_scale = scale;
+  return SWAPMOE_OK;
+}
+
 int32_t swapmoe_forward_block(swapmoe_layer_t* L, const void* x, void* residual, void* out, int32_t T, swapmoe_adapters_t* adapters,
                               const int32_t* ids, void* stream) {
   if (!L || T < 0 || (adapters == nullptr) != (ids == nullptr)) return SWAPMOE_ERR_INVALID_ARG;
@@ -872,12 +884,23 @@ int32_t swapmoe_forward_block(swapmoe_layer_t* L, const void* x, void* residual,
     const int32_t rc = swapmoe_adapters_check(adapters, c.d_model, c.d_model, c.dtype, T);
     if (rc != SWAPMOE_OK) return rc;
   }
-  swapmoe_rms_norm_t n;
-  std::memset(&n, 0, sizeof(n));
-  n.x = x; n.residual = residual; n.residual_out = residual; n.weight = L->norm_weight; n.out = L->x_norm;
-  n.x_stride = n.residual_stride = n.residual_out_stride = n.out_stride = c.d_model;
-  n.n_rows = T; n.d = c.d_model; n.dtype = n.residual_dtype = c.dtype; n.eps = L->norm_eps;
-  int32_t rc = rms_norm_run(&n, stream, L->use_pdl, &L->launches);
+  int32_t rc;
+  if (L->post_norm) {
+    swapmoe_block_norm_t n;
+    std::memset(&n, 0, sizeof(n));
+    n.x = x; n.residual = residual; n.residual_out = residual; n.post_weight = L->post_weight; n.gate = L->post_gate; n.weight = L->norm_weight;
+    n.out = L->x_norm;
+    n.x_stride = n.residual_stride = n.residual_out_stride = n.out_stride = c.d_model;
+    n.n_rows = T; n.d = c.d_model; n.dtype = n.residual_dtype = c.dtype; n.eps = L->norm_eps; n.post_eps = L->post_eps; n.scale = L->post_scale;
+    rc = block_norm_run(&n, stream, L->use_pdl, &L->launches);
+  } else {
+    swapmoe_rms_norm_t n;
+    std::memset(&n, 0, sizeof(n));
+    n.x = x; n.residual = residual; n.residual_out = residual; n.weight = L->norm_weight; n.out = L->x_norm;
+    n.x_stride = n.residual_stride = n.residual_out_stride = n.out_stride = c.d_model;
+    n.n_rows = T; n.d = c.d_model; n.dtype = n.residual_dtype = c.dtype; n.eps = L->norm_eps;
+    rc = rms_norm_run(&n, stream, L->use_pdl, &L->launches);
+  }
   if (rc != SWAPMOE_OK) return rc;
   rc = forward_checked(L, L->x_norm, nullptr, out, T, stream);
   if (rc != SWAPMOE_OK || !adapters) return rc;

@@ -270,3 +270,52 @@ def test_streams_and_graphs():
     binding.block_norm(x, r, w, EPS, out=want, post_weight=w)
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+# ------------------------------------------------------------------ a layer's own block
+def test_post_norm_refusals():
+    L = binding.lib()
+    assert L.swapmoe_set_post_norm(None, 256, 1e-6, None, 1.0) == -1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [1, 7, 130])
+def test_a_layers_block_with_sandwich_norms(T, dtype):
+    """forward_block adds the normed, gated and scaled x: the same bits as block_norm and the layer's own forward, one after the other."""
+    import numpy as np
+    import torch
+    from harness import Case
+    from paper_2308_15030_b200 import inputs as I
+    cfg = I.LayerConfig("post", I.BF16 if dtype == "bf16" else I.F32, T=T, d=128, f=256, E=8, k=2, K=4, seed=3)
+    case = Case(cfg)
+    L, dt = case.layer, torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    normal = lambda *s: torch.empty(*s, device="cuda").normal_(0.0, 1.0, generator=gen).to(dt)  # noqa: E731
+    x, r, w, pw, g = normal(T, 128), normal(T, 128), normal(128), normal(128), normal(128)
+    L.set_norm(w, EPS)
+    plain, plain_r = torch.empty_like(x), r.clone()
+    L.forward_block(x, plain_r, plain)
+    for kw in (dict(weight=pw, eps=EPS, gate=g, scale=0.3), dict(weight=pw, eps=1e-3), dict(gate=g), dict(scale=-1.5)):
+        L.set_post_norm(**kw)
+        out, ro = torch.empty_like(x), r.clone()
+        n0 = L.launch_count
+        L.forward_block(x, ro, out)
+        launches = L.launch_count - n0
+        n, want_r, want = torch.empty_like(x), torch.empty_like(r), torch.empty_like(x)
+        binding.block_norm(x, r, w, EPS, out=n, residual_out=want_r, post_weight=kw.get("weight"), post_eps=kw.get("eps", EPS), gate=kw.get("gate"),
+                           scale=kw.get("scale", 1.0))
+        n0 = L.launch_count
+        L.forward(n, want)
+        assert launches == L.launch_count - n0 + 1
+        torch.cuda.synchronize()
+        assert torch.equal(ro, want_r) and torch.equal(out, want)
+    L.set_post_norm()
+    out, ro = torch.empty_like(x), r.clone()
+    L.forward_block(x, ro, out)
+    assert torch.equal(out, plain) and torch.equal(ro, plain_r)
+    for bad in (dict(weight=pw[:64]), dict(gate=g.float() if dtype == "bf16" else g.bfloat16()), dict(weight=pw.cpu()), dict(scale=float("nan")),
+                dict(weight=pw, eps=-1.0)):
+        with pytest.raises(binding.SwapMoEError) as e:
+            L.set_post_norm(**bad)
+        assert e.value.status == -1
