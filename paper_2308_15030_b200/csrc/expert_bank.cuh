@@ -30,6 +30,8 @@ struct BankArgs {
   int32_t* n_tiles;             // [0] tiles, [1] most rows of one, [2] rows with the slots' padding
   long long x_stride;
   int P, S, k, d, per_cta;      // pairs, ..., pairs of a CTA
+  int cols[2], k_blocks[2];     // weight tiles of a slot, k-blocks of a tile: of the two products
+  int pairs;                    // CTA pairs that walk the tiles
   int direct;
 };
 
@@ -52,6 +54,28 @@ __global__ void __launch_bounds__(kBankThreads) bank_count_kernel(const __grid_c
   __syncthreads();
   for (int s = threadIdx.x; s < a.S; s += kBankThreads)
     a.cta_base[(size_t)blockIdx.x * a.S + s] = s_count[s] ? atomicAdd(&a.counts[s], s_count[s]) : 0;
+}
+
+// Most rows of a token tile, by a warp.  Slots of up to 128 rows: one tile each.  Else of 128, 160 ... 256 the one whose rounds of tiles over
+// the pairs of CTAs cost least in both products (int8_tile_cost): a round that only a few pairs have work for costs as much as a full one (4096 x
+// 14336, eight slots: 38 tiles of 256 are 8.2 rounds of the second product, and take nine).
+__device__ __forceinline__ int bank_tile_cap(const BankArgs& a, const int* s_count) {
+  const int lane = threadIdx.x & 31;
+  int most = 0;
+  for (int s = lane; s < a.S; s += 32) most = max(most, s_count[s]);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (most <= 128) return most <= 64 ? 64 : 128;
+  int best = 256;
+  float least = CUDART_INF_F;
+  const float inv = 1.f / (float)a.pairs;
+  for (int cap = 128; cap <= 256; cap += 32) {
+    int n = 0;
+    for (int s = lane; s < a.S; s += 32) n += (s_count[s] + cap - 1) / cap;
+    const float tiles = (float)__reduce_add_sync(0xffffffffu, n) * inv;
+    const float cost = (ceilf(tiles * (float)a.cols[0]) * (float)a.k_blocks[0] + ceilf(tiles * (float)a.cols[1]) * (float)a.k_blocks[1]) * (float)int8_tile_cost(cap);
+    if (cost < least) { least = cost; best = cap; }
+  }
+  return best;
 }
 
 __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_constant__ BankArgs a) {
@@ -82,10 +106,7 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
   __syncthreads();
   if (warp == 0) {
     // slot offsets, and by the first CTA the list of tiles
-    int most = 0;
-    for (int s = lane; s < a.S; s += 32) most = max(most, s_count[s]);
-    most = __reduce_max_sync(0xffffffffu, most);
-    const int cap = most > 128 ? 256 : most > 64 ? 128 : 64;
+    const int cap = blockIdx.x == 0 ? bank_tile_cap(a, s_count) : 256;       // (of no use to the others)
     int row0 = 0, tile0 = 0;
     for (int s0 = 0; s0 < a.S; s0 += 32) {
       const int s = s0 + lane, count = s < a.S ? s_count[s] : 0;

@@ -42,6 +42,10 @@ struct I8GemmArgs {
   int32_t* largest;         // [rows] largest magnitude of a row of hidden values, as its bits (ReLU, SwiGLU: zero before)
 };
 
+// What a k-block of a tile costs by the tile's tokens: its bytes, 256 weight rows and the tokens (4096 x 14336: a round of 128 tokens 10.5 us, of 256
+// 13.4; eight slots of about 1000 rows, both products: tiles of up to 256 rows 1050 us, of about 128 1390).
+__host__ __device__ constexpr int int8_tile_cost(int tokens) { return 256 + tokens; }
+
 // Instruction descriptor: int8 x int8 -> int32, both operands K-major, M x N tile.
 __host__ __device__ constexpr uint32_t make_idesc_int8(int M, int N) {
   return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -468,14 +472,13 @@ inline int int8_gemm_init(int sm_count) {
   return n < sm_count / 2 ? n : sm_count / 2;
 }
 
-// Rows of a token tile for T rows and n_col_tiles weight tiles on n_pairs pairs of CTAs: the height whose rounds of tiles cost least.  A
-// tile's k-block takes the longer of its tensor clocks (2 per token) and its loads (32 KB of weights per pair weigh like 112 tokens).
+// Rows of a token tile for T rows and n_col_tiles weight tiles on n_pairs pairs of CTAs: the height whose rounds of tiles cost least.
 inline int int8_tile_height(int T, int n_col_tiles, int n_pairs) {
   int best = 256;
   long long least = -1;
   for (int h = 256; h >= 32; h -= 32) {
     const long long tiles = (long long)((T + h - 1) / h) * n_col_tiles;
-    const long long cost = (tiles + n_pairs - 1) / n_pairs * (h > 112 ? h : 112);
+    const long long cost = (tiles + n_pairs - 1) / n_pairs * int8_tile_cost(h);
     if (least < 0 || cost < least) { least = cost; best = h; }
   }
   return best;

@@ -449,6 +449,8 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   a.n_tiles = b->n_tiles;
   a.x_stride = x_stride; a.P = P; a.S = c.n_slots; a.k = c.top_k; a.d = c.d_model;
   a.direct = P <= kBankDirectPairs;
+  a.cols[0] = (c.d_ff + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); a.k_blocks[0] = (c.d_model + kI8BK - 1) / kI8BK;
+  a.cols[1] = (c.d_model + 255) / 256; a.k_blocks[1] = (c.d_ff + kI8BK - 1) / kI8BK; a.pairs = pairs;
   // eight pairs a CTA (one per warp) where that makes no more CTAs than run at once
   a.per_cta = (P + 2 * b->dev.sms - 1) / (2 * b->dev.sms);
   if (a.per_cta < 8) a.per_cta = 8;
@@ -463,7 +465,7 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   I8GemmArgs g = {};
   g.tiles = b->tiles; g.n_tiles = b->n_tiles; g.row_group = 1 << 30; g.height = 256; g.early = 1;
   g.C = b->h; g.x_scales = b->row_scales; g.w_scales = b->in_scales; g.ldc = c.d_ff; g.n_cols = c.d_ff; g.largest = b->row_largest;
-  g.n_col_tiles = (c.d_ff + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); g.k_blocks = (c.d_model + kI8BK - 1) / kI8BK; g.w_rows = c.d_ff;
+  g.n_col_tiles = a.cols[0]; g.k_blocks = a.k_blocks[0]; g.w_rows = c.d_ff;
   const int epi = swiglu ? kI8Swiglu : kI8Relu;
   long long work = max_tiles * g.n_col_tiles;
   if (e == cudaSuccess)
@@ -479,7 +481,7 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
     e = turns == 4 ? launch_kernel(bank_quantize_kernel<4>, units, dim3(kBankThreads), 0, st, pdl, q)
                    : launch_kernel(bank_quantize_kernel<8>, units, dim3(kBankThreads), 0, st, pdl, q);
   g.C = b->y; g.x_scales = b->h_scales; g.w_scales = b->out_scales; g.ldc = c.d_model; g.n_cols = c.d_model; g.largest = nullptr; g.early = 2;
-  g.n_col_tiles = (c.d_model + 255) / 256; g.k_blocks = (c.d_ff + kI8BK - 1) / kI8BK; g.w_rows = c.d_model;
+  g.n_col_tiles = a.cols[1]; g.k_blocks = a.k_blocks[1]; g.w_rows = c.d_model;
   work = max_tiles * g.n_col_tiles;
   if (e == cudaSuccess)
     e = launch_kernel(int8_gemm_kernel(kI8F32), dim3(2 * (unsigned)std::min<long long>(work, pairs)), dim3(kI8Threads), int8_smem_bytes(kI8F32), st,
