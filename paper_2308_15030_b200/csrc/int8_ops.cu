@@ -53,6 +53,13 @@ int32_t current_device(Device* d) {
   }
   if (major != 10) return SWAPMOE_ERR_UNSUPPORTED;       // kernels are built for sm_100a only
   std::lock_guard<std::mutex> hold(lock);
+  const void* const wide[] = {(const void*)bank_stream_out_kernel<bf16, 1>, (const void*)bank_stream_out_kernel<bf16, 2>,
+                              (const void*)bank_stream_out_kernel<float, 1>, (const void*)bank_stream_out_kernel<float, 2>};
+  for (const void* k : wide)
+    if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kBankOutRowBytes) != cudaSuccess) {
+      cudaGetLastError();
+      return SWAPMOE_ERR_CUDA;
+    }
   const int pairs = int8_gemm_init(sms);
   if (pairs < 1 || cudaFuncSetAttribute(int8_split_kernel<bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitMaxSmem) != cudaSuccess ||
       cudaFuncSetAttribute(int8_split_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitMaxSmem) != cudaSuccess) {
@@ -247,7 +254,7 @@ cudaError_t bank_stream(const BankStreamArgs& a, bool swiglu, int slots, cudaStr
   const cudaError_t e = swiglu ? launch_kernel(bank_stream_in_kernel<true, kN>, grid, block, 0, st, pdl, a)
                                : launch_kernel(bank_stream_in_kernel<false, kN>, grid, block, 0, st, pdl, a);
   if (e != cudaSuccess) return e;
-  return launch_kernel(bank_stream_out_kernel<T, kN>, dim3(a.d / 16), dim3(kBankOutThreads), 0, st, pdl, a);
+  return launch_kernel(bank_stream_out_kernel<T, kN>, dim3(a.d / 16), dim3(kBankOutThreads), (size_t)a.P * bank_row_bytes(a.F), st, pdl, a);
 }
 template <typename T>
 cudaError_t bank_stream(const BankStreamArgs& a, bool swiglu, int slots, cudaStream_t st, bool pdl) {
@@ -433,9 +440,10 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool pdl = standalone_pdl(), swiglu = c.act == SWAPMOE_ACT_SWIGLU;
   const int P = T * c.top_k, pairs = b->dev.pairs;
-  // Few pairs on small experts: two launches that take the weights straight to registers.  us, that form / the general one: 1024 x 512 top-4
-  // 4 pairs 6.9 / 17, 16 pairs 16.5 / 19; 2048 x 1024 4 pairs 12.6 / 18, 8 pairs 19.6 / 21; 1024 x 4096 2 pairs 16 / 17, 4 pairs 25.7 / 22.
-  if (P <= kStreamMaxPairs && 3ll * P * c.d_model * c.d_ff <= 25ll << 20) {
+  // Few pairs on small experts: two launches that take the weights straight to registers.  us, that form / the general one: 512 x 704 top-2 8
+  // pairs 6.7 / 15, 16 pairs 12.4 / 17; 768 x 2112 8 pairs 15.9 / 22, 16 pairs 35.7 / 25; 2048 x 1024 top-4 8 pairs 19.0 / 22.3, 12 pairs 26 / 23;
+  // 1024 x 4096 4 pairs 13.6 / 25, 8 pairs 33 / 29.
+  if (P <= kStreamMaxPairs && P * bank_row_bytes(c.d_ff) <= kBankOutRowBytes && 3ll * P * c.d_model * c.d_ff <= 60ll << 20) {
     BankStreamArgs q;
     q.x8 = static_cast<const int8_t*>(x); q.w_in = b->w_in; q.w_out = b->w_out; q.x_scales = x_scales; q.in_scales = b->in_scales;
     q.out_scales = b->out_scales; q.weights = weights; q.slots = slots; q.h = b->h; q.largest = b->largest; q.out = out;

@@ -8,7 +8,7 @@
 //
 // With experts (up to 16 pairs of token and choice) the same in two launches: the first takes the rows of W_in of every slot that is asked for
 // (SwiGLU: both products of sixteen hidden units), applies the activation and leaves h in fp32 with the largest magnitude of every 16 values; the second
-// takes rows of W_out, fetched before the first has finished, quantises h on the way to the mma, and adds a token's choices in their order.
+// takes rows of W_out, fetched before the first has finished, and all of h to 8 bits in shared memory, and adds a token's choices in their order.
 #pragma once
 #include "quantize_rows.cuh"
 
@@ -61,9 +61,9 @@ struct StreamTile {
         }
   }
   // The warp's share of the contraction, from column c0 on.  tokens(n, c): 16 columns of this lane's token of tile n from column c on.
-  // fetched: the first batch is in registers already.
+  // fetched: the first batch is in registers already.  used: tiles of tokens that hold some (mma's rate for 8-bit integers is low).
   template <typename Tokens>
-  __device__ __forceinline__ void run(const int8_t* const (&rows)[kM][2], Tokens tokens, int c0, int turn, int K, bool fetched) {
+  __device__ __forceinline__ void run(const int8_t* const (&rows)[kM][2], Tokens tokens, int used, int c0, int turn, int K, bool fetched) {
 #pragma unroll
     for (int m = 0; m < kM; ++m)
 #pragma unroll
@@ -80,6 +80,7 @@ struct StreamTile {
         if (c - own < K) {                                   // the same for the warp
 #pragma unroll
           for (int n = 0; n < kN; ++n) {
+            if (kN > 1 && n >= used) break;
             const uint4 x = tokens(n, c);
 #pragma unroll
             for (int m = 0; m < kM; ++m) {
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(kStreamThreads) int8_stream_kernel(const __gri
   Tile tile;
   pdl_wait();
   pdl_trigger();
-  tile.run(rows, [&](int, int c) { return load_bytes16<false>(x + c, x != nullptr ? a.K - c : 0); }, stream_column(), kStreamTurn, a.K, false);
+  tile.run(rows, [&](int, int c) { return load_bytes16<false>(x + c, x != nullptr ? a.K - c : 0); }, 1, stream_column(), kStreamTurn, a.K, false);
   tile.put(s_part);
   __syncthreads();
   const int i = threadIdx.x, token = i >> 4, r = i & 15, n = n0 + r;
@@ -219,7 +220,8 @@ __global__ void __launch_bounds__(kStreamThreads) bank_stream_in_kernel(const __
   const int r = threadIdx.x & 15;
   const float* ws = a.in_scales + (size_t)slot * kM * a.F + f0 + r;
   const float w0 = ws[0], w1 = kSwiglu ? ws[a.F] : 0.f;
-  tile.run(rows, [&](int n, int c) { return load_bytes16<false>(x[n] + c, x[n] != nullptr ? a.d - c : 0); }, stream_column(), kStreamTurn, a.d, true);
+  tile.run(rows, [&](int n, int c) { return load_bytes16<false>(x[n] + c, x[n] != nullptr ? a.d - c : 0); }, (count + 7) / 8,
+           stream_column(), kStreamTurn, a.d, true);
   tile.put(s_part);
   __syncthreads();
   for (int i0 = 0; i0 < count * 16; i0 += kStreamThreads) {
@@ -260,6 +262,9 @@ __device__ __forceinline__ uint4 quantize16(const float* h, float divisor, float
 // all warps), the warps of a slot take turns of its columns.
 constexpr int kBankOutThreads = 512;
 constexpr int kBankOutWarps = kBankOutThreads / 32;
+// Two rows that a warp reads side by side start half of the banks apart.
+__host__ __device__ constexpr int bank_row_bytes(int F) { return (F + 127) / 128 * 128 + 64; }
+constexpr int kBankOutRowBytes = 64 * 1024;                  // most shared memory for them
 static_assert(kStreamMaxPairs * 16 <= kBankOutThreads && kStreamMaxPairs <= 32, "a thread per pair and channel, a lane per pair");
 
 template <typename T, int kN>
@@ -269,6 +274,7 @@ __global__ void __launch_bounds__(kBankOutThreads) bank_stream_out_kernel(const 
   __shared__ float s_y[kStreamMaxPairs * 16];
   __shared__ float s_scale[kStreamMaxPairs], s_inverse[kStreamMaxPairs], s_divisor[kStreamMaxPairs], s_weight[kStreamMaxPairs];
   __shared__ BankLists s_lists;
+  extern __shared__ __align__(16) int8_t s_rows[];           // the pairs' rows in 8 bits, bank_row_bytes apart
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n0 = (int)blockIdx.x * 16, r = threadIdx.x & 15;
   // slots and weights are older than the kernel in front: the first are fetched while it runs
   if (warp == 0) bank_lists(a, &s_lists);
@@ -307,23 +313,20 @@ __global__ void __launch_bounds__(kBankOutThreads) bank_stream_out_kernel(const 
     }
   }
   __syncthreads();
+  const int row_bytes = bank_row_bytes(a.F);
+  for (int i = threadIdx.x; i < n_pairs * (a.F / 16); i += kBankOutThreads) {
+    const int p = i / (a.F / 16), c = (i - p * (a.F / 16)) * 16;
+    *reinterpret_cast<uint4*>(s_rows + p * row_bytes + c) = quantize16(a.h + (size_t)s_lists.pair[p] * a.F + c, s_divisor[p], s_inverse[p]);
+  }
+  __syncthreads();
   for (int u0 = 0; u0 < n_slots; u0 += side) {
     const int u = u0 + mine;
     if (u0 > 0) fetch(u);
     const int start = u < n_slots ? s_lists.start[u] : 0, count = u < n_slots ? s_lists.start[u + 1] - start : 0;
-    const float* h[kN];
-    float divisor[kN], inverse[kN];
-#pragma unroll
-    for (int n = 0; n < kN; ++n) {
-      const int i = n * 8 + (lane >> 2);
-      const bool have = i < count;
-      h[n] = have ? a.h + (size_t)s_lists.pair[start + i] * a.F : nullptr;
-      divisor[n] = have ? s_divisor[start + i] : 1.f;
-      inverse[n] = have ? s_inverse[start + i] : 1.f;
-    }
     tile.run(rows, [&](int n, int c) {
-      return h[n] != nullptr && c < a.F ? quantize16(h[n] + c, divisor[n], inverse[n]) : make_uint4(0u, 0u, 0u, 0u);
-    }, c0, turn, count > 0 ? a.F : 0, true);
+      const int i = n * 8 + (lane >> 2);
+      return i < count && c < a.F ? *reinterpret_cast<const uint4*>(s_rows + (start + i) * row_bytes + c) : make_uint4(0u, 0u, 0u, 0u);
+    }, (count + 7) / 8, c0, turn, count > 0 ? a.F : 0, true);
     tile.put(s_part);
     __syncthreads();
     if (own < n_pairs && own_slot >= u0 && own_slot < u0 + side)
