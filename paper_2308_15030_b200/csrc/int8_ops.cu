@@ -372,7 +372,8 @@ int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_ex
     *q.p = at;
     at += (q.bytes + 255) / 256 * 256;
   }
-  bool ok = cudaMemset(b->counts, 0, kBankMaxSlots * 4) == cudaSuccess;
+  // (the default stream's work is not ordered before that of other streams)
+  bool ok = cudaMemset(b->counts, 0, kBankMaxSlots * 4) == cudaSuccess && cudaStreamSynchronize(nullptr) == cudaSuccess;
   for (int i = 0; i < 4; ++i)
     ok = ok && int8_encode_operand(enc, &b->map_x[i], b->rows8, R, d, d, 128 >> i) && int8_encode_operand(enc, &b->map_h[i], b->h8, R, f, f, 128 >> i);
   ok = ok && int8_encode_2d(enc, &b->map_h_out, b->h, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, f, f, nin == 2 ? 16 : 32, kI8Chunk, CU_TENSOR_MAP_SWIZZLE_NONE) &&
@@ -498,6 +499,7 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   m.y = b->y; m.pair_row = b->pair_row; m.weights = weights; m.counts = b->counts; m.out = out; m.out_stride = out_stride;
   m.T = T; m.k = c.top_k; m.d = c.d_model; m.S = c.n_slots; m.vec = rows_aligned(out, T, out_stride, elem, 4 * elem);
   if (e == cudaSuccess) e = c.dtype == SWAPMOE_BF16 ? bank_combine_launch<bf16>(m, st, pdl) : bank_combine_launch<float>(m, st, pdl);
+  if (e != cudaSuccess) cudaMemsetAsync(b->counts, 0, kBankMaxSlots * 4, st);          // what the last kernel would have left
   return launched(e);
 }
 

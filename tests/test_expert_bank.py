@@ -267,6 +267,45 @@ def test_refusals_of_a_bank():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,F,S,k,T", [(64, 32768, 2, 1, 1), (64, 32768, 2, 2, 19), (32768, 64, 2, 1, 3), (32768, 64, 1, 2, 40), (4096, 4096, 2, 2, 3),
+                                       (1024, 1024, 16, 16, 1), (256, 256, 16, 4, 4), (256, 192, 5, 8, 2)])
+def test_widest_experts_and_few_pairs(d, F, S, k, T):
+    c = Case(T, d, F, S, k)
+    c.check(c.run())
+
+
+@pytest.mark.gpu
+def test_two_banks_at_once():
+    """Banks of their own workspace on streams of their own, small and large calls side by side."""
+    import torch
+    banks = [Case(T, 512, 320, 8, 2, seed=T) for T in (1500, 2300, 3, 70)]
+    want = [c.run() for c in banks]
+    streams, outs = [torch.cuda.Stream() for _ in banks], [torch.zeros_like(w) for w in want]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c, st, o in zip(banks, streams, outs):
+            c.run(o, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    assert binding.matmul_status() == (0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [2, 300])
+def test_an_expert_is_swapped_in_place(T):
+    """Weights are not copied: what is written into a slot between two calls, on the same stream, is what the next call multiplies."""
+    import torch
+    c = Case(T, 192, 256, 6, 2)
+    c.check(c.run())
+    for e in (1, 4):
+        c.w_in[e].copy_(torch.randint(-127, 128, c.w_in[e].shape, device="cuda").to(torch.int8))
+        c.in_scales[e].mul_(0.5)
+        c.w_out[e].neg_()
+        out = c.run()
+        c.check(out)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 45, 1200])
 def test_a_served_block(T):
     """Norms around the block, the router's product, routing to resident experts, experts, and the shared projection with its adapters,

@@ -213,3 +213,23 @@ def test_offsets_beyond_32_bits(pad):
     for rows in (slice(0, 50), slice(35780, 35830), slice(T - 50, T)):
         want = (x[rows].float() @ w.float().t()).bfloat16()             # sums below 2^24: exact, one rounding each
         assert torch.equal(out[rows], want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 20, 100, 400])
+def test_right_behind_what_writes_its_operands(T):
+    """Rows and weights come from the kernels directly in front, which a dependent launch may overlap."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    K, N = 640, 384
+    x8, xs, w8, ws = (torch.empty(T, K, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda"), torch.empty(N, K, dtype=torch.int8, device="cuda"),
+                      torch.empty(N, device="cuda"))
+    out = torch.empty(T, N, device="cuda")
+    for _ in range(20):
+        x, w = torch.empty(T, K, device="cuda").normal_(generator=gen), torch.empty(N, K, device="cuda").normal_(generator=gen)
+        torch.cuda.synchronize()
+        binding.quantize_rows(x, x8, xs)
+        binding.quantize_rows(w, w8, ws)
+        binding.matmul_scaled(x8, xs, w8, ws, out)
+        want = (x8.double() @ w8.double().t()) * xs.double()[:, None] * ws.double()
+        assert bool(((out.double() - want).abs() <= 4 * 2.0 ** -24 * want.abs()).all())
