@@ -168,6 +168,14 @@ struct swapmoe_expert_bank {
 
 namespace {
 
+// Token tiles per scheduling group (see decode_tile) of `rows` rows of k bytes, `height` rows a tile: those of a group stay in L2 across its weight
+// tiles.  16 MB of them, six tiles at least; all in one group up to 24 MB.  us at 6 / 10 / 20 / all tiles a group: experts of 4096 x 14336, 8192 pairs,
+// first product 690 / 691 / 703 / 753, second 323 / 333 / 346 / 358; 16000 pairs, first product 1305 / 1263 / 1226 / 1416.
+int row_group(long long rows, long long k, int height) {
+  if (rows * k <= 24ll << 20) return 1 << 30;
+  return (int)std::max(6ll, (16ll << 20) / (height * k));
+}
+
 // A product of a whole matrix (matmul_scaled).
 int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t st, bool pdl) {
   const PFN_encodeTiled enc = encoder();
@@ -177,12 +185,7 @@ int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t s
   g.ldc = p.out_stride; g.n_cols = p.n; g.n_col_tiles = (p.n + 255) / 256; g.k_blocks = (p.k + kI8BK - 1) / kI8BK; g.w_rows = p.n;
   g.T = p.n_tokens;
   g.height = int8_tile_height(p.n_tokens, g.n_col_tiles, dev.pairs);
-  g.row_group = 1 << 30;
-  // Token rows of a group stay in L2 across its weight tiles: 20 MB of them (as in tc_gemm_pair)
-  if ((long long)p.n_tokens * p.k > (24ll << 20)) {
-    g.row_group = (int)((20ll << 20) / ((long long)g.height * p.k));
-    if (g.row_group < 4) g.row_group = 4;
-  }
+  g.row_group = row_group(p.n_tokens, p.k, g.height);
   const size_t elem = p.dtype == SWAPMOE_BF16 ? 2 : 4;
   g.direct = !rows_aligned(p.out, 2, p.out_stride, elem, 16);
   const long long xs = p.n_tokens > 1 ? p.x_stride : (p.k + 15) / 16 * 16, ws = p.n > 1 ? p.w_stride : (p.k + 15) / 16 * 16;
@@ -472,7 +475,7 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   const long long rows = std::min<long long>(b->max_rows, (P + 31ll * std::min(P, c.n_slots) + 31) / 32 * 32);
   const long long max_tiles = (P + 63) / 64 + std::min(P, c.n_slots);
   I8GemmArgs g = {};
-  g.tiles = b->tiles; g.n_tiles = b->n_tiles; g.row_group = 1 << 30; g.height = 256; g.early = 1;
+  g.tiles = b->tiles; g.n_tiles = b->n_tiles; g.height = 256; g.early = 1; g.row_group = row_group(P, c.d_model, 256);
   g.C = b->h; g.x_scales = b->row_scales; g.w_scales = b->in_scales; g.ldc = c.d_ff; g.n_cols = c.d_ff; g.largest = b->row_largest;
   g.n_col_tiles = a.cols[0]; g.k_blocks = a.k_blocks[0]; g.w_rows = c.d_ff;
   const int epi = swiglu ? kI8Swiglu : kI8Relu;
@@ -489,7 +492,7 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   if (e == cudaSuccess)
     e = turns == 4 ? launch_kernel(bank_quantize_kernel<4>, units, dim3(kBankThreads), 0, st, pdl, q)
                    : launch_kernel(bank_quantize_kernel<8>, units, dim3(kBankThreads), 0, st, pdl, q);
-  g.C = b->y; g.x_scales = b->h_scales; g.w_scales = b->out_scales; g.ldc = c.d_model; g.n_cols = c.d_model; g.largest = nullptr; g.early = 2;
+  g.C = b->y; g.x_scales = b->h_scales; g.w_scales = b->out_scales; g.ldc = c.d_model; g.n_cols = c.d_model; g.largest = nullptr; g.early = 2; g.row_group = row_group(P, c.d_ff, 256);
   g.n_col_tiles = a.cols[1]; g.k_blocks = a.k_blocks[1]; g.w_rows = c.d_model;
   work = max_tiles * g.n_col_tiles;
   if (e == cudaSuccess)

@@ -275,6 +275,14 @@ def test_widest_experts_and_few_pairs(d, F, S, k, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,F,S,k,T", [(4096, 64, 3, 1, 7000), (64, 4096, 5, 2, 3500), (2048, 2048, 2, 2, 6500)])
+def test_rows_beyond_a_scheduling_group(d, F, S, k, T):
+    """More rows than stay in L2 at once: both products walk them in groups."""
+    c = Case(T, d, F, S, k)
+    c.check(c.run())
+
+
+@pytest.mark.gpu
 def test_two_banks_at_once():
     """Banks of their own workspace on streams of their own, small and large calls side by side."""
     import torch

@@ -133,6 +133,7 @@ def test_all_lowest_values(T):
 def test_several_rounds_of_tiles():
     _check(3000, 384, 2300)
     _check(2100, 1100, 5200, "fp32")
+    _check(7001, 4096, 900)                                             # groups of token tiles
 
 
 @pytest.mark.gpu
