@@ -15,7 +15,8 @@ namespace swapmoe {
 constexpr int kBankMaxSlots = 256;
 constexpr int kBankThreads = 256;
 constexpr int kBankMaxCtas = 512;               // CTAs of the count and gather kernels
-constexpr int kBankDirectPairs = 4096;          // up to here every CTA of the gather kernel counts all pairs itself
+constexpr int kBankDirectPairs = 2048;          // up to here every CTA of the gather kernel counts all pairs itself (us of both, itself / count kernel:
+                                                // 1024 pairs 8.0 / 9.2, 4000 12.7 / 11.4, 14000 18 / 12.7)
 
 struct BankArgs {
   const int8_t* x8;
@@ -78,6 +79,33 @@ __device__ __forceinline__ int bank_tile_cap(const BankArgs& a, const int* s_cou
   return best;
 }
 
+// Rows of x8 to their places by the CTA's warps, kRows of them and eight pieces of 16 bytes a lane on their way at once.
+template <int kRows>
+__device__ __forceinline__ void bank_copy_rows(const BankArgs& a, const int* s_row, int pair0, int n) {
+  constexpr int kPieces = 8 / kRows, kWarps = kBankThreads / 32;
+  const int lane = threadIdx.x & 31, quads = a.d / 16;
+  for (int i = threadIdx.x >> 5; i < n; i += kRows * kWarps)
+    for (int c0 = lane; c0 < quads; c0 += 32 * kPieces) {
+      uint4 v[kRows][kPieces];
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const int j = i + r * kWarps;
+        const uint4* src = reinterpret_cast<const uint4*>(a.x8 + (size_t)((pair0 + min(j, n - 1)) / a.k) * a.x_stride);
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u)
+          if (j < n && c0 + 32 * u < quads) v[r][u] = src[c0 + 32 * u];
+      }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const int j = i + r * kWarps, to = j < n ? s_row[j] : -1;
+        uint4* dst = reinterpret_cast<uint4*>(a.rows8 + (size_t)max(to, 0) * a.d);
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u)
+          if (to >= 0 && c0 + 32 * u < quads) dst[c0 + 32 * u] = v[r][u];
+      }
+    }
+}
+
 __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_constant__ BankArgs a) {
   __shared__ int s_count[kBankMaxSlots], s_at[kBankMaxSlots], s_off[kBankMaxSlots];
   __shared__ int s_row[kBankThreads];
@@ -89,13 +117,11 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
   pdl_trigger();
   __syncthreads();
   if (a.direct) {
-    for (int b = 0; b < a.P; b += kBankThreads) {
-      const int p = b + threadIdx.x, s = p < a.P ? bank_slot(a, p) : -1;
-      const unsigned same = __match_any_sync(0xffffffffu, s), front = __ballot_sync(0xffffffffu, p < p0);
-      if (s >= 0 && (same & ((1u << lane) - 1u)) == 0) {
-        atomicAdd(&s_count[s], __popc(same));
-        if (same & front) atomicAdd(&s_at[s], __popc(same & front));
-      }
+    for (int p = threadIdx.x; p < a.P; p += kBankThreads) {
+      const int s = bank_slot(a, p);
+      if (s < 0) continue;
+      atomicAdd(&s_count[s], 1);
+      if (p < p0) atomicAdd(&s_at[s], 1);
     }
   } else {
     for (int s = threadIdx.x; s < a.S; s += kBankThreads) {
@@ -151,22 +177,9 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
     }
     s_row[threadIdx.x] = row;
     __syncthreads();
-    for (int i = warp; i < n; i += kBankThreads / 32) {
-      const int to = s_row[i];
-      if (to < 0) continue;
-      const uint4* src = reinterpret_cast<const uint4*>(a.x8 + (size_t)((b + i) / a.k) * a.x_stride);
-      uint4* dst = reinterpret_cast<uint4*>(a.rows8 + (size_t)to * a.d);
-      const int quads = a.d / 16;
-      for (int c0 = lane; c0 < quads; c0 += 256) {
-        uint4 v[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-          if (c0 + 32 * u < quads) v[u] = src[c0 + 32 * u];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-          if (c0 + 32 * u < quads) dst[c0 + 32 * u] = v[u];
-      }
-    }
+    if (a.d <= 1024) bank_copy_rows<4>(a, s_row, b, n);
+    else if (a.d <= 2048) bank_copy_rows<2>(a, s_row, b, n);
+    else bank_copy_rows<1>(a, s_row, b, n);
     __syncthreads();
   }
 }
