@@ -61,6 +61,25 @@ __device__ __forceinline__ void umma_int8_pair(uint32_t tmem_d, uint64_t desc_a,
       "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// Sixteen lanes x sixteen columns of tensor memory as the fragments of 8 x 8 matrices: v[4 j + 2 i + e] is lane l / 4 + 8 i, column 8 j + 2 (l % 4) + e.
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t taddr, uint32_t* v) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(taddr)
+               : "memory");
+}
+// Loads out of tensor memory have arrived in v: what uses it stays behind this.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
+                 "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+               :
+               : "memory");
+}
+// Four 8 x 8 matrices of 16-bit values, transposed; lane 8 m + r has the place of row r of matrix m.
+__device__ __forceinline__ void store_matrices_transposed(uint32_t at, uint32_t m0, uint32_t m1, uint32_t m2, uint32_t m3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(m0), "r"(m1), "r"(m2), "r"(m3) : "memory");
+}
 }  // namespace ptx
 
 constexpr int kI8EpiWarps = 16;
@@ -264,7 +283,11 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     // -------------------------------------------------------------------- epilogue (own 128 weight rows)
     const int q = warp & 3;                    // TMEM lane quarter this warp may read
     const int part = (warp - 4) >> 2;          // the warps of a quarter take turns with the chunks of tokens
-    const int odd = lane & 1, hi = lane >> 4;
+    // bf16 and SwiGLU: a lane holds rows l / 4 + 8 i + 16 h of the warp's 32 (SwiGLU: unit l / 4 + 8 i of matrix h) and tokens
+    // 8 j + 2 (l % 4) + e of a chunk's 16, v[8 h + 4 j + 2 i + e]; else lane l holds row l and all sixteen.
+    constexpr bool kFragments = EPI == kI8Bf16 || kSwiglu;
+    constexpr int kRows = kFragments ? 4 : 1;  // weight rows of a lane
+    const int row8 = lane >> 2, two = 2 * (lane & 3);
     constexpr int kBox = int8_box_bytes(EPI);
     unsigned char* const stg0 = smem + int8_ring_bytes(EPI) + 1024 + (warp - 4) * 2 * kBox;
     float* s_scale = reinterpret_cast<float*>(smem + int8_ring_bytes(EPI) + 1024 + 2 * kI8EpiWarps * kBox) + (warp - 4) * kI8Chunk;
@@ -274,26 +297,27 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     uint32_t acc_phase = 0;
     bool ok = true;
     // What a tile needs from memory comes while the tiles before it are worked on: its descriptor two steps ahead, its scales one.
-    struct Scales { float w, bias, token; };
-    auto col_of = [&](int t, int* col0) {                      // first of this warp's output columns (32; SwiGLU 16), and this lane's
+    struct Scales { float w[kRows], bias[EPI == kI8Bf16 ? 4 : 1], token; };
+    auto first_col = [&](int t) {                              // of this warp's output columns (32; SwiGLU 16)
       int rt = 0, ct = 0;
       if (t < total) decode_tile(t, n_row_tiles, a.n_col_tiles, a.row_group, &rt, &ct);
-      *col0 = kSwiglu ? (ct * 8 + (int)rank * 4 + q) * 16 : ct * 2 * kTcBM + (int)rank * kTcBM + q * 32;
-      return kSwiglu ? *col0 + (lane & 15) : *col0 + lane;
+      return kSwiglu ? (ct * 8 + (int)rank * 4 + q) * 16 : ct * 2 * kTcBM + (int)rank * kTcBM + q * 32;
     };
     auto token_scale = [&](const TileDesc& td, int c) {
       const int token = kI8Chunk * c + (lane & (kI8Chunk - 1));
       return token < td.rows ? a.x_scales[td.row0 + token] : 0.f;
     };
     auto scales_of = [&](int t, const TileDesc& td) {
-      Scales s = {0.f, 0.f, 0.f};
-      int col0;
-      const int col = col_of(t, &col0);
+      Scales s = {};
+      const int col0 = first_col(t);
       if (t >= total) return s;
       s.token = token_scale(td, part);
-      if (col < a.n_cols) {
-        s.w = kSwiglu ? a.w_scales[((size_t)td.phys * 2 + hi) * a.n_cols + col] : a.w_scales[(size_t)td.phys * a.w_rows + col];
-        if (!kSwiglu && a.bias != nullptr) s.bias = a.bias[col];
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {                        // r = 2 h + i
+        const int col = kSwiglu ? col0 + 8 * (r & 1) + row8 : kFragments ? col0 + 8 * r + row8 : col0 + lane;
+        if (col >= a.n_cols) continue;
+        s.w[r] = kSwiglu ? a.w_scales[((size_t)td.phys * 2 + (r >> 1)) * a.n_cols + col] : a.w_scales[(size_t)td.phys * a.w_rows + col];
+        if (!kSwiglu && a.bias != nullptr) s.bias[r] = a.bias[col];
       }
       return s;
     };
@@ -301,13 +325,12 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     Scales s_next = scales_of(pair, td_next);
     for (int t = pair; t < total && ok; t += n_pairs) {
       const TileDesc td = td_next;
-      const float w_scale = s_next.w, bias = s_next.bias;
-      float next = s_next.token;                             // scales of the tokens, a chunk ahead
+      const Scales scales = s_next;
+      float next = scales.token;                             // scales of the tokens, a chunk ahead
       td_next = td_after;
       td_after = at_step(t + 2 * n_pairs);
       s_next = scales_of(t + n_pairs, td_next);
-      int col0;
-      const int col = col_of(t, &col0);
+      const int col0 = first_col(t), col = col0 + lane;
       const bool col_ok = col0 < a.n_cols;
       const int last = (td.rows - 1) / kI8Chunk;             // the tile's last chunk
       const int my_last = part <= last ? last - (last - part) % kI8EpiParts : -1;              // this warp's last one (-1: none)
@@ -322,56 +345,67 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         if (lane == 0) ptx::mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)acc);
       };
       uint32_t v[kI8Chunk];
-      __syncwarp();                                          // the tensor-memory load is one of the whole warp
+      auto load = [&](int first) {                             // (a load of the whole warp)
+        if (kFragments) {
+          ptx::tmem_ld_fragments(taddr + (uint32_t)first, v);
+          ptx::tmem_ld_fragments(taddr + (16u << 16) + (uint32_t)first, v + 8);
+        } else {
+          ptx::tmem_ld16(taddr + (uint32_t)first, v);
+        }
+      };
+      __syncwarp();
       if (my_last < 0) release();
-      else ptx::tmem_ld16(taddr + (uint32_t)(kI8Chunk * part), v);
+      else load(kI8Chunk * part);
 #pragma unroll 1
       for (int c = part; c <= last; c += kI8EpiParts) {
         const int t0 = kI8Chunk * c, left = td.rows - t0;    // valid tokens of this chunk (may exceed its size)
         __syncwarp();                                        // the scales of the chunk before have been read
         if (lane < kI8Chunk) s_scale[lane] = next;
         next = token_scale(td, c + kI8EpiParts);
-        ptx::tmem_ld_wait();
+        ptx::tmem_ld_wait_for(v);
         float f[kI8Chunk];
 #pragma unroll
         for (int j = 0; j < kI8Chunk; ++j) f[j] = (float)(int)v[j];
         __syncwarp();
         // the next chunk comes out of tensor memory while this one is worked on
         if (c == my_last) release();
-        else ptx::tmem_ld16(taddr + (uint32_t)(t0 + kI8Chunk * kI8EpiParts), v);
+        else load(t0 + kI8Chunk * kI8EpiParts);
         if (!col_ok) continue;
+        if (kFragments) {
 #pragma unroll
-        for (int j = 0; j < kI8Chunk; j += 4) {
-          const float4 x = *reinterpret_cast<const float4*>(s_scale + j);
-          mul2(f[j], f[j + 1], w_scale, w_scale);
-          mul2(f[j], f[j + 1], x.x, x.y);
-          mul2(f[j + 2], f[j + 3], w_scale, w_scale);
-          mul2(f[j + 2], f[j + 3], x.z, x.w);
-        }
-        if (kSwiglu) {
-          // lanes l and l + 16 hold the two products of hidden unit l & 15: the lower one finishes token 2 i, the upper one token 2 i + 1
+          for (int j = 0; j < 2; ++j) {
+            const float2 x = *reinterpret_cast<const float2*>(s_scale + 8 * j + two);
 #pragma unroll
-          for (int i = 0; i < kI8Chunk / 2; ++i) {
-            const float v0 = f[2 * i], v1 = f[2 * i + 1];
-            const float r = __shfl_xor_sync(0xffffffffu, hi ? v0 : v1, 16);
-            const float x1 = hi ? r : v0, x3 = hi ? v1 : r;
-            f[i] = __fdividef(x1, 1.f + __expf(-x1)) * x3;   // (two steps of 2^-23 at most: what follows has 8 bits)
+            for (int r = 0; r < kRows; ++r) {
+              float &f0 = f[8 * (r >> 1) + 4 * j + 2 * (r & 1)], &f1 = f[8 * (r >> 1) + 4 * j + 2 * (r & 1) + 1];
+              mul2(f0, f1, scales.w[r], scales.w[r]);
+              mul2(f0, f1, x.x, x.y);
+              if (EPI == kI8Bf16) add2(f0, f1, scales.bias[EPI == kI8Bf16 ? r : 0], scales.bias[EPI == kI8Bf16 ? r : 0]);
+            }
           }
         } else {
 #pragma unroll
+          for (int j = 0; j < kI8Chunk; j += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(s_scale + j);
+            mul2(f[j], f[j + 1], scales.w[0], scales.w[0]);
+            mul2(f[j], f[j + 1], x.x, x.y);
+            mul2(f[j + 2], f[j + 3], scales.w[0], scales.w[0]);
+            mul2(f[j + 2], f[j + 3], x.z, x.w);
+          }
+#pragma unroll
           for (int j = 0; j < kI8Chunk; ++j) {
-            f[j] += bias;
+            f[j] += scales.bias[0];
             if (EPI == kI8Relu) f[j] = f[j] < 0.f ? 0.f : f[j];                              // NaN stays NaN
           }
         }
-        if (a.direct) {
+        if (kSwiglu)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            f[i] = __fdividef(f[i], 1.f + __expf(-f[i])) * f[8 + i];       // (two steps of 2^-23 at most: what follows has 8 bits)
+        if (EPI == kI8F32 && a.direct) {
 #pragma unroll
           for (int j = 0; j < kI8Chunk; ++j)
-            if (!kSwiglu && j < left && col < a.n_cols) {
-              const size_t at = (size_t)(td.row0 + t0 + j) * a.ldc + col;
-              if (EPI == kI8Bf16) static_cast<bf16*>(a.C)[at] = __float2bfloat16_rn(f[j]);
-              else static_cast<float*>(a.C)[at] = f[j];
-            }
+            if (j < left && col < a.n_cols) static_cast<float*>(a.C)[(size_t)(td.row0 + t0 + j) * a.ldc + col] = f[j];
           continue;
         }
         // Boxes of 16 tokens leave through the TMA unit.  Rows of a listed tile up to the next multiple of 16 are stored with the valid
@@ -381,16 +415,28 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         if (lane == 0) ptx::tma_store_wait_read_but_one();     // the box before the last one has left
         __syncwarp();
         if (kSwiglu) {
-          float* w = reinterpret_cast<float*>(stg) + hi * 16 + (lane & 15);    // [16 tokens][16 units]
+          // [16 tokens][16 units] with the 64-byte swizzle; lanes of units 4 ... 7 begin with their odd token, whose row lies in the other banks
+          const int swap = (lane >> 4) & 1;
 #pragma unroll
-          for (int i = 0; i < kI8Chunk / 2; ++i) w[32 * i] = f[i];
+          for (int u = 0; u < 8; ++u) {
+            const int j = u >> 2, i = (u >> 1) & 1, e = (u & 1) ^ swap, token = 8 * j + two + e;
+            const float odd_value = f[4 * j + 2 * i + 1], even_value = f[4 * j + 2 * i];
+            reinterpret_cast<float*>(stg)[token * 16 + 4 * ((2 * i + (row8 >> 2)) ^ (two >> 1)) + (row8 & 3)] = e ? odd_value : even_value;
+          }
         } else if (EPI == kI8Bf16) {
-          // neighbouring lanes trade, so that each holds two output columns of one token
-          uint32_t* w = reinterpret_cast<uint32_t*>(stg) + odd * 16 + (lane >> 1);      // [16 tokens][32 columns]
+          // [16 tokens][32 columns] with the 64-byte swizzle, eight tokens a store; this lane has the place of token l % 8, columns 8 (l / 8) ... + 7
+          const uint32_t at = ptx::smem_u32(stg) + (uint32_t)((lane & 7) * 64 + 16 * ((lane >> 3) ^ ((lane >> 1) & 3)));
 #pragma unroll
-          for (int i = 0; i < kI8Chunk / 2; ++i) {
-            const float r = __shfl_xor_sync(0xffffffffu, odd ? f[2 * i] : f[2 * i + 1], 1);
-            w[32 * i] = odd ? pack_bf16x2(r, f[2 * i + 1]) : pack_bf16x2(f[2 * i], r);
+          for (int j = 0; j < 2; ++j)
+            ptx::store_matrices_transposed(at + 512u * j, pack_bf16x2(f[4 * j], f[4 * j + 1]), pack_bf16x2(f[4 * j + 2], f[4 * j + 3]),
+                                           pack_bf16x2(f[8 + 4 * j], f[8 + 4 * j + 1]), pack_bf16x2(f[8 + 4 * j + 2], f[8 + 4 * j + 3]));
+          if (a.direct) {                                      // (the box is a way between the lanes)
+            __syncwarp();
+            for (int j = 0; j < min(left, kI8Chunk); ++j)
+              if (col < a.n_cols)
+                static_cast<bf16*>(a.C)[(size_t)(td.row0 + t0 + j) * a.ldc + col] =
+                    reinterpret_cast<const bf16*>(stg)[j * 32 + 8 * ((lane >> 3) ^ ((j >> 1) & 3)) + (lane & 7)];
+            continue;
           }
         } else {
           float* w = reinterpret_cast<float*>(stg) + lane;     // [16 tokens][32 columns]
@@ -411,7 +457,7 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
             most = max_magnitude(max_magnitude(most, u.x, u.y), u.z, u.w);
           }
           most = max_magnitude(most, __shfl_xor_sync(0xffffffffu, most, 1), 0.f);
-          if (odd == 0 && lane / 2 < left) atomicMax(a.largest + td.row0 + t0 + lane / 2, __float_as_int(most) & 0x7fffffff);
+          if ((lane & 1) == 0 && lane / 2 < left) atomicMax(a.largest + td.row0 + t0 + lane / 2, __float_as_int(most) & 0x7fffffff);
         }
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
@@ -435,6 +481,9 @@ inline I8GemmKernel int8_gemm_kernel(int epi) {
   return epi == kI8Bf16 ? int8_gemm_pair_kernel<kI8Bf16> : epi == kI8F32 ? int8_gemm_pair_kernel<kI8F32>
          : epi == kI8Relu ? int8_gemm_pair_kernel<kI8Relu> : int8_gemm_pair_kernel<kI8Swiglu>;
 }
+
+// How a staged box of results lies in shared memory (rows of 64 bytes: swizzled, for the stores that transpose).
+inline CUtensorMapSwizzle int8_out_swizzle(int epi) { return int8_box_bytes(epi) == 1024 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE; }
 
 // View of a row-major matrix [rows, cols] with a box of box_cols x box_rows elements (type: unsigned bytes, bf16 or fp32).
 inline bool int8_encode_2d(PFN_encodeTiled enc, CUtensorMap* m, const void* base, CUtensorMapDataType type, uint64_t elem, uint64_t rows,

@@ -202,7 +202,7 @@ int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t s
     if (!(half & (128 >> i))) mx[i] = mx[have];              // not used
   if (g.direct) mc = mw;                                     // not used
   else if (!int8_encode_2d(enc, &mc, p.out, p.dtype == SWAPMOE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, elem,
-                           p.n_tokens, p.n, p.out_stride, 32, kI8Chunk, CU_TENSOR_MAP_SWIZZLE_NONE))
+                           p.n_tokens, p.n, p.out_stride, 32, kI8Chunk, int8_out_swizzle(p.dtype == SWAPMOE_BF16 ? kI8Bf16 : kI8F32)))
     return SWAPMOE_ERR_CUDA;
   const int epi = p.dtype == SWAPMOE_BF16 ? kI8Bf16 : kI8F32;
   const long long work = (long long)((p.n_tokens + g.height - 1) / g.height) * g.n_col_tiles;
@@ -379,8 +379,8 @@ int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_ex
   bool ok = cudaMemset(b->counts, 0, kBankMaxSlots * 4) == cudaSuccess && cudaStreamSynchronize(nullptr) == cudaSuccess;
   for (int i = 0; i < 4; ++i)
     ok = ok && int8_encode_operand(enc, &b->map_x[i], b->rows8, R, d, d, 128 >> i) && int8_encode_operand(enc, &b->map_h[i], b->h8, R, f, f, 128 >> i);
-  ok = ok && int8_encode_2d(enc, &b->map_h_out, b->h, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, f, f, nin == 2 ? 16 : 32, kI8Chunk, CU_TENSOR_MAP_SWIZZLE_NONE) &&
-       int8_encode_2d(enc, &b->map_y_out, b->y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, d, d, 32, kI8Chunk, CU_TENSOR_MAP_SWIZZLE_NONE);
+  ok = ok && int8_encode_2d(enc, &b->map_h_out, b->h, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, f, f, nin == 2 ? 16 : 32, kI8Chunk, int8_out_swizzle(nin == 2 ? kI8Swiglu : kI8Relu)) &&
+       int8_encode_2d(enc, &b->map_y_out, b->y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, R, d, d, 32, kI8Chunk, int8_out_swizzle(kI8F32));
   if (!ok) {
     cudaGetLastError();
     swapmoe_expert_bank_destroy(b);
