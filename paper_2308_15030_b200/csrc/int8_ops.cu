@@ -251,17 +251,18 @@ int32_t matmul_stream(const swapmoe_matmul_t& p, cudaStream_t st, bool pdl) {
 }
 
 // Experts of few pairs.
-template <typename T, int kN>
-cudaError_t bank_stream(const BankStreamArgs& a, bool swiglu, int slots, cudaStream_t st, bool pdl) {
-  const dim3 grid(a.F / 16, slots), block(kStreamThreads);
-  const cudaError_t e = swiglu ? launch_kernel(bank_stream_in_kernel<true, kN>, grid, block, 0, st, pdl, a)
-                               : launch_kernel(bank_stream_in_kernel<false, kN>, grid, block, 0, st, pdl, a);
-  if (e != cudaSuccess) return e;
-  return launch_kernel(bank_stream_out_kernel<T, kN>, dim3(a.d / 16), dim3(kBankOutThreads), (size_t)a.P * bank_row_bytes(a.F), st, pdl, a);
+cudaError_t bank_stream_in(const BankStreamArgs& a, bool swiglu, cudaStream_t st, bool pdl) {
+  const int pairs = std::min(a.in_tokens, a.T) * a.k;
+  const dim3 grid(a.F / 16, std::min(pairs, a.S), (a.T + a.in_tokens - 1) / a.in_tokens), block(kStreamThreads);
+  if (swiglu) return pairs <= 8 ? launch_kernel(bank_stream_in_kernel<true, 1>, grid, block, 0, st, pdl, a) : launch_kernel(bank_stream_in_kernel<true, 2>, grid, block, 0, st, pdl, a);
+  return pairs <= 8 ? launch_kernel(bank_stream_in_kernel<false, 1>, grid, block, 0, st, pdl, a) : launch_kernel(bank_stream_in_kernel<false, 2>, grid, block, 0, st, pdl, a);
 }
 template <typename T>
-cudaError_t bank_stream(const BankStreamArgs& a, bool swiglu, int slots, cudaStream_t st, bool pdl) {
-  return a.P <= 8 ? bank_stream<T, 1>(a, swiglu, slots, st, pdl) : bank_stream<T, 2>(a, swiglu, slots, st, pdl);
+cudaError_t bank_stream_out(const BankStreamArgs& a, cudaStream_t st, bool pdl) {
+  const int pairs = std::min(a.out_tokens, a.T) * a.k;
+  const dim3 grid(a.d / 16, 1, (a.T + a.out_tokens - 1) / a.out_tokens), block(kBankOutThreads);
+  const size_t smem = (size_t)pairs * bank_row_bytes(a.F);
+  return pairs <= 8 ? launch_kernel(bank_stream_out_kernel<T, 1>, grid, block, smem, st, pdl, a) : launch_kernel(bank_stream_out_kernel<T, 2>, grid, block, smem, st, pdl, a);
 }
 
 }  // namespace
@@ -360,7 +361,7 @@ int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_ex
       {reinterpret_cast<void**>(&b->h), R * f * 4}, {reinterpret_cast<void**>(&b->y), R * d * 4},
       {reinterpret_cast<void**>(&b->row_scales), R * 4}, {reinterpret_cast<void**>(&b->h_scales), R * 4},
       {reinterpret_cast<void**>(&b->row_pair), R * 4}, {reinterpret_cast<void**>(&b->row_largest), R * 4}, {reinterpret_cast<void**>(&b->pair_row), (size_t)P * 4},
-      {reinterpret_cast<void**>(&b->largest), (size_t)kStreamMaxPairs * (f / 16) * 4},
+      {reinterpret_cast<void**>(&b->largest), (size_t)std::min<long long>(P, kStreamPairs) * (f / 16) * 4},
       {reinterpret_cast<void**>(&b->counts), kBankMaxSlots * 4}, {reinterpret_cast<void**>(&b->cta_base), (size_t)kBankMaxCtas * c.n_slots * 4},
       {reinterpret_cast<void**>(&b->n_tiles), 16}, {reinterpret_cast<void**>(&b->tiles), n_tiles * sizeof(TileDesc)}};
   size_t bytes = 0;
@@ -444,16 +445,24 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool pdl = standalone_pdl(), swiglu = c.act == SWAPMOE_ACT_SWIGLU;
   const int P = T * c.top_k, pairs = b->dev.pairs;
-  // Few pairs on small experts: two launches that take the weights straight to registers.  us, that form / the general one: 512 x 704 top-2 8
-  // pairs 6.7 / 15, 16 pairs 12.4 / 17; 768 x 2112 8 pairs 15.9 / 22, 16 pairs 35.7 / 25; 2048 x 1024 top-4 8 pairs 19.0 / 22.3, 12 pairs 26 / 23;
-  // 1024 x 4096 4 pairs 13.6 / 25, 8 pairs 33 / 29.
-  if (P <= kStreamMaxPairs && P * bank_row_bytes(c.d_ff) <= kBankOutRowBytes && 3ll * P * c.d_model * c.d_ff <= 60ll << 20) {
+  cudaError_t e = cudaSuccess;
+  // Few pairs on small experts: two launches that take the weights straight to registers.  us, that form / the general one: 512 x 704 top-2 20
+  // pairs 11.9 / 17.9, 32 pairs 13.1 / 18.6, 48 pairs 16.9 / 18.3; 1024 x 512 top-4 24 pairs 14.4 / 20.8, 40 pairs 21.8 / 24.9, 64 pairs 27.0 / 25.2; 512 x
+  // 256 top-8 64 pairs 13.4 / 22.9, 128 pairs 24.7 / 23.9; 768 x 2112 top-2 12 pairs 18.1 / 29.2, 22 pairs 32 / 28; 2048 x 1024 top-4 16 pairs 25.2 / 29.7;
+  // 1024 x 4096 top-2 8 pairs 23.0 / 29.5.
+  const int share = kStreamMaxPairs / c.top_k, fit = kBankOutRowBytes / (c.top_k * bank_row_bytes(c.d_ff));       // tokens that a CTA may take
+  if (P <= kStreamPairs && fit > 0 && 3ll * P * c.d_model * c.d_ff <= (P <= 16 ? 100ll : 68ll) << 20) {
     BankStreamArgs q;
     q.x8 = static_cast<const int8_t*>(x); q.w_in = b->w_in; q.w_out = b->w_out; q.x_scales = x_scales; q.in_scales = b->in_scales;
     q.out_scales = b->out_scales; q.weights = weights; q.slots = slots; q.h = b->h; q.largest = b->largest; q.out = out;
     q.x_stride = x_stride; q.out_stride = out_stride; q.P = P; q.S = c.n_slots; q.k = c.top_k; q.d = c.d_model; q.F = c.d_ff; q.T = T;
-    const int most = std::min(P, c.n_slots);
-    return launched(c.dtype == SWAPMOE_BF16 ? bank_stream<bf16>(q, swiglu, most, st, pdl) : bank_stream<float>(q, swiglu, most, st, pdl));
+    q.in_tokens = share;
+    // the second kernel's CTAs take fewer tokens where that keeps more SMs at work, one CTA on each and with 64 KB of weights at least
+    const long long groups = std::max(1ll, std::min<long long>(b->dev.sms / (c.d_model / 16), (long long)P * 16 * c.d_ff >> 16));
+    q.out_tokens = std::min(std::min(share, fit), (int)((T + groups - 1) / groups));
+    e = bank_stream_in(q, swiglu, st, pdl);
+    if (e == cudaSuccess) e = c.dtype == SWAPMOE_BF16 ? bank_stream_out<bf16>(q, st, pdl) : bank_stream_out<float>(q, st, pdl);
+    return launched(e);
   }
   BankArgs a;
   a.x8 = static_cast<const int8_t*>(x); a.x_scales = x_scales; a.slots = slots; a.rows8 = b->rows8; a.row_scales = b->row_scales;
@@ -468,7 +477,6 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   if (a.per_cta < 8) a.per_cta = 8;
   const int ctas = (P + a.per_cta - 1) / a.per_cta;
   if (ctas > kBankMaxCtas) return SWAPMOE_ERR_UNSUPPORTED;
-  cudaError_t e = cudaSuccess;
   if (!a.direct) e = launch_kernel(bank_count_kernel, dim3(ctas), dim3(kBankThreads), 0, st, pdl, a);
   if (e == cudaSuccess) e = launch_kernel(bank_gather_kernel, dim3(ctas), dim3(kBankThreads), 0, st, pdl, a);
 

@@ -6,9 +6,10 @@
 // is on its way at once; their sums meet in shared memory.  Against a ring of TMA stages with tensor memory behind it a call has no barriers to
 // set up, no tensor memory to take and no ring to fill.
 //
-// With experts (up to 16 pairs of token and choice) the same in two launches: the first takes the rows of W_in of every slot that is asked for
-// (SwiGLU: both products of sixteen hidden units), applies the activation and leaves h in fp32 with the largest magnitude of every 16 values; the second
-// takes rows of W_out, fetched before the first has finished, and all of h to 8 bits in shared memory, and adds a token's choices in their order.
+// With experts (up to 64 pairs of token and choice) the same in two launches, whose CTAs serve whole tokens of up to 16 pairs each: the first takes
+// the rows of W_in of every slot that its tokens ask for (SwiGLU: both products of sixteen hidden units), applies the activation and leaves h in fp32
+// with the largest magnitude of every 16 values; the second takes rows of W_out, fetched before the first has finished, and its tokens' h to 8 bits
+// in shared memory, and adds a token's choices in their order.
 #pragma once
 #include "quantize_rows.cuh"
 
@@ -17,7 +18,8 @@ namespace swapmoe {
 constexpr int kStreamThreads = 256;
 constexpr int kStreamWarps = kStreamThreads / 32;
 constexpr int kStreamTurn = kStreamWarps * 64;                // columns that a CTA's warps take in one turn
-constexpr int kStreamMaxPairs = 16;
+constexpr int kStreamPairs = 64;                              // pairs of a call
+constexpr int kStreamMaxPairs = 16;                           // pairs of a CTA's tokens
 
 __device__ __forceinline__ void mma_int8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -159,7 +161,20 @@ struct BankStreamArgs {
   void* out;
   long long x_stride, out_stride;
   int P, S, k, d, F, T;
+  int in_tokens, out_tokens;    // tokens of a CTA of the two kernels
 };
+
+// The share of `tokens` tokens that belongs to this CTA (blockIdx.z).
+template <typename T>
+__device__ __forceinline__ BankStreamArgs bank_share(const BankStreamArgs& whole, int tokens) {
+  BankStreamArgs a = whole;
+  const int t0 = (int)blockIdx.z * tokens;
+  a.T = min(tokens, a.T - t0); a.P = a.T * a.k;
+  a.x8 += (size_t)t0 * a.x_stride; a.x_scales += t0; a.slots += t0 * a.k; a.weights += t0 * a.k;
+  a.h += (size_t)t0 * a.k * a.F; a.largest += (size_t)t0 * a.k * (a.F / 16);
+  a.out = static_cast<T*>(a.out) + (size_t)t0 * a.out_stride;
+  return a;
+}
 
 // The pairs by the slots they ask for: slots in the order of their first pair.
 struct BankLists {
@@ -190,9 +205,10 @@ __device__ __forceinline__ void bank_lists(const BankStreamArgs& a, BankLists* l
   if (lane == 0) l->n = __popc(leaders);
 }
 
-// h of sixteen hidden units of one slot for all its pairs.
+// h of sixteen hidden units of one slot for the pairs that the CTA's tokens have there.
 template <bool kSwiglu, int kN>
-__global__ void __launch_bounds__(kStreamThreads) bank_stream_in_kernel(const __grid_constant__ BankStreamArgs a) {
+__global__ void __launch_bounds__(kStreamThreads) bank_stream_in_kernel(const __grid_constant__ BankStreamArgs whole) {
+  const BankStreamArgs a = bank_share<char>(whole, whole.in_tokens);
   constexpr int kM = kSwiglu ? 2 : 1;
   typedef StreamTile<kM, kN, 4 / kM> Tile;
   __shared__ int s_part[kStreamWarps * kM * kN * 8 * 16];
@@ -258,7 +274,7 @@ __device__ __forceinline__ uint4 quantize16(const float* h, float divisor, float
   return make_uint4(b[0], b[1], b[2], b[3]);
 }
 
-// Sixteen channels of the result for all tokens.  The CTA's warps share the slots out among them: as many slots side by side as there are (up to
+// Sixteen channels of the result for the CTA's tokens.  The CTA's warps share the slots out among them: as many slots side by side as there are (up to
 // all warps), the warps of a slot take turns of its columns.
 constexpr int kBankOutThreads = 512;
 constexpr int kBankOutWarps = kBankOutThreads / 32;
@@ -268,7 +284,8 @@ constexpr int kBankOutRowBytes = 64 * 1024;                  // most shared memo
 static_assert(kStreamMaxPairs * 16 <= kBankOutThreads && kStreamMaxPairs <= 32, "a thread per pair and channel, a lane per pair");
 
 template <typename T, int kN>
-__global__ void __launch_bounds__(kBankOutThreads) bank_stream_out_kernel(const __grid_constant__ BankStreamArgs a) {
+__global__ void __launch_bounds__(kBankOutThreads) bank_stream_out_kernel(const __grid_constant__ BankStreamArgs whole) {
+  const BankStreamArgs a = bank_share<T>(whole, whole.out_tokens);
   typedef StreamTile<1, kN, 4> Tile;
   __shared__ int s_part[kBankOutWarps * kN * 8 * 16];
   __shared__ float s_y[kStreamMaxPairs * 16];

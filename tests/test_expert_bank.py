@@ -275,6 +275,20 @@ def test_widest_experts_and_few_pairs(d, F, S, k, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,F,S,k,T", [(512, 256, 128, 8, 7), (512, 704, 16, 2, 24), (1024, 512, 64, 4, 10), (768, 2112, 32, 2, 7), (64, 64, 4, 3, 21),
+                                       (128, 128, 5, 5, 11), (256, 128, 3, 16, 4), (64, 192, 9, 1, 64), (192, 4096, 6, 7, 3), (4096, 64, 40, 6, 10)])
+@pytest.mark.parametrize("act,dtype", [("swiglu", "bf16"), ("relu", "fp32")])
+def test_few_pairs_in_several_groups_of_tokens(d, F, S, k, T, act, dtype):
+    c = Case(T, d, F, S, k, act, dtype)
+    c.check(c.run())
+    c = Case(T, d, F, S, k, act, dtype, none=0.3)
+    c.slots[T - 1] = -1                                                  # the last token has no expert
+    c.check(c.run())
+    c = Case(T, d, F, S, k, act, dtype, only=S - 1)
+    c.check(c.run())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d,F,S,k,T", [(4096, 64, 3, 1, 7000), (64, 4096, 5, 2, 3500), (2048, 2048, 2, 2, 6500)])
 def test_rows_beyond_a_scheduling_group(d, F, S, k, T):
     """More rows than stay in L2 at once: both products walk them in groups."""
