@@ -210,22 +210,38 @@ int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t s
                                 int8_smem_bytes(epi), st, pdl, mw, mx[0], mx[1], mx[2], mx[3], mc, g));
 }
 
-// The same for up to kSplitMaxTokens tokens, a cluster for each 128 rows of weights.
+// Tokens of a cluster and its CTAs, by what a CTA has to do in ns: its bytes, (128 + cols) 128 a k-block at 87 GB/s; the sums' exchange, and
+// what becomes of them, by token.  More CTAs than SMs only where nothing is shared.  us with one group of tokens / as picked: 1024 x 1024 at 32, 64, 128
+// tokens 3.3 / 3.0, 3.9 / 3.1, 5.3 / 3.5; 2048 -> 512 3.6 / 3.3, 4.3 / 3.3, 5.9 / 3.5; 4096 -> 1024 4.6 / 4.5, 5.2 / 4.8, 6.9 / 5.2; CTAs of a cluster at 16
+// tokens, 1 / 2 / 4 / 8: 4096 x 4096 9.0 / 6.9 / 5.7 / 6.8, 4096 -> 1024 8.3 / 5.7 / 4.1 / 3.8, 1024 x 1024 3.6 / 3.3 / 2.9 / 3.4.
+struct SplitShape { int cols, cluster; };
+SplitShape split_shape(int T, int n_tiles, int k_blocks, int sms) {
+  constexpr int kExchange[4] = {0, 700, 800, 650}, kToken[4] = {16, 16, 16, 36};
+  SplitShape best = {0, 1};
+  long long least = -1;
+  for (int most = kSplitMaxTokens; most >= 16; most /= 2)
+    for (int i = 0; i < 4; ++i) {
+      const int cluster = 1 << i, groups = (T + most - 1) / most, step = std::max(16, 4 * cluster);
+      if (i > 0 && 2 * cluster > k_blocks) continue;
+      if ((i > 0 || most < kSplitMaxTokens) && (long long)n_tiles * groups * cluster > sms) continue;
+      const int cols = ((T + groups - 1) / groups + step - 1) / step * step;
+      const long long cost = (k_blocks + cluster - 1) / cluster * (128ll + cols) * 3 / 2 + kToken[i] * cols + kExchange[i];
+      if (least < 0 || cost < least) { least = cost; best = SplitShape{cols, cluster}; }
+    }
+  return best;
+}
+
+// The same with a cluster for each 128 rows of weights and up to kSplitMaxTokens tokens.
 int32_t matmul_split(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t st, bool pdl) {
   const PFN_encodeTiled enc = encoder();
   if (!enc) return SWAPMOE_ERR_CUDA;
   I8SplitArgs g;
   g.out = p.out; g.x_scales = p.x_scales; g.w_scales = p.w_scales; g.bias = p.bias; g.ldc = p.out_stride;
   g.T = p.n_tokens; g.N = p.n; g.k_blocks = (p.k + kI8BK - 1) / kI8BK;
-  const int tiles = (p.n + kTcBM - 1) / kTcBM;
-  // One CTA an SM at most, with two k-blocks at least; a cluster of eight only where a quarter of the columns would leave half the SMs idle
-  // and still be sixteen k-blocks.  us at 1 / 2 / 4 / 8 CTAs, 16 and 64 tokens: 4096 x 4096 9.0 / 6.9 / 5.7 / 6.8 and 12.0 / 9.4 / 7.6 / 9.0;
-  // 4096 -> 1024 8.3 / 5.7 / 4.1 / 3.8 and 9.8 / 7.5 / 5.5 / 4.7; 1024 x 1024 3.6 / 3.3 / 2.9 / 3.4 and 4.9 / 5.1 / 4.2 / 4.3.
-  int cluster = 1;
-  while (cluster < 4 && 2 * cluster * tiles <= dev.sms && 4 * cluster <= g.k_blocks) cluster *= 2;
-  if (cluster == 4 && 16 * tiles <= dev.sms && g.k_blocks >= 32) cluster = 8;
-  const int step = std::max(16, 4 * cluster);
-  g.cols = (p.n_tokens + step - 1) / step * step;
+  const int n_tiles = (p.n + kTcBM - 1) / kTcBM;
+  const SplitShape shape = split_shape(p.n_tokens, n_tiles, g.k_blocks, dev.sms);
+  const int cluster = shape.cluster;
+  g.cols = shape.cols;
   g.share = (g.k_blocks + cluster - 1) / cluster;
   const int stage = kSplitABytes + g.cols * kI8BK;
   g.n_stages = std::max(1, std::min(std::min(g.share, kSplitMaxStages), kSplitRoom / stage));
@@ -233,7 +249,7 @@ int32_t matmul_split(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t 
   CUtensorMap mw, mx;
   if (!int8_encode_operand(enc, &mw, p.w, p.n, p.k, ws, 128) || !int8_encode_operand(enc, &mx, p.x, p.n_tokens, p.k, xs, g.cols)) return SWAPMOE_ERR_CUDA;
   const size_t smem = 1024 + int8_split_area(g.cols, g.n_stages);
-  const dim3 grid(tiles * cluster), block(kSplitThreads);
+  const dim3 grid(n_tiles * cluster, (p.n_tokens + g.cols - 1) / g.cols), block(kSplitThreads);
   return launched(p.dtype == SWAPMOE_BF16 ? launch_cluster(int8_split_kernel<bf16>, cluster, grid, block, smem, st, pdl, mw, mx, g)
                                           : launch_cluster(int8_split_kernel<float>, cluster, grid, block, smem, st, pdl, mw, mx, g));
 }
@@ -308,14 +324,16 @@ int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* p, void* stream) {
   const int32_t rc = current_device(&dev);
   if (rc != SWAPMOE_OK) return rc;
   // Few tokens and a small matrix: the weights straight to registers.  Few tokens, or few tiles: the contraction shared.  us for 8 tokens,
-  // registers / shared: 1024 x 1024 2.2 / 3.0, 2048 x 2048 2.7 / 4, 4096 -> 1024 3.9 / 3.7, 4096 x 4096 6.2 / 5.7, 4096 -> 14336 15.8 / 11.9.
-  // Shared / CTA pairs at 32, 64, 96, 128 tokens: 4096 x 4096 6.1 / 9.9, 7.1 / 10.2, 8.4 / 10.5, 9.4 / 10.6; 1024 -> 4096 3.6 / 4.8, 4.3 / 5.1,
-  // 5.4 / 5.4, 6.4 / 5.4; 4096 -> 14336 12.5 / 12.5, 14.4 / 12.8, 16.2 / 13.1, 17.0 / 13.4.
+  // registers / shared: 1024 x 1024 2.2 / 2.9, 2048 x 2048 2.7 / 4, 4096 -> 1024 3.9 / 3.7, 4096 x 4096 6.2 / 5.7, 4096 -> 14336 15.8 / 11.9.
+  // Shared / CTA pairs: 4096 -> 14336 at 32, 64 tokens 12.5 / 12.5, 14.4 / 12.8; 1024 -> 4096 at 64, 96, 128 4.2 / 5.1, 4.4 / 5.4, 6.4 / 5.9;
+  // 4096 x 4096 at 128, 160, 256 9.6 / 10.6, 9.5 / 11.1, 11.4 / 11.3; 14336 -> 4096 at 200 25.3 / 28.3; 4096 -> 1024 at 256, 512, 1024 6.1 / 10.5,
+  // 8.7 / 10.8, 10.6 / 11.1; 2048 x 2048 at 256, 384 6.2 / 7.5, 8.2 / 7.7; 1024 x 1024 at 256, 320 3.6 / 5.3, 5.5 / 5.4; 512 x 512 at 512 2.8 / 4.4.
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (p->n_tokens <= kStreamTokens && p->k <= 2048 && (long long)p->k * p->n <= 6ll << 20) return matmul_stream(*p, st, standalone_pdl());
   const int tiles = (p->n + kTcBM - 1) / kTcBM;
   const int shared = 4 * tiles <= dev.sms ? (p->k >= 2048 ? kSplitMaxTokens : 96) : 2 * tiles <= dev.sms ? 64 : 32;
-  if (p->n_tokens <= shared) return matmul_split(*p, dev, st, standalone_pdl());
+  const int group = p->k >= 2048 ? 128 : 64, ctas = p->k >= 4096 ? 2 : 4;
+  if (p->n_tokens <= shared || (long long)ctas * tiles * ((p->n_tokens + group - 1) / group) <= dev.sms) return matmul_split(*p, dev, st, standalone_pdl());
   return matmul_pair(*p, dev, st, standalone_pdl());
 }
 

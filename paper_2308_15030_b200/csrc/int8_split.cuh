@@ -1,8 +1,9 @@
-// Products of 8-bit integers for up to 128 tokens on matrices of few tiles: a cluster shares the contraction of a tile.
+// Products of 8-bit integers on few tiles, for up to 128 tokens and more on narrow matrices: a cluster shares the contraction of a tile.
 //
-// With up to 128 tokens a matrix has n / 128 tiles, too few for the SMs that its bytes should come through.  Each CTA of a cluster takes a share of
-// the k-blocks of 128 weight rows x all tokens (tcgen05 kind::i8, operands by TMA), and the shares are added as integers, so that neither the
-// split nor its order changes a bit: every CTA collects the tokens of its rank from the others' shared memory, scales them and stores them.
+// n / 128 tiles for each group of up to 128 tokens are too few for the SMs that the bytes should come through: an SM takes in 87 GB/s at most, which is
+// what bounds a CTA.  Each CTA of a cluster takes a share of the k-blocks of 128 weight rows x all tokens of the group (tcgen05 kind::i8, operands by
+// TMA), and the shares are added as integers, so that neither the split nor its order changes a bit: every CTA collects the tokens of its rank from
+// the others' shared memory, scales them and stores them.
 // Roles (320 threads): warp 0 = TMA producer, warp 1 = TMEM allocation and MMA issuer, warps 2-9 = sums out of
 // tensor memory, and what is done with them.  No load uses cluster multicast; every wait is bounded.
 #pragma once
@@ -22,7 +23,7 @@ struct I8SplitArgs {
   const float *x_scales, *w_scales, *bias;
   long long ldc;
   int32_t T, N, k_blocks, share;       // share: k-blocks of a CTA
-  int32_t cols, n_stages;              // tokens rounded up to a multiple of 16 and of 4 x CTAs of a cluster; stages of the ring
+  int32_t cols, n_stages;              // tokens of a cluster, a multiple of 16 and of 4 x its CTAs; stages of the ring
 };
 
 namespace ptx {
@@ -41,7 +42,7 @@ __host__ __device__ inline int int8_split_area(int cols, int n_stages) {
   return ring > sums ? ring : sums;
 }
 
-template <typename T>
+template <typename Out>
 __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
                                                                    const __grid_constant__ I8SplitArgs a) {
   extern __shared__ unsigned char smem_raw[];
@@ -56,7 +57,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const int n0 = (int)(blockIdx.x / size) * kTcBM;
+  const int n0 = (int)(blockIdx.x / size) * kTcBM, first = (int)blockIdx.y * a.cols, T = a.T - first;       // first token, tokens from there on
   const int q = warp & 3, part = (warp - 2) >> 2, n = n0 + q * 32 + lane;   // warps 2-9: the quarter of tensor memory that the warp may read, and its weight row
   float w_scale = 0.f, bias = 0.f;
   const int kb0 = (int)rank * a.share, kb1 = min(a.k_blocks, kb0 + a.share), blocks = max(0, kb1 - kb0);
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
       if (ptx::elect_one()) {
         ptx::mbar_expect_tx(&full[stage], (uint32_t)(kSplitABytes + x_bytes));
         ptx::tma_load_2d(sW + stage * kSplitABytes, &tmW, &full[stage], (kb0 + i) * kI8BK, n0);
-        ptx::tma_load_2d(sX + stage * x_bytes, &tmX, &full[stage], (kb0 + i) * kI8BK, 0);
+        ptx::tma_load_2d(sX + stage * x_bytes, &tmX, &full[stage], (kb0 + i) * kI8BK, first);
       }
       __syncwarp();
       if (++stage == a.n_stages) { stage = 0; phase ^= 1u; }
@@ -133,7 +134,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
         if (a.bias != nullptr) bias = a.bias[n];
       }
       const int t = q * 32 + lane;
-      if (part == 0) s_x_scale[t] = t < a.T ? a.x_scales[t] : 0.f;
+      if (part == 0) s_x_scale[t] = t < T ? a.x_scales[first + t] : 0.f;
       if (blocks > 0) {
         warp_wait(&done, 0u, abort_flag, status, 43);
         ptx::tc_fence_after();
@@ -182,7 +183,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
   if (warp < 2 || n >= a.N) return;
   const int t0 = (int)rank * mine;
 #pragma unroll 2
-  for (int i = part; i < mine / 4 && t0 + 4 * i < a.T; i += 2) {
+  for (int i = part; i < mine / 4 && t0 + 4 * i < T; i += 2) {
     int4 v = s_sums[i * kTcBM + q * 32 + lane];
     for (int o = 1; o < (int)size; ++o) {
       const int4 u = s_sums[(o * (mine / 4) + i) * kTcBM + q * 32 + lane];
@@ -191,11 +192,11 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
     const float4 xs = *reinterpret_cast<const float4*>(s_x_scale + t0 + 4 * i);
     const float f[4] = {(float)v.x * w_scale * xs.x + bias, (float)v.y * w_scale * xs.y + bias, (float)v.z * w_scale * xs.z + bias,
                         (float)v.w * w_scale * xs.w + bias};
-    T* out = static_cast<T*>(a.out) + (size_t)(t0 + 4 * i) * a.ldc + n;
+    Out* out = static_cast<Out*>(a.out) + (size_t)(first + t0 + 4 * i) * a.ldc + n;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (t0 + 4 * i + j < a.T) {
-        if constexpr (sizeof(T) == 2) out[j * a.ldc] = __float2bfloat16_rn(f[j]);
+      if (t0 + 4 * i + j < T) {
+        if constexpr (sizeof(Out) == 2) out[j * a.ldc] = __float2bfloat16_rn(f[j]);
         else out[j * a.ldc] = f[j];
       }
   }
