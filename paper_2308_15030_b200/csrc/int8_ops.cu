@@ -211,9 +211,10 @@ int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t s
 }
 
 // Tokens of a cluster and its CTAs, by what a CTA has to do in ns: its bytes, (128 + cols) 128 a k-block at 87 GB/s; the sums' exchange, and
-// what becomes of them, by token.  More CTAs than SMs only where nothing is shared.  us with one group of tokens / as picked: 1024 x 1024 at 32, 64, 128
-// tokens 3.3 / 3.0, 3.9 / 3.1, 5.3 / 3.5; 2048 -> 512 3.6 / 3.3, 4.3 / 3.3, 5.9 / 3.5; 4096 -> 1024 4.6 / 4.5, 5.2 / 4.8, 6.9 / 5.2; CTAs of a cluster at 16
-// tokens, 1 / 2 / 4 / 8: 4096 x 4096 9.0 / 6.9 / 5.7 / 6.8, 4096 -> 1024 8.3 / 5.7 / 4.1 / 3.8, 1024 x 1024 3.6 / 3.3 / 2.9 / 3.4.
+// what becomes of them, by token; clusters of eight on more than half of the SMs start late.  More CTAs than SMs only where nothing is shared.
+// us with one group of tokens / as picked: 1024 x 1024 at 32, 64, 128 tokens 3.3 / 2.9, 3.9 / 3.1, 5.3 / 3.5; 2048 -> 512 3.6 / 3.3, 4.3 / 3.3, 5.9 / 3.5;
+// 4096 -> 1024 at 64, 128 5.2 / 4.8, 6.9 / 5.1; CTAs of a cluster at 16 tokens, 1 / 2 / 4 / 8: 4096 x 4096 9.0 / 6.9 / 5.7 / 6.8, 4096 -> 1024 8.3 / 5.7 /
+// 4.1 / 3.8, 1024 x 1024 3.6 / 3.3 / 2.9 / 3.4.
 struct SplitShape { int cols, cluster; };
 SplitShape split_shape(int T, int n_tiles, int k_blocks, int sms) {
   constexpr int kExchange[4] = {0, 700, 800, 650}, kToken[4] = {16, 16, 16, 36};
@@ -223,9 +224,10 @@ SplitShape split_shape(int T, int n_tiles, int k_blocks, int sms) {
     for (int i = 0; i < 4; ++i) {
       const int cluster = 1 << i, groups = (T + most - 1) / most, step = std::max(16, 4 * cluster);
       if (i > 0 && 2 * cluster > k_blocks) continue;
-      if ((i > 0 || most < kSplitMaxTokens) && (long long)n_tiles * groups * cluster > sms) continue;
+      const long long ctas = (long long)n_tiles * groups * cluster;
+      if ((i > 0 || most < kSplitMaxTokens) && ctas > sms) continue;
       const int cols = ((T + groups - 1) / groups + step - 1) / step * step;
-      const long long cost = (k_blocks + cluster - 1) / cluster * (128ll + cols) * 3 / 2 + kToken[i] * cols + kExchange[i];
+      const long long cost = (k_blocks + cluster - 1) / cluster * (128ll + cols) * 3 / 2 + kToken[i] * cols + kExchange[i] + (i == 3 && 2 * ctas > sms ? 100 : 0);
       if (least < 0 || cost < least) { least = cost; best = SplitShape{cols, cluster}; }
     }
   return best;
