@@ -137,6 +137,36 @@ def test_several_rounds_of_tiles():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,K,N", [(9, 4096, 1000), (37, 1024, 1000), (90, 8192, 100), (130, 2048, 500), (129, 64, 4), (257, 4111, 513), (333, 600, 33),
+                                   (512, 1024, 257), (640, 14336, 257), (1000, 512, 100), (2000, 4096, 40), (4600, 256, 128)])
+@pytest.mark.parametrize("dtype,out_pad", [("bf16", 0), ("fp32", 3)])
+def test_narrow_matrices_in_several_groups_of_tokens(T, K, N, dtype, out_pad):
+    _check(T, K, N, dtype, bias=True, out_pad=out_pad, x_pad=(16 - K) % 16 + 16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [129, 200, 600, 1100])
+@pytest.mark.parametrize("K,N", [(16, 5008), (129, 4999), (1003, 6033), (2048, 4800)])
+@pytest.mark.parametrize("dtype,out_pad", [("bf16", 0), ("bf16", 1), ("bf16", 8), ("fp32", 0), ("fp32", 1)])
+def test_wide_matrices(T, K, N, dtype, out_pad):
+    _check(T, K, N, dtype, bias=K % 2 == 1, out_pad=out_pad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,N", [(300, 4864), (900, 2560)])
+def test_all_lowest_values_of_wide_matrices(T, N):
+    import torch
+    K = 131071
+    x = torch.full((T, K + 1), -128, dtype=torch.int8, device="cuda")[:, :K]
+    w = torch.full((N, K + 1), -128, dtype=torch.int8, device="cuda")[:, :K]
+    out = torch.empty(T, N, device="cuda")
+    one = torch.ones(max(T, N), device="cuda")
+    binding.matmul_scaled(x, one[:T].contiguous(), w, one[:N].contiguous(), out)
+    assert bool((out == float(torch.tensor(2 ** 14 * K, dtype=torch.float32))).all())
+    assert binding.matmul_status() == (0, 0)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 40, 300])
 def test_scales_that_are_not_finite_or_zero(T):
     import torch
