@@ -213,8 +213,8 @@ int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t s
 
 // Tokens of a cluster and its CTAs, by what a CTA has to do in ns: its bytes, (128 + cols) 128 a k-block at 87 GB/s; the sums' exchange, and
 // what becomes of them, by token; clusters of eight on more than half of the SMs start late.  More CTAs than SMs only where nothing is shared.
-// us with one group of tokens / as picked: 1024 x 1024 at 32, 64, 128 tokens 3.3 / 2.9, 3.9 / 3.1, 5.3 / 3.5; 2048 -> 512 3.6 / 3.3, 4.3 / 3.3, 5.9 / 3.5;
-// 4096 -> 1024 at 64, 128 5.2 / 4.8, 6.9 / 5.1; CTAs of a cluster at 16 tokens, 1 / 2 / 4 / 8: 4096 x 4096 9.0 / 6.9 / 5.7 / 6.8, 4096 -> 1024 8.3 / 5.7 /
+// us with one group of tokens / as picked: 1024 x 1024 at 32, 64, 128 tokens 3.7 / 3.4, 4.3 / 3.4, 5.6 / 3.7; 2048 -> 512 4.1 / 3.8, 4.7 / 3.8, 6.4 / 3.8;
+// 4096 -> 1024 at 64, 128 5.2 / 4.8, 7.0 / 5.1; CTAs of a cluster at 16 tokens, 1 / 2 / 4 / 8: 4096 x 4096 9.0 / 6.9 / 5.7 / 6.8, 4096 -> 1024 8.3 / 5.7 /
 // 4.1 / 3.8, 1024 x 1024 3.6 / 3.3 / 2.9 / 3.4.
 struct SplitShape { int cols, cluster; };
 SplitShape split_shape(int T, int n_tiles, int k_blocks, int sms) {
@@ -327,10 +327,10 @@ int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* p, void* stream) {
   const int32_t rc = current_device(&dev);
   if (rc != SWAPMOE_OK) return rc;
   // Few tokens and a small matrix: the weights straight to registers.  Few tokens, or few tiles: the contraction shared.  us for 8 tokens,
-  // registers / shared: 1024 x 1024 2.2 / 2.9, 2048 x 2048 2.7 / 4, 4096 -> 1024 3.9 / 3.7, 4096 x 4096 6.2 / 5.7, 4096 -> 14336 15.8 / 11.9.
-  // Shared / CTA pairs: 4096 -> 14336 at 32, 64 tokens 12.5 / 12.5, 14.4 / 12.8; 1024 -> 4096 at 64, 96, 128 4.2 / 5.1, 4.4 / 5.4, 6.4 / 5.9;
+  // registers / shared: 1024 x 1024 2.4 / 3.4, 2048 x 2048 3.3 / 4.2, 4096 -> 1024 4.7 / 4.5, 4096 x 4096 6.3 / 5.9, 4096 -> 14336 15.8 / 12.6.
+  // Shared / CTA pairs: 4096 -> 14336 at 32, 64 tokens 12.5 / 12.5, 14.4 / 12.8; 1024 -> 4096 at 64, 96, 128 4.2 / 5.1, 4.5 / 5.4, 6.4 / 5.9;
   // 4096 x 4096 at 128, 160, 256 9.6 / 10.6, 9.5 / 11.1, 11.4 / 11.3; 14336 -> 4096 at 200 25.3 / 28.3; 4096 -> 1024 at 256, 512, 1024 6.1 / 10.5,
-  // 8.7 / 10.8, 10.6 / 11.1; 2048 x 2048 at 256, 384 6.2 / 7.5, 8.2 / 7.7; 1024 x 1024 at 256, 320 3.6 / 5.3, 5.5 / 5.4; 512 x 512 at 512 2.8 / 4.4.
+  // 8.7 / 10.8, 10.6 / 11.1; 2048 x 2048 at 256, 384 6.2 / 7.6, 8.2 / 7.7; 1024 x 1024 at 256, 320 4.0 / 5.6, 5.7 / 5.6; 512 x 512 at 512 3.1 / 4.5.
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (p->n_tokens <= kStreamTokens && p->k <= 2048 && (long long)p->k * p->n <= 6ll << 20) return matmul_stream(*p, st, standalone_pdl());
   const int tiles = (p->n + kTcBM - 1) / kTcBM;
