@@ -5,7 +5,7 @@
 // Bound by HBM and, next to it, by instructions.  A team of warps holds a row in registers between its maximum and its rounding, bf16 rows
 // as they are stored, two values a register: a team of eight warps then holds rows of 16384, and as many teams fit an SM as keep
 // enough bytes in flight.  A value costs five instructions: products, sums and maxima go two at a time, rounding is the addition of 1.5 2^23, whose
-// sum has the integer in its lowest byte.
+// sum has the integer in its lowest byte.  8192 rows of 14336 bf16: 63 us, 5.6 TB/s (a plain copy 6.5); 61 rows of 4096 2.0 us.
 #pragma once
 #include <type_traits>
 
