@@ -315,7 +315,7 @@ int32_t swapmoe_quantize_rows(const swapmoe_quantize_rows_t* p, void* stream) {
 int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* p, void* stream) {
   if (!p || p->n_tokens < 0 || p->k < 1 || p->n < 1) return SWAPMOE_ERR_INVALID_ARG;
   if (p->dtype != SWAPMOE_F32 && p->dtype != SWAPMOE_BF16) return SWAPMOE_ERR_INVALID_ARG;
-  if (p->k > kI8MaxK) return SWAPMOE_ERR_UNSUPPORTED;
+  if (p->k > kI8MaxK || p->n > INT32_MAX - 256 || p->n_tokens > INT32_MAX - 256) return SWAPMOE_ERR_UNSUPPORTED;      // (tiles behind the end keep to int32)
   if (p->n_tokens == 0) return SWAPMOE_OK;
   const size_t elem = p->dtype == SWAPMOE_BF16 ? 2 : 4;
   if (!p->x || !p->x_scales || !p->w || !p->w_scales || !p->out || p->x_stride < p->k || p->w_stride < p->k || p->out_stride < p->n)

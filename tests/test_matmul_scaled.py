@@ -30,6 +30,11 @@ def test_no_arguments_and_no_tokens():
     assert binding.lib().swapmoe_matmul_scaled(ctypes.byref(_args(n_tokens=0, x=None)), None) == 0
 
 
+@pytest.mark.parametrize("kw", [dict(n=2 ** 31 - 1, out_stride=2 ** 31), dict(n_tokens=2 ** 31 - 256), dict(n=2 ** 31 - 256, out_stride=2 ** 31)])
+def test_sizes_beyond_int32_are_refused(kw):
+    assert binding.lib().swapmoe_matmul_scaled(ctypes.byref(_args(**kw)), None) == -7
+
+
 def test_tensor_checks():
     import torch
     i8 = dict(dtype=torch.int8)
