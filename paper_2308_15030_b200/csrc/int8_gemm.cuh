@@ -37,7 +37,7 @@ struct I8GemmArgs {
   int32_t w_rows;           // weight rows per slot
   int32_t row_group;        // token tiles per scheduling group (see decode_tile)
   int32_t T, height;        // height: multiple of 32, up to 256
-  int32_t direct;           // rows of C that the TMA unit cannot store: elements leave one by one
+  int32_t direct;           // rows of C that the TMA unit cannot store: elements leave one by one (2: bf16 ones two by two)
   // 1: the kernel in front holds no tensor memory and has waited for all before it: pairs get ready while it runs.  2: and the list of
   // tiles and the weights are older than it: the first boxes of weights are requested too.
   int32_t early;
@@ -289,7 +289,7 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     // 8 j + 2 (l % 4) + e of a chunk's 16, v[8 h + 4 j + 2 i + e]; else lane l holds row l and all sixteen.
     constexpr bool kFragments = EPI == kI8Bf16 || kSwiglu;
     constexpr int kRows = kFragments ? 4 : 1;  // weight rows of a lane
-    const int row8 = lane >> 2, two = 2 * (lane & 3);
+    const int row8 = lane >> 2, two = 2 * (lane & 3), hi = lane >> 4;
     constexpr int kBox = int8_box_bytes(EPI);
     unsigned char* const stg0 = smem + int8_ring_bytes(EPI) + 1024 + (warp - 4) * 2 * kBox;
     float* s_scale = reinterpret_cast<float*>(smem + int8_ring_bytes(EPI) + 1024 + 2 * kI8EpiWarps * kBox) + (warp - 4) * kI8Chunk;
@@ -418,7 +418,7 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         __syncwarp();
         if (kSwiglu) {
           // [16 tokens][16 units] with the 64-byte swizzle; lanes of units 4 ... 7 begin with their odd token, whose row lies in the other banks
-          const int swap = (lane >> 4) & 1;
+          const int swap = hi;
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
             const int j = u >> 2, i = (u >> 1) & 1, e = (u & 1) ^ swap, token = 8 * j + two + e;
@@ -434,10 +434,20 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
                                            pack_bf16x2(f[8 + 4 * j], f[8 + 4 * j + 1]), pack_bf16x2(f[8 + 4 * j + 2], f[8 + 4 * j + 3]));
           if (a.direct) {                                      // (the box is a way between the lanes)
             __syncwarp();
-            for (int j = 0; j < min(left, kI8Chunk); ++j)
-              if (col < a.n_cols)
-                static_cast<bf16*>(a.C)[(size_t)(td.row0 + t0 + j) * a.ldc + col] =
-                    reinterpret_cast<const bf16*>(stg)[j * 32 + 8 * ((lane >> 3) ^ ((j >> 1) & 3)) + (lane & 7)];
+            if (a.direct == 2) {
+              const int pair = lane & 15;
+#pragma unroll
+              for (int j = hi; j < kI8Chunk; j += 2)
+                if (j < left && col0 + 2 * pair < a.n_cols)
+                  *reinterpret_cast<uint32_t*>(static_cast<bf16*>(a.C) + (size_t)(td.row0 + t0 + j) * a.ldc + col0 + 2 * pair) =
+                      reinterpret_cast<const uint32_t*>(stg)[j * 16 + 4 * ((pair >> 2) ^ ((j >> 1) & 3)) + (pair & 3)];
+            } else {
+#pragma unroll
+              for (int j = 0; j < kI8Chunk; ++j)
+                if (j < left && col < a.n_cols)
+                  static_cast<bf16*>(a.C)[(size_t)(td.row0 + t0 + j) * a.ldc + col] =
+                      reinterpret_cast<const bf16*>(stg)[j * 32 + 8 * ((lane >> 3) ^ ((j >> 1) & 3)) + (lane & 7)];
+            }
             continue;
           }
         } else {

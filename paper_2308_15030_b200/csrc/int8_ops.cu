@@ -189,6 +189,7 @@ int32_t matmul_pair(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t s
   const size_t elem = p.dtype == SWAPMOE_BF16 ? 2 : 4;
   // The TMA unit stores sixteen bytes or none of them: a row that ends inside of sixteen is stored by elements, as is one that begins there.
   g.direct = !rows_aligned(p.out, 2, p.out_stride, elem, 16) || p.n * elem % 16 != 0;
+  if (g.direct && elem == 2 && p.n % 2 == 0 && rows_aligned(p.out, 2, p.out_stride, elem, 4)) g.direct = 2;
   const long long xs = p.n_tokens > 1 ? p.x_stride : (p.k + 15) / 16 * 16, ws = p.n > 1 ? p.w_stride : (p.k + 15) / 16 * 16;
   CUtensorMap mw, mx[4], mc;
   if (!int8_encode_operand(enc, &mw, p.w, p.n, p.k, ws, 128)) return SWAPMOE_ERR_CUDA;

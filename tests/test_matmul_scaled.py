@@ -158,6 +158,13 @@ def test_wide_matrices(T, K, N, dtype, out_pad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,K,N", [(130, 200, 5002), (333, 1024, 5028), (700, 640, 4838)])
+@pytest.mark.parametrize("out_pad", [0, 1, 2, 4, 10])
+def test_rows_of_an_even_width(T, K, N, out_pad):
+    _check(T, K, N, "bf16", bias=True, out_pad=out_pad)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T,N", [(300, 4864), (900, 2560)])
 def test_all_lowest_values_of_wide_matrices(T, N):
     import torch
