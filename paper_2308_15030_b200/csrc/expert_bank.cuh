@@ -35,7 +35,6 @@ struct BankArgs {
   int P, S, k, d, per_cta;      // pairs, ..., pairs of a CTA
   int cols[2], k_blocks[2];     // weight tiles of a slot, k-blocks of a tile: of the two products
   int pairs;                    // CTA pairs that walk the tiles
-  int direct;
 };
 
 __device__ __forceinline__ int bank_slot(const BankArgs& a, int p) {
@@ -108,61 +107,57 @@ __device__ __forceinline__ void bank_copy_rows(const BankArgs& a, const int* s_r
     }
 }
 
+// Slot offsets, by a warp; with `lists` also the list of tiles, and what says that the slots' padding holds no pairs.
+__device__ __forceinline__ void bank_offsets(const BankArgs& a, const int* s_count, int* s_off, bool lists) {
+  const int lane = threadIdx.x & 31;
+  const int cap = lists ? bank_tile_cap(a, s_count) : 256;                   // (of no use without)
+  int row0 = 0, tile0 = 0;
+  for (int s0 = 0; s0 < a.S; s0 += 32) {
+    const int s = s0 + lane, count = s < a.S ? s_count[s] : 0;
+    // a slot's rows in as few tiles as the cap allows, by 32 and as even as that can be
+    const int padded = (count + 31) & ~31, used = (count + cap - 1) / cap;
+    int rows = padded, tiles = used;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, rows, o), v = __shfl_up_sync(0xffffffffu, tiles, o);
+      if (lane >= o) { rows += u; tiles += v; }
+    }
+    const int off = row0 + rows - padded;
+    if (s < a.S) s_off[s] = off;
+    if (lists) {
+      for (int i = 0, at = 0; i < used; ++i) {
+        const int units = padded / 32, height = (units / used + (i < units % used ? 1 : 0)) * 32;
+        TileDesc td;
+        td.phys = td.slot = s; td.row0 = off + at; td.rows = min(height, count - at);
+        a.tiles[tile0 + tiles - used + i] = td;
+        at += height;
+      }
+      for (int r = count; r < padded; ++r) a.row_pair[off + r] = -1;
+    }
+    row0 += __shfl_sync(0xffffffffu, rows, 31);
+    tile0 += __shfl_sync(0xffffffffu, tiles, 31);
+  }
+  if (lists && lane == 0) { a.n_tiles[0] = tile0; a.n_tiles[1] = cap; a.n_tiles[2] = row0; }
+}
+
+__device__ __forceinline__ void bank_place(const BankArgs& a, int p, int row, float x_scale) {
+  a.row_pair[row] = p;
+  a.largest[row] = 0;
+  a.row_scales[row] = x_scale;
+}
+
 __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_constant__ BankArgs a) {
   __shared__ int s_count[kBankMaxSlots], s_at[kBankMaxSlots], s_off[kBankMaxSlots];
   __shared__ int s_row[kBankThreads];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int p0 = blockIdx.x * a.per_cta, p1 = min(a.P, p0 + a.per_cta);
-  if (a.direct)
-    for (int s = threadIdx.x; s < a.S; s += kBankThreads) s_count[s] = s_at[s] = 0;
   pdl_wait();
   pdl_trigger();
-  __syncthreads();
-  if (a.direct) {
-    for (int p = threadIdx.x; p < a.P; p += kBankThreads) {
-      const int s = bank_slot(a, p);
-      if (s < 0) continue;
-      atomicAdd(&s_count[s], 1);
-      if (p < p0) atomicAdd(&s_at[s], 1);
-    }
-  } else {
-    for (int s = threadIdx.x; s < a.S; s += kBankThreads) {
-      s_count[s] = __ldcg(a.counts + s);
-      s_at[s] = a.cta_base[(size_t)blockIdx.x * a.S + s];
-    }
+  for (int s = threadIdx.x; s < a.S; s += kBankThreads) {
+    s_count[s] = __ldcg(a.counts + s);
+    s_at[s] = a.cta_base[(size_t)blockIdx.x * a.S + s];
   }
   __syncthreads();
-  if (warp == 0) {
-    // slot offsets, and by the first CTA the list of tiles
-    const int cap = blockIdx.x == 0 ? bank_tile_cap(a, s_count) : 256;       // (of no use to the others)
-    int row0 = 0, tile0 = 0;
-    for (int s0 = 0; s0 < a.S; s0 += 32) {
-      const int s = s0 + lane, count = s < a.S ? s_count[s] : 0;
-      // a slot's rows in as few tiles as the cap allows, by 32 and as even as that can be
-      const int padded = (count + 31) & ~31, used = (count + cap - 1) / cap;
-      int rows = padded, tiles = used;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, rows, o), v = __shfl_up_sync(0xffffffffu, tiles, o);
-        if (lane >= o) { rows += u; tiles += v; }
-      }
-      const int off = row0 + rows - padded;
-      if (s < a.S) s_off[s] = off;
-      if (blockIdx.x == 0) {
-        for (int i = 0, at = 0; i < used; ++i) {
-          const int units = padded / 32, height = (units / used + (i < units % used ? 1 : 0)) * 32;
-          TileDesc td;
-          td.phys = td.slot = s; td.row0 = off + at; td.rows = min(height, count - at);
-          a.tiles[tile0 + tiles - used + i] = td;
-          at += height;
-        }
-        for (int r = count; r < padded; ++r) a.row_pair[off + r] = -1;
-      }
-      row0 += __shfl_sync(0xffffffffu, rows, 31);
-      tile0 += __shfl_sync(0xffffffffu, tiles, 31);
-    }
-    if (blockIdx.x == 0 && lane == 0) { a.n_tiles[0] = tile0; a.n_tiles[1] = cap; a.n_tiles[2] = row0; }
-  }
+  if (threadIdx.x < 32) bank_offsets(a, s_count, s_off, blockIdx.x == 0);
   __syncthreads();
   for (int b = p0; b < p1; b += kBankThreads) {
     const int p = b + threadIdx.x, n = min(kBankThreads, p1 - b);
@@ -171,9 +166,7 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
       const int s = bank_slot(a, p);
       if (s >= 0) {
         row = s_off[s] + atomicAdd(&s_at[s], 1);
-        a.row_pair[row] = p;
-        a.largest[row] = 0;
-        a.row_scales[row] = a.x_scales[p / a.k];
+        bank_place(a, p, row, a.x_scales[p / a.k]);
       }
       a.pair_row[p] = row;
     }
@@ -184,6 +177,56 @@ __global__ void __launch_bounds__(kBankThreads) bank_gather_kernel(const __grid_
     else bank_copy_rows<1>(a, s_row, b, n);
     __syncthreads();
   }
+}
+
+// The same for up to kBankDirectPairs pairs, without a count kernel: every CTA counts all pairs.  A warp takes a pair, whose row (its first 4096
+// columns) is asked for before the pairs are counted; the last CTA takes none and makes the lists.
+constexpr int kBankDirectWarps = kBankThreads / 32;
+__global__ void __launch_bounds__(kBankThreads) bank_gather_direct_kernel(const __grid_constant__ BankArgs a) {
+  __shared__ int s_count[kBankMaxSlots], s_at[kBankMaxSlots];
+  constexpr int kPieces = 8;
+  const int lane = threadIdx.x & 31, p0 = blockIdx.x * kBankDirectWarps, p = p0 + (threadIdx.x >> 5), quads = a.d / 16;
+  const bool lists = blockIdx.x == gridDim.x - 1, mine = !lists && p < a.P;
+  for (int s = threadIdx.x; s < a.S; s += kBankThreads) s_count[s] = s_at[s] = 0;
+  pdl_wait();
+  pdl_trigger();
+  const int slot = mine ? bank_slot(a, p) : -1, token = mine ? p / a.k : 0;
+  const float x_scale = mine ? a.x_scales[token] : 0.f;
+  const uint4* src = reinterpret_cast<const uint4*>(a.x8 + (size_t)token * a.x_stride);
+  uint4 v[kPieces];
+#pragma unroll
+  for (int u = 0; u < kPieces; ++u)
+    if (mine && lane + 32 * u < quads) v[u] = src[lane + 32 * u];
+  __syncthreads();
+  for (int q = threadIdx.x; q < a.P; q += kBankThreads) {
+    const int s = bank_slot(a, q);
+    if (s < 0) continue;
+    atomicAdd(&s_count[s], 1);
+    if (q < p0) atomicAdd(&s_at[s], 1);
+  }
+  __syncthreads();
+  if (lists) {
+    if (threadIdx.x < 32) bank_offsets(a, s_count, s_at, true);
+    return;
+  }
+  if (!mine) return;
+  int off = 0, row = -1;
+  for (int s = lane; s < slot; s += 32) off += (s_count[s] + 31) & ~31;
+  off = __reduce_add_sync(0xffffffffu, off);
+  if (lane == 0) {
+    if (slot >= 0) {
+      row = off + atomicAdd(&s_at[slot], 1);
+      bank_place(a, p, row, x_scale);
+    }
+    a.pair_row[p] = row;
+  }
+  row = __shfl_sync(0xffffffffu, row, 0);
+  if (row < 0) return;
+  uint4* dst = reinterpret_cast<uint4*>(a.rows8 + (size_t)row * a.d);
+#pragma unroll
+  for (int u = 0; u < kPieces; ++u)
+    if (lane + 32 * u < quads) dst[lane + 32 * u] = v[u];
+  for (int c = lane + 32 * kPieces; c < quads; c += 32) dst[c] = src[c];
 }
 
 // Hidden values to 8 bits by the rows' largest magnitudes, as quantize_rows does it: a warp per row and 128 kTurns columns, so that the values

@@ -491,16 +491,18 @@ int32_t swapmoe_expert_bank_forward(swapmoe_expert_bank_t* b, const void* x, int
   a.row_pair = b->row_pair; a.pair_row = b->pair_row; a.largest = b->row_largest; a.counts = b->counts; a.cta_base = b->cta_base; a.tiles = b->tiles;
   a.n_tiles = b->n_tiles;
   a.x_stride = x_stride; a.P = P; a.S = c.n_slots; a.k = c.top_k; a.d = c.d_model;
-  a.direct = P <= kBankDirectPairs;
   a.cols[0] = (c.d_ff + (swiglu ? 127 : 255)) / (swiglu ? 128 : 256); a.k_blocks[0] = (c.d_model + kI8BK - 1) / kI8BK;
   a.cols[1] = (c.d_model + 255) / 256; a.k_blocks[1] = (c.d_ff + kI8BK - 1) / kI8BK; a.pairs = pairs;
-  // eight pairs a CTA (one per warp) where that makes no more CTAs than run at once
-  a.per_cta = (P + 2 * b->dev.sms - 1) / (2 * b->dev.sms);
-  if (a.per_cta < 8) a.per_cta = 8;
-  const int ctas = (P + a.per_cta - 1) / a.per_cta;
-  if (ctas > kBankMaxCtas) return SWAPMOE_ERR_UNSUPPORTED;
-  if (!a.direct) e = launch_kernel(bank_count_kernel, dim3(ctas), dim3(kBankThreads), 0, st, pdl, a);
-  if (e == cudaSuccess) e = launch_kernel(bank_gather_kernel, dim3(ctas), dim3(kBankThreads), 0, st, pdl, a);
+  if (P <= kBankDirectPairs) {
+    a.per_cta = kBankDirectWarps;
+    e = launch_kernel(bank_gather_direct_kernel, dim3((P + a.per_cta - 1) / a.per_cta + 1), dim3(kBankThreads), 0, st, pdl, a);
+  } else {
+    a.per_cta = std::max(8, (P + 2 * b->dev.sms - 1) / (2 * b->dev.sms));
+    const int ctas = (P + a.per_cta - 1) / a.per_cta;
+    if (ctas > kBankMaxCtas) return SWAPMOE_ERR_UNSUPPORTED;
+    e = launch_kernel(bank_count_kernel, dim3(ctas), dim3(kBankThreads), 0, st, pdl, a);
+    if (e == cudaSuccess) e = launch_kernel(bank_gather_kernel, dim3(ctas), dim3(kBankThreads), 0, st, pdl, a);
+  }
 
   const long long rows = std::min<long long>(b->max_rows, (P + 31ll * std::min(P, c.n_slots) + 31) / 32 * 32);
   const long long max_tiles = (P + 63) / 64 + std::min(P, c.n_slots);
