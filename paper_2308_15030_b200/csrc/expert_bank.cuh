@@ -17,8 +17,9 @@ namespace swapmoe {
 constexpr int kBankMaxSlots = 256;
 constexpr int kBankThreads = 256;
 constexpr int kBankMaxCtas = 512;               // CTAs of the count and gather kernels
-constexpr int kBankDirectPairs = 2048;          // up to here every CTA of the gather kernel counts all pairs itself (us of both, itself / count kernel:
-                                                // 1024 pairs 8.0 / 9.2, 4000 12.7 / 11.4, 14000 18 / 12.7)
+constexpr int kBankDirectPairs = 4096;          // up to here every CTA of the gather kernel counts all pairs itself (us of a call, itself / count kernel: 64
+                                                // experts of 1024 x 512, 256 pairs 29.4 / 32.0, 4000 50.3 / 52.1, 6000 62.6 / 58.8; 16 of 4096 x 512, 4000
+                                                // pairs 77.3 / 79.4, 8000 126 / 122)
 
 struct BankArgs {
   const int8_t* x8;
