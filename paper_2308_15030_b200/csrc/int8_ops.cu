@@ -329,15 +329,14 @@ int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* p, void* stream) {
   if (rc != SWAPMOE_OK) return rc;
   // Few tokens and a small matrix: the weights straight to registers.  Few tokens, or few tiles: the contraction shared.  us for 8 tokens,
   // registers / shared: 1024 x 1024 2.4 / 3.4, 2048 x 2048 3.3 / 4.2, 4096 -> 1024 4.7 / 4.5, 4096 x 4096 6.3 / 5.9, 4096 -> 14336 15.8 / 12.6.
-  // Shared / CTA pairs: 4096 -> 14336 at 32, 64 tokens 12.5 / 12.5, 14.4 / 12.8; 1024 -> 4096 at 64, 96, 128 4.2 / 5.1, 4.5 / 5.4, 6.4 / 5.9;
-  // 4096 x 4096 at 128, 160, 256 9.6 / 10.6, 9.5 / 11.1, 11.4 / 11.3; 14336 -> 4096 at 200 25.3 / 28.3; 4096 -> 1024 at 256, 512, 1024 6.1 / 10.5,
-  // 8.7 / 10.8, 10.6 / 11.1; 2048 x 2048 at 256, 384 6.2 / 7.6, 8.2 / 7.7; 1024 x 1024 at 256, 320 4.0 / 5.6, 5.7 / 5.6; 512 x 512 at 512 3.1 / 4.5.
+  // Shared / CTA pairs: 4096 -> 14336 at 32, 64 tokens 12.5 / 12.5, 14.4 / 12.8; 1024 -> 4096 at 128, 256, 320 4.5 / 6.0, 5.3 / 6.2, 6.4 / 6.6; 1024 x
+  // 1024 at 256, 1024, 1536 4.0 / 5.6, 5.0 / 6.1, 6.4 / 6.5; 2048 x 2048 at 256, 512, 1024 6.2 / 7.6, 7.1 / 7.8, 9.3 / 8.4; 4096 x 4096 at 128, 256, 320
+  // 9.8 / 10.6, 11.6 / 11.4, 13.8 / 12.3; 4096 -> 1024 at 256, 1024 6.1 / 10.5, 10.6 / 11.1; 14336 -> 4096 at 200 25.3 / 28.3; 512 x 512 at 1024 3.4 / 4.8.
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (p->n_tokens <= kStreamTokens && p->k <= 2048 && (long long)p->k * p->n <= 6ll << 20) return matmul_stream(*p, st, standalone_pdl());
   const int tiles = (p->n + kTcBM - 1) / kTcBM;
-  const int shared = 4 * tiles <= dev.sms ? (p->k >= 2048 ? kSplitMaxTokens : 96) : 2 * tiles <= dev.sms ? 64 : 32;
-  const int group = p->k >= 2048 ? 128 : 64, ctas = p->k >= 4096 ? 2 : 4;
-  if (p->n_tokens <= shared || (long long)ctas * tiles * ((p->n_tokens + group - 1) / group) <= dev.sms) return matmul_split(*p, dev, st, standalone_pdl());
+  const long long groups = p->k >= 4096 ? 2 * ((p->n_tokens + 127) / 128) : (p->n_tokens + 63) / 64;        // (14336 -> 2048 at 576 31.4 / 28.4)
+  if (p->n_tokens <= 32 || (2 * tiles <= dev.sms && tiles * groups <= dev.sms)) return matmul_split(*p, dev, st, standalone_pdl());
   return matmul_pair(*p, dev, st, standalone_pdl());
 }
 
