@@ -158,6 +158,19 @@ def test_wide_matrices(T, K, N, dtype, out_pad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 31, 33, 61, 64, 65, 96, 97, 128])
+@pytest.mark.parametrize("K,N,dtype,out_pad", [(1000, 9600, "bf16", 0), (650, 9601, "fp32", 2), (2100, 19200, "fp32", 0)])
+def test_few_tokens_of_wide_matrices(T, K, N, dtype, out_pad):
+    _check(T, K, N, dtype, bias=N % 2 == 0, out_pad=out_pad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,K,N", [(6500, 4096, 640), (13000, 2064, 300)])
+def test_rows_beyond_a_scheduling_group(T, K, N):
+    _check(T, K, N, "bf16", bias=True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T,K,N", [(130, 200, 5002), (333, 1024, 5028), (700, 640, 4838)])
 @pytest.mark.parametrize("out_pad", [0, 1, 2, 4, 10])
 def test_rows_of_an_even_width(T, K, N, out_pad):
