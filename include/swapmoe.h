@@ -595,7 +595,8 @@ int32_t swapmoe_matmul_status(int32_t* detail, void* stream);
  *   out[t] = sum_j weights[t, j] * E_slots[t, j](x[t]),   E_s(x) = W_out act(W_in x)
  * x is int8 with a scale per row, the products are those of swapmoe_matmul_scaled, act(W_in x) is fp32 and goes to 8 bits by rows as
  * swapmoe_quantize_rows does it, and the results are added in fp32 in the order of j.  slots and weights are what swapmoe_route writes: a slot that is
- * negative, or not in the bank, is left out (a token without any has zeros); a slot may be named twice.
+ * negative, or not in the bank, is left out (a token without any has zeros); a slot may be named twice.  A token's result has the same bits whatever
+ * other tokens its call holds.
  * Like a layer, a bank may be driven from one stream at a time (its workspace is used by every call, captured ones too), on its device. */
 typedef struct swapmoe_expert_bank swapmoe_expert_bank_t; /* opaque, owned by the library */
 typedef struct {

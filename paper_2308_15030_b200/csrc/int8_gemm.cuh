@@ -14,7 +14,7 @@
 #pragma once
 #include "launch.cuh"
 #include "pair_common.cuh"
-#include "rms_norm.cuh"
+#include "quantize_rows.cuh"
 
 namespace swapmoe {
 
@@ -403,7 +403,7 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         if (kSwiglu)
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            f[i] = __fdividef(f[i], 1.f + __expf(-f[i])) * f[8 + i];       // (two steps of 2^-23 at most: what follows has 8 bits)
+            f[i] = silu(f[i]) * f[8 + i];
         if (EPI == kI8F32 && a.direct) {
 #pragma unroll
           for (int j = 0; j < kI8Chunk; ++j)

@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kStreamThreads) bank_stream_in_kernel(const __
     if (mine) {
       const float xs = a.x_scales[p / a.k];
       h = (float)Tile::sum(s_part, 0, t, r, 0, kStreamWarps) * w0 * xs;
-      if constexpr (kSwiglu) h = silu_from_exp(h, __expf(-h)) * ((float)Tile::sum(s_part, 1, t, r, 0, kStreamWarps) * w1 * xs);
+      if constexpr (kSwiglu) h = silu(h) * ((float)Tile::sum(s_part, 1, t, r, 0, kStreamWarps) * w1 * xs);
       else h = h < 0.f ? 0.f : h;
       a.h[(size_t)p * a.F + f0 + r] = h;
     }

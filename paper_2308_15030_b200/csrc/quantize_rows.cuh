@@ -35,6 +35,10 @@ __device__ __forceinline__ float largest_of(const RowPiece<bf16>& p) {
   return max_magnitude(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), 0.f);
 }
 
+// silu(x) in fp32, the same bits in every kernel that makes hidden values of it: which of two integers a value next to their border becomes must not
+// hang on the form that a call takes.  The exponential is within 2 + 1.17 |x| steps of 2^-23, the quotient as a division rounds it (silu_from_exp).
+__device__ __forceinline__ float silu(float x) { return silu_from_exp(x, __expf(-x)); }
+
 // Scale of a row whose largest magnitude is `most`: rows of zeros are divided by 2^-120 and have scale 0.
 __device__ __forceinline__ float quantize_divisor(float most) {
   const float q = __fdiv_rn(most, kInt8Max);
@@ -117,7 +121,7 @@ __global__ void __launch_bounds__(kChunks == 1 ? 1024 : 512) quantize_rows_kerne
         float u[8];
         norm_load8<kVec>(x + a.d, first(j), lane, d, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[j].v[i] = silu_from_exp(y[j].v[i], __expf(-y[j].v[i])) * u[i];
+        for (int i = 0; i < 8; ++i) y[j].v[i] = silu(y[j].v[i]) * u[i];
       }
     }
   } else {
