@@ -567,7 +567,8 @@ int32_t swapmoe_quantize_rows(const swapmoe_quantize_rows_t* args, void* stream)
 
 /* A product of 8-bit integers with a scale for each token and each channel (the projection that adapters stand beside):
  *   out[t, n] = x_scales[t] * w_scales[n] * sum_k x[t, k] * w[n, k] + bias[n]
- * The sums are exact; scaling and bias are fp32, and the result is rounded once.  Rows of x and w start at multiples of 16 bytes (k
+ * The sums are exact; scaling and bias are fp32 (the product with x_scales and the bias in one rounding), and the result is rounded once: a token's
+ * result has the same bits whatever other tokens its call holds.  Rows of x and w start at multiples of 16 bytes (k
  * itself is free); out takes any start and stride that keep elements aligned, and rows of whole sixteens of bytes at multiples of 16 leave fastest.  Nothing
  * behind column n or row n_tokens is written; out must not overlap an input.  Calls may run side by side.  Every wait inside
  * the kernels is bounded (swapmoe_matmul_status).  Errors: INVALID_ARG, UNSUPPORTED (k > SWAPMOE_MATMUL_MAX_K, n or n_tokens within 256 of the

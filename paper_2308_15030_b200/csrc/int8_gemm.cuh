@@ -44,6 +44,13 @@ struct I8GemmArgs {
   int32_t* largest;         // [rows] largest magnitude of a row of hidden values, as its bits (ReLU, SwiGLU: zero before)
 };
 
+// (sum * w_scale) of two tokens to results: times the tokens' scales plus the bias in one rounding, as all forms of the product do it.
+__device__ __forceinline__ void scaled2(float& a, float& b, float x0, float x1, float bias) {
+  float u = bias, v = bias;
+  fma2(u, v, a, b, x0, x1);
+  a = u; b = v;
+}
+
 // What a k-block of a tile costs by the tile's tokens: its bytes, 256 weight rows and the tokens (4096 x 14336: a round of 128 tokens 10.5 us, of 256
 // 13.4; eight slots of about 1000 rows, both products: tiles of up to 256 rows 1050 us, of about 128 1390).
 __host__ __device__ constexpr int int8_tile_cost(int tokens) { return 256 + tokens; }
@@ -381,8 +388,8 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
             for (int r = 0; r < kRows; ++r) {
               float &f0 = f[8 * (r >> 1) + 4 * j + 2 * (r & 1)], &f1 = f[8 * (r >> 1) + 4 * j + 2 * (r & 1) + 1];
               mul2(f0, f1, scales.w[r], scales.w[r]);
-              mul2(f0, f1, x.x, x.y);
-              if (EPI == kI8Bf16) add2(f0, f1, scales.bias[EPI == kI8Bf16 ? r : 0], scales.bias[EPI == kI8Bf16 ? r : 0]);
+              if (EPI == kI8Bf16) scaled2(f0, f1, x.x, x.y, scales.bias[EPI == kI8Bf16 ? r : 0]);
+              else mul2(f0, f1, x.x, x.y);
             }
           }
         } else {
@@ -390,15 +397,13 @@ int8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
           for (int j = 0; j < kI8Chunk; j += 4) {
             const float4 x = *reinterpret_cast<const float4*>(s_scale + j);
             mul2(f[j], f[j + 1], scales.w[0], scales.w[0]);
-            mul2(f[j], f[j + 1], x.x, x.y);
             mul2(f[j + 2], f[j + 3], scales.w[0], scales.w[0]);
-            mul2(f[j + 2], f[j + 3], x.z, x.w);
+            scaled2(f[j], f[j + 1], x.x, x.y, scales.bias[0]);
+            scaled2(f[j + 2], f[j + 3], x.z, x.w, scales.bias[0]);
           }
+          if (EPI == kI8Relu)
 #pragma unroll
-          for (int j = 0; j < kI8Chunk; ++j) {
-            f[j] += scales.bias[0];
-            if (EPI == kI8Relu) f[j] = f[j] < 0.f ? 0.f : f[j];                              // NaN stays NaN
-          }
+            for (int j = 0; j < kI8Chunk; ++j) f[j] = f[j] < 0.f ? 0.f : f[j];               // NaN stays NaN
         }
         if (kSwiglu)
 #pragma unroll

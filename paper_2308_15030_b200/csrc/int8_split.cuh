@@ -191,8 +191,8 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
       v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
     }
     const float4 xs = *reinterpret_cast<const float4*>(s_x_scale + t0 + 4 * i);
-    const float f[4] = {(float)v.x * w_scale * xs.x + bias, (float)v.y * w_scale * xs.y + bias, (float)v.z * w_scale * xs.z + bias,
-                        (float)v.w * w_scale * xs.w + bias};
+    const float f[4] = {fmaf((float)v.x * w_scale, xs.x, bias), fmaf((float)v.y * w_scale, xs.y, bias), fmaf((float)v.z * w_scale, xs.z, bias),
+                        fmaf((float)v.w * w_scale, xs.w, bias)};
     Out* out = static_cast<Out*>(a.out) + (size_t)(first + t0 + 4 * i) * a.ldc + n;
 #pragma unroll
     for (int j = 0; j < 4; ++j)

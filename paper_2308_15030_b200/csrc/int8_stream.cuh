@@ -148,9 +148,8 @@ __global__ void __launch_bounds__(kStreamThreads) int8_stream_kernel(const __gri
   __syncthreads();
   const int i = threadIdx.x, token = i >> 4, r = i & 15, n = n0 + r;
   if (token >= a.T || n >= a.N) return;
-  float f = (float)Tile::sum(s_part, 0, token, r, 0, kStreamWarps) * a.w_scales[n] * a.x_scales[token];
-  if (a.bias != nullptr) f += a.bias[n];
-  norm_store(static_cast<T*>(a.out) + (size_t)token * a.out_stride + n, f);
+  const float f = (float)Tile::sum(s_part, 0, token, r, 0, kStreamWarps) * a.w_scales[n], bias = a.bias != nullptr ? a.bias[n] : 0.f;
+  norm_store(static_cast<T*>(a.out) + (size_t)token * a.out_stride + n, fmaf(f, a.x_scales[token], bias));
 }
 
 // ------------------------------------------------------------------ experts

@@ -7,7 +7,7 @@ from paper_2308_15030_b200 import binding
 def _quantized(n, k, gen, std=1.0):
     import torch
     v = torch.empty(n, k, device="cuda").normal_(0.0, std, generator=gen)
-    q, s = torch.empty(n, k, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+    q, s = torch.empty(n, k + -k % 16, dtype=torch.int8, device="cuda")[:, :k], torch.empty(n, device="cuda")
     binding.quantize_rows(v, q, s)
     return q, s
 
@@ -37,6 +37,34 @@ def test_a_tokens_experts_do_not_hang_on_the_batch(d, F, S, k, act, dtype):
     for n in (1, 3, 64 // k, 64 // k + 1, 300, T):                       # up to 64 pairs, and more; the last is beyond 4096
         out = torch.empty(n, d, device="cuda").to(torch.float32 if dtype == "fp32" else torch.bfloat16)
         bank.forward(x[:n], xs[:n], slots[:n], weights[:n], out)
+        outs.append(out)
+    for out in outs[:-1]:
+        assert torch.equal(out, outs[-1][: len(out)]), len(out)
+    assert binding.matmul_status() == (0, 0)
+
+
+# ------------------------------------------------------------------ products
+def _pair_width():
+    """Columns of a matrix whose tiles of 128 are more than half of the SMs: calls of more than 32 tokens then run on CTA pairs."""
+    import torch
+    return 128 * (torch.cuda.get_device_properties(0).multi_processor_count // 2 + 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("K,extra,dtype", [(512, 0, "fp32"), (512, 0, "bf16"), (200, 5, "fp32"), (336, 2, "bf16"), (128, 7, "bf16")])
+@pytest.mark.parametrize("bias", [True, False])
+def test_a_tokens_product_does_not_hang_on_the_batch(K, extra, dtype, bias):
+    """The same tokens in calls of up to eight (weights straight to registers), of 9 to 32 (clusters) and of more (CTA pairs)."""
+    import torch
+    N, T = _pair_width() + extra, 300
+    gen = torch.Generator(device="cuda").manual_seed(K + extra)
+    (x, xs), (w, ws) = _quantized(T, K, gen, 2.0), _quantized(N, K, gen, K ** -0.5)
+    b = torch.empty(N, device="cuda").normal_(0.0, 2.0, generator=gen) if bias else None
+    assert K * N <= 6 << 20
+    outs = []
+    for n in (1, 8, 20, 32, 70, T):
+        out = torch.empty(n, N, device="cuda").to(torch.float32 if dtype == "fp32" else torch.bfloat16)
+        binding.matmul_scaled(x[:n], xs[:n], w, ws, out, bias=b)
         outs.append(out)
     for out in outs[:-1]:
         assert torch.equal(out, outs[-1][: len(out)]), len(out)
