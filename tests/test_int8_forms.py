@@ -69,3 +69,111 @@ def test_a_tokens_product_does_not_hang_on_the_batch(K, extra, dtype, bias):
     for out in outs[:-1]:
         assert torch.equal(out, outs[-1][: len(out)]), len(out)
     assert binding.matmul_status() == (0, 0)
+
+
+# Products on CTA pairs, which serve every large matrix, in the places that a call can stand in.
+PLACES = [("bf16", 0, 0), ("bf16", 0, 1), ("bf16", 2, 0), ("fp32", 0, 0), ("fp32", 1, 3)]          # dtype, columns beyond the tiles, columns behind a row
+
+
+def _product(T, K, N, dtype, gen, pad):
+    import torch
+    (x, xs), (w, ws) = _quantized(T, K, gen, 2.0), _quantized(N, K, gen, K ** -0.5)
+    out = torch.zeros(T, N + pad, device="cuda").to(torch.float32 if dtype == "fp32" else torch.bfloat16)[:, :N]
+    return [x, xs, w, ws, out]
+
+
+def _near(out, x, xs, w, ws):
+    """Exact sums, two products in fp32, and the result's own rounding."""
+    import torch
+    want = (x.double() @ w.double().t()) * xs.double()[:, None] * ws.double()
+    half = 2.0 ** -8 if out.dtype == torch.bfloat16 else 2.0 ** -24
+    assert bool(((out.double() - want).abs() <= (3.01 * 2.0 ** -24 + 1.001 * half) * want.abs()).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,extra,pad", PLACES)
+@pytest.mark.parametrize("T", [48, 400])
+def test_pairs_right_behind_what_writes_their_operands(T, dtype, extra, pad):
+    import torch
+    K, N = 640, _pair_width() + extra
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    x8, xs, w8, ws, out = _product(T, K, N, dtype, gen, pad)
+    for i in range(10):
+        x, w = torch.empty(T, K, device="cuda").normal_(0.0, 1.0 + i, generator=gen), torch.empty(N, K, device="cuda").normal_(generator=gen)
+        torch.cuda.synchronize()
+        binding.quantize_rows(x, x8, xs)
+        binding.quantize_rows(w, w8, ws)
+        binding.matmul_scaled(x8, xs, w8, ws, out)
+        _near(out, x8, xs, w8, ws)
+        # and one product right behind another, on its result
+        binding.matmul_scaled(x8, xs, w8, ws, out)
+        n8, ns = torch.empty(T, N + -N % 16, dtype=torch.int8, device="cuda")[:, :N], torch.empty(T, device="cuda")
+        m8, ms = _quantized(N, N, gen, N ** -0.5) if i == 0 else (m8, ms)
+        back = torch.empty(T, N, device="cuda", dtype=out.dtype)
+        torch.cuda.synchronize()
+        binding.matmul_scaled(x8, xs, w8, ws, out)
+        binding.quantize_rows(out, n8, ns)
+        binding.matmul_scaled(n8, ns, m8, ms, back)
+        if i in (0, 9):
+            _near(back, n8, ns, m8, ms)
+    assert binding.matmul_status() == (0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,extra,pad", PLACES)
+def test_pairs_in_a_graph_and_on_two_streams(dtype, extra, pad):
+    """Two products on CTA pairs side by side, one beside a product on clusters, and one captured and replayed with other operands."""
+    import torch
+    K, N, T = 1024, _pair_width() + extra, 300
+    gen = torch.Generator(device="cuda").manual_seed(N + pad)
+    sets = [_product(T, K, N, dtype, gen, pad), _product(T, K, N, dtype, gen, pad), _product(60, K, 640, dtype, gen, 0), _product(20, K, N, dtype, gen, pad)]
+    want = []
+    for s in sets:
+        binding.matmul_scaled(*s)
+        _near(s[4], *s[:4])
+        want.append(s[4].clone())
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for a, b in ((0, 1), (0, 2), (3, 1)):
+        for i in (a, b):
+            sets[i][4].zero_()
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for i, st in zip((a, b), streams):
+                binding.matmul_scaled(*sets[i], stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(sets[a][4], want[a]) and torch.equal(sets[b][4], want[b]), (a, b)
+    graph, fixed = torch.cuda.CUDAGraph(), [t.clone() for t in sets[0][:4]]
+    out = torch.zeros_like(want[0])
+    fixed[0], fixed[2] = sets[0][0].contiguous().clone(), sets[0][2].contiguous().clone()
+    with torch.cuda.graph(graph):
+        binding.matmul_scaled(*fixed, out)
+        binding.matmul_scaled(*fixed, out)
+    for i in (1, 0, 1):
+        for a, b in zip(fixed, sets[i]):
+            a.copy_(b)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i])
+    assert binding.matmul_status() == (0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,extra,pad", PLACES)
+def test_pairs_with_scales_that_are_not_finite_or_zero(dtype, extra, pad):
+    import torch
+    K, N, T = 160, _pair_width() + extra, 300
+    gen = torch.Generator(device="cuda").manual_seed(pad)
+    x, xs, w, ws, out = _product(T, K, N, dtype, gen, pad)
+    binding.matmul_scaled(x, xs, w, ws, out)
+    first = out.clone()
+    for bad in (float("nan"), float("inf"), 0.0):
+        xs2, ws2 = xs.clone(), ws.clone()
+        xs2[T // 2], ws2[N - 1] = bad, bad
+        binding.matmul_scaled(x, xs2, w, ws2, out)
+        want = (x.double() @ w.double().t()) * xs2.double()[:, None] * ws2.double()
+        assert bool((torch.isnan(out) == torch.isnan(want)).all())
+        infinite, fine = torch.isinf(want), torch.ones_like(out, dtype=torch.bool)
+        fine[T // 2], fine[:, N - 1] = False, False
+        assert torch.equal(out[fine], first[fine])                      # the others keep their bits
+        assert torch.equal(out[infinite].double(), want[infinite])
