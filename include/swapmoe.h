@@ -589,8 +589,14 @@ int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* args, void* stream);
 
 /* Waits for `stream` and returns the status word that the 8-bit products of this process keep on the CURRENT device: SWAPMOE_OK, or
  * SWAPMOE_ERR_DEVICE_TIMEOUT if a bounded wait of swapmoe_matmul_scaled or of an expert bank gave up since the last call (*detail, may be NULL,
- * names the wait).  The word is cleared. */
+ * names the wait).  The word is taken as a whole: it is clear when the call returns, and a timeout, on whatever stream, is reported by one call.
+ * Not while `stream` is captured.  Errors: CUDA. */
 int32_t swapmoe_matmul_status(int32_t* detail, void* stream);
+
+/* Failure-detection self-test of that word, as swapmoe_selftest_bounded_wait is of a layer's: on the CURRENT device one small kernel waits for
+ * limit_ms (1..1000) on an mbarrier that nothing completes, gives up and returns; the next swapmoe_matmul_status is
+ * SWAPMOE_ERR_DEVICE_TIMEOUT with detail 99.  Errors: INVALID_ARG, CUDA. */
+int32_t swapmoe_selftest_matmul_wait(int32_t limit_ms, void* stream);
 
 /* Experts in 8-bit integers behind a router (Section 2; half the bytes of a resident expert in bf16, and half of what a swap moves):
  *   out[t] = sum_j weights[t, j] * E_slots[t, j](x[t]),   E_s(x) = W_out act(W_in x)

@@ -43,6 +43,7 @@ EXPORTS = [
     "swapmoe_adapters_create", "swapmoe_adapters_destroy", "swapmoe_adapters_set_weights", "swapmoe_adapters_forward",
     "swapmoe_adapters_check", "swapmoe_set_gate", "swapmoe_set_norm", "swapmoe_set_post_norm", "swapmoe_forward_block",
     "swapmoe_block_norm", "swapmoe_quantize_rows", "swapmoe_matmul_scaled", "swapmoe_matmul_status",
+    "swapmoe_selftest_matmul_wait",
     "swapmoe_expert_bank_create", "swapmoe_expert_bank_destroy", "swapmoe_expert_bank_set_weights", "swapmoe_expert_bank_forward",
 ]
 
@@ -168,6 +169,7 @@ def lib() -> ctypes.CDLL:
         L.swapmoe_quantize_rows.argtypes = [ctypes.POINTER(QuantizeRowsArgs), vp]
         L.swapmoe_matmul_scaled.argtypes = [ctypes.POINTER(MatmulArgs), vp]
         L.swapmoe_matmul_status.argtypes = [vp, vp]
+        L.swapmoe_selftest_matmul_wait.argtypes = [i32, vp]
         L.swapmoe_expert_bank_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(ExpertBankConfig)]
         L.swapmoe_expert_bank_destroy.argtypes = [vp]
         L.swapmoe_expert_bank_set_weights.argtypes = [vp] * 5
@@ -385,10 +387,15 @@ def matmul_scaled(x8, x_scales, w8, w_scales, out, bias=None, stream=None) -> No
 
 
 def matmul_status(stream=None):
-    """(status, detail) of the 8-bit products on the current device since the last call: (0, 0), or what timed out."""
+    """(status, detail) of the 8-bit products on the current device since the last call, whatever their streams: (0, 0), or what timed out."""
     detail = ctypes.c_int32(0)
     st = lib().swapmoe_matmul_status(ctypes.byref(detail), _stream_ptr(stream))
     return int(st), int(detail.value)
+
+
+def selftest_matmul_wait(limit_ms: int = 20, stream=None) -> None:
+    """One wait that runs out, for the status word behind :func:`matmul_status`."""
+    _check(lib().swapmoe_selftest_matmul_wait(int(limit_ms), _stream_ptr(stream)), "swapmoe_selftest_matmul_wait")
 
 
 class ExpertBank:

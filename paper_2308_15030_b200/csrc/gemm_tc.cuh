@@ -54,19 +54,8 @@ __host__ __device__ constexpr uint32_t make_idesc_bf16(int M, int N) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-// Self-test of the bounded wait: one thread waits on an mbarrier that nobody will ever complete,
-// with a short limit; the wait must give up, record `code` and let the kernel return normally.
 __global__ void bounded_wait_selftest_kernel(int32_t* status, int code, unsigned long long limit_ns) {
-  __shared__ uint64_t bar;
-  __shared__ int abort_flag;
-  if (threadIdx.x == 0) {
-    ptx::mbar_init(&bar, 1);
-    abort_flag = 0;
-    ptx::fence_barrier_init();
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) bounded_wait(&bar, 0u, &abort_flag, status, code, limit_ns);
-  __syncthreads();
+  bounded_wait_selftest(status, code, limit_ns);
 }
 
 // ----------------------------------------------------------------------------- epilogue stores

@@ -270,6 +270,14 @@ int32_t matmul_stream(const swapmoe_matmul_t& p, cudaStream_t st, bool pdl) {
                                           : launch_kernel(int8_stream_kernel<float>, grid, block, 0, st, pdl, a));
 }
 
+// The status word, taken: what another stream's kernels write meanwhile is either in it or stays for the next call.
+__device__ int32_t g_int8_taken[2];
+__global__ void take_status_kernel() {
+  g_int8_taken[0] = atomicExch(&g_int8_status[0], 0);
+  g_int8_taken[1] = atomicExch(&g_int8_status[1], 0);
+}
+__global__ void matmul_wait_selftest_kernel(unsigned long long limit_ns) { bounded_wait_selftest(g_int8_status, 99, limit_ns); }
+
 // Experts of few pairs.
 cudaError_t bank_stream_in(const BankStreamArgs& a, bool swiglu, cudaStream_t st, bool pdl) {
   const int pairs = std::min(a.in_tokens, a.T) * a.k;
@@ -341,16 +349,26 @@ int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* p, void* stream) {
 }
 
 int32_t swapmoe_matmul_status(int32_t* detail, void* stream) {
-  int32_t s[2] = {0, 0};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  static const int32_t zero[2] = {0, 0};
-  if (cudaMemcpyFromSymbolAsync(s, g_int8_status, sizeof(s), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess ||
-      (s[0] != 0 && cudaMemcpyToSymbolAsync(g_int8_status, zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st) != cudaSuccess)) {
-    cudaGetLastError();
-    return SWAPMOE_ERR_CUDA;
+  int32_t s[2] = {0, 0};
+  cudaError_t e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess) {
+    // one call at a time: they share the place that what was taken passes through
+    static std::mutex lock;
+    std::lock_guard<std::mutex> hold(lock);
+    e = launch_kernel(take_status_kernel, dim3(1), dim3(1), 0, st, false);
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbolAsync(s, g_int8_taken, sizeof(s), 0, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
   }
-  if (detail) *detail = s[1];
+  if (e != cudaSuccess) return launched(e);
+  if (detail) *detail = s[0] ? s[1] : 0;
   return s[0] ? SWAPMOE_ERR_DEVICE_TIMEOUT : SWAPMOE_OK;
+}
+
+int32_t swapmoe_selftest_matmul_wait(int32_t limit_ms, void* stream) {
+  if (limit_ms < 1 || limit_ms > 1000) return SWAPMOE_ERR_INVALID_ARG;
+  return launched(launch_kernel(matmul_wait_selftest_kernel, dim3(1), dim3(32), 0, static_cast<cudaStream_t>(stream), false,
+                                (unsigned long long)limit_ms * 1000000ull));
 }
 
 int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_expert_bank_config_t* cfg) {

@@ -153,7 +153,22 @@ __device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity, vol
   }
 }
 
-// The same by a whole converged warp: true when the phase has completed for every lane.
+// Self-test of the bounded wait, by a CTA: one thread waits on an mbarrier that nobody will ever complete,
+// with a short limit; the wait must give up, record `code` and let the kernel return normally.
+__device__ __forceinline__ void bounded_wait_selftest(int32_t* status, int code, uint64_t limit_ns) {
+  __shared__ uint64_t bar;
+  __shared__ int abort_flag;
+  if (threadIdx.x == 0) {
+    ptx::mbar_init(&bar, 1);
+    abort_flag = 0;
+    ptx::fence_barrier_init();
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) bounded_wait(&bar, 0u, &abort_flag, status, code, limit_ns);
+  __syncthreads();
+}
+
+// The bounded wait by a whole converged warp: true when the phase has completed for every lane.
 template <bool kPeer = false>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status,
                                           int code) {

@@ -12,6 +12,49 @@ def _quantized(n, k, gen, std=1.0):
     return q, s
 
 
+# ------------------------------------------------------------------ the status word
+@pytest.mark.parametrize("limit_ms", [0, -1, 1001])
+def test_the_self_tests_limit_is_checked(limit_ms):
+    assert binding.lib().swapmoe_selftest_matmul_wait(limit_ms, None) == -1
+
+
+@pytest.mark.gpu
+def test_a_timeout_is_reported_once_whatever_the_stream():
+    """A wait that runs out ends its kernel, the next status call names it, and the word is clear when that call returns: a call on another stream,
+    which nothing orders behind the first one's, finds none."""
+    import torch
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    assert binding.matmul_status() == (0, 0)
+    for _ in range(5):
+        binding.selftest_matmul_wait(limit_ms=5, stream=a)
+        assert binding.matmul_status(stream=a) == (-6, 99)              # SWAPMOE_ERR_DEVICE_TIMEOUT, wait code
+        assert binding.matmul_status(stream=b) == (0, 0)
+    binding.selftest_matmul_wait(limit_ms=5, stream=a)
+    a.synchronize()
+    assert binding.matmul_status(stream=b) == (-6, 99)                  # on another stream than the wait's
+    assert binding.matmul_status(stream=a) == (0, 0)
+
+
+@pytest.mark.gpu
+def test_status_calls_of_many_threads_report_one_timeout_once():
+    import threading
+    import torch
+    binding.selftest_matmul_wait(limit_ms=5)
+    torch.cuda.synchronize()
+    streams, got, gate = [torch.cuda.Stream() for _ in range(8)], [], threading.Barrier(8)
+
+    def ask(stream):
+        gate.wait()
+        for _ in range(20):
+            got.append(binding.matmul_status(stream=stream))
+    threads = [threading.Thread(target=ask, args=(s,)) for s in streams]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert sorted(set(got)) == [(-6, 99), (0, 0)] and got.count((-6, 99)) == 1 and len(got) == 160
+
+
 # ------------------------------------------------------------------ experts
 @pytest.mark.gpu
 @pytest.mark.parametrize("d,F,S,k", [(512, 704, 16, 2), (256, 320, 8, 1), (1024, 512, 64, 4), (128, 2112, 5, 3)])
