@@ -31,6 +31,7 @@ constexpr int kF32PairASlotBase = 2 * kF32PairBN;                      // first 
 constexpr int kF32PairSmemBytes = kF32PairStages * kF32PairStageBytes + 2048 + kTcEpiStageBytes;
 static_assert(kF32PairASlotBase + kF32ASlots * kF32ASlotCols <= 512, "tensor memory");
 static_assert(kF32PairSmemBytes <= 227 * 1024 && kF32PairStageBytes % 1024 == 0, "shared memory per CTA, swizzle atoms");
+static_assert(!fits_beside_cluster(kF32PairSmemBytes), "tensor memory is not shared with clusters");
 
 namespace ptx {
 __device__ __forceinline__ void umma_bf16_ts_pair(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc,

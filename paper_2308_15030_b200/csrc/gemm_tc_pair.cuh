@@ -28,6 +28,7 @@ __host__ __device__ constexpr int pair_warp_bytes(int epi) { return epi == kTcEp
 // as 96: 69632 of the SM's 65536).
 __host__ __device__ constexpr int pair_smem_bytes(int epi) { return kPairStageArea + 2048 + 8 * pair_warp_bytes(epi); }
 static_assert(pair_smem_bytes(kTcEpiReluBf16) + 1024 + 12288 <= 228 * 1024, "beside a CTA of the permutation");
+static_assert(!fits_beside_cluster(pair_smem_bytes(kTcEpiScatterBf16)), "tensor memory is not shared with clusters");
 
 namespace ptx {
 __device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc,

@@ -105,6 +105,7 @@ __host__ __device__ constexpr int int8_stages(int epi, int max_tokens) {
 // ... and the scales of a warp's tokens
 __host__ __device__ constexpr int int8_smem_bytes(int epi) { return int8_ring_bytes(epi) + 2048 + kI8EpiWarps * (2 * int8_box_bytes(epi) + 4 * kI8Chunk); }
 static_assert(int8_smem_bytes(kI8F32) <= 227 * 1024 && int8_smem_bytes(kI8Bf16) <= 227 * 1024, "what a CTA may have");
+static_assert(!fits_beside_cluster(int8_smem_bytes(kI8F32)) && !fits_beside_cluster(int8_smem_bytes(kI8Bf16)), "tensor memory is not shared with clusters");
 static_assert(int8_stages(kI8F32, 64) * (kPairABytes + 32 * kI8BK) <= int8_ring_bytes(kI8F32) && int8_stages(kI8Bf16, 64) <= kPairMaxStages, "stages fit");
 
 template <int EPI>

@@ -252,7 +252,7 @@ int32_t matmul_split(const swapmoe_matmul_t& p, const Device& dev, cudaStream_t 
   const long long xs = p.n_tokens > 1 ? p.x_stride : (p.k + 15) / 16 * 16, ws = p.n > 1 ? p.w_stride : (p.k + 15) / 16 * 16;
   CUtensorMap mw, mx;
   if (!int8_encode_operand(enc, &mw, p.w, p.n, p.k, ws, 128) || !int8_encode_operand(enc, &mx, p.x, p.n_tokens, p.k, xs, g.cols)) return SWAPMOE_ERR_CUDA;
-  const size_t smem = 1024 + int8_split_area(g.cols, g.n_stages);
+  const size_t smem = std::max(1024 + int8_split_area(g.cols, g.n_stages), kClusterMinSmem);
   const dim3 grid(n_tiles * cluster, (p.n_tokens + g.cols - 1) / g.cols), block(kSplitThreads);
   return launched(p.dtype == SWAPMOE_BF16 ? launch_cluster(int8_split_kernel<bf16>, cluster, grid, block, smem, st, pdl, mw, mx, g)
                                           : launch_cluster(int8_split_kernel<float>, cluster, grid, block, smem, st, pdl, mw, mx, g));

@@ -14,6 +14,12 @@ constexpr int kPairStageArea = 6 * (kPairABytes + kPairBBytes);   // 6 stages of
 constexpr int kPairMaxStages = 9;
 __device__ __forceinline__ int pair_stages(int max_tokens) { return max_tokens > 128 ? 6 : max_tokens > 64 ? 8 : 9; }
 
+// Shared memory that a CTA takes at least if it waits for its cluster with tensor memory in hand: none of a GEMM on CTA pairs, which takes all
+// columns of two SMs, then fits its SM beside it.  (One SM's columns would be the cluster's, the other's the pair's, and either wait for the
+// rest.)
+constexpr int kClusterMinSmem = 28 * 1024;
+constexpr bool fits_beside_cluster(int pair_smem) { return pair_smem + kClusterMinSmem + 2 * 1024 <= 228 * 1024; }       // (the system keeps 1 KB of each)
+
 namespace ptx {
 
 __device__ __forceinline__ uint32_t cluster_ctarank() {
