@@ -570,8 +570,9 @@ int32_t swapmoe_quantize_rows(const swapmoe_quantize_rows_t* args, void* stream)
  * The sums are exact; scaling and bias are fp32 (the product with x_scales and the bias in one rounding), and the result is rounded once: a token's
  * result has the same bits whatever other tokens its call holds.  Rows of x and w start at multiples of 16 bytes (k
  * itself is free); out takes any start and stride that keep elements aligned, and rows of whole sixteens of bytes at multiples of 16 leave fastest.  Nothing
- * behind column n or row n_tokens is written; out must not overlap an input.  Calls may run side by side.  Every wait inside
- * the kernels is bounded (swapmoe_matmul_status).  Errors: INVALID_ARG, UNSUPPORTED (k > SWAPMOE_MATMUL_MAX_K, n or n_tokens within 256 of the
+ * behind column n or row n_tokens is written; out must not overlap an input.  Calls may run side by side.  Inside the kernels every wait for a copy or
+ * a product (on an mbarrier) is bounded, and reported by swapmoe_matmul_status; the barriers of a cluster, which its CTAs reach behind those, and the allocation of
+ * tensor memory, which another kernel's CTA on the same SM may delay until it ends, have no limit of their own.  Errors: INVALID_ARG, UNSUPPORTED (k > SWAPMOE_MATMUL_MAX_K, n or n_tokens within 256 of the
  * largest int32), CUDA. */
 #define SWAPMOE_MATMUL_MAX_K 131071
 typedef struct {

@@ -9,7 +9,8 @@
 // producer, warp 1 = MMA issuer (even CTA only), warp 2 = TMEM allocation, warps 4-19 = epilogue of the CTA's own 128 weight rows, which
 // overlaps the next tile's MMAs through two accumulators.  Sixteen warps, sixteen tokens at a time: what an epilogue does is a chain of
 // instructions that wait for one another, and with short contractions it sets the pace: a round of 256 tokens takes 1.5 us at 512 columns without an
-// epilogue and 3.2 with it, 2.6 and 4.0 at 1024, 10.7 and 11.5 at 4096.  No load uses cluster multicast; every wait is bounded.
+// epilogue and 3.2 with it, 2.6 and 4.0 at 1024, 10.7 and 11.5 at 4096.  No load uses cluster multicast.  Every mbarrier wait is
+// bounded; the cluster barriers behind them and the allocation of tensor memory (a CTA has its SM to itself) are not.
 // 8192 tokens, 4096 -> 14336: 288 us, 3.3 POP/s (twice the rate of a bf16 library product: 3.3); 61 tokens 13.6 us, 4.3 TB/s of weights.
 #pragma once
 #include "launch.cuh"

@@ -5,7 +5,8 @@
 // TMA), and the shares are added as integers, so that neither the split nor its order changes a bit: every CTA collects the tokens of its rank from
 // the others' shared memory, scales them and stores them.
 // Roles (320 threads): warp 0 = TMA producer, warp 1 = TMEM allocation and MMA issuer, warps 2-9 = sums out of
-// tensor memory, and what is done with them.  No load uses cluster multicast; every wait is bounded.
+// tensor memory, and what is done with them.  No load uses cluster multicast.  Every mbarrier wait is bounded; the cluster barriers behind them
+// are not, nor is the allocation of tensor memory (three CTAs an SM take 384 of its 512 columns; kernels beside them wait for no cluster with theirs).
 // 1 token, 4096 x 4096: 4.4 us where the weights lie in L2, 5.8 from memory; 256 tokens, 4096 -> 1024 6.1 us (CTA pairs 10.5).
 #pragma once
 #include "int8_gemm.cuh"
