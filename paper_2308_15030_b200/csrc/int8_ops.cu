@@ -53,6 +53,10 @@ int32_t current_device(Device* d) {
   }
   if (major != 10) return SWAPMOE_ERR_UNSUPPORTED;       // kernels are built for sm_100a only
   std::lock_guard<std::mutex> hold(lock);
+  if (ready[dev].load(std::memory_order_relaxed)) {      // another thread was first: what it wrote may be read by others already
+    *d = known[dev];
+    return SWAPMOE_OK;
+  }
   const void* const wide[] = {(const void*)bank_stream_out_kernel<bf16, 1>, (const void*)bank_stream_out_kernel<bf16, 2>,
                               (const void*)bank_stream_out_kernel<float, 1>, (const void*)bank_stream_out_kernel<float, 2>};
   for (const void* k : wide)

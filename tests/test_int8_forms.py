@@ -220,3 +220,48 @@ def test_pairs_with_scales_that_are_not_finite_or_zero(dtype, extra, pad):
         fine[T // 2], fine[:, N - 1] = False, False
         assert torch.equal(out[fine], first[fine])                      # the others keep their bits
         assert torch.equal(out[infinite].double(), want[infinite])
+
+
+# ------------------------------------------------------------------ the first calls of a process
+FIRST_CALLS = """
+import threading, torch
+from paper_2308_15030_b200 import binding
+torch.cuda.set_device(0)
+gate, bad = threading.Barrier(8), []
+x, w = torch.randn(40, 256, device="cuda"), torch.randn(300, 256, device="cuda")
+one = torch.ones(256, device="cuda")
+torch.cuda.synchronize()
+
+def work(i):
+    try:
+        stream = torch.cuda.Stream()
+        x8, xs, w8, ws = torch.empty(40, 256, dtype=torch.int8, device="cuda"), torch.empty(40, device="cuda"), torch.empty(300, 256, dtype=torch.int8, device="cuda"), torch.empty(300, device="cuda")
+        n, out = torch.empty_like(x), torch.empty(40, 300, device="cuda")
+        torch.cuda.synchronize()
+        gate.wait()
+        if i % 2:
+            binding.block_norm(x, None, one, 1e-6, out=n, stream=stream)
+        binding.quantize_rows(x, x8, xs, stream=stream)
+        binding.quantize_rows(w, w8, ws, stream=stream)
+        binding.matmul_scaled(x8, xs, w8, ws, out, stream=stream)
+        stream.synchronize()
+        want = (x8.double() @ w8.double().t()) * xs.double()[:, None] * ws.double()
+        assert bool(((out.double() - want).abs() <= 4 * 2.0 ** -24 * want.abs()).all())
+    except Exception as e:
+        bad.append(repr(e))
+threads = [threading.Thread(target=work, args=(i,)) for i in range(8)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert not bad, bad
+print("fine")
+"""
+
+
+@pytest.mark.gpu
+def test_first_calls_of_a_process_from_many_threads():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, env={**os.environ, "PYTHONPATH": root}, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
