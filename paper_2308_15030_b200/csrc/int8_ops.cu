@@ -28,51 +28,51 @@ static_assert(SWAPMOE_MATMUL_MAX_K == kI8MaxK, "the header's limit");
 namespace {
 
 struct Device {
-  int id, sms, pairs;                     // SMs; CTA pairs that run at once
+  int id, sms, pairs;                     // SMs; CTA pairs of the products that run at once (product_device)
 };
+constexpr int kManyDevices = 64;
 
-// The current device, its kernels' limits set once.
+// The current device.  (Threads whose first calls meet find the same values.)
 int32_t current_device(Device* d) {
-  constexpr int kMany = 64;
-  static std::mutex lock;
-  static Device known[kMany];
-  static std::atomic<bool> ready[kMany];
+  static std::atomic<int> known[kManyDevices];           // SMs, 0: not asked yet
   int dev = 0, major = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) {
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= kManyDevices) {
     cudaGetLastError();
     return SWAPMOE_ERR_CUDA;
   }
-  if (dev < kMany && ready[dev].load(std::memory_order_acquire)) {
-    *d = known[dev];
-    return SWAPMOE_OK;
-  }
-  if (dev >= kMany || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
-    cudaGetLastError();
-    return SWAPMOE_ERR_CUDA;
-  }
-  if (major != 10) return SWAPMOE_ERR_UNSUPPORTED;       // kernels are built for sm_100a only
-  std::lock_guard<std::mutex> hold(lock);
-  if (ready[dev].load(std::memory_order_relaxed)) {      // another thread was first: what it wrote may be read by others already
-    *d = known[dev];
-    return SWAPMOE_OK;
-  }
-  const void* const wide[] = {(const void*)bank_stream_out_kernel<bf16, 1>, (const void*)bank_stream_out_kernel<bf16, 2>,
-                              (const void*)bank_stream_out_kernel<float, 1>, (const void*)bank_stream_out_kernel<float, 2>};
-  for (const void* k : wide)
-    if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kBankOutRowBytes) != cudaSuccess) {
+  sms = known[dev].load(std::memory_order_relaxed);
+  if (sms == 0) {
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
       cudaGetLastError();
       return SWAPMOE_ERR_CUDA;
     }
-  const int pairs = int8_gemm_init(sms);
-  if (pairs < 1 || cudaFuncSetAttribute(int8_split_kernel<bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitMaxSmem) != cudaSuccess ||
-      cudaFuncSetAttribute(int8_split_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitMaxSmem) != cudaSuccess) {
+    if (major != 10) return SWAPMOE_ERR_UNSUPPORTED;     // kernels are built for sm_100a only
+    known[dev].store(sms, std::memory_order_relaxed);
+  }
+  *d = Device{dev, sms, 0};
+  return SWAPMOE_OK;
+}
+
+// The same with the products' kernels ready: their limits set once, which loads them.
+int32_t product_device(Device* d) {
+  static std::atomic<int> known[kManyDevices];           // pairs, 0: not ready
+  const int32_t rc = current_device(d);
+  if (rc != SWAPMOE_OK) return rc;
+  d->pairs = known[d->id].load(std::memory_order_acquire);
+  if (d->pairs > 0) return SWAPMOE_OK;
+  const void* const wide[] = {(const void*)bank_stream_out_kernel<bf16, 1>, (const void*)bank_stream_out_kernel<bf16, 2>,
+                              (const void*)bank_stream_out_kernel<float, 1>, (const void*)bank_stream_out_kernel<float, 2>};
+  bool ok = true;
+  for (const void* k : wide) ok = ok && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kBankOutRowBytes) == cudaSuccess;
+  ok = ok && cudaFuncSetAttribute(int8_split_kernel<bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitMaxSmem) == cudaSuccess &&
+       cudaFuncSetAttribute(int8_split_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitMaxSmem) == cudaSuccess;
+  if (ok) d->pairs = int8_gemm_init(d->sms);
+  if (d->pairs < 1) {
     cudaGetLastError();
     return SWAPMOE_ERR_CUDA;
   }
-  known[dev] = Device{dev, sms, pairs};
-  ready[dev].store(true, std::memory_order_release);
-  *d = known[dev];
+  known[d->id].store(d->pairs, std::memory_order_release);
   return SWAPMOE_OK;
 }
 
@@ -337,7 +337,7 @@ int32_t swapmoe_matmul_scaled(const swapmoe_matmul_t* p, void* stream) {
       misaligned(p->x_scales, 4) || misaligned(p->w_scales, 4) || misaligned(p->bias, 4))
     return SWAPMOE_ERR_INVALID_ARG;
   Device dev;
-  const int32_t rc = current_device(&dev);
+  const int32_t rc = product_device(&dev);
   if (rc != SWAPMOE_OK) return rc;
   // Few tokens and a small matrix: the weights straight to registers.  Few tokens, or few tiles: the contraction shared.  us for 8 tokens,
   // registers / shared: 1024 x 1024 2.4 / 3.4, 2048 x 2048 3.3 / 4.2, 4096 -> 1024 4.7 / 4.5, 4096 x 4096 6.3 / 5.9, 4096 -> 14336 15.8 / 12.6.
@@ -386,7 +386,7 @@ int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_ex
       (long long)c.max_tokens * c.top_k >= 1 << 24 || (long long)c.n_slots * nin * c.d_ff >= 1ll << 31 || (long long)c.n_slots * c.d_model >= 1ll << 31)
     return SWAPMOE_ERR_UNSUPPORTED;
   Device dev;
-  const int32_t rc = current_device(&dev);
+  const int32_t rc = product_device(&dev);
   if (rc != SWAPMOE_OK) return rc;
   const PFN_encodeTiled enc = encoder();
   if (!enc) return SWAPMOE_ERR_CUDA;
