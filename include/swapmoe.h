@@ -514,8 +514,10 @@ int32_t swapmoe_forward_block(swapmoe_layer_t* layer, const void* x_dev, void* r
  *   p = x * post_weight / sqrt(mean(x^2) + post_eps)      (p = x without a post_weight)
  *   h = residual + scale * gate * p                       (no residual: 0; no gate: 1);  residual_out = h (rounded to residual_dtype)
  *   y = h * weight / sqrt(mean(h^2) + eps);  out = y (rounded to dtype)
- *   scales = max |y| / m, out8 = y / scales: e4m3 (m = 448) or integers (m = 127; nearest, ties to even), one scale per row (group =
+ *   scales = max |y| / m, out8 = y / scales: e4m3 (m = 448) or integers (m = 127), rounded to nearest, one scale per row (group =
  *            0) or per `group` consecutive columns (32, 64, 128 or 256; the last group may be shorter)
+ * Both quotients are products with a reciprocal, the scale within 2^-21 of itself and y / scales within 2^-21 of itself as they are rounded: a value as
+ * near as that to the middle of two 8-bit ones may become either (swapmoe_quantize_rows divides).
  * The gate is one row for all (gate_stride = 0) or a row of its own for each (gate_stride >= d).  Without a weight only residual_out is
  * written (behind the last block).  Everything is computed in fp32; the ends of its range, zeros, infinities and NaN are as in
  * swapmoe_rms_norm (integers of a NaN: 0).  Strides count elements; any start and stride that keep elements aligned are taken, and rows

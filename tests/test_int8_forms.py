@@ -265,3 +265,28 @@ def test_first_calls_of_a_process_from_many_threads():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, env={**os.environ, "PYTHONPATH": root}, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
+
+
+# ------------------------------------------------------------------ the 8-bit rows behind the norms
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d", [(3, 512), (700, 768), (40, 1003), (2000, 4096)])
+@pytest.mark.parametrize("group", [0, 32, 128])
+@pytest.mark.parametrize("type8", ["int8", "e4m3"])
+def test_8_bit_rows_of_the_norm_are_those_of_its_rows(T, d, group, type8):
+    """Scales and 8-bit values against the norm's own fp32 rows, within the reciprocals' errors that the header gives: 2^-21 of the scale and of the quotient."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(T + d)
+    x, r = torch.empty(T, d, device="cuda").normal_(generator=gen), torch.empty(T, d, device="cuda").normal_(0.0, 3.0, generator=gen)
+    w = torch.empty(d, device="cuda").normal_(1.0, 0.3, generator=gen)
+    n, top = -(-d // group) if group else 1, 127.0 if type8 == "int8" else 448.0
+    out, s = torch.empty_like(x), torch.empty(T, n, device="cuda")
+    q = torch.empty(T, d, device="cuda").to(torch.int8 if type8 == "int8" else torch.float8_e4m3fn)
+    binding.block_norm(x, r, w, 1e-6, out=out, post_weight=w, out8=q, scales=s, group=group)
+    y, width, eps = out.double(), group or d, 2.0 ** -21
+    most = torch.nn.functional.pad(y.abs(), (0, n * width - d)).view(T, n, width).amax(2)
+    assert bool(((s.double() - most / top).abs() <= eps * most / top).all())
+    t = y / s.double()[:, torch.arange(d, device="cuda") // width]
+    # half a step: of integers 0.5; of e4m3 2^-4 of the value, or 2^-10 below its normal range
+    step = torch.full_like(t, 0.5) if type8 == "int8" else torch.clamp(t.abs() * 2.0 ** -4, min=2.0 ** -10)
+    assert bool(((q.float().double() - t).abs() <= step + 1.07 * eps * t.abs()).all())
+    assert float(q.float().abs().max()) == top
