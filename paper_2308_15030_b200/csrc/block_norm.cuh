@@ -5,8 +5,9 @@
 // second norm is taken of the sum before it is rounded.
 //
 // Bound by HBM, and next to it by the chain of a row: loads, an exchange between the warps for each sum, weights, stores.  A team of warps
-// holds a row, eight columns per lane and chunk of 256, and an SM as many teams as its registers hold: x and a bf16 residual stay packed until
-// they are added, which makes room for five CTAs of eight warps instead of four.  Where 8-bit rows have one scale, the largest |h w| of the
+// holds a row, eight columns per lane and chunk of 256, and an SM as many teams as its registers hold; x and a bf16 residual stay packed until
+// they are added.  Four CTAs of eight warps an SM, 64 registers a thread: at five the kernel spills 28 to 36 bytes a thread (16384 x 4096 bf16 on an fp32
+// residual, gate, rows out 131 us, 124 with four; e4m3 by groups 142, 135; integers with one scale 143, 138).  Where 8-bit rows have one scale, the largest |h w| of the
 // row is found in the same exchange as the second sum: the largest |y| is that times the row's positive factor, to three roundings (y is (h s) w).
 // 8-bit values are products with the scale's reciprocal: dividing instead, as quantize_rows does, takes longer (16384 rows of 4096 to integers
 // with one scale 138 -> 148 us), for integers that differ where y's own error decides.
@@ -369,7 +370,7 @@ inline cudaError_t block_norm_launch_typed(BlockNormArgs a, bool vec, int sm_cou
   a.per_column = 1.f / (float)a.d;
   auto go = [&](auto kernel) { return launch_kernel(kernel, grid, block, 0, st, pdl, a); };
   const bool row8 = a.out8 != nullptr && a.group == 0;
-  constexpr int kWide = 32 * kNormMaxWarps, kCtas = sizeof(T) == 2 ? 5 : 4;
+  constexpr int kWide = 32 * kNormMaxWarps, kCtas = 4;
   if (vec && few) return row8 ? go(block_norm_kernel<T, R, 1, true, true, kWide, 1>) : go(block_norm_kernel<T, R, 1, true, false, kWide, 1>);
   if (vec && a.warps_per_row <= 8)
     return row8 ? go(block_norm_kernel<T, R, 2, true, true, 256, kCtas>) : go(block_norm_kernel<T, R, 2, true, false, 256, kCtas>);
