@@ -290,3 +290,71 @@ def test_8_bit_rows_of_the_norm_are_those_of_its_rows(T, d, group, type8):
     step = torch.full_like(t, 0.5) if type8 == "int8" else torch.clamp(t.abs() * 2.0 ** -4, min=2.0 ** -10)
     assert bool(((q.float().double() - t).abs() <= step + 1.07 * eps * t.abs()).all())
     assert float(q.float().abs().max()) == top
+
+
+# ------------------------------------------------------------------ a served block, step by step
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 45, 1200])
+def test_every_step_of_a_served_block(T):
+    """Norms, the router's product, routing to resident experts, experts, shared projection, adapters beside it and the next block's norms:
+    what each step writes against its definition in 64 bits on what the step before left."""
+    import numpy as np
+    import torch
+    from test_adapters import _reference as adapters_reference
+    from test_expert_bank import Case
+    from test_route_groups import REL, TINY, reference as route_reference
+    d, F, E, S, k, EPS = 512, 320, 32, 12, 2, 1e-6
+    c = Case(T, d, F, S, k)
+    gen = torch.Generator(device="cuda").manual_seed(T + 1)
+    normal = lambda *s, std=1.0: torch.empty(*s, device="cuda").normal_(0.0, std, generator=gen)  # noqa: E731
+    x, stream, w, pw = normal(T, d).bfloat16(), normal(T, d, std=2.0), normal(d).bfloat16(), normal(d).bfloat16()
+
+    def norms(x, r, scale):
+        """h and y of the norms around a block, and how far fp32 may be off: a norm under 40 roundings, as its own tests derive."""
+        x64, f32 = x.double(), 40 * 2.0 ** -24
+        p = scale * x64 * pw.double() / torch.sqrt((x64 * x64).mean(1, keepdim=True) + EPS)
+        h = r.double() + p
+        root = torch.sqrt((h * h).mean(1, keepdim=True) + EPS)
+        y = h * w.double() / root
+        off_h = f32 * p.abs() + 2.0 ** -24 * h.abs()
+        return h, y, off_h, off_h * w.double().abs() / root + y.abs() * (f32 + torch.sqrt((off_h * off_h).mean(1, keepdim=True)) / root)
+    n8, ns, before = torch.empty(T, d, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda"), stream.clone()
+    binding.block_norm(x, stream, w, EPS, residual_out=stream, post_weight=pw, scale=0.5, out8=n8, scales=ns)
+    h, y, off_h, off_y = norms(x, before, 0.5)
+    assert bool(((stream.double() - h).abs() <= off_h + 2.0 ** -24 * h.abs()).all())
+    most = y.abs().amax(1, keepdim=True) / 127.0
+    assert bool(((ns.double()[:, None] - most).abs() <= 2.0 ** -21 * most + off_y.amax(1, keepdim=True) / 127.0).all())
+    assert bool(((n8.double() * ns.double()[:, None] - y).abs() <= (0.5 + 127 * 2.0 ** -21) * ns.double()[:, None] + off_y).all())
+    # the router
+    (wr8, wrs), logits = _quantized(E, d, gen, d ** -0.5), torch.empty(T, E, device="cuda")
+    binding.matmul_scaled(n8, ns, wr8, wrs, logits)
+    _near(logits, n8, ns, wr8, wrs)
+    table = torch.full((E,), -1, dtype=torch.int32, device="cuda")
+    table[torch.randperm(E, device="cuda", generator=gen)[:S]] = torch.arange(S, dtype=torch.int32, device="cuda")
+    experts, weights, slots = (torch.empty(T, k, dtype=t, device="cuda") for t in (torch.int32, torch.float32, torch.int32))
+    binding.route(binding.Gate(renorm=True), logits, experts, weights, expert_to_slot=table, slots=slots)
+    e, wt, s = route_reference(logits.cpu().numpy(), k, "softmax", 1, 1, 1, True, 1.0, table=table.cpu().numpy())
+    assert np.array_equal(experts.cpu().numpy(), e) and np.array_equal(slots.cpu().numpy(), s)
+    assert np.all(np.abs(weights.cpu().numpy().astype(np.float64) - wt) <= REL * wt + TINY)
+    # the experts
+    c.x, c.xs, c.slots, c.weights = n8, ns, slots, weights
+    out = c.run()
+    c.check(out)
+    # the projection that all tokens share, and each token's adapter beside it
+    (wp8, wps), shared = _quantized(d, d, gen, d ** -0.5), torch.empty(T, d, dtype=torch.bfloat16, device="cuda")
+    binding.matmul_scaled(n8, ns, wp8, wps, shared)
+    _near(shared, n8, ns, wp8, wps)
+    n16, ids = (n8.float() * ns[:, None]).bfloat16(), torch.randint(-1, 3, (T,), device="cuda", generator=gen).to(torch.int32)
+    A, B = normal(3, 8, d, std=d ** -0.5).bfloat16(), normal(3, d, 8, std=0.3).bfloat16()
+    bank, both = binding.AdapterBank(3, d, d, 8, binding.BF16, max_tokens=T), torch.empty_like(shared)
+    bank.set_weights(A, B)
+    bank.forward(n16, ids, shared, both)
+    want, slack = adapters_reference(n16, shared, None, A, B, torch.ones(3, device="cuda"), ids, "bf16")
+    assert bool(((both.double() - want).abs() <= slack).all())
+    # the next block's norms
+    total, nxt, new = (out.float() + both.float()).bfloat16(), torch.empty_like(out), torch.empty_like(stream)
+    binding.block_norm(total, stream, w, EPS, out=nxt, residual_out=new, post_weight=pw)
+    h, y, off_h, off_y = norms(total, stream, 1.0)
+    assert bool(((new.double() - h).abs() <= off_h + 2.0 ** -24 * h.abs()).all())
+    assert bool(((nxt.double() - y).abs() <= 1.001 * 2.0 ** -8 * y.abs() + off_y + 1e-40).all())
+    assert binding.matmul_status() == (0, 0)
