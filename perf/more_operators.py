@@ -189,7 +189,7 @@ def prepare(case, seed):
         s.scales = torch.empty(T, device=dev)
     else:
         s.out = torch.empty(T, case["N"] if case["op"] == "matmul" else case["d"], dtype=_dtype(case), device=dev)
-        s.bank = None
+        s.bank = _bank(s) if own and case["op"] == "experts" else None
     return s
 
 
@@ -259,12 +259,18 @@ def _matmul_plain(s):
     return (y if s.bias is None else y + s.bias).to(s.out.dtype)
 
 
-def _experts_own(s):
+def _bank(s):
+    # made once, before the first token
     binding, c = _library(), s.case
-    if s.bank is None:
-        s.bank = binding.ExpertBank(c["slots"], c["d"], c["F"], c["k"], binding.F32 if c["dtype"] == "fp32" else binding.BF16,
-                                    act=binding.ACT_SWIGLU if c["act"] == "swiglu" else binding.ACT_RELU, max_tokens=c["T"])
-        s.bank.set_weights(s.w_in, s.in_scales, s.w_out, s.out_scales)
+    bank = binding.ExpertBank(c["slots"], c["d"], c["F"], c["k"], binding.F32 if c["dtype"] == "fp32" else binding.BF16,
+                              act=binding.ACT_SWIGLU if c["act"] == "swiglu" else binding.ACT_RELU, max_tokens=c["T"])
+    bank.set_weights(s.w_in, s.in_scales, s.w_out, s.out_scales)
+    return bank
+
+
+def _experts_own(s):
+    if s.bank is None:                                                 # (inputs that were made for the plain form)
+        s.bank = _bank(s)
     s.bank.forward(s.x8, s.x_scales, s.slots, s.weights, s.out)
     return s.out
 
