@@ -18,6 +18,7 @@
 namespace swapmoe {
 
 constexpr float kInt8Max = 127.f;
+constexpr int kBlockNormCtas = 4;        // CTAs of eight warps an SM
 
 struct BlockNormArgs {
   const void *x, *residual, *post_weight, *gate, *weight;
@@ -370,7 +371,7 @@ inline cudaError_t block_norm_launch_typed(BlockNormArgs a, bool vec, int sm_cou
   a.per_column = 1.f / (float)a.d;
   auto go = [&](auto kernel) { return launch_kernel(kernel, grid, block, 0, st, pdl, a); };
   const bool row8 = a.out8 != nullptr && a.group == 0;
-  constexpr int kWide = 32 * kNormMaxWarps, kCtas = 4;
+  constexpr int kWide = 32 * kNormMaxWarps, kCtas = kBlockNormCtas;
   if (vec && few) return row8 ? go(block_norm_kernel<T, R, 1, true, true, kWide, 1>) : go(block_norm_kernel<T, R, 1, true, false, kWide, 1>);
   if (vec && a.warps_per_row <= 8)
     return row8 ? go(block_norm_kernel<T, R, 2, true, true, 256, kCtas>) : go(block_norm_kernel<T, R, 2, true, false, 256, kCtas>);

@@ -292,6 +292,20 @@ def test_8_bit_rows_of_the_norm_are_those_of_its_rows(T, d, group, type8):
     assert float(q.float().abs().max()) == top
 
 
+def test_the_norm_of_wide_batches_does_not_spill(tmp_path):
+    import os
+    from test_kernel_resources_host import NVCC, ptxas_properties
+    if not os.path.exists(NVCC):
+        pytest.skip("needs nvcc")
+    forms = ["%s, %s, 2, true, %s, 256, kBlockNormCtas" % (t, r, row8) for t, r in (("bf16", "float"), ("bf16", "bf16"), ("float", "float"))
+             for row8 in ("true", "false")]
+    source = '#include "block_norm.cuh"\nnamespace swapmoe {\n' + "".join(
+        "template __global__ void block_norm_kernel<%s>(BlockNormArgs);\n" % f for f in forms) + "}\n"
+    props = {n: v for n, v in ptxas_properties(source, tmp_path).items() if "block_norm_kernel" in n}
+    assert len(props) == len(forms)
+    assert all(v == (0, 0, 0) for v in props.values()), props
+
+
 # ------------------------------------------------------------------ a served block, step by step
 @pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 45, 1200])
