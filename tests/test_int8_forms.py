@@ -300,7 +300,7 @@ def test_the_norm_of_wide_batches_does_not_spill(tmp_path):
     forms = ["%s, %s, 2, true, %s, 256, kBlockNormCtas" % (t, r, row8) for t, r in (("bf16", "float"), ("bf16", "bf16"), ("float", "float"))
              for row8 in ("true", "false")]
     source = '#include "block_norm.cuh"\nnamespace swapmoe {\n' + "".join(
-        "template __global__ void block_norm_kernel<%s>(BlockNormArgs);\n" % f for f in forms) + "}\n"
+        "template __global__ void block_norm_kernel<%s>(const __grid_constant__ BlockNormArgs);\n" % f for f in forms) + "}\n"
     props = {n: v for n, v in ptxas_properties(source, tmp_path).items() if "block_norm_kernel" in n}
     assert len(props) == len(forms)
     assert all(v == (0, 0, 0) for v in props.values()), props
