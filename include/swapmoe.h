@@ -601,13 +601,14 @@ int32_t swapmoe_matmul_status(int32_t* detail, void* stream);
  * SWAPMOE_ERR_DEVICE_TIMEOUT with detail 99.  Errors: INVALID_ARG, CUDA. */
 int32_t swapmoe_selftest_matmul_wait(int32_t limit_ms, void* stream);
 
-/* Experts in 8-bit integers behind a router (Section 2; half the bytes of a resident expert in bf16, and half of what a swap moves):
+/* Experts in 8-bit integers behind a router (Section 2; half the bytes of a resident expert in bf16):
  *   out[t] = sum_j weights[t, j] * E_slots[t, j](x[t]),   E_s(x) = W_out act(W_in x)
  * x is int8 with a scale per row, the products are those of swapmoe_matmul_scaled, act(W_in x) is fp32 and goes to 8 bits by rows as
  * swapmoe_quantize_rows does it, and the results are added in fp32 in the order of j.  slots and weights are what swapmoe_route writes: a slot that is
  * negative, or not in the bank, is left out (a token without any has zeros); a slot may be named twice.  A token's result has the same bits whatever
  * other tokens its call holds.
- * Like a layer, a bank may be driven from one stream at a time (its workspace is used by every call, captured ones too), on its device. */
+ * Like a layer, a bank may be driven from one stream at a time (its workspace is used by every call, captured ones too), on its device.  The layers'
+ * loader, spare slots and importance scores do not know banks: the caller swaps experts by copies of its own (swapmoe_expert_bank_set_weights). */
 typedef struct swapmoe_expert_bank swapmoe_expert_bank_t; /* opaque, owned by the library */
 typedef struct {
   int32_t n_slots;          /* resident experts, 1 .. 256                                           */
@@ -617,8 +618,9 @@ typedef struct {
   int32_t act;              /* SWAPMOE_ACT_RELU or SWAPMOE_ACT_SWIGLU                               */
   int32_t max_tokens;       /* largest n_tokens of any forward; the workspace is sized for it       */
 } swapmoe_expert_bank_config_t;
-/* Allocates the bank's workspace on the CURRENT device.  *out is written only on success.  Errors: INVALID_ARG, UNSUPPORTED (sizes beyond
- * the above; max_tokens * top_k of 2^24 and more), CUDA, NO_MEMORY. */
+/* Allocates the bank's workspace on the CURRENT device: rows * (5 d_model + 5 d_ff + 20) bytes and up to 1 MB, rows = max_tokens * top_k + 31 for each slot
+ * (8192 tokens, top-2 of 8 slots of 4096 x 14336: 1.5 GB, of which the hidden rows in fp32 are 0.95).  *out is written only on success.  Errors:
+ * INVALID_ARG, UNSUPPORTED (sizes beyond the above; max_tokens * top_k of 2^24 and more), CUDA, NO_MEMORY. */
 int32_t swapmoe_expert_bank_create(swapmoe_expert_bank_t** out, const swapmoe_expert_bank_config_t* cfg);
 /* The caller must have synchronised the streams that used the bank.  NULL is accepted. */
 int32_t swapmoe_expert_bank_destroy(swapmoe_expert_bank_t* bank);

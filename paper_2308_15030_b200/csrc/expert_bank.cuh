@@ -7,7 +7,8 @@
 //   gather: slot offsets, token tiles, rows of x8 with their scales to their places
 //   product, activation in fp32 with the rows' largest magnitudes; rows to 8 bits; product; combine.
 // The products are bound by the weights' bytes or the tensor cores, the rest by HBM.  Eight experts of 4096 x 14336, 8192 pairs: 690 and 330 us of
-// products, hidden rows 86 (6.8 TB/s), combine 25, gather 9; 64 experts of 2048 x 1024, 244 pairs: 73 us, 64 of them the products'.
+// products, hidden rows 86 (6.8 TB/s), combine 25, gather 9 in a short run; whole calls 1160 to 1355 in a graph and 1385 to 1435 back to back, by what the power
+// cap leaves of the clock.  64 experts of 2048 x 1024, 244 pairs: 73 us, 64 of them the products'.
 #pragma once
 #include "int8_gemm.cuh"
 #include "quantize_rows.cuh"

@@ -11,7 +11,8 @@
 // instructions that wait for one another, and with short contractions it sets the pace: a round of 256 tokens takes 1.5 us at 512 columns without an
 // epilogue and 3.2 with it, 2.6 and 4.0 at 1024, 10.7 and 11.5 at 4096.  No load uses cluster multicast.  Every mbarrier wait is
 // bounded; the cluster barriers behind them and the allocation of tensor memory (a CTA has its SM to itself) are not.
-// 8192 tokens, 4096 -> 14336: 288 us, 3.3 POP/s (twice the rate of a bf16 library product: 3.3); 61 tokens 13.6 us, 4.3 TB/s of weights.
+// 8192 tokens, 4096 -> 14336: 288 to 302 us in a short graph, 3.2 to 3.3 POP/s (twice the rate of a bf16 library product: 3.3); calls back to back 336 to 345
+// under the power cap, 2.8 POP/s (twice the library's there: 2.8).  61 tokens 13.6 us, 4.3 TB/s of weights.
 #pragma once
 #include "launch.cuh"
 #include "pair_common.cuh"
